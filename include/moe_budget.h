@@ -51,8 +51,8 @@ extern "C" {
 /* ---- status codes ---- */
 #define MOE_OK 0
 #define MOE_ERR_INVALID_ARG (-1)  /* bad size, null pointer, unsupported shape */
-#define MOE_ERR_RANGE (-2)        /* expert id outside [0, E) */
-#define MOE_ERR_NONFINITE (-3)    /* NaN or +-inf router logit */
+#define MOE_ERR_RANGE (-2)        /* expert id outside [0, E); sequence outside its cache or token array */
+#define MOE_ERR_NONFINITE (-3)    /* NaN or +-inf router logit, or key or value to be quantised */
 #define MOE_ERR_BUDGET (-4)       /* budget below one expert, or a step needs more experts than fit */
 #define MOE_ERR_NOT_PINNED (-5)   /* host store is not page-locked (hipHostMalloc) memory */
 #define MOE_ERR_HIP (-6)          /* a HIP runtime call failed */
@@ -242,6 +242,97 @@ MOE_API int moe_attention_decode(float *x, int H, int n_heads, int n_kv, int hea
                                  const void *w_o, void *k_cache, void *v_cache, int max_pos, int p, float theta,
                                  void *workspace, size_t workspace_bytes, void *stream);
 
+
+/* ======================================================================= */
+/* 4-bit key/value cache and int4 projections (memory-constrained execution, */
+/* sec. 5: what attention does not hold, expert slots can)                   */
+/* ======================================================================= */
+
+/* The cache of one layer: uint8 [n_seq][n_kv][max_pos / 32][36 head_dim], 1.125 head_dim bytes per position and
+ * head for key and value together (bf16: 4 head_dim).  Every group of 64 dims of a head at one position is held
+ * as codes u in 0..15 with a base m and a scale s in bf16, and stands for the values s u + m:
+ *   m = bf16(min x);  s = bf16(fp32(max x - m) * fp32(1/15)), or 0 where that is below 2^-126;
+ *   u = the integer nearest to fp32(x - m) / s, ties to even, within 0..15 (0 where s is 0).
+ * The order of the bytes inside a block of 32 positions is the library's own: moe_kv4_append writes it,
+ * moe_kv4_read gives the values.  Bytes that were never written may hold anything.
+ *
+ * The calls below take a batch of n_seq sequences, sequence b at cache entry b:
+ *   q_start  device int32 [n_seq + 1], ascending: sequence b's tokens are the rows q_start[b] .. q_start[b + 1)
+ *            of the flat token arrays, at most max_q of them; rows from q_start[n_seq] on are not touched.
+ *            NULL: one token per sequence (T = n_seq, max_q is taken as 1).
+ *   kv_len   device int32 [n_seq]: positions of sequence b, its tokens included -- they are the last ones, token
+ *            i of n at position kv_len[b] - n + i.  A token before position 0 is padding.
+ * A token range that does not fit T or max_q counts as empty, a length outside [0, max_pos] as 0; both raise
+ * MOE_ERR_RANGE in the device flags.
+ * Limits: head_dim 64, 128, 192 or 256; max_pos a multiple of 32, at most MOE_KV4_MAX_POS; n_seq and n_kv at most
+ * 65535; max_q times the heads per key/value head at most 2^24.  Token arrays are [T][heads][head_dim] with
+ * `stride` elements (at least heads * head_dim) from token to token; they, their strides in bytes, the cache and
+ * the workspace must be multiples of 16 bytes.  T or n_seq 0 is a no-op.  dtype: MOE_F32 or MOE_BF16. */
+#define MOE_KV4_GROUP 64
+#define MOE_KV4_BLOCK 32
+#define MOE_KV4_MAX_POS (1 << 26)
+
+/* Bytes of a cache (0 for an unsupported shape). */
+MOE_API size_t moe_kv4_cache_bytes(int n_seq, int n_kv, int head_dim, int max_pos);
+
+/* Quantise the tokens' keys and values into the cache.  A group with a value that is not finite, or whose range
+ * is not, is stored as zeros and raises MOE_ERR_NONFINITE in the device flags.  Positions other than the
+ * tokens' keep what they hold. */
+MOE_API int moe_kv4_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T,
+                           int n_seq, int n_kv, int head_dim, int max_pos, const int32_t *q_start, int max_q,
+                           const int32_t *kv_len, void *cache, size_t cache_bytes, void *stream);
+
+/* The values that the cache holds at the tokens' positions (rounded to dtype), zeros for padding: k, v out;
+ * either may be NULL. */
+MOE_API int moe_kv4_read(const void *cache, size_t cache_bytes, int T, int n_seq, int n_kv, int head_dim, int max_pos,
+                         const int32_t *q_start, int max_q, const int32_t *kv_len, void *k, void *v, int dtype,
+                         long long k_stride, long long v_stride, void *stream);
+
+/* Device workspace bytes moe_kv4_attention needs (either dtype; 0 for an unsupported shape). */
+MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q,
+                                                 int max_pos);
+
+/* Attention of the tokens over the cache: out = sum_p softmax_p(scale q . K_p) V_p over the positions p up to the
+ * token's own, with window > 0 the last `window` of those (window <= 2^30); query head j reads key/value head
+ * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums; the
+ * products are exact (MOE_BF16 queries) or take queries as three bf16 terms (MOE_F32, exact too); probabilities
+ * enter the value products as two bf16 terms (MOE_F32: within 2^-16) or rounded to bf16 (MOE_BF16: 2^-8).
+ *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
+ *   out        device, as q with out_stride, same dtype
+ *   scale      any finite factor, as a rule 1 / sqrt(head_dim)
+ *   workspace  device, >= moe_kv4_attention_workspace_bytes(...) (may be NULL when that is 0) */
+MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *cache, size_t cache_bytes, int T,
+                              int n_seq, int n_heads, int n_kv, int head_dim, int max_pos, const int32_t *q_start,
+                              int max_q, const int32_t *kv_len, int window, float scale, void *out,
+                              long long out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* y[t] = add[t] + W h[t] for T <= MOE_MAX_DECODE_TOKENS tokens, h = x, or with MOE_ROUTE_RMSNORM in flags
+ * h = x / sqrt(mean(x^2) + 1e-6).
+ *   x    device fp32 [T x K], 16-byte aligned, K a multiple of 128
+ *   w    device MOE_INT4G128 matrix [N x K], 16-byte aligned: packed nibbles [N x K/2], then bf16 scales [N x K/128]
+ *   add  device fp32 [T x N], or NULL; may be y
+ *   y    device fp32 [T x N], apart from x
+ * Exact products, fp32 sums.  T == 0 or N == 0 is a no-op. */
+MOE_API int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
+                            void *stream);
+
+/* Device workspace bytes moe_attention_decode_int4 needs (0 for an unsupported shape). */
+MOE_API size_t moe_attention_decode_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos);
+
+/* moe_attention_decode's block with int4 projections and a 4-bit cache, for one token of each of T sequences
+ * (T <= MOE_MAX_DECODE_TOKENS), in place on x (device fp32 [T x H]): the same arithmetic, with the rotated keys
+ * and the values of the tokens quantised into the cache (entry t, position kv_len[t] - 1) before attention reads
+ * them.  A sequence of length 0 stores nothing and its attention is 0.  A length outside [0, max_pos] raises
+ * MOE_ERR_RANGE and counts as 0.
+ *   w_qkv    device MOE_INT4G128 [(n_heads + 2 n_kv) head_dim x H]: query rows, key rows, value rows
+ *   w_o      device MOE_INT4G128 [H x n_heads head_dim]
+ *   cache    device, moe_kv4_cache_bytes(T, n_kv, head_dim, max_pos) bytes
+ *   kv_len   device int32 [T], the tokens included
+ * Needs H and n_heads * head_dim multiples of 128, head_dim and max_pos as above, n_heads <= 1024, theta > 1. */
+MOE_API int moe_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
+                                      const void *w_o, void *cache, size_t cache_bytes, int max_pos,
+                                      const int32_t *kv_len, float theta, void *workspace, size_t workspace_bytes,
+                                      void *stream);
 
 /* ======================================================================= */
 /* Expert residency: slot table in HBM, misses filled from pinned host      */
@@ -444,8 +535,8 @@ MOE_API int moe_host_expert_ffn(moe_host_tier *t, const float *x, int H, int I, 
 
 typedef struct moe_stack moe_stack;
 
-/* A decoder self-attention block before each MoE block (moe_attention_decode),
- * in place of the identity. */
+/* A decoder self-attention block before each MoE block (moe_attention_decode, or
+ * moe_attention_decode_int4), in place of the identity. */
 typedef struct {
     int n_heads, n_kv, head_dim, max_pos;
     float theta;                    /* rotary base */
@@ -454,6 +545,10 @@ typedef struct {
     const void *const *w_o;         /* host array [L] of device bf16 [H x n_heads head_dim] */
     void *const *k_cache;           /* host array [L] of device key caches, layout of moe_attention_decode */
     void *const *v_cache;           /* host array [L] of device value caches */
+    int int4;                       /* 1: the block of moe_attention_decode_int4 -- w_qkv and w_o are MOE_INT4G128
+                                       matrices, k_cache[l] is layer l's 4-bit cache of one sequence (keys and
+                                       values; v_cache is not read and may be NULL), max_pos a multiple of 32.
+                                       0: bf16 weights and caches */
 } moe_attention_desc;
 
 typedef struct {

@@ -28,6 +28,7 @@ MOE_CACHE_PRELOAD, MOE_CACHE_HOST_SIM, MOE_CACHE_DEVICE, MOE_CACHE_FILL_CLOCK = 
 EVENT_HIT, EVENT_MISS, EVENT_PREFETCH, EVENT_HOST = 0, 1, 2, 3
 MOE_SLOT_HOST = -2
 MAX_DECODE_TOKENS = 16
+MOE_KV4_GROUP, MOE_KV4_BLOCK = 64, 32
 
 
 class MoeError(RuntimeError):
@@ -58,7 +59,8 @@ EVENT_DTYPE = np.dtype([("t", "<i4"), ("layer", "<i4"), ("expert", "<i4"),
 class AttentionDesc(C.Structure):
     _fields_ = [("n_heads", C.c_int), ("n_kv", C.c_int), ("head_dim", C.c_int), ("max_pos", C.c_int),
                 ("theta", C.c_float), ("start_pos", C.c_int), ("w_qkv", C.POINTER(C.c_void_p)),
-                ("w_o", C.POINTER(C.c_void_p)), ("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p))]
+                ("w_o", C.POINTER(C.c_void_p)), ("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p)),
+                ("int4", C.c_int)]
 
 
 class StackDesc(C.Structure):
@@ -79,7 +81,7 @@ def lib() -> C.CDLL:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is not built: run __graft_entry__.build()")
         L = C.CDLL(LIB_PATH)
-        P, I, SZ, U64P = C.c_void_p, C.c_int, C.c_size_t, C.POINTER(C.c_uint64)
+        P, I, SZ, U64P, LL = C.c_void_p, C.c_int, C.c_size_t, C.POINTER(C.c_uint64), C.c_longlong
         sig = {
             "moe_init": [I], "moe_last_error": [], "moe_sync_check": [P],
             "moe_route_topk": [P, P, I, I, I, I, I, P, P, P, P, I, P, P],
@@ -88,6 +90,14 @@ def lib() -> C.CDLL:
             "moe_expert_ffn_grouped_noalloc": [P, I, I, I, I, I, P, P, P, P, SZ, I, P, P, I, P],
             "moe_combine": [P, P, P, I, I, I, P, I, P],
             "moe_attention_decode": [P, I, I, I, I, P, P, P, P, I, I, C.c_float, P, SZ, P],
+            "moe_kv4_cache_bytes": [I, I, I, I],
+            "moe_kv4_append": [P, P, I, LL, LL, I, I, I, I, I, P, I, P, P, SZ, P],
+            "moe_kv4_read": [P, SZ, I, I, I, I, I, P, I, P, P, P, I, LL, LL, P],
+            "moe_kv4_attention_workspace_bytes": [I, I, I, I, I, I, I],
+            "moe_kv4_attention": [P, I, LL, P, SZ, I, I, I, I, I, I, P, I, P, I, C.c_float, P, LL, P, SZ, P],
+            "moe_matvec_int4": [P, P, I, I, I, P, P, I, P],
+            "moe_attention_decode_int4_workspace_bytes": [I, I, I, I, I],
+            "moe_attention_decode_int4": [P, I, I, I, I, I, P, P, P, SZ, I, P, C.c_float, P, SZ, P],
             "moe_prefill_workspace_bytes": [I, I, I, I, I],
             "moe_prefill_grouped": [P, I, I, I, I, I, P, P, P, P, SZ, I, P, P, P, SZ, I, P],
             "expert_cache_create": [C.POINTER(CacheDesc), C.POINTER(P)],
@@ -119,6 +129,8 @@ def lib() -> C.CDLL:
         L.moe_last_error.restype = C.c_char_p
         L.moe_ffn_workspace_bytes.restype = SZ
         L.moe_prefill_workspace_bytes.restype = SZ
+        for name in ("moe_kv4_cache_bytes", "moe_kv4_attention_workspace_bytes", "moe_attention_decode_int4_workspace_bytes"):
+            getattr(L, name).restype = SZ
         _lib = L
     return _lib
 
@@ -320,6 +332,227 @@ def moe_attention_decode(x, w_qkv, w_o, k_cache, v_cache, p: int, n_heads: int, 
     return x
 
 
+# ------------------------------------------------------- 4-bit cache, int4 projections ---
+def _here(*tensors):
+    """The tensors' common device, which has to be the current one (the library launches there)."""
+    import torch
+    devs = {t.device for t in tensors if t is not None}
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("the tensors must be device tensors")
+    if devs != {torch.device("cuda", torch.cuda.current_device())}:
+        raise ValueError(f"the tensors are on {sorted(map(str, devs))}, the current device is cuda:{torch.cuda.current_device()}")
+    return devs.pop()
+
+
+class _On:
+    """The stream a call runs on: its handle, and the tensors that must outlive the call's work on it.
+
+    A tensor made here for a call on another stream than the current one belongs to that stream, and the
+    caller's tensors are marked as used there, so that none is handed out again before the work has run."""
+
+    def __init__(self, stream):
+        import torch
+        self.handle = _stream(stream)
+        self.other = None
+        if stream is not None and self.handle != _stream(None):
+            self.other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle)
+
+    def empty(self, shape, dtype, device):
+        import torch
+        if self.other is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(self.other):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+    def used(self, *tensors):
+        if self.other is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.other)
+
+
+def _float_code(t, name):
+    import torch
+    code = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected float32 or bfloat16")
+    return code
+
+
+def _rows(t, name, heads, d, T=None, dtype=None):
+    """(pointer, elements from token to token) of a token array [T, heads, d]; only the tokens may be strided."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or (T is not None and t.shape[0] != T):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{'T' if T is None else T}, {heads}, {d}]")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: the heads and dims of a token must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _kv4_shape(cache):
+    """(n_seq, n_kv, head_dim, max_pos) of a cache made by kv4_cache."""
+    import torch
+    if cache.dtype is not torch.uint8 or cache.dim() != 4 or cache.shape[3] not in (36 * 64, 36 * 128, 36 * 192, 36 * 256):
+        raise ValueError(f"cache {cache.dtype} {tuple(cache.shape)} is no 4-bit cache (uint8 [n_seq, n_kv, blocks, 36 head_dim])")
+    if not cache.is_contiguous():
+        raise ValueError("cache must be contiguous")
+    return cache.shape[0], cache.shape[1], cache.shape[3] // 36, cache.shape[2] * MOE_KV4_BLOCK
+
+
+def _kv4_batch(cache, T, kv_len, q_start, max_q):
+    import torch
+    n_seq = cache.shape[0]
+    if kv_len.numel() != n_seq:
+        raise ValueError(f"kv_len has {kv_len.numel()} entries, the cache {n_seq} sequences")
+    if q_start is not None and q_start.numel() != n_seq + 1:
+        raise ValueError(f"q_start has {q_start.numel()} entries, expected {n_seq + 1}")
+    return (_dev(kv_len, "kv_len", torch.int32), _dev(q_start, "q_start", torch.int32),
+            1 if q_start is None else max(T, 1) if max_q is None else max_q)
+
+
+def moe_kv4_cache_bytes(n_seq: int, n_kv: int, head_dim: int, max_pos: int) -> int:
+    return int(lib().moe_kv4_cache_bytes(n_seq, n_kv, head_dim, max_pos))
+
+
+def kv4_cache(n_seq: int, n_kv: int, head_dim: int, max_pos: int, device=None):
+    """An empty 4-bit cache of one layer: uint8 [n_seq, n_kv, max_pos / 32, 36 head_dim] on the device."""
+    import torch
+    n = moe_kv4_cache_bytes(n_seq, n_kv, head_dim, max_pos)
+    if n == 0 and n_seq != 0:
+        raise MoeError(-1, "kv4_cache", lib().moe_last_error().decode(errors="replace"))
+    return torch.empty((n_seq, n_kv, max_pos // MOE_KV4_BLOCK, 36 * head_dim), dtype=torch.uint8,
+                       device="cuda" if device is None else device)
+
+
+def moe_kv4_append(k, v, cache, kv_len, q_start=None, max_q: int | None = None, stream=None):
+    """Quantise the tokens' keys and values (fp32 or bf16 [T, n_kv, d], tokens may be strided) into the cache, at
+    the last positions of their sequences (kv_len int32 [n_seq], the tokens included; q_start int32 [n_seq + 1]:
+    sequence b's rows, None for one token each; max_q: most tokens of a sequence, T by default)."""
+    n_seq, n_kv, d, max_pos = _kv4_shape(cache)
+    T = k.shape[0]
+    kp, ks = _rows(k, "k", n_kv, d)
+    vp, vs = _rows(v, "v", n_kv, d, T, k.dtype)
+    lp, qp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    _here(k, v, cache, kv_len, q_start)
+    on = _On(stream)
+    _check(lib().moe_kv4_append(kp, vp, _float_code(k, "k"), ks, vs, T, n_seq, n_kv, d, max_pos, qp, mq, lp,
+                                _dev(cache, "cache"), cache.numel(), on.handle), "moe_kv4_append")
+    on.used(k, v, cache, kv_len, q_start)
+
+
+def moe_kv4_read(cache, kv_len, T: int, q_start=None, max_q: int | None = None, k_out=None, v_out=None, dtype=None,
+                 stream=None):
+    """The values that the cache holds at the positions of T tokens (batch as for moe_kv4_append); returns
+    (k, v), each [T, n_kv, d] of `dtype` (bf16 unless k_out / v_out say otherwise)."""
+    import torch
+    n_seq, n_kv, d, max_pos = _kv4_shape(cache)
+    given = k_out if k_out is not None else v_out
+    dtype = given.dtype if given is not None else torch.bfloat16 if dtype is None else dtype
+    lp, qp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    device = _here(cache, kv_len, q_start, k_out, v_out)
+    on = _On(stream)
+    k_out = on.empty((T, n_kv, d), dtype, device) if k_out is None else k_out
+    v_out = on.empty((T, n_kv, d), dtype, device) if v_out is None else v_out
+    kp, ks = _rows(k_out, "k_out", n_kv, d, T, dtype)
+    vp, vs = _rows(v_out, "v_out", n_kv, d, T, dtype)
+    _check(lib().moe_kv4_read(_dev(cache, "cache"), cache.numel(), T, n_seq, n_kv, d, max_pos, qp, mq, lp, kp, vp,
+                              _float_code(k_out, "k_out"), ks, vs, on.handle), "moe_kv4_read")
+    on.used(cache, kv_len, q_start, k_out, v_out)
+    return k_out, v_out
+
+
+def moe_kv4_attention_workspace_bytes(T: int, n_seq: int, n_heads: int, n_kv: int, head_dim: int, max_q: int,
+                                      max_pos: int) -> int:
+    return int(lib().moe_kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, max_q, max_pos))
+
+
+def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, window: int = 0,
+                      scale: float | None = None, out=None, workspace=None, stream=None):
+    """Causal attention of the tokens' queries (fp32 or bf16 [T, n_heads, d]) over the 4-bit cache, with
+    window > 0 over the last `window` positions (batch as for moe_kv4_append; scale 1 / sqrt(d) by default);
+    returns out [T, n_heads, d] of q's type.  Rows from q_start[-1] on are not written."""
+    import torch
+    n_seq, n_kv, d, max_pos = _kv4_shape(cache)
+    if q.dim() != 3:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [T, n_heads, {d}]")
+    T, n_heads = q.shape[0], q.shape[1]
+    qp, qs = _rows(q, "q", n_heads, d)
+    lp, sp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    device = _here(q, cache, kv_len, q_start, out, workspace)
+    on = _On(stream)
+    out = on.empty((T, n_heads, d), q.dtype, device) if out is None else out
+    op, os_ = _rows(out, "out", n_heads, d, T, q.dtype)
+    if workspace is None:
+        n = moe_kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, d, mq, max_pos)
+        workspace = on.empty(max(n, 256), torch.uint8, device)
+    _check(lib().moe_kv4_attention(qp, _float_code(q, "q"), qs, _dev(cache, "cache"), cache.numel(), T, n_seq, n_heads,
+                                   n_kv, d, max_pos, sp, mq, lp, window, d ** -0.5 if scale is None else scale, op, os_,
+                                   _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                   on.handle), "moe_kv4_attention")
+    on.used(q, cache, kv_len, q_start, out, workspace)
+    return out
+
+
+def _int4_matrix(w, name, N, K):
+    """Pointer of a MOE_INT4G128 matrix [N x K] held as a uint8 tensor."""
+    import torch
+    p = _dev(w, name, torch.uint8)
+    if w.numel() < N * K // 2 + N * (K // 128) * 2:
+        raise ValueError(f"{name} has {w.numel()} bytes, a [{N} x {K}] int4 matrix {N * K // 2 + N * (K // 128) * 2}")
+    return p
+
+
+def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, stream=None):
+    """y = add + W h for the tokens x (fp32 [T, K], T <= 16), h = x or its RMS norm; w: uint8 bytes of the
+    MOE_INT4G128 matrix [N x K]; add fp32 [T, N] (may be y); returns y [T, N]."""
+    import torch
+    T, K = x.shape
+    device = _here(x, w, add, y)
+    on = _On(stream)
+    y = on.empty((T, N), torch.float32, device) if y is None else y
+    for t, name in ((y, "y"), (add, "add")):
+        if t is not None and t.numel() != T * N:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{T}, {N}]")
+    _check(lib().moe_matvec_int4(_dev(x, "x", torch.float32), _int4_matrix(w, "w", N, K), T, N, K,
+                                 _dev(add, "add", torch.float32), _dev(y, "y", torch.float32),
+                                 MOE_ROUTE_RMSNORM if rmsnorm else 0, on.handle), "moe_matvec_int4")
+    on.used(x, w, add, y)
+    return y
+
+
+def moe_attention_decode_int4_workspace_bytes(T: int, n_heads: int, n_kv: int, head_dim: int, max_pos: int) -> int:
+    return int(lib().moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos))
+
+
+def moe_attention_decode_int4(x, w_qkv, w_o, cache, kv_len, n_heads: int, theta: float = 1.0e6, workspace=None,
+                              stream=None):
+    """x <- x + W_o Attn(rmsnorm(x)), in place on the fp32 tensor x [T, H], one token of each of T sequences, with
+    int4 projections (uint8 bytes) and the 4-bit cache, whose position kv_len[t] - 1 of sequence t is written."""
+    import torch
+    T, H = x.shape
+    n_seq, n_kv, d, max_pos = _kv4_shape(cache)
+    if n_seq != T or kv_len.numel() != T:
+        raise ValueError(f"{T} tokens need a cache of {T} sequences (has {n_seq}) and as many lengths (has {kv_len.numel()})")
+    device = _here(x, w_qkv, w_o, cache, kv_len, workspace)
+    on = _On(stream)
+    if workspace is None:
+        workspace = on.empty(max(moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, d, max_pos), 256),
+                             torch.uint8, device)
+    _check(lib().moe_attention_decode_int4(
+        _dev(x, "x", torch.float32), T, H, n_heads, n_kv, d, _int4_matrix(w_qkv, "w_qkv", (n_heads + 2 * n_kv) * d, H),
+        _int4_matrix(w_o, "w_o", H, n_heads * d), _dev(cache, "cache"), cache.numel(), max_pos,
+        _dev(kv_len, "kv_len", torch.int32), theta, _dev(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), on.handle), "moe_attention_decode_int4")
+    on.used(x, w_qkv, w_o, cache, kv_len, workspace)
+    return x
+
+
 def moe_combine(y_partial, weights, y_shared=None, y_out=None, accumulate: bool = False, stream=None):
     """y[t] = sum_j weights[t,j] * y_partial[t,j] (+ y_shared[t])."""
     import torch
@@ -462,11 +695,21 @@ class MoeStack:
         self._keep = (router_w, shared_w, cache)
         att = None
         if attention is not None:  # dict: n_heads, n_kv, head_dim, max_pos, theta, start_pos, w_qkv, w_o, k_cache, v_cache
+            # or, with "int4": True, int4 matrices and `cache` (a 4-bit cache of one sequence per layer) in place of the last two
+            int4 = bool(attention.get("int4", False))
             arr = lambda ts, nm: (C.c_void_p * len(ts))(*[_dev(t, nm) for t in ts])
-            self._att_arrays = [arr(attention[nm], nm) for nm in ("w_qkv", "w_o", "k_cache", "v_cache")]
+            if int4:
+                nh, nk, hd = attention["n_heads"], attention["n_kv"], attention["head_dim"]
+                for i, c in enumerate(attention["cache"]):
+                    if _kv4_shape(c) != (1, nk, hd, attention["max_pos"]):
+                        raise ValueError(f"cache of layer {i} is for {_kv4_shape(c)}, expected (1, {nk}, {hd}, {attention['max_pos']})")
+                    _int4_matrix(attention["w_qkv"][i], "w_qkv", (nh + 2 * nk) * hd, H)
+                    _int4_matrix(attention["w_o"][i], "w_o", H, nh * hd)
+            self._att_arrays = [arr(attention[nm], nm) for nm in (("w_qkv", "w_o", "cache", "cache") if int4 else
+                                                                  ("w_qkv", "w_o", "k_cache", "v_cache"))]
             att = AttentionDesc(attention["n_heads"], attention["n_kv"], attention["head_dim"], attention["max_pos"],
                                 attention.get("theta", 1.0e6), attention.get("start_pos", 0),
-                                *[C.cast(a, C.POINTER(C.c_void_p)) for a in self._att_arrays])
+                                *[C.cast(a, C.POINTER(C.c_void_p)) for a in self._att_arrays], int(int4))
             self._att = att
             self._keep = self._keep + (attention,)
         d = StackDesc(len(router_w), H, I, E, k, w_dtype, router_dtype,

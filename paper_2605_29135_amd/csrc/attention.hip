@@ -29,6 +29,7 @@ using dev::kWave;
 using dev::wave_sum;
 using dev::BF16;
 using dev::dpp;
+using dev::rope_cs;
 
 constexpr int kAttnChunk = 64;  // positions per block (one partial per query head) in the partial kernel
 
@@ -45,19 +46,6 @@ __device__ __forceinline__ uint16_t f32_to_bf16_rne(float f) {
 }
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
-
-// Rotation of dimension pair (i, i + d/2) at position p: angle p * theta^(-2i/d).  The angle is formed and
-// reduced to [-pi, pi] in double, so thousands of positions keep full single precision in cos and sin.
-__device__ __forceinline__ void rope_cs(int p, int i, int d, float theta, float &c, float &s) {
-    const double inv_freq = exp2(-2.0 * double(i) / double(d) * log2(double(theta)));
-    const double ang = double(p) * inv_freq;
-    constexpr double kTwoPi = 6.283185307179586;
-    const double r = fma(-rint(ang * (1.0 / kTwoPi)), kTwoPi, ang);
-    double sd, cd;
-    sincos(r, &sd, &cd);
-    c = float(cd);
-    s = float(sd);
-}
 
 // Block = one chunk of 64 positions of key/value head g (blockIdx.y), 8 waves of 8 positions.  The block first
 // brings its group's queries to their final form (RMS norm over each head, rotation at p), and the block of the

@@ -3,10 +3,13 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <string>
 
 #include "internal.h"
+#include "kv4.h"
 #include "../../include/moe_budget.h"
 
 namespace moe {
@@ -99,8 +102,8 @@ int moe_sync_check(void *stream) {
         return fail_hip(e, "reading device error flags");
     if (v) {
         if ((e = hipMemset(flags, 0, sizeof v)) != hipSuccess) return fail_hip(e, "clearing device error flags");
-        if (v & moe::kErrRange) return fail(MOE_ERR_RANGE, "an expert id was outside [0, E)");
-        if (v & moe::kErrNonfinite) return fail(MOE_ERR_NONFINITE, "a router logit was NaN or infinite");
+        if (v & moe::kErrRange) return fail(MOE_ERR_RANGE, "an expert id was outside [0, E), or a sequence outside its cache or token array");
+        if (v & moe::kErrNonfinite) return fail(MOE_ERR_NONFINITE, "a router logit, or a key or value to be quantised, was not finite");
         if (v & moe::kErrNotResident) return fail(MOE_ERR_NOT_RESIDENT, "an expert had no slot");
         if (v & moe::kErrBudget) return fail(MOE_ERR_BUDGET, "a device lookup needed more experts than slots");
     }
@@ -263,6 +266,192 @@ int moe_attention_decode(float *x, int H, int n_heads, int n_kv, int head_dim, c
                                                       static_cast<uint16_t *>(k_cache), static_cast<uint16_t *>(v_cache),
                                                       max_pos, p, theta, workspace, static_cast<hipStream_t>(stream)),
                          "attention launch");
+}
+
+namespace {
+
+// What moe_kv4_* and moe_attention_decode_int4 ask of the cache's shape.
+int check_kv4_shape(const char *what, int n_seq, int n_kv, int head_dim, int max_pos) {
+    if (n_seq < 0 || n_seq > 65535 || n_kv < 1 || n_kv > 65535)
+        return fail(MOE_ERR_INVALID_ARG, "%s: need 0 <= n_seq, 1 <= n_kv, both at most 65535 (n_seq=%d n_kv=%d)", what,
+                    n_seq, n_kv);
+    if (head_dim != 64 && head_dim != 128 && head_dim != 192 && head_dim != 256)
+        return fail(MOE_ERR_INVALID_ARG, "%s: head_dim must be 64, 128, 192 or 256 (head_dim=%d)", what, head_dim);
+    if (max_pos < MOE_KV4_BLOCK || max_pos % MOE_KV4_BLOCK || max_pos > MOE_KV4_MAX_POS)
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_pos must be a multiple of %d up to %d (max_pos=%d)", what,
+                    MOE_KV4_BLOCK, MOE_KV4_MAX_POS, max_pos);
+    return MOE_OK;
+}
+
+// And of the batch; max_q becomes 1 without q_start.
+int check_kv4_batch(const char *what, int dtype, int T, int n_seq, int heads, int n_kv, const int32_t *q_start, int *max_q) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16)
+        return fail(MOE_ERR_INVALID_ARG, "%s: dtype must be MOE_F32 or MOE_BF16 (dtype=%d)", what, dtype);
+    if (T < 0) return fail(MOE_ERR_INVALID_ARG, "%s: T=%d", what, T);
+    if (heads < 1 || heads % n_kv)
+        return fail(MOE_ERR_INVALID_ARG, "%s: n_heads must be a multiple of n_kv (%d, %d)", what, heads, n_kv);
+    if (!q_start) {
+        if (T != n_seq)
+            return fail(MOE_ERR_INVALID_ARG, "%s: without q_start T must be n_seq (%d, %d)", what, T, n_seq);
+        *max_q = 1;
+    }
+    if (T > 0 && (*max_q < 1 || (long long)*max_q * (heads / n_kv) > (1 << 24)))
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_q=%d outside [1, 2^24 / (n_heads / n_kv)]", what, *max_q);
+    return MOE_OK;
+}
+
+// A token array: 16-byte rows, not overlapping.
+bool rows_ok(const void *p, long long stride, int heads, int head_dim, int dtype) {
+    const long long size = dtype == MOE_F32 ? 4 : 2;
+    return aligned16(p) && stride >= (long long)heads * head_dim && stride <= (1ll << 40) && stride * size % 16 == 0;
+}
+
+int check_kv4_cache(const char *what, const void *cache, size_t cache_bytes, int n_seq, int n_kv, int head_dim, int max_pos,
+                    const int32_t *kv_len) {
+    if (!cache || !kv_len) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned16(cache)) return fail(MOE_ERR_INVALID_ARG, "%s: the cache must be 16-byte aligned", what);
+    const size_t need = moe_kv4_cache_bytes(n_seq, n_kv, head_dim, max_pos);
+    if (cache_bytes < need)
+        return fail(MOE_ERR_INVALID_ARG, "%s: cache of %zu bytes, need %zu", what, cache_bytes, need);
+    return MOE_OK;
+}
+
+}  // namespace
+
+size_t moe_kv4_cache_bytes(int n_seq, int n_kv, int head_dim, int max_pos) {
+    if (check_kv4_shape("kv4 cache", n_seq, n_kv, head_dim, max_pos) != MOE_OK) return 0;
+    return size_t(n_seq) * n_kv * (max_pos / moe::kv4::kPos) * moe::kv4::block_bytes(head_dim);
+}
+
+int moe_kv4_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T, int n_seq,
+                   int n_kv, int head_dim, int max_pos, const int32_t *q_start, int max_q, const int32_t *kv_len,
+                   void *cache, size_t cache_bytes, void *stream) {
+    int st = check_kv4_shape("kv4 append", n_seq, n_kv, head_dim, max_pos);
+    if (st == MOE_OK) st = check_kv4_batch("kv4 append", dtype, T, n_seq, n_kv, n_kv, q_start, &max_q);
+    if (st != MOE_OK) return st;
+    if (T == 0 || n_seq == 0) return MOE_OK;
+    if (!k || !v) return fail(MOE_ERR_INVALID_ARG, "kv4 append: NULL pointer");
+    if (!rows_ok(k, k_stride, n_kv, head_dim, dtype) || !rows_ok(v, v_stride, n_kv, head_dim, dtype))
+        return fail(MOE_ERR_INVALID_ARG, "kv4 append: k and v need 16-byte aligned rows of at least n_kv * head_dim elements");
+    if ((st = check_kv4_cache("kv4 append", cache, cache_bytes, n_seq, n_kv, head_dim, max_pos, kv_len)) != MOE_OK) return st;
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::kv4::Batch batch{q_start, kv_len, T, n_seq, std::min(max_q, T), max_pos};
+    return finish_launch(moe::launch_kv4_append(k, v, dtype, k_stride, v_stride, batch, n_kv, head_dim, cache, eflags,
+                                                static_cast<hipStream_t>(stream)),
+                         "kv4 append launch");
+}
+
+int moe_kv4_read(const void *cache, size_t cache_bytes, int T, int n_seq, int n_kv, int head_dim, int max_pos,
+                 const int32_t *q_start, int max_q, const int32_t *kv_len, void *k, void *v, int dtype,
+                 long long k_stride, long long v_stride, void *stream) {
+    int st = check_kv4_shape("kv4 read", n_seq, n_kv, head_dim, max_pos);
+    if (st == MOE_OK) st = check_kv4_batch("kv4 read", dtype, T, n_seq, n_kv, n_kv, q_start, &max_q);
+    if (st != MOE_OK) return st;
+    if (T == 0 || n_seq == 0) return MOE_OK;
+    if (!k && !v) return fail(MOE_ERR_INVALID_ARG, "kv4 read: k and v are both NULL");
+    if ((k && !rows_ok(k, k_stride, n_kv, head_dim, dtype)) || (v && !rows_ok(v, v_stride, n_kv, head_dim, dtype)))
+        return fail(MOE_ERR_INVALID_ARG, "kv4 read: k and v need 16-byte aligned rows of at least n_kv * head_dim elements");
+    if ((st = check_kv4_cache("kv4 read", cache, cache_bytes, n_seq, n_kv, head_dim, max_pos, kv_len)) != MOE_OK) return st;
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::kv4::Batch batch{q_start, kv_len, T, n_seq, std::min(max_q, T), max_pos};
+    return finish_launch(moe::launch_kv4_read(cache, batch, n_kv, head_dim, k, v, dtype, k_stride, v_stride, eflags,
+                                              static_cast<hipStream_t>(stream)),
+                         "kv4 read launch");
+}
+
+size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q, int max_pos) {
+    // (a caller without q_start may pass any max_q of at least 1: a plan for 1 is then what runs)
+    const int32_t some = 0;
+    if (check_kv4_shape("kv4 attention", n_seq, n_kv, head_dim, max_pos) != MOE_OK ||
+        check_kv4_batch("kv4 attention", MOE_F32, T, n_seq, n_heads, n_kv, &some, &max_q) != MOE_OK || T == 0 || n_seq == 0)
+        return 0;
+    size_t n = moe::kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, std::min(max_q, T), max_pos);
+    if (T == n_seq) n = std::max(n, moe::kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, 1, max_pos));
+    return n;
+}
+
+int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *cache, size_t cache_bytes, int T, int n_seq,
+                      int n_heads, int n_kv, int head_dim, int max_pos, const int32_t *q_start, int max_q,
+                      const int32_t *kv_len, int window, float scale, void *out, long long out_stride, void *workspace,
+                      size_t workspace_bytes, void *stream) {
+    int st = check_kv4_shape("kv4 attention", n_seq, n_kv, head_dim, max_pos);
+    if (st == MOE_OK) st = check_kv4_batch("kv4 attention", dtype, T, n_seq, n_heads, n_kv, q_start, &max_q);
+    if (st != MOE_OK) return st;
+    if (window < 0 || window > (1 << 30))
+        return fail(MOE_ERR_INVALID_ARG, "kv4 attention: window=%d outside [0, 2^30]", window);
+    if (!std::isfinite(scale)) return fail(MOE_ERR_INVALID_ARG, "kv4 attention: scale must be finite");
+    if (T == 0 || n_seq == 0) return MOE_OK;
+    if (!q || !out) return fail(MOE_ERR_INVALID_ARG, "kv4 attention: NULL pointer");
+    if (!rows_ok(q, q_stride, n_heads, head_dim, dtype) || !rows_ok(out, out_stride, n_heads, head_dim, dtype))
+        return fail(MOE_ERR_INVALID_ARG,
+                    "kv4 attention: q and out need 16-byte aligned rows of at least n_heads * head_dim elements");
+    if ((st = check_kv4_cache("kv4 attention", cache, cache_bytes, n_seq, n_kv, head_dim, max_pos, kv_len)) != MOE_OK)
+        return st;
+    max_q = std::min(max_q, T);
+    const size_t need = moe::kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, max_q, max_pos);
+    if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+        return fail(MOE_ERR_INVALID_ARG, "kv4 attention: needs a 16-byte aligned workspace of %zu bytes (%zu given)", need,
+                    workspace ? workspace_bytes : size_t(0));
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::kv4::Batch batch{q_start, kv_len, T, n_seq, max_q, max_pos};
+    return finish_launch(moe::launch_kv4_attention(q, dtype, q_stride, cache, batch, n_heads, n_kv, head_dim, window, scale,
+                                                   out, out_stride, workspace, eflags, static_cast<hipStream_t>(stream)),
+                         "kv4 attention launch");
+}
+
+int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
+                    void *stream) {
+    if (T < 0 || T > MOE_MAX_DECODE_TOKENS)
+        return fail(MOE_ERR_INVALID_ARG, "matvec: T=%d outside [0, %d]", T, MOE_MAX_DECODE_TOKENS);
+    if (N < 0 || N > (1 << 28) || K < 128 || K % 128 || K > (1 << 24))
+        return fail(MOE_ERR_INVALID_ARG, "matvec: need 0 <= N <= 2^28 and K a multiple of 128 up to 2^24 (N=%d K=%d)", N, K);
+    if (T == 0 || N == 0) return MOE_OK;
+    if (!x || !w || !y) return fail(MOE_ERR_INVALID_ARG, "matvec: NULL pointer");
+    if (!aligned16(x) || !aligned16(w)) return fail(MOE_ERR_INVALID_ARG, "matvec: x and w must be 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(add)) & 3)
+        return fail(MOE_ERR_INVALID_ARG, "matvec: add and y must be 4-byte aligned");
+    const auto xa = reinterpret_cast<uintptr_t>(x), ya = reinterpret_cast<uintptr_t>(y);
+    if (xa < ya + sizeof(float) * size_t(T) * N && ya < xa + sizeof(float) * size_t(T) * K)
+        return fail(MOE_ERR_INVALID_ARG, "matvec: y overlaps x");
+    return finish_launch(moe::launch_matvec_int4(x, w, T, N, K, add, y, flags & MOE_ROUTE_RMSNORM,
+                                                 static_cast<hipStream_t>(stream)),
+                         "matvec launch");
+}
+
+size_t moe_attention_decode_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos) {
+    if (T < 1 || T > MOE_MAX_DECODE_TOKENS ||
+        !moe::attention_int4_shape_supported(128, n_heads, n_kv, head_dim, max_pos))
+        return 0;
+    return moe::attention_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos);
+}
+
+int moe_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
+                              const void *w_o, void *cache, size_t cache_bytes, int max_pos, const int32_t *kv_len,
+                              float theta, void *workspace, size_t workspace_bytes, void *stream) {
+    if (T < 0 || T > MOE_MAX_DECODE_TOKENS)
+        return fail(MOE_ERR_INVALID_ARG, "attention int4: T=%d outside [0, %d]", T, MOE_MAX_DECODE_TOKENS);
+    if (!moe::attention_int4_shape_supported(H, n_heads, n_kv, head_dim, max_pos))
+        return fail(MOE_ERR_INVALID_ARG, "attention int4: unsupported shape (H %d, heads %d/%d, head_dim %d, max_pos %d)", H,
+                    n_heads, n_kv, head_dim, max_pos);
+    if (!(theta > 1.f)) return fail(MOE_ERR_INVALID_ARG, "attention int4: rotary base must exceed 1");
+    if (T == 0) return MOE_OK;
+    if (!x || !w_qkv || !w_o || !workspace) return fail(MOE_ERR_INVALID_ARG, "attention int4: NULL pointer");
+    if (!aligned16(x) || !aligned16(w_qkv) || !aligned16(w_o) || !aligned16(workspace))
+        return fail(MOE_ERR_INVALID_ARG, "attention int4: buffers must be 16-byte aligned");
+    const int st = check_kv4_cache("attention int4", cache, cache_bytes, T, n_kv, head_dim, max_pos, kv_len);
+    if (st != MOE_OK) return st;
+    const size_t need = moe::attention_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos);
+    if (workspace_bytes < need)
+        return fail(MOE_ERR_INVALID_ARG, "attention int4: workspace of %zu bytes, need %zu", workspace_bytes, need);
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    return finish_launch(moe::launch_attention_decode_int4(x, T, H, n_heads, n_kv, head_dim, w_qkv, w_o, cache, max_pos,
+                                                           kv_len, theta, workspace, eflags,
+                                                           static_cast<hipStream_t>(stream)),
+                         "attention int4 launch");
 }
 
 int moe_hbm_read_probe(const void *buf, size_t bytes, float *sink, void *stream) {

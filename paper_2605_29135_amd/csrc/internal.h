@@ -185,6 +185,30 @@ hipError_t launch_attention_decode(float *x, int H, int n_heads, int n_kv, int h
                                    const void *w_o, uint16_t *k_cache, uint16_t *v_cache, int max_pos, int p,
                                    float theta, void *workspace, hipStream_t s);
 
+// 4-bit key/value cache (kv4_store.hip, kv4_attention.hip; layout and Batch in kv4.h).
+namespace kv4 {
+struct Batch;
+}
+hipError_t launch_kv4_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride,
+                             const kv4::Batch &batch, int n_kv, int d, void *cache, int *err, hipStream_t s);
+hipError_t launch_kv4_read(const void *cache, const kv4::Batch &batch, int n_kv, int d, void *k, void *v, int dtype,
+                           long long k_stride, long long v_stride, int *err, hipStream_t s);
+size_t kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int d, int max_q, int max_pos);
+hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, const void *cache, const kv4::Batch &batch,
+                                int n_heads, int n_kv, int d, int window, float scale, void *out, long long out_stride,
+                                void *workspace, int *err, hipStream_t s);
+
+// int4-g128 matrix-vector products (matvec_int4.hip): y = add + W h, h = x or its RMS norm; y may be add.
+hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, bool norm,
+                              hipStream_t s);
+
+// Decoder self-attention of one token per sequence with int4 weights and a 4-bit cache (attention_int4.hip).
+bool attention_int4_shape_supported(int H, int n_heads, int n_kv, int head_dim, int max_pos);
+size_t attention_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos);
+hipError_t launch_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
+                                        const void *w_o, void *cache, int max_pos, const int32_t *kv_len, float theta,
+                                        void *workspace, int *err, hipStream_t s);
+
 bool ffn_shape_supported(int H, int I, int dtype);
 bool router_shape_supported(int H, int dtype);
 

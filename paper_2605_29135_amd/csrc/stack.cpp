@@ -69,6 +69,7 @@ struct moe_stack {
     std::vector<const void *> a_wqkv, a_wo;
     std::vector<void *> a_k, a_v;
     void *attn_ws = nullptr;
+    int *attn_len = nullptr;       // device: positions with this step's (the 4-bit cache's kernels read it there)
     int attn_pos = 0;              // position of the next decode step
     int last_attn_pos = -1;        // position of the last one
     hipGraphExec_t graph_exec = nullptr;  // one-token decode step captured for replay (device residency)
@@ -125,6 +126,22 @@ int wait_published_ids(moe_stack *s, uint32_t seq, hipStream_t strm) {
         for (int j = 0; j < s->d.k; ++j) s->host_w[size_t(j)] = w[j];
     }
     return MOE_OK;
+}
+
+// Layer l's attention block for the token at position p, in place on x; set_len: tell the 4-bit cache's kernels
+// the length first (once per step, for all its layers).
+hipError_t launch_attention(moe_stack *s, int l, float *x, int p, bool set_len, int *eflags, hipStream_t strm) {
+    const moe_attention_desc &a = s->ad;
+    if (!a.int4)
+        return moe::launch_attention_decode(x, s->d.H, a.n_heads, a.n_kv, a.head_dim, s->a_wqkv[l], s->a_wo[l],
+                                            static_cast<uint16_t *>(s->a_k[l]), static_cast<uint16_t *>(s->a_v[l]),
+                                            a.max_pos, p, a.theta, s->attn_ws, strm);
+    if (set_len) {
+        const hipError_t e = moe::launch_set_int(s->attn_len, p + 1, strm);
+        if (e != hipSuccess) return e;
+    }
+    return moe::launch_attention_decode_int4(x, 1, s->d.H, a.n_heads, a.n_kv, a.head_dim, s->a_wqkv[l], s->a_wo[l],
+                                             s->a_k[l], a.max_pos, s->attn_len, a.theta, s->attn_ws, eflags, strm);
 }
 
 // Speculative prefetch after layer l of a one-token step: the next layer's (the
@@ -213,6 +230,7 @@ int moe_stack_destroy(moe_stack *s) {
     if (s->dev_step) (void)hipFree(s->dev_step);
     if (s->all_experts) (void)hipFree(s->all_experts);
     if (s->attn_ws) (void)hipFree(s->attn_ws);
+    if (s->attn_len) (void)hipFree(s->attn_len);
     if (s->host) moe_host_tier_destroy(s->host);
     if (s->h_pub) (void)hipHostFree(s->h_pub);
     if (s->y_pub) (void)hipHostFree(s->y_pub);
@@ -237,11 +255,14 @@ int moe_stack_create(const moe_stack_desc *d, moe_stack **out) {
     if (d->cache && moe::cache_device(d->cache) && (d->prefetch > 0 || d->recall > 0))
         return moe::fail(MOE_ERR_INVALID_ARG, "stack: prefetch and recall need host lookups (not MOE_CACHE_DEVICE)");
     if (const moe_attention_desc *a = d->attention) {
-        if (!moe::attention_shape_supported(d->H, a->n_heads, a->n_kv, a->head_dim, a->max_pos) || !(a->theta > 1.f) ||
-            a->start_pos < 0 || a->start_pos >= a->max_pos || !a->w_qkv || !a->w_o || !a->k_cache || !a->v_cache)
+        const bool shape = a->int4
+                               ? moe::attention_int4_shape_supported(d->H, a->n_heads, a->n_kv, a->head_dim, a->max_pos)
+                               : moe::attention_shape_supported(d->H, a->n_heads, a->n_kv, a->head_dim, a->max_pos);
+        if (!shape || (a->int4 != 0 && a->int4 != 1) || !(a->theta > 1.f) || a->start_pos < 0 ||
+            a->start_pos >= a->max_pos || !a->w_qkv || !a->w_o || !a->k_cache || (!a->int4 && !a->v_cache))
             return moe::fail(MOE_ERR_INVALID_ARG, "stack: unsupported attention block");
         for (int l = 0; l < d->n_layers; ++l)
-            if (!a->w_qkv[l] || !a->w_o[l] || !a->k_cache[l] || !a->v_cache[l])
+            if (!a->w_qkv[l] || !a->w_o[l] || !a->k_cache[l] || (!a->int4 && !a->v_cache[l]))
                 return moe::fail(MOE_ERR_INVALID_ARG, "stack: attention buffers of layer %d missing", l);
         if (d->max_prefill_tokens > 0 || d->max_tokens != 1)
             return moe::fail(MOE_ERR_INVALID_ARG, "stack: an attention block decodes one token per step (no prefill)");
@@ -308,13 +329,14 @@ int moe_stack_create(const moe_stack_desc *d, moe_stack **out) {
             s->a_wqkv.push_back(a->w_qkv[l]);
             s->a_wo.push_back(a->w_o[l]);
             s->a_k.push_back(a->k_cache[l]);
-            s->a_v.push_back(a->v_cache[l]);
+            s->a_v.push_back(a->int4 ? nullptr : a->v_cache[l]);
         }
         s->ad.w_qkv = s->ad.w_o = nullptr;
         s->ad.k_cache = s->ad.v_cache = nullptr;
         s->attn_pos = a->start_pos;
-        if ((e = hipMalloc(&s->attn_ws, moe::attention_workspace_bytes(a->n_heads, a->n_kv, a->head_dim, a->max_pos))) !=
-            hipSuccess)
+        const size_t n = a->int4 ? moe::attention_int4_workspace_bytes(1, a->n_heads, a->n_kv, a->head_dim, a->max_pos)
+                                 : moe::attention_workspace_bytes(a->n_heads, a->n_kv, a->head_dim, a->max_pos);
+        if ((e = hipMalloc(&s->attn_ws, n)) != hipSuccess || (e = hipMalloc(&s->attn_len, sizeof(int))) != hipSuccess)
             return bail(e, "stack attention workspace");
     }
     s->d.attention = nullptr;  // the caller's descriptor need not outlive the call
@@ -376,10 +398,7 @@ int enqueue_decode(moe_stack *s, int step, float *x, int T, const float *logit_b
                                                      : "stack step: the attention caches are full");
     for (int l = 0; l < d.n_layers; ++l) {
         if (s->attn) {
-            hipError_t ea = moe::launch_attention_decode(x, d.H, s->ad.n_heads, s->ad.n_kv, s->ad.head_dim,
-                                                         s->a_wqkv[l], s->a_wo[l], static_cast<uint16_t *>(s->a_k[l]),
-                                                         static_cast<uint16_t *>(s->a_v[l]), s->ad.max_pos,
-                                                         s->attn_pos, s->ad.theta, s->attn_ws, strm);
+            hipError_t ea = launch_attention(s, l, x, s->attn_pos, l == 0, eflags, strm);
             if (ea != hipSuccess) return moe::fail_hip(ea, "stack step: attention");
         }
         int32_t *ids = ids_out ? ids_out + size_t(l) * T * d.k : s->ids;
@@ -704,10 +723,7 @@ int moe_stack_kernel_time(moe_stack *s, int which, int n, void *stream, double *
     auto enqueue = [&](const LastLayer &ll, int r) -> hipError_t {
         const int l = ll.layer;
         if (which == 4)
-            return moe::launch_attention_decode(s->scratch_x, d.H, s->ad.n_heads, s->ad.n_kv, s->ad.head_dim,
-                                                s->a_wqkv[l], s->a_wo[l], static_cast<uint16_t *>(s->a_k[l]),
-                                                static_cast<uint16_t *>(s->a_v[l]), s->ad.max_pos, s->last_attn_pos,
-                                                s->ad.theta, s->attn_ws, cs);
+            return launch_attention(s, l, s->scratch_x, s->last_attn_pos, false, eflags, cs);  // (its length still stands)
         if (which == 0) {
             hipError_t r = moe::launch_router_logits(s->scratch_x, s->router_w[l], d.router_dtype, T, d.H, d.E, nullptr,
                                                      s->logits, true, s->scratch_y, cs);

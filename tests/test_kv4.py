@@ -1,0 +1,744 @@
+"""The 4-bit key/value cache, the attention over it, int4 matrix-vector products and the block made of them,
+against plain 64-bit implementations."""
+import ctypes as C
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_29135_amd as moe
+from paper_2605_29135_amd import binding
+
+F32, BF16 = torch.float32, torch.bfloat16
+GROUP = 64
+EPS = 1e-6
+
+
+# ------------------------------------------------------------------------------------- plain 64-bit forms ---
+def quantised(x):
+    """(codes, scale, base) of each group of 64 of the last dimension, float64 [..., d/64, 64 | 1 | 1], by the
+    cache's definition: the base and scale in bf16, x - base and the range in fp32, the quotient exact."""
+    x = x.float().unflatten(-1, (-1, GROUP))
+    m = x.amin(-1, keepdim=True).to(BF16).float()
+    s = ((x.amax(-1, keepdim=True) - m) * torch.tensor(1 / 15, dtype=F32)).to(BF16).float()
+    s = torch.where(s >= 2.0 ** -126, s, torch.zeros_like(s))
+    bad = ~(torch.isfinite(x).all(-1, keepdim=True) & torch.isfinite(s) & torch.isfinite(m))
+    s, m, x = (torch.where(bad, torch.zeros_like(t), t) for t in (s, m, x))
+    t = (x - m).double()
+    u = torch.where(s > 0, torch.round(t / torch.where(s > 0, s, torch.ones_like(s)).double()), torch.zeros_like(t))
+    return u.clamp(0, 15), s.double(), m.double()
+
+
+def held(x):
+    u, s, m = quantised(x)
+    return (u * s + m).flatten(-2)
+
+
+def magnitude(x):
+    """What the kernels' exact partial products of a held value can amount to: (16 + u) s + 16 s + |m|."""
+    u, s, m = quantised(x)
+    return ((32 + u) * s + m.abs()).flatten(-2)
+
+
+def attend(q, ks, vs, ns, ls, G, window, scale):
+    """Plain attention and its error bound: q [T, heads, d] float64; ks, vs: per sequence [L, n_kv, d] vectors
+    before quantisation.  The bound per output is the sum of the roundings on its way:
+      scores: exact products in fp32 sums of at most 32 partial results (2^-24 each of what they amount to),
+              then two roundings on the way to the exponent; an error e of a score changes a probability by e;
+      exponentials and the sum: 2^-20 together;
+      probabilities: times the scale (2^-24) and into bf16 terms: 2^-16 (two terms) or 2^-8 (one)."""
+    T, heads, d = q.shape
+    out = torch.zeros((T, heads, d), dtype=torch.float64)
+    amount = torch.zeros((T, heads, d), dtype=torch.float64)  # sum of P x magnitude
+    shift = torch.zeros((T, heads, 1), dtype=torch.float64)   # largest error of a score
+    t0 = 0
+    for n, L, k, v in zip(ns, ls, ks, vs):
+        for i in range(n):
+            P = L - n + i
+            if P < 0:
+                continue
+            first = max(0, P - window + 1) if window else 0
+            for h in range(heads):
+                K, V = held(k[first:P + 1, h // G]), held(v[first:P + 1, h // G])
+                z = (K @ q[t0 + i, h]) * scale
+                p = torch.softmax(z, 0)
+                out[t0 + i, h] = p @ V
+                amount[t0 + i, h] = p @ magnitude(v[first:P + 1, h // G])
+                e = (magnitude(k[first:P + 1, h // G]) @ q[t0 + i, h].abs()) * abs(scale) * 2.0 ** -19
+                shift[t0 + i, h] = (e + z.abs() * 2.0 ** -22).max()
+        t0 += n
+    return out, amount, shift
+
+
+def attention_tolerance(ref, amount, shift, dtype):
+    term = 2.0 ** -16 if dtype is F32 else 2.0 ** -8
+    return amount * (2 * shift + 2.0 ** -20 + term) + ref.abs() * torch.finfo(dtype).eps / 2 + 1e-30
+
+
+def int4_matrix(N, K, gen, sigma=0.02):
+    """(bytes as stored, float64 values) of a random int4-g128 matrix."""
+    w = torch.randn((N, K // 128, 128), generator=gen) * sigma
+    s = (w.abs().amax(-1, keepdim=True) / 7).to(BF16)
+    q = torch.clamp(torch.round(w / s.float()), -8, 7)
+    nib = q.to(torch.int32).view(N, K // 2, 2) & 15
+    raw = (nib[..., 0] | (nib[..., 1] << 4)).to(torch.uint8).flatten()
+    return torch.cat([raw, s.flatten().view(torch.uint8)]), (q.double() * s.double()).view(N, K)
+
+
+def batch(ns, ls, extra=0):
+    starts = np.concatenate([[0], np.cumsum(ns)]).astype(np.int32)
+    return (torch.from_numpy(starts).cuda(), torch.tensor(ls, dtype=torch.int32).cuda(), int(starts[-1]) + extra)
+
+
+def fill(cache, byte=0xFF):
+    """What was never written may be anything: scales and bases of NaN."""
+    cache.fill_(byte)
+    return cache
+
+
+def put(ks, vs, cache, dtype):
+    """Append whole sequences (lists of [L, n_kv, d])."""
+    ls = [k.shape[0] for k in ks]
+    qs, kl, T = batch(ls, ls)
+    if T:
+        moe.moe_kv4_append(torch.cat(ks).to(dtype).cuda(), torch.cat(vs).to(dtype).cuda(), cache, kl, q_start=qs)
+
+
+# ---------------------------------------------------------------------------------------- refusals (CPU) ---
+OK_PTR = 1 << 20  # an aligned address that no refused call touches
+
+
+def refused(name, *args):
+    code = getattr(moe.lib(), name)(*args)
+    assert code == -1, (name, args, code)
+    assert moe.lib().moe_last_error()
+
+
+def test_cache_bytes():
+    assert moe.moe_kv4_cache_bytes(1, 1, 64, 32) == 36 * 64
+    assert moe.moe_kv4_cache_bytes(3, 4, 128, 4096) == 3 * 4 * 128 * 36 * 128
+    assert moe.moe_kv4_cache_bytes(1024, 64, 256, 1 << 26) == 1024 * 64 * (1 << 21) * 36 * 256  # past 32 bits
+    for bad in [(1, 1, 63, 32), (1, 1, 96, 32), (1, 1, 320, 32), (1, 0, 64, 32), (-1, 1, 64, 32), (1, 1, 64, 0),
+                (1, 1, 64, 33), (1, 1, 64, (1 << 26) + 32), (65536, 1, 64, 32), (1, 65536, 64, 32)]:
+        assert moe.moe_kv4_cache_bytes(*bad) == 0, bad
+    with pytest.raises(moe.MoeError):
+        moe.kv4_cache(1, 1, 80, 32, device="cpu")
+    assert moe.kv4_cache(2, 3, 64, 96, device="cpu").shape == (2, 3, 3, 36 * 64)
+
+
+def test_append_and_read_refusals():
+    big = 1 << 40
+    good = dict(k=OK_PTR, v=OK_PTR, dtype=0, ks=256, vs=256, T=4, n_seq=2, n_kv=4, d=64, mp=64, q_start=OK_PTR, max_q=4,
+                kv_len=OK_PTR, cache=OK_PTR, bytes=big)
+    bads = [dict(k=None), dict(v=None), dict(k=OK_PTR + 8), dict(dtype=2), dict(dtype=-1), dict(ks=255), dict(vs=258),
+            dict(ks=252), dict(T=-1), dict(n_seq=-1), dict(n_kv=0), dict(d=32), dict(d=100), dict(mp=48), dict(mp=0),
+            dict(q_start=None), dict(max_q=0), dict(max_q=-3), dict(max_q=(1 << 24) + 1), dict(kv_len=None),
+            dict(cache=None), dict(cache=OK_PTR + 4), dict(bytes=2 * 4 * 2 * 36 * 64 - 1), dict(n_seq=70000)]
+    for b in bads:
+        a = {**good, **b}
+        refused("moe_kv4_append", a["k"], a["v"], a["dtype"], a["ks"], a["vs"], a["T"], a["n_seq"], a["n_kv"], a["d"],
+                a["mp"], a["q_start"], a["max_q"], a["kv_len"], a["cache"], a["bytes"], None)
+        if b in (dict(k=None), dict(v=None)):
+            continue
+        refused("moe_kv4_read", a["cache"], a["bytes"], a["T"], a["n_seq"], a["n_kv"], a["d"], a["mp"], a["q_start"],
+                a["max_q"], a["kv_len"], a["k"], a["v"], a["dtype"], a["ks"], a["vs"], None)
+    refused("moe_kv4_read", OK_PTR, big, 4, 2, 4, 64, 64, OK_PTR, 4, OK_PTR, None, None, 0, 256, 256, None)
+    # nothing to do: no pointer is looked at
+    assert moe.lib().moe_kv4_append(None, None, 0, 0, 0, 0, 2, 4, 64, 64, OK_PTR, 0, None, None, 0, None) == 0
+    assert moe.lib().moe_kv4_read(None, 0, 0, 0, 4, 64, 64, None, 0, None, None, None, 0, 0, 0, None) == 0
+
+
+def test_attention_refusals():
+    big = 1 << 40
+    good = dict(q=OK_PTR, dtype=1, qs=512, cache=OK_PTR, bytes=big, T=2, n_seq=2, heads=8, n_kv=4, d=64, mp=4096,
+                q_start=None, max_q=1, kv_len=OK_PTR, window=0, scale=0.125, out=OK_PTR, os=512, ws=OK_PTR, wb=big)
+    bads = [dict(q=None), dict(out=None), dict(q=OK_PTR + 2), dict(out=OK_PTR + 8), dict(qs=508), dict(os=516),
+            dict(dtype=3), dict(T=3), dict(heads=9), dict(heads=0), dict(n_kv=0), dict(d=48), dict(mp=4097),
+            dict(window=-1), dict(window=(1 << 30) + 1), dict(scale=math.inf), dict(scale=math.nan), dict(cache=None),
+            dict(kv_len=None), dict(bytes=100), dict(ws=None), dict(ws=OK_PTR + 4), dict(wb=16),
+            dict(q_start=OK_PTR, max_q=0), dict(q_start=OK_PTR, max_q=1 << 24)]
+    for b in bads:
+        a = {**good, **b}
+        refused("moe_kv4_attention", a["q"], a["dtype"], a["qs"], a["cache"], a["bytes"], a["T"], a["n_seq"], a["heads"],
+                a["n_kv"], a["d"], a["mp"], a["q_start"], a["max_q"], a["kv_len"], a["window"], a["scale"], a["out"],
+                a["os"], a["ws"], a["wb"], None)
+    assert moe.moe_kv4_attention_workspace_bytes(2, 2, 8, 4, 64, 1, 4096) > 0
+    assert moe.moe_kv4_attention_workspace_bytes(2, 2, 9, 4, 64, 1, 4096) == 0
+    assert moe.moe_kv4_attention_workspace_bytes(2, 2, 8, 4, 65, 1, 4096) == 0
+    assert moe.lib().moe_kv4_attention(None, 0, 0, None, 0, 0, 0, 8, 4, 64, 32, None, 0, None, 0, 1.0, None, 0, None, 0, None) == 0
+
+
+def test_matvec_and_block_refusals():
+    far = OK_PTR + (1 << 30)
+    for a in [(OK_PTR, OK_PTR, 17, 64, 128, None, far, 0), (OK_PTR, OK_PTR, -1, 64, 128, None, far, 0),
+              (OK_PTR, OK_PTR, 1, -1, 128, None, far, 0), (OK_PTR, OK_PTR, 1, 64, 64, None, far, 0),
+              (OK_PTR, OK_PTR, 1, 64, 0, None, far, 0), (None, OK_PTR, 1, 64, 128, None, far, 0),
+              (OK_PTR, None, 1, 64, 128, None, far, 0), (OK_PTR, OK_PTR, 1, 64, 128, None, None, 0),
+              (OK_PTR + 4, OK_PTR, 1, 64, 128, None, far, 0), (OK_PTR, OK_PTR + 8, 1, 64, 128, None, far, 0),
+              (OK_PTR, OK_PTR, 1, 64, 128, None, far + 2, 0), (OK_PTR, OK_PTR, 1, 64, 128, far + 1, far, 0),
+              (OK_PTR, OK_PTR, 1, 64, 128, None, OK_PTR, 0), (OK_PTR, OK_PTR, 1, 64, 128, None, OK_PTR + 508, 0)]:
+        refused("moe_matvec_int4", *a, None)
+    assert moe.lib().moe_matvec_int4(None, None, 0, 64, 128, None, None, 0, None) == 0
+    assert moe.lib().moe_matvec_int4(None, None, 3, 0, 128, None, None, 0, None) == 0
+    big = 1 << 40
+    good = dict(x=OK_PTR, T=2, H=256, nh=4, kv=2, d=64, wq=OK_PTR, wo=OK_PTR, cache=OK_PTR, cb=big, mp=64, kl=OK_PTR,
+                theta=1e4, ws=OK_PTR, wb=big)
+    for b in [dict(x=None), dict(x=OK_PTR + 4), dict(T=17), dict(T=-1), dict(H=200), dict(nh=5), dict(kv=0), dict(d=80),
+              dict(nh=1, kv=1), dict(wq=None), dict(wo=OK_PTR + 2), dict(cache=None), dict(cb=10), dict(mp=50),
+              dict(kl=None), dict(theta=1.0), dict(theta=math.nan), dict(ws=None), dict(wb=100), dict(nh=1026, kv=2)]:
+        a = {**good, **b}
+        refused("moe_attention_decode_int4", a["x"], a["T"], a["H"], a["nh"], a["kv"], a["d"], a["wq"], a["wo"], a["cache"],
+                a["cb"], a["mp"], a["kl"], a["theta"], a["ws"], a["wb"], None)
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, 4, 2, 64, 64) > 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(17, 4, 2, 64, 64) == 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, 4, 2, 96, 64) == 0
+
+
+def test_binding_refuses_host_tensors_and_shapes():
+    cache = moe.kv4_cache(1, 2, 64, 32, device="cpu")
+    k = torch.zeros((1, 2, 64))
+    kl = torch.ones(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        moe.moe_kv4_append(k, k, cache, kl)
+    with pytest.raises(ValueError):
+        moe.moe_kv4_append(k, k, cache[..., :-4], kl)
+    with pytest.raises(ValueError):
+        moe.moe_kv4_attention(k, cache.view(torch.int8), kl)
+    with pytest.raises(ValueError):
+        moe.moe_matvec_int4(torch.zeros((1, 128)), torch.zeros(64 * 64 + 128, dtype=torch.uint8), 64)
+
+
+# ------------------------------------------------------------------------------------------ store (GPU) ---
+def vectors(shape, gen, kind):
+    x = torch.randn(shape, generator=gen)
+    if kind == "wide":     # ranges of very different size, group by group
+        x = x * torch.exp2(torch.randint(-60, 60, (*shape[:-1], shape[-1] // 64, 1), generator=gen).float()).expand(
+            *shape[:-1], shape[-1] // 64, 64).reshape(shape)
+    elif kind == "ties":   # quotients that lie on a half
+        x = torch.randint(0, 31, shape, generator=gen).float() * 0.5
+        x[..., 0::64], x[..., 1::64] = 0.0, 15.0
+        x = x * torch.exp2(torch.randint(-3, 3, (1,), generator=gen).float())
+    elif kind == "offset":  # a base far from the range
+        x = x * 0.01 + 100.0
+    elif kind == "equal":   # no range at all, in some groups
+        x[..., :64] = x[..., :1]
+    elif kind == "tiny":
+        x = x * 2.0 ** -124
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,n_kv", [(64, 1), (128, 3), (192, 2), (256, 2)])
+@pytest.mark.parametrize("kind", ["normal", "wide", "ties", "offset", "equal", "tiny"])
+def test_append_then_read_gives_the_defined_values(dtype, d, n_kv, kind):
+    gen = torch.Generator().manual_seed(d + n_kv)
+    ls = [1, 31, 32, 33, 100, 0, 64]
+    ks = [vectors((L, n_kv, d), gen, kind).to(dtype) for L in ls]
+    vs = [vectors((L, n_kv, d), gen, kind).to(dtype) for L in ls]
+    cache = fill(moe.kv4_cache(len(ls), n_kv, d, 128))
+    put(ks, vs, cache, dtype)
+    qs, kl, T = batch(ls, ls)
+    k, v = moe.moe_kv4_read(cache, kl, T, q_start=qs, dtype=dtype)
+    moe.moe_sync_check()
+    assert torch.equal(k.cpu(), held(torch.cat(ks)).float().to(dtype))
+    assert torch.equal(v.cpu(), held(torch.cat(vs)).float().to(dtype))
+
+
+@pytest.mark.gpu
+def test_append_in_pieces_equals_at_once_and_leaves_the_rest():
+    """Tokens that start and end inside a block, one at a time and in chunks: the same bytes as in one call."""
+    gen = torch.Generator().manual_seed(5)
+    n_kv, d, L = 2, 128, 150
+    k, v = (torch.randn((L, n_kv, d), generator=gen).cuda() for _ in range(2))
+    whole, parts = (moe.kv4_cache(1, n_kv, d, 160) for _ in range(2))
+    whole.zero_()
+    parts.zero_()
+    moe.moe_kv4_append(k, v, whole, torch.tensor([L], dtype=torch.int32).cuda(),
+                       q_start=torch.tensor([0, L], dtype=torch.int32).cuda())
+    at = 0
+    for n in [1, 1, 5, 30, 1, 33, 64, 14, 1]:
+        at += n
+        moe.moe_kv4_append(k[at - n:at], v[at - n:at], parts, torch.tensor([at], dtype=torch.int32).cuda(),
+                           q_start=torch.tensor([0, n], dtype=torch.int32).cuda())
+    assert at == L and torch.equal(whole, parts)
+    before = parts.clone()
+    moe.moe_kv4_append(k[:1], v[:1], parts, torch.tensor([40], dtype=torch.int32).cuda())
+    kl = torch.tensor([L], dtype=torch.int32).cuda()
+    qs = torch.tensor([0, L], dtype=torch.int32).cuda()
+    a, b = moe.moe_kv4_read(before, kl, L, q_start=qs), moe.moe_kv4_read(parts, kl, L, q_start=qs)
+    for x, y, src in ((a[0], b[0], k), (a[1], b[1], v)):
+        assert torch.equal(torch.cat([x[:39], x[40:]]), torch.cat([y[:39], y[40:]]))
+        assert torch.equal(y[39].cpu(), held(src[:1].cpu()).float().to(BF16)[0])
+    moe.moe_sync_check()
+
+
+@pytest.mark.gpu
+def test_store_padding_untouched_rows_strides_and_bad_lengths():
+    gen = torch.Generator().manual_seed(6)
+    n_kv, d = 3, 64
+    ns, ls = [4, 0, 3, 2], [2, 7, 40, 2]  # the first sequence's first two tokens are padding
+    qs, kl, T = batch(ns, ls, extra=3)    # three rows behind the last sequence
+    wide = torch.randn((T, 5, n_kv, d), generator=gen).cuda()
+    k, v = wide[:, 1], wide[:, 3]         # tokens strided, as in a fused projection
+    cache = fill(moe.kv4_cache(4, n_kv, d, 64))
+    moe.moe_kv4_append(k, v, cache, kl, q_start=qs)
+    out = torch.full((T, 2, n_kv, d), 7.0, device="cuda")
+    moe.moe_kv4_read(cache, kl, T, q_start=qs, k_out=out[:, 0], v_out=out[:, 1])
+    moe.moe_sync_check()
+    for x, y in ((k, out[:, 0]), (v, out[:, 1])):
+        ref = held(x.cpu()).float()
+        ref[:2] = 0
+        ref[9:] = 7.0
+        assert torch.equal(y.cpu(), ref)
+    # a length past the cache stores nothing and reads as zeros; a token range that does not fit is empty
+    before = cache.clone()
+    bad_len = torch.tensor([2, 7, 65, -1], dtype=torch.int32).cuda()
+    moe.moe_kv4_append(k[4:], v[4:], cache, bad_len, q_start=torch.tensor([0, 0, 0, 3, 5], dtype=torch.int32).cuda())
+    with pytest.raises(moe.MoeError) as e:
+        moe.moe_sync_check()
+    assert e.value.code == -2 and torch.equal(before, cache)
+    for start in ([0, 0, 0, 0, 99], [-1, 0, 0, 0, 0], [0, 4, 2, 2, 2], [0, 0, 0, 0, 5]):
+        kw = dict(max_q=4) if start[-1] == 5 else {}
+        got = torch.full((6, n_kv, d), 7.0, device="cuda")
+        moe.moe_kv4_read(cache, kl, 6, q_start=torch.tensor(start, dtype=torch.int32).cuda(), k_out=got, **kw)
+        with pytest.raises(moe.MoeError) as e:
+            moe.moe_sync_check()
+        assert e.value.code == -2
+        bad = [i for i in range(4) if start[i] < 0 or start[i + 1] < start[i] or start[i + 1] > 6 or start[i + 1] - start[i] > kw.get("max_q", 6)]
+        for i in range(4):
+            if i in bad and start[i] >= 0 and start[i + 1] > start[i]:
+                assert (got[start[i]:] == 7.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, 3.4e38])
+def test_append_of_values_that_are_not_finite(value):
+    gen = torch.Generator().manual_seed(7)
+    k, v = torch.randn((40, 2, 128), generator=gen), torch.randn((40, 2, 128), generator=gen)
+    k[3, 1, 70], v[35, 0, 1] = value, value
+    if value == 3.4e38:  # finite, but the range is not
+        k[3, 1, 71], v[35, 0, 2] = -value, -value
+    cache = fill(moe.kv4_cache(1, 2, 128, 64))
+    qs, kl, T = batch([40], [40])
+    moe.moe_kv4_append(k.cuda(), v.cuda(), cache, kl, q_start=qs)
+    with pytest.raises(moe.MoeError) as e:
+        moe.moe_sync_check()
+    assert e.value.code == -3
+    a, b = moe.moe_kv4_read(cache, kl, T, q_start=qs, dtype=F32)
+    assert (a[3, 1, 64:] == 0).all() and (b[35, 0, :64] == 0).all()
+    assert torch.equal(a.cpu(), held(k).float()) and torch.equal(b.cpu(), held(v).float())
+    moe.moe_sync_check()
+
+
+# -------------------------------------------------------------------------------------- attention (GPU) ---
+CASES = [  # (d, n_kv, group, tokens, lengths, max_pos, window)
+    (128, 2, 8, [1, 1, 1], [1, 33, 300], 512, 0),
+    (128, 1, 16, [1], [97], 128, 0),
+    (64, 2, 1, [1, 1], [64, 5], 64, 0),
+    (64, 3, 7, [3, 5, 0, 2], [3, 200, 9, 41], 224, 0),
+    (128, 2, 3, [20, 1, 7], [20, 70, 64], 96, 0),
+    (128, 1, 8, [70], [133], 160, 0),
+    (128, 1, 20, [2, 9], [150, 9], 160, 0),
+    (192, 1, 4, [1, 6], [40, 66], 96, 0),
+    (256, 2, 2, [1, 17], [65, 40], 96, 0),
+    (256, 1, 8, [5], [45], 64, 0),
+    (128, 2, 4, [1, 40], [200, 100], 256, 33),
+    (64, 1, 2, [4, 4], [130, 64], 160, 1),
+    (64, 2, 4, [6, 5, 3, 1], [2, 0, 3, 0], 32, 0),      # padded tokens, sequences without a position
+    (128, 1, 4, [40, 1], [7, 0], 64, 5),
+]
+
+
+def attention_case(d, n_kv, G, ns, ls, max_pos, window, dtype, seed=0, scale=None, amplitude=1.0):
+    gen = torch.Generator().manual_seed(seed + d)
+    ks = [torch.randn((L, n_kv, d), generator=gen) * amplitude + 0.3 for L in ls]
+    vs = [torch.randn((L, n_kv, d), generator=gen) for L in ls]
+    cache = fill(moe.kv4_cache(len(ls), n_kv, d, max_pos))
+    put(ks, vs, cache, F32)
+    q = torch.randn((sum(ns), n_kv * G, d), generator=gen).to(dtype)
+    ref, amount, shift = attend(q.double(), ks, vs, ns, ls, G, window, d ** -0.5 if scale is None else scale)
+    return cache, q, ref, attention_tolerance(ref, amount, shift, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_attention_matches_the_plain_form(case, dtype):
+    d, n_kv, G, ns, ls, max_pos, window = CASES[case]
+    cache, q, ref, tol = attention_case(*CASES[case], dtype)
+    qs, kl, T = batch(ns, ls)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns), window=window)
+    moe.moe_sync_check()
+    assert out.dtype is dtype
+    err = (out.cpu().double() - ref).abs()
+    assert (err <= tol).all(), float((err / tol).max())
+    t = 0
+    for n, L in zip(ns, ls):  # padding gives exact zeros
+        assert (out[t:t + max(0, n - L)] == 0).all()
+        t += n
+    if all(n == 1 for n in ns):  # the form without q_start, and a looser bound on the tokens
+        assert torch.equal(moe.moe_kv4_attention(q.cuda(), cache, kl, window=window), out)
+    # twice the same bits
+    assert torch.equal(moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns), window=window), out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_strides_rows_behind_and_loose_max_q(dtype):
+    case = (128, 2, 4, [3, 1, 2], [40, 1, 90], 96, 0)
+    cache, q, ref, tol = attention_case(*case, dtype)
+    qs, kl, T = batch(case[3], case[4], extra=2)
+    wide = torch.full((T, 24, 128), float("nan"), dtype=dtype, device="cuda")
+    wide[:6, 8:16] = q.cuda()
+    out = torch.full((T, 16, 128), 3.0, dtype=dtype, device="cuda")
+    moe.moe_kv4_attention(wide[:, 8:16], cache, kl, q_start=qs, out=out[:, 4:12])
+    moe.moe_sync_check()
+    assert ((out[:6, 4:12].cpu().double() - ref).abs() <= tol).all()
+    assert (out[6:] == 3).all() and (out[:, :4] == 3).all() and (out[:, 12:] == 3).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
+def test_attention_scales(dtype, scale):
+    """Scores that are all equal, turned round, and so far apart that few positions count."""
+    case = (128, 1, 4, [2, 1], [70, 40], 96, 0)
+    cache, q, ref, tol = attention_case(*case, dtype, scale=scale)
+    qs, kl, _ = batch(case[3], case[4])
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, scale=scale)
+    assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 9])
+def test_attention_long_and_split(n):
+    """Enough positions that they are split over blocks, and a maximum that moves from split to split."""
+    gen = torch.Generator().manual_seed(11)
+    d, n_kv, G, L = 128, 1, 2, 5000
+    k = torch.randn((L, n_kv, d), generator=gen) * 0.2
+    k[4321] += 2.0
+    v = torch.randn((L, n_kv, d), generator=gen)
+    cache = fill(moe.kv4_cache(1, n_kv, d, 5024))
+    put([k], [v], cache, F32)
+    q = torch.randn((n, G, d), generator=gen)
+    ref, amount, shift = attend(q.double(), [k], [v], [n], [L], G, 0, d ** -0.5)
+    qs, kl, _ = batch([n], [L])
+    assert moe.moe_kv4_attention_workspace_bytes(n, 1, G, n_kv, d, n, 5024) > 0
+    for dtype in (F32, BF16):
+        qd = q.to(dtype)
+        if dtype is BF16:
+            ref, amount, shift = attend(qd.double(), [k], [v], [n], [L], G, 0, d ** -0.5)
+        out = moe.moe_kv4_attention(qd.cuda(), cache, kl, q_start=qs, max_q=n)
+        err = (out.cpu().double() - ref).abs()
+        tol = attention_tolerance(ref, amount, shift, dtype)
+        assert (err <= tol).all(), float((err / tol).max())
+    moe.moe_sync_check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_bad_batch_and_values(dtype):
+    case = (64, 1, 2, [2, 1, 1], [10, 40, 3], 64, 0)
+    cache, q, ref, tol = attention_case(*case, dtype)
+    qs, kl, T = batch(case[3], case[4])
+    bad = kl.clone()
+    bad[1] = 65
+    out = moe.moe_kv4_attention(q.cuda(), cache, bad, q_start=qs)
+    with pytest.raises(moe.MoeError) as e:
+        moe.moe_sync_check()
+    assert e.value.code == -2
+    assert (out[2] == 0).all()
+    good = [0, 1, 3]
+    assert ((out.cpu().double() - ref).abs() <= tol)[good].all()
+    out = torch.full_like(out, 5.0)
+    moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=torch.tensor([0, 2, 1, 9], dtype=torch.int32).cuda(), out=out)
+    with pytest.raises(moe.MoeError) as e:
+        moe.moe_sync_check()
+    assert e.value.code == -2 and (out[2:] == 5).all()
+    assert ((out.cpu().double() - ref).abs() <= tol)[:2].all()
+    # a query that is not finite spoils its own head's row and no other
+    for value in (math.nan, math.inf):
+        qb = q.clone()
+        qb[0, 1, 5] = value
+        out = moe.moe_kv4_attention(qb.cuda(), cache, kl, q_start=qs).cpu().double()
+        ok = torch.ones((T, 2), dtype=torch.bool)
+        ok[0, 1] = False
+        assert ((out - ref).abs() <= tol)[ok].all() and not torch.isfinite(out[0, 1]).any()
+    moe.moe_sync_check()
+
+
+# ----------------------------------------------------------------------------------- int4 products (GPU) ---
+def matvec_reference(x, w, add, norm):
+    """Value and bound: exact products of (24 + q) s x in fp32 sums: a group's sum of at most 12 partial results
+    plus 24 times the sum of x, the groups' scaled sums (K / 128 of them), the terms and the norm: 2^-24 of
+    what they amount to for each of at most 32 + K / 128 roundings."""
+    h = x.double()
+    r = torch.ones((x.shape[0], 1), dtype=torch.float64)
+    if norm:
+        r = 1 / torch.sqrt(h.square().mean(1, keepdim=True) + EPS)
+    K = x.shape[1]
+    q, s = w
+    y = (h * r) @ (q * s).T
+    amount = (h.abs() * r) @ ((48 + q.abs()) * s.abs()).T
+    tol = amount * (32 + K // 128) * 2.0 ** -24 + y.abs() * 2.0 ** -21
+    if add is not None:
+        y = y + add.double()
+    return y, tol + y.abs() * 2.0 ** -24
+
+
+def int4_parts(raw, N, K):
+    b = raw[:N * K // 2].to(torch.int32)
+    q = torch.stack([b & 15, b >> 4], -1).flatten().view(N, K)
+    q = torch.where(q > 7, q - 16, q).double()
+    s = raw[N * K // 2:].clone().view(BF16).double().view(N, K // 128).repeat_interleave(128, 1)
+    return q, s
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 2, 3, 5, 6, 8, 11, 16])
+@pytest.mark.parametrize("N,K", [(1, 128), (15, 256), (17, 2048), (100, 1408), (33, 4224), (16, 8192)])
+def test_matvec_matches_the_plain_form(T, N, K):
+    gen = torch.Generator().manual_seed(T * 1000 + N)
+    raw, _ = int4_matrix(N, K, gen)
+    parts = int4_parts(raw, N, K)
+    x = torch.randn((T, K), generator=gen) * torch.exp2(torch.randint(-20, 20, (T, 1), generator=gen).float())
+    add = torch.randn((T, N), generator=gen)
+    wd, xd, ad = raw.cuda(), x.cuda(), add.cuda()
+    for norm in (False, True):
+        for a in (None, add):
+            y = moe.moe_matvec_int4(xd, wd, N, add=None if a is None else ad, rmsnorm=norm)
+            ref, tol = matvec_reference(x, parts, a, norm)
+            err = (y.cpu().double() - ref).abs()
+            assert (err <= tol).all(), float((err / tol).max())
+    y = ad.clone()  # in place on what is added
+    moe.moe_matvec_int4(xd, wd, N, y=y, add=y)
+    assert torch.equal(y, moe.moe_matvec_int4(xd, wd, N, add=ad))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 7])
+def test_matvec_many_rows(T):
+    """Enough rows that blocks take several items."""
+    gen = torch.Generator().manual_seed(T)
+    N, K = 40007, 512
+    raw, _ = int4_matrix(N, K, gen)
+    parts = int4_parts(raw, N, K)
+    x = torch.randn((T, K), generator=gen)
+    y = torch.full((T * N + 64,), 9.0, device="cuda")
+    moe.moe_matvec_int4(x.cuda(), raw.cuda(), N, y=y[:T * N].view(T, N), rmsnorm=True)
+    ref, tol = matvec_reference(x, parts, None, True)
+    err = (y[:T * N].view(T, N).cpu().double() - ref).abs()
+    assert (err <= tol).all() and (y[T * N:] == 9).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 9])
+def test_matvec_values_that_are_not_finite_or_huge(T):
+    gen = torch.Generator().manual_seed(3)
+    N, K = 40, 256
+    raw, _ = int4_matrix(N, K, gen)
+    q, s = int4_parts(raw, N, K)
+    x = torch.randn((T, K), generator=gen)
+    x[0, 5] = math.inf
+    x[1] = x[1] * 1e38
+    y = moe.moe_matvec_int4(x.cuda(), raw.cuda(), N).cpu().double()
+    w0 = (q * s)[:, 5]
+    assert torch.equal(torch.isnan(y[0]), w0 == 0)
+    assert (y[0][w0 > 0] == math.inf).all() and (y[0][w0 < 0] == -math.inf).all()
+    ref, tol = matvec_reference(x[1:], (q, s), None, False)
+    fits = ref.abs() < 3.0e38  # (what does not fit may come out infinite)
+    assert ((y[1:] - ref).abs() <= tol)[fits].all()
+
+
+# ------------------------------------------------------------------------- graphs, streams, together (GPU) ---
+@pytest.mark.gpu
+def test_captured_decode_step_replays_with_new_lengths():
+    """Projection, append and attention of a batch captured once: replays at other lengths and inputs, with eager
+    work of the same kind between them, equal the eager calls."""
+    gen = torch.Generator().manual_seed(21)
+    B, n_kv, G, d, H, max_pos = 3, 2, 4, 64, 256, 2048
+    rows = (G + 2) * n_kv * d
+    raw, _ = int4_matrix(rows, H, gen, 0.1)
+    raw = raw.cuda()
+    cache = fill(moe.kv4_cache(B, n_kv, d, max_pos))
+    lens = [5, 700, 1900]
+    put([torch.randn((L, n_kv, d), generator=gen) for L in lens], [torch.randn((L, n_kv, d), generator=gen) for L in lens],
+        cache, F32)
+    x = torch.randn((B, H), generator=gen).cuda()
+    kv_len = torch.tensor(lens, dtype=torch.int32).cuda() + 1
+    ws = torch.empty(max(256, moe.moe_kv4_attention_workspace_bytes(B, B, G * n_kv, n_kv, d, 1, max_pos)),
+                     dtype=torch.uint8, device="cuda")
+    qkv, out = torch.empty((B, rows), device="cuda"), torch.empty((B, G * n_kv, d), device="cuda")
+
+    def step(cache, x, kv_len, qkv, out, ws):
+        moe.moe_matvec_int4(x, raw, rows, y=qkv, rmsnorm=True)
+        t = qkv.view(B, -1, d)
+        moe.moe_kv4_append(t[:, G * n_kv:(G + 1) * n_kv], t[:, (G + 1) * n_kv:], cache, kv_len)
+        moe.moe_kv4_attention(t[:, :G * n_kv], cache, kv_len, out=out, workspace=ws)
+
+    eager = cache.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(cache, x, kv_len, qkv, out, ws)
+    ref = torch.empty_like(out)
+    for i in range(4):
+        x.copy_(torch.randn((B, H), generator=gen))
+        if i:
+            kv_len += 1
+        graph.replay()
+        step(eager, x, kv_len, torch.empty_like(qkv), ref, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+    assert torch.equal(cache, eager)
+    moe.moe_sync_check()
+
+
+@pytest.mark.gpu
+def test_calls_on_another_stream():
+    gen = torch.Generator().manual_seed(22)
+    k = torch.randn((64, 2, 128), generator=gen).cuda()
+    q = torch.randn((64, 4, 128), generator=gen).cuda()
+    qs, kl, T = batch([64], [64])
+    cache, other = moe.kv4_cache(1, 2, 128, 64), moe.kv4_cache(1, 2, 128, 64)
+    moe.moe_kv4_append(k, k, cache, kl, q_start=qs)
+    ref = moe.moe_kv4_attention(q, cache, kl, q_start=qs)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    moe.moe_kv4_append(k, k, other, kl, q_start=qs, stream=side)
+    out = moe.moe_kv4_attention(q, other, kl, q_start=qs, stream=side.cuda_stream)
+    back = moe.moe_kv4_read(other, kl, T, q_start=qs, stream=side)
+    side.synchronize()
+    assert torch.equal(out, ref) and torch.equal(back[0], moe.moe_kv4_read(cache, kl, T, q_start=qs)[0])
+    moe.moe_sync_check(side)
+
+
+def rope(v, p, theta):
+    d = v.shape[-1]
+    ang = p * theta ** (-2 * torch.arange(d // 2, dtype=torch.float64) / d)
+    a, b = v[..., :d // 2], v[..., d // 2:]
+    return torch.cat([a * torch.cos(ang) - b * torch.sin(ang), b * torch.cos(ang) + a * torch.sin(ang)], -1)
+
+
+def normed(v):
+    return v / torch.sqrt(v.square().mean(-1, keepdim=True) + EPS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n_kv,G,lens", [(128, 2, 4, [1, 70, 33]), (64, 1, 2, [100]), (256, 1, 2, [5, 64]), (192, 2, 1, [40]),
+                                           (128, 1, 8, [0, 12, 96, 31, 32, 1])])
+def test_block_matches_its_parts(d, n_kv, G, lens):
+    """The block's new keys and values lie within a step of the quantiser of the 64-bit ones, and its output is that
+    of 64-bit attention over what the cache then holds."""
+    gen = torch.Generator().manual_seed(d + G)
+    T, H, nh, max_pos, theta = len(lens), 256, G * n_kv, 128, 1.0e4
+    rows = (nh + 2 * n_kv) * d
+    rq, wq = int4_matrix(rows, H, gen, 0.05)
+    ro, wo = int4_matrix(H, nh * d, gen, 0.05)
+    cache = fill(moe.kv4_cache(T, n_kv, d, max_pos))
+    put([torch.randn((max(L - 1, 0), n_kv, d), generator=gen) for L in lens],
+        [torch.randn((max(L - 1, 0), n_kv, d), generator=gen) for L in lens], cache, F32)
+    x = torch.randn((T, H), generator=gen)
+    xd, kl = x.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    moe.moe_attention_decode_int4(xd, rq.cuda(), ro.cuda(), cache, kl, nh, theta)
+    moe.moe_sync_check()
+    qs, _, n = batch(lens, lens)
+    K, V = (t.cpu().double() for t in moe.moe_kv4_read(cache, kl, n, q_start=qs, dtype=F32))
+    qkv = (normed(x.double()) @ wq.T).view(T, -1, d)
+    y = x.double().clone()
+    at = 0
+    for t, L in enumerate(lens):
+        if L:
+            q = rope(normed(qkv[t, :nh]), L - 1, theta)
+            kn, vn = rope(normed(qkv[t, nh:nh + n_kv]), L - 1, theta), qkv[t, nh + n_kv:]
+            for got, want in ((K[at + L - 1], kn), (V[at + L - 1], vn)):
+                w = want.view(n_kv, -1, GROUP)
+                step = (w.amax(-1, keepdim=True) - w.amin(-1, keepdim=True)) / 15
+                # half a step, the scale's rounding over 15 steps, the base's
+                bound = step * (0.5 + 15 * 2.0 ** -8) + w.abs().amax(-1, keepdim=True) * 2.0 ** -8 + 1e-5
+                assert ((got.view_as(w) - w).abs() <= bound).all()
+            att = torch.empty((nh, d), dtype=torch.float64)
+            for h in range(nh):
+                p = torch.softmax(K[at:at + L, h // G] @ q[h] / math.sqrt(d), 0)
+                att[h] = p @ V[at:at + L, h // G]
+            y[t] += wo @ att.flatten()
+        at += L
+    # 2^-16 of the probabilities' terms, scores within 2^-16 and the projections' sums, on outputs of sum |w| |att|
+    tol = wo.abs().sum(1).max() * 4.0 * 2.0 ** -14 / math.sqrt(nh * d) + 1e-5
+    assert ((xd.cpu().double() - y).abs() <= tol).all(), float((xd.cpu().double() - y).abs().max() / tol)
+    for t, L in enumerate(lens):
+        if L == 0:
+            assert torch.equal(xd[t].cpu(), x[t])
+
+
+@pytest.mark.gpu
+def test_block_bad_length_changes_nothing_else():
+    gen = torch.Generator().manual_seed(1)
+    d, n_kv, G, H, T = 64, 2, 2, 128, 2
+    rq, _ = int4_matrix((G + 2) * n_kv * d, H, gen)
+    ro, _ = int4_matrix(H, G * n_kv * d, gen)
+    cache = moe.kv4_cache(T, n_kv, d, 32)
+    cache.zero_()
+    x = torch.randn((T, H), generator=gen).cuda()
+    one, good = x.clone(), cache.clone()
+    moe.moe_attention_decode_int4(one, rq.cuda(), ro.cuda(), good, torch.tensor([4, 0], dtype=torch.int32).cuda(), G * n_kv)
+    moe.moe_sync_check()
+    for L in (33, -2):
+        y, c = x.clone(), cache.clone()
+        moe.moe_attention_decode_int4(y, rq.cuda(), ro.cuda(), c, torch.tensor([4, L], dtype=torch.int32).cuda(), G * n_kv)
+        with pytest.raises(moe.MoeError) as e:
+            moe.moe_sync_check()
+        assert e.value.code == -2
+        assert torch.equal(y, one) and torch.equal(c, good)
+
+
+@pytest.mark.gpu
+def test_stack_with_int4_attention_equals_its_blocks():
+    """A decode stack with int4 attention blocks: every step is the block, then a stack of that layer alone."""
+    gen = torch.Generator().manual_seed(31)
+    L, H, I, E, k, d, n_kv, G, max_pos, steps = 2, 256, 128, 8, 2, 64, 2, 2, 64, 5
+    nh = G * n_kv
+    expert = 3 * H * I * 2
+    host = moe.PinnedBuffer(L * E * expert)
+    w = (torch.randn(L * E * 3 * H * I, generator=gen) * 0.02).to(BF16)
+    host.array[:] = w.view(torch.uint8).numpy()
+    router = [(torch.randn((E, H), generator=gen) * 0.05).to(BF16).cuda() for _ in range(L)]
+    wq = [int4_matrix((nh + 2 * n_kv) * d, H, gen)[0].cuda() for _ in range(L)]
+    wo = [int4_matrix(H, nh * d, gen)[0].cuda() for _ in range(L)]
+
+    def cache_of(l0, n):
+        return moe.ExpertCache(n, E, expert, n * E * expert, host.ptr + l0 * E * expert, E * expert, expert, preload=True)
+
+    kv = [moe.kv4_cache(1, n_kv, d, max_pos) for _ in range(L)]
+    for c in kv:
+        c.zero_()
+    ref_kv = [c.clone() for c in kv]
+    att = dict(n_heads=nh, n_kv=n_kv, head_dim=d, max_pos=max_pos, theta=1.0e4, start_pos=0, w_qkv=wq, w_o=wo, cache=kv, int4=True)
+    both = cache_of(0, L)
+    stack = moe.MoeStack(both, H, I, E, k, moe.MOE_BF16, moe.MOE_BF16, router, attention=att)
+    singles = [moe.MoeStack(cache_of(l, 1), H, I, E, k, moe.MOE_BF16, moe.MOE_BF16, router[l:l + 1]) for l in range(L)]
+    for t in range(steps):
+        x0 = torch.randn((1, H), generator=gen)
+        x, y = x0.cuda(), x0.cuda()
+        (stack.decode_graph if t == 3 else stack.decode_step)(t, x)
+        kl = torch.tensor([t + 1], dtype=torch.int32).cuda()
+        for l in range(L):
+            moe.moe_attention_decode_int4(y, wq[l], wo[l], ref_kv[l], kl, nh, 1.0e4)
+            singles[l].decode_step(t, y)
+        torch.cuda.synchronize()
+        assert torch.equal(x, y)
+        assert all(torch.equal(a, b) for a, b in zip(kv, ref_kv))
+    assert stack.kernel_time(4, 5) > 0
+    moe.moe_sync_check()
+    full = dict(att, start_pos=max_pos - 1)
+    stack = moe.MoeStack(both, H, I, E, k, moe.MOE_BF16, moe.MOE_BF16, router, attention=full)
+    stack.decode_step(0, torch.zeros((1, H), device="cuda"))
+    with pytest.raises(moe.MoeError):
+        stack.decode_step(1, torch.zeros((1, H), device="cuda"))
+    for bad in (dict(max_pos=48), dict(head_dim=48), dict(start_pos=max_pos), dict(cache=[moe.kv4_cache(2, n_kv, d, max_pos)] * 2)):
+        with pytest.raises((moe.MoeError, ValueError)):
+            moe.MoeStack(both, H, I, E, k, moe.MOE_BF16, moe.MOE_BF16, router, attention=dict(att, **bad))

@@ -294,9 +294,9 @@ MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, 
 
 /* Attention of the tokens over the cache: out = sum_p softmax_p(scale q . K_p) V_p over the positions p up to the
  * token's own, with window > 0 the last `window` of those (window <= 2^30); query head j reads key/value head
- * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums; the
- * products are exact (MOE_BF16 queries) or take queries as three bf16 terms (MOE_F32, exact too); probabilities
- * enter the value products as two bf16 terms (MOE_F32: within 2^-16) or rounded to bf16 (MOE_BF16: 2^-8).
+ * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums;
+ * queries enter exactly (MOE_BF16) or as two fp16 terms (MOE_F32: 2^-22 of the head's largest element), probabilities
+ * times scales rounded to fp16 (2^-11) or as two fp16 terms (2^-22).  Elements of q up to 2^100 in magnitude.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
  *   out        device, as q with out_stride, same dtype
  *   scale      any finite factor, as a rule 1 / sqrt(head_dim)

@@ -1,11 +1,18 @@
 // kv4_attention.hip -- attention over the 4-bit cache (layout in kv4.h), one or many tokens per sequence.
 //
-// With K = s_g u + m_g per group g of 64 dims, q . K_p = sum_g s_gp (q_g . u_gp) + m_gp (sum of q_g): the codes
-// enter the matrix products as they are (bf16 of 16 + u is one shift and one bit operation for two codes; the
-// products start at -16 times the sum of q_g), and the scales multiply fp32 sums of exact products.  The value
-// side is sum_p (P_p s_gp) u_p + P_p m_gp.  Scores are formed transposed (positions x rows), so that a lane
-// holds one row's probabilities of the positions that are its operand of the value product (P stays in
-// registers), and the outputs as dims x rows, so that a row's running maximum and sum belong to its lane.
+// With K = s_g u + m_g per group g of 64 dims, q . K_p = sum_g s_gp (q_g . u_gp) + m_gp (sum of q_g), and the value
+// side is sum_p (P_p s_gp) (u_p - 8) + P_p (m_gp + 8 s_gp).  Four bits at the bottom of an fp16 are the subnormal
+// u 2^-24 (at bits 4-7: 16 u 2^-24, the 16 taken out of the other operand), so one bit operation makes two operands
+// of a matrix product, and where they have to be normal or centred one packed fma does it; every product is exact.
+// Scores are formed transposed (positions x rows), so that a lane holds one row's probabilities of the positions that
+// are its operand of the value product (they stay in registers), and the outputs as dims x rows, so that a row's
+// running maximum and sum belong to its lane.
+//
+// fp16 reaches far enough because both other operands are scaled by powers of two: a row's query so that its
+// largest element is in [2^14, 2^15), the values' scales so that the largest the wave has met is at most 2^15
+// (the outputs so far are scaled along when that grows).  Queries: bf16 ones are exact, fp32 ones are two terms
+// (2^-22 of the row's largest).  P s: rounded to fp16 (2^-11, bf16 tensors) or two terms (2^-22).  What multiplies
+// the bases is fp32.
 //
 // A row is a (token, query head of the group) pair; a wave takes NT tiles of 16 rows over every fourth block
 // of 32 positions, and the block's waves join their (max, sum, output) through LDS.  With few rows the
@@ -15,6 +22,7 @@
 #include "kv4.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace moe {
 namespace {
@@ -22,287 +30,585 @@ namespace {
 using namespace kv4;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
-constexpr int kMaxSplits = 128;
+constexpr int kTarget = 512;  // blocks that fill the device, where rows and heads alone give fewer
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
+__device__ __forceinline__ floatx4 mfma(f16x8 a, f16x8 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-// bf16 16 + u of a word's eight codes: 16 is 0x4180, its mantissa's lowest bit but three is worth one.
-__device__ __forceinline__ bf16x8 codes16(uint32_t w) {
-    constexpr uint32_t M = 0x00780078u, B = 0x41804180u;
-    return operand(((w << 3) & M) | B, ((w >> 1) & M) | B, ((w >> 5) & M) | B, ((w >> 9) & M) | B);
+// The eight codes of a word as fp16: u 2^-24 (elements 0, 1, 4, 5) and 16 u 2^-24 (elements 2, 3, 6, 7).
+__device__ __forceinline__ f16x8 raw_codes(uint32_t w) {
+    constexpr uint32_t L = 0x000F000Fu, H = 0x00F000F0u;
+    const uint32_t v = w >> 8;
+    return __builtin_bit_cast(f16x8, make_uint4(w & L, w & H, v & L, v & H));
 }
-constexpr uint32_t kMinus16 = 0xC180C180u;  // bf16 -16 twice
+constexpr bool high_code(int i) { return i & 2; }
+// Keys.  A subnormal operand's products are aligned as if it were 2^-14: sums lose up to 10 of their bits, which the
+// scores of bf16 queries can spare (about 1e-5); fp32 queries meet u 2^-9 and 16 u 2^-9.
+template <bool F32> constexpr int kKeyExp = F32 ? -9 : -24;
+template <bool F32>
+__device__ __forceinline__ f16x8 key_codes(uint32_t w) {
+    const f16x8 u = raw_codes(w);
+    return F32 ? u * _Float16(0x1p15f) : u;
+}
+// Values: (u - 8) 2^-9.  Sums of P s u over a long cache would only grow, while what is left
+// of them after P m is the mean of values of either sign (of 131071 positions: hundreds of times less).
+constexpr int kValueExp = -9;
+__device__ __forceinline__ f16x8 value_codes(uint32_t w) {
+    constexpr _Float16 m = 0x1p15f, n = 0x1p11f, a = -0x1p-6f;
+    return raw_codes(w) * f16x8{m, m, n, n, m, m, n, n} + f16x8{a, a, a, a, a, a, a, a};
+}
 
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // round to nearest even
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 v = {__bf16(lo), __bf16(hi)};
     return __builtin_bit_cast(uint32_t, v);
 }
-__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// Eight fp32 values as TERMS bf16 operands, each rounding what the ones before it leave (one term: the
-// rounded values, within 2^-8; two terms leave at most 2^-16 of a value, three nothing of its 24 bits).
+__device__ __forceinline__ f16x2 pack_f16(float lo, float hi) {
+    const f16x2 v = {_Float16(lo), _Float16(hi)};
+    return v;
+}
+__device__ __forceinline__ f16x8 join8(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// a b, rounded: what is subtracted from it later meets the same number (contracted into an fma it would be another).
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+    float v = a * b;
+    asm("" : "+v"(v));
+    return v;
+}
+// Eight values as TERMS fp16 operands, the second rounding what the first leaves.
 template <int TERMS>
-__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&t)[TERMS]) {
-    float r[8];
+__device__ __forceinline__ void split(const float (&x)[8], f16x8 (&t)[TERMS]) {
+    f16x2 h[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = x[e];
+    for (int e = 0; e < 4; ++e) h[e] = pack_f16(x[2 * e], x[2 * e + 1]);
+    t[0] = join8(h[0], h[1], h[2], h[3]);
+    if constexpr (TERMS == 2) {
+        f16x2 l[4];
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
-            if (k + 1 < TERMS) {
-                r[2 * e] -= low_half(w[e]);
-                r[2 * e + 1] -= high_half(w[e]);
-            }
-        }
-        t[k] = operand(w[0], w[1], w[2], w[3]);
+        for (int e = 0; e < 4; ++e) l[e] = pack_f16(x[2 * e] - float(h[e][0]), x[2 * e + 1] - float(h[e][1]));
+        t[1] = join8(l[0], l[1], l[2], l[3]);
     }
+}
+
+// What f makes of v over the four lanes (n, 0..3).
+template <typename F>
+__device__ __forceinline__ float over_c(float v, F f) {
+    auto pair = [](auto r) { return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1])); };
+    float2 u = pair(__builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    v = f(u.x, u.y);
+    u = pair(__builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return f(u.x, u.y);
+}
+__device__ __forceinline__ float max_over_c(float v) {
+    return over_c(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_over_c(float v) {
+    return over_c(v, [](float a, float b) { return a + b; });
+}
+// The value of lane n ^ 8.
+template <typename T>
+__device__ __forceinline__ T other_half(T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xF, 0xF, false));
+}
+// Sums over the lanes up to this one.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+#define SCAN(CTRL, ROWS) v += uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, ROWS, 0xF, true))
+    SCAN(0x111, 0xF);  // row_shr:1
+    SCAN(0x112, 0xF);
+    SCAN(0x114, 0xF);
+    SCAN(0x118, 0xF);
+    SCAN(0x142, 0xA);  // row_bcast:15 into rows 1 and 3
+    SCAN(0x143, 0xC);  // row_bcast:31 into rows 2 and 3
+#undef SCAN
+    return v;
 }
 
 struct AttendArgs {
     const void *q;
     void *out;
     const uint8_t *cache;
-    float *part;  // [T][heads][splits][d + 4]: unnormalised output, maximum, sum (more than one split)
+    float *part;  // [unit][head][tile][16 NT rows][d + 4]: unnormalised output, maximum (log2), sum
     long long q_stride, out_stride;
-    int n_heads, n_kv, group, window, splits;
+    int n_heads, n_kv, group, window;
+    int target;  // splits of a whole batch (0: every sequence in one piece)
+    int tiles;   // row tiles of the largest sequence
     float scale;  // times log2(e)
     Batch batch;
     int *err;
 };
 
-// grid: (splits x row tiles, key/value head, sequence)
-template <int NG, int NT, bool F32>
-__global__ __launch_bounds__(kAttBlock) void kv4_attend_kernel(AttendArgs a) {
-    constexpr int d = NG * kGroup, QT = F32 ? 3 : 1, PT = F32 ? 2 : 1;
-    __shared__ float4 out_sh[kAttWaves][16][d / 4 + 1];
-    __shared__ float max_sh[kAttWaves][16], sum_sh[kAttWaves][16];
-    const Seq s = sequence(a.batch, blockIdx.z);
-    const int h = blockIdx.y, split_i = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
-    if (s.bad && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(a.err, kErrRange);
-    const int G = a.group, rows = s.n * G, row0 = tile * 16 * NT;
+// Blocks of positions that a sequence's tokens see.
+__device__ __forceinline__ int seen_blocks(const Seq &s, int window) {
+    if (s.n == 0 || s.len == 0) return 0;
+    return (s.len - 1) / kPos + 1 - (window ? max(0, s.len - s.n - window + 1) / kPos : 0);
+}
+
+// The split of a batch: sequences are cut into pieces of `chunk` blocks of positions, at least one per wave, so
+// that there are about `target` of them in all; a sequence has at least one piece.  Every wave works it out for
+// itself.  by_unit: which piece is number `want`; otherwise, the pieces of sequence `want`.
+struct Piece {
+    Seq s;
+    int seq, split, chunk;
+    int first, count;  // of the sequence's pieces (count 0: there is no such piece)
+};
+__device__ __forceinline__ Piece find_piece(const Batch &b, int window, int target, int want, bool by_unit, int *err) {
+    const int lane = threadIdx.x & 63;
+    uint32_t total = 0;  // (a batch that is split has fewer than kTarget sequences of at most 2^21 blocks)
+    Seq s{0, 0, 0, false};
+    int nb = 0;
+    auto look = [&](int base) {
+        s = Seq{0, 0, 0, false};
+        if (base + lane < b.n_seq) s = sequence(b, base + lane);
+        nb = seen_blocks(s, window);
+    };
+#pragma unroll 1
+    for (int base = 0; base < b.n_seq; base += 64) {
+        look(base);
+        if (err && s.bad) atomicOr(err, kErrRange);
+        total += uint32_t(__builtin_amdgcn_readlane(int(wave_scan(uint32_t(nb))), 63));
+    }
+    Piece p{};
+    p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), kAttWaves);
+    int before = 0;
+#pragma unroll 1
+    for (int base = 0; base < b.n_seq; base += 64) {
+        if (b.n_seq > 64) look(base);
+        const int count = s.n ? max(1, (nb + p.chunk - 1) / p.chunk) : 0;
+        const int upto = int(wave_scan(uint32_t(count))), first = before + upto - count;
+        const bool mine = by_unit ? want >= first && want < first + count : base + lane == want;
+        const unsigned long long hit = __ballot(mine);
+        if (hit) {
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll(hit) - 1);
+            p.seq = base + l;
+            p.first = __builtin_amdgcn_readlane(first, l);
+            p.count = __builtin_amdgcn_readlane(count, l);
+            p.s.t0 = __builtin_amdgcn_readlane(s.t0, l);
+            p.s.n = __builtin_amdgcn_readlane(s.n, l);
+            p.s.len = __builtin_amdgcn_readlane(s.len, l);
+            p.split = by_unit ? want - p.first : 0;
+            return p;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return p;
+}
+
+template <bool F32>
+__device__ __forceinline__ void store4(void *out, size_t at, float4 v) {
+    if constexpr (F32) *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = v;
+    else
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+
+// grid: (row tiles, key/value head, sequence), or with a target (pieces, key/value head, row tiles).
+// HALF: at most 8 rows.  They fill columns 0-7 and again 8-15, and lane (n, c) takes row n % 8's scores of the
+// positions of tile n / 8 alone: half the arithmetic per lane; the probabilities of tile 1 are handed to the lanes
+// of column n - 8 as operands.
+template <int NG, int NT, bool F32, bool HALF>
+__global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_kernel(AttendArgs a) {
+    constexpr int d = NG * kGroup, TERMS = F32 ? 2 : 1, ROWS = HALF ? 8 : 16, PP = HALF ? 4 : 8;
+    constexpr int UB = NG <= 2 && NT == 1 && (HALF || !F32 || NG == 1) ? 2 : 1;  // blocks of positions at a time
+    static_assert(!HALF || NT == 1);
+    __shared__ float4 out_sh[kAttWaves][ROWS][d / 4 + 1];
+    __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
+    const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+    const int half = HALF ? n >> 3 : 0, n_row = HALF ? n & 7 : n;
+    int tile = blockIdx.x;
+    Piece piece{};
+    int *err = blockIdx.x == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr;
+    if (a.target) {
+        tile = blockIdx.z;
+        piece = find_piece(a.batch, a.window, a.target, blockIdx.x, true, tile == 0 ? err : nullptr);
+        if (piece.count == 0) return;
+    } else {
+        piece.seq = blockIdx.z;
+        piece.count = 1;
+        piece.s = sequence(a.batch, piece.seq);
+        if (piece.s.bad && err && lane == 0) atomicOr(err, kErrRange);
+    }
+    const Seq &s = piece.s;
+    const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
     if (row0 >= rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+
+    // Blocks of positions: those that some row of the tile sees, this piece's share of them.
+    const int p_first = s.len - s.n + row0 / G;                               // position of the tile's first row
+    const int p_last = s.len - s.n + min(s.n - 1, (row0 + ROWS * NT - 1) / G);  // of its last row
+    const int b_first = a.window ? max(0, s.len - s.n - a.window + 1) / kPos : 0;
+    const int t_first = a.window ? max(0, p_first - a.window + 1) / kPos : 0;
+    const int t_end = p_last < 0 ? 0 : p_last / kPos + 1;
+    const int b0 = max(t_first, b_first + piece.split * piece.chunk);
+    const int b1 = piece.split == piece.count - 1 ? t_end : min(t_end, b_first + (piece.split + 1) * piece.chunk);
+    const uint8_t *seq = a.cache + (size_t(piece.seq) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
+
+    // A block's operands as they lie in the cache.  Keys and values are loaded one block ahead, each as soon as
+    // the present block's have been used; past the wave's last block the last one is loaded again.
+    uint4 kc[UB][NG], vc[UB][NG];
+    uint32_t ks[UB][NG][PP / 2], vs[UB][NG][PP / 2], vm[UB][NG][PP / 2], km[UB];
+    auto load_pairs = [&](const uint8_t *p, uint32_t (&v)[PP / 2]) __attribute__((always_inline)) {
+        if constexpr (HALF) {
+            const uint2 u = *reinterpret_cast<const uint2 *>(p + c * 16 + half * 8);
+            v[0] = u.x, v[1] = u.y;
+        } else {
+            const uint4 u = dev::load16(p + c * 16);
+            v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+        }
+    };
+    // (the u-th of the wave's next blocks, the first again where there is none)
+    auto block_at = [&](int b, int u) { return seq + size_t(b + u * kAttWaves < b1 ? b + u * kAttWaves : b) * block_bytes(d); };
+    auto load_k = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < UB; ++u) {
+            const uint8_t *block = block_at(b, u);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                kc[u][g] = dev::load16(block + k_codes(d) + g * 1024 + lane * 16);
+                load_pairs(block + k_scales(d) + g * 64, ks[u][g]);
+            }
+            km[u] = *reinterpret_cast<const uint32_t *>(block + k_bases(d) + min(c, NG - 1) * 64 + n * 4);
+        }
+    };
+    auto load_v = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < UB; ++u) {
+            const uint8_t *block = block_at(b, u);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                vc[u][g] = dev::load16(block + v_codes(d) + g * 1024 + lane * 16);
+                load_pairs(block + v_scales(d) + g * 64, vs[u][g]);
+                load_pairs(block + v_bases(d) + g * 64, vm[u][g]);
+            }
+        }
+    };
+    // (a row past the last repeats it and is not stored)
+    constexpr int QV = F32 ? 2 : 1;  // 16-byte loads per 8 elements of q
+    uint4 qraw[NT][2 * NG][QV];
+    auto row_of = [&](int t) { return min(row0 + 16 * t + n_row, rows - 1); };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row_of(t), i = row / G;
+        const size_t at = size_t(s.t0 + i) * a.q_stride + size_t(h * G + row - i * G) * d + 8 * c;
+#pragma unroll
+        for (int j = 0; j < 2 * NG; ++j)
+#pragma unroll
+            for (int e = 0; e < QV; ++e)
+                qraw[t][j][e] = dev::load16(static_cast<const uint8_t *>(a.q) + (at + 32 * j) * (F32 ? 4 : 2) + 16 * e);
+    }
+    // (no branch: a wave without a block reads the cache's first, and uses none of it)
+    {
+        const int b = b0 + wave < b1 ? b0 + wave : 0;
+        load_k(b);
+        load_v(b);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 
     // The tile's rows: their queries as operands (k = dims), their last visible position.
     int last[NT];
-    bf16x8 bq[NT][2 * NG][QT], bm[NT];
-    floatx4 init[NT][NG];  // -16 sum of q_g
+    float zs[NT];  // from a score as formed to log2 units
+    f16x8 bq[NT][2 * NG][TERMS];
+    bf16x8 bm[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int row = row0 + 16 * t + n, i = row / G, head = h * G + row % G;
-        const bool live = row < rows;
-        last[t] = live ? s.len - s.n + i : -1;
-        const size_t at = live ? size_t(s.t0 + i) * a.q_stride + size_t(head) * d : 0;
+        last[t] = s.len - s.n + row_of(t) / G;
+        float x[2 * NG][8], top = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * NG; ++j) {
+            const uint4 u = qraw[t][j][0], v = qraw[t][j][QV - 1];
             if constexpr (F32) {
-                float x[8];
-                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 32 * j + 8 * c);
-                float4 u = make_float4(0.f, 0.f, 0.f, 0.f), v = u;
-                if (live) u = dev::load_f4(p), v = dev::load_f4(p + 1);
-                x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-                split<QT>(x, bq[t][j]);
+                const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = __uint_as_float(w[e]);
             } else {
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (live) u = dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * j + 8 * c));
-                bq[t][j][0] = __builtin_bit_cast(bf16x8, u);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[j][2 * e] = low_half(w[e]);
+                    x[j][2 * e + 1] = high_half(w[e]);
+                }
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
         }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            floatx4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = QT - 1; k >= 0; --k)
-#pragma unroll
-                for (int j = 2 * g; j < 2 * g + 2; ++j)
-                    z = mfma(operand(kMinus16, kMinus16, kMinus16, kMinus16), bq[t][j][k], z);
-            init[t][g] = z;
-        }
-        // The bases' product: elements (c, 0..2) are the three terms of the sum of q over group c.
+        top = max_over_c(top);
+        // 2^e takes the row's largest element to [2^14, 2^15).  (From 2^103 on, which the limits of a call leave
+        // out, it would not fit fp16; an infinity or NaN stays one.)
+        int e2 = 0;
+        if (top > 0.f && top < INFINITY) e2 = min(max(14 - ilogbf(top), -88), 148);
+        zs[t] = fmaxf(ldexpf(fabsf(a.scale), -kKeyExp<F32> - e2), 0x1p-126f);
         float sum = 0.f;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) sum = c == g ? init[t][g][0] * -0.0625f : sum;
-        const float x[8] = {sum, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        bf16x8 w[3];
-        split<3>(x, w);
-        const uint32_t w0 = __builtin_bit_cast(uint4, w[0]).x, w1 = __builtin_bit_cast(uint4, w[1]).x;
-        bm[t] = operand((w0 & 0xffffu) | (w1 << 16), __builtin_bit_cast(uint4, w[2]).x & 0xffffu, 0, 0);
+        for (int g = 0; g < NG; ++g) {
+            float sg = 0.f;
+#pragma unroll
+            for (int j = 2 * g; j < 2 * g + 2; ++j) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = ldexpf(a.scale < 0.f ? -x[j][e] : x[j][e], e2);
+                    sg += y;
+                    x[j][e] = high_code(e) ? y * 0.0625f : y;
+                }
+                split<TERMS>(x[j], bq[t][j]);
+            }
+            sg = sum_over_c(sg);
+            sum = c == g ? sg : sum;
+        }
+        // The bases' product: elements (c, 0..2) are the sum of q over group c as three bf16 terms.
+        sum = ldexpf(sum, kKeyExp<F32>);
+        const uint32_t w1 = bf16_rne(sum);
+        const float r1 = sum - bf16_float(w1);
+        const uint32_t w2 = bf16_rne(r1);
+        const uint32_t w3 = bf16_rne(r1 - bf16_float(w2));
+        bm[t] = __builtin_bit_cast(bf16x8, make_uint4(w1 | (w2 << 16), w3, 0, 0));
     }
 
-    // Blocks of positions: those that some row of the tile sees, this split's share of them.
-    const int p_first = s.len - s.n + row0 / G;                               // of the tile's first row
-    const int p_last = s.len - s.n + min(s.n - 1, (row0 + 16 * NT - 1) / G);  // of its last row
-    const int b_first = a.window ? max(0, p_first - a.window + 1) / kPos : 0;
-    const int b_end = p_last < 0 ? b_first : p_last / kPos + 1;
-    const int share = max((b_end - b_first + a.splits - 1) / a.splits, kAttWaves);
-    const int b0 = b_first + split_i * share, b1 = min(b_end, b0 + share);
-    const uint8_t *seq = a.cache + (size_t(blockIdx.z) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
-
-    floatx4 acc[NT][4 * NG], add[NT][NG];  // outputs (dims x rows); what all the dims of a group share
-    float mx[NT], sum[NT];
+    // A row's sums hold 2^boost P with P = exp2(score - off), off the largest score so far, in log2 units; 2^boost
+    // takes the largest value scale so far to about 2^15.  When either changes, the sums so far are scaled along.
+    // (An off with the boost in it would cost P 4 bits: the exponent is rounded at its own size.)
+    floatx4 acc[NT][4 * NG];  // sum of P s (u - 8) (dims x rows), times 2^(boost + kValueExp)
+    float add[NT][NG];        // sum of P (m + 8 s), this lane's positions
+    float mx[NT], off[NT], sum[NT];
+    uint32_t top_s = 0;  // largest bf16 of the exponent of the largest value scale so far
+    int boost = 0;
+    float boost_f = 1.f;  // 2^boost
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         mx[t] = -INFINITY;
-        sum[t] = 0.f;
+        off[t] = sum[t] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int g = 0; g < NG; ++g) add[t][g] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < NG; ++g) add[t][g] = 0.f;
     }
-#pragma unroll 1
-    for (int b = b0 + wave; b < b1; b += kAttWaves) {
-        const uint8_t *block = seq + size_t(b) * block_bytes(d);
-        uint4 kc[NG], vc[NG], ks[NG], vs[NG], vm[NG];
+    // The wave's blocks b, b + kAttWaves, ... (U of them), whose operands are loaded; `next`: what to load meanwhile.
+    auto step = [&](auto blocks, int b, int next) __attribute__((always_inline)) {
+        constexpr int U = decltype(blocks)::value;
+        // ---- scores
+        float p[NT][U][PP];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            kc[g] = dev::load16(block + k_codes(d) + g * 1024 + lane * 16);
-            ks[g] = dev::load16(block + k_scales(d) + g * 64 + c * 16);
-            vc[g] = dev::load16(block + v_codes(d) + g * 1024 + lane * 16);
-            vs[g] = dev::load16(block + v_scales(d) + g * 64 + c * 16);
-            vm[g] = dev::load16(block + v_bases(d) + g * 64 + c * 16);
+        for (int u = 0; u < U; ++u) {
+            floatx4 z0[NT], y0[NT][NG];
+#pragma unroll
+            for (int tau = 0; tau < 2; ++tau) {
+                const uint32_t m2 = tau ? (km[u] & 0xffff0000u) | (km[u] >> 16) : (km[u] << 16) | (km[u] & 0xffffu);
+                const bf16x8 ma = __builtin_bit_cast(bf16x8, make_uint4(m2, m2, m2, m2));
+                f16x8 kf[2 * NG];
+#pragma unroll
+                for (int j = 0; j < 2 * NG; ++j) {
+                    const int w = tau * 2 * NG + j;
+                    kf[j] = key_codes<F32>(reinterpret_cast<const uint32_t *>(&kc[u][w / 4])[w % 4]);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    floatx4 z = mfma(ma, bm[t], floatx4{0.f, 0.f, 0.f, 0.f}), y[NG];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        y[g] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+                            for (int j = 2 * g; j < 2 * g + 2; ++j) y[g] = mfma(kf[j], bq[t][j][k], y[g]);
+                    }
+                    if constexpr (HALF) {
+                        if (tau == 0) {
+                            z0[t] = z;
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) y0[t][g] = y[g];
+                            continue;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            z[r] = half ? z[r] : z0[t][r];
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) y[g][r] = half ? y[g][r] : y0[t][g][r];
+                        }
+                    }
+                    constexpr int stride = HALF ? 0 : 4;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            const uint32_t w = ks[u][g][(stride * tau + r) / 2];
+                            z[r] = fmaf(r & 1 ? high_half(w) : low_half(w), y[g][r], z[r]);
+                        }
+                        p[t][u][stride * tau + r] = z[r];
+                    }
+                }
+            }
         }
-        const uint32_t km = *reinterpret_cast<const uint32_t *>(block + k_bases(d) + min(c, NG - 1) * 64 + n * 4);
-        if (b * kPos + kPos > s.len) {
+        __builtin_amdgcn_sched_barrier(0);  // (what is next waits for the values: it stays behind the keys' loads)
+        load_k(next);
+        __builtin_amdgcn_sched_barrier(0);
+        // ---- softmax
+        const int past = b + (U - 1) * kAttWaves;  // the last of the blocks
+        if (past * kPos + kPos > s.len) {
             // Positions that hold nothing yet may hold anything: their probabilities are 0, and 0 times what
             // lies there has to be 0.
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t keep = 0;
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int k = 2 * i + e, p = b * kPos + 16 * (k >> 2) + 4 * c + (k & 3);
-                    keep |= p < s.len ? 0xffffu << (16 * e) : 0u;
+                for (int i = 0; i < PP / 2; ++i) {
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int k = 2 * i + e, at = (b + u * kAttWaves) * kPos + 16 * (half + (k >> 2)) + 4 * c + (k & 3);
+                        keep |= at < s.len ? 0xffffu << (16 * e) : 0u;
+                    }
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        vs[u][g][i] &= keep;
+                        vm[u][g][i] &= keep;
+                    }
                 }
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    reinterpret_cast<uint32_t *>(&vs[g])[i] &= keep;
-                    reinterpret_cast<uint32_t *>(&vm[g])[i] &= keep;
-                }
-            }
         }
-        bf16x8 kf[2][2 * NG], vf[4 * NG];
+        u16x2 most = {0, 0};
 #pragma unroll
-        for (int w = 0; w < 4 * NG; ++w) {
-            kf[w / (2 * NG)][w % (2 * NG)] = codes16(reinterpret_cast<const uint32_t *>(&kc[w / 4])[w % 4]);
-            vf[w] = codes16(reinterpret_cast<const uint32_t *>(&vc[w / 4])[w % 4]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int i = 0; i < PP / 2; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, vs[u][g][i]));
+        const uint32_t most_s = max(most[0], most[1]);
+        const bool scales_rose = __any(most_s > top_s);
+        float rise = 1.f;
+        if (scales_rose) {
+            const int e = int(dev::wave_reduce_u32<true>(most_s) >> 7), was = boost;
+            top_s = (uint32_t(e) << 7) | 0x7fu;
+            boost = min(141 - e, 100);  // (sums over up to 2^26 positions stay finite)
+            boost_f = ldexpf(1.f, boost);
+            rise = ldexpf(1.f, min(boost - was, 126));  // (it rises from its start only: the sums are still zeros)
         }
-        const bool full = b * kPos + kPos - 1 <= p_first && (!a.window || b * kPos > p_last - a.window);
+        const bool full = past * kPos + kPos - 1 <= p_first && (!a.window || b * kPos > p_last - a.window);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float x[8];
-#pragma unroll
-            for (int tau = 0; tau < 2; ++tau) {
-                const uint32_t m2 = tau ? (km >> 16) * 0x10001u : (km & 0xffffu) * 0x10001u;
-                floatx4 z = mfma(operand(m2, m2, m2, m2), bm[t], floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    floatx4 y = init[t][g];
-#pragma unroll
-                    for (int k = QT - 1; k >= 0; --k)
-#pragma unroll
-                        for (int j = 2 * g; j < 2 * g + 2; ++j) y = mfma(kf[tau][j], bq[t][j][k], y);
-                    const uint32_t *sc = reinterpret_cast<const uint32_t *>(&ks[g]) + 2 * tau;
-                    z[0] = fmaf(low_half(sc[0]), y[0], z[0]);
-                    z[1] = fmaf(high_half(sc[0]), y[1], z[1]);
-                    z[2] = fmaf(low_half(sc[1]), y[2], z[2]);
-                    z[3] = fmaf(high_half(sc[1]), y[3], z[3]);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[4 * tau + r] = z[r] * a.scale;
-            }
             if (!full) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int p = b * kPos + 16 * (k >> 2) + 4 * c + (k & 3);
-                    if (p > last[t] || (a.window && p <= last[t] - a.window)) x[k] = -INFINITY;
-                }
-            }
-            float top = x[0];
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+                    for (int k = 0; k < PP; ++k) {
+                        const int at = (b + u * kAttWaves) * kPos + 16 * (half + (k >> 2)) + 4 * c + (k & 3);
+                        if (at > last[t] || (a.window && at <= last[t] - a.window)) p[t][u][k] = -INFINITY;
+                    }
+            }
+            float top = p[t][0][0];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < PP; ++k) top = fmaxf(top, p[t][u][k]);
+            if constexpr (HALF) top = fmaxf(top, other_half(top));
+            top = max_over_c(top);
             const float was = mx[t], now = fmaxf(was, top);
-            if (__any(now > was)) {  // some row's maximum rose: what it has so far is scaled down
-                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(was - now);
+            if (scales_rose || __any(now > was)) {
+                const float to = now == -INFINITY ? 0.f : product(now, zs[t]);
+                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[t] - to) * rise;
                 mx[t] = now;
+                off[t] = to;
                 sum[t] *= f;
 #pragma unroll
                 for (int i = 0; i < 4 * NG; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[t][i][r] *= f;
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) add[t][g][r] *= f;
+                for (int g = 0; g < NG; ++g) add[t][g] *= f;
             }
-            const float base = now == -INFINITY ? 0.f : now;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] = __builtin_amdgcn_exp2f(x[k] - base);
-                sum[t] += x[k];
-            }
-            bf16x8 bp[PT];
-            split<PT>(x, bp);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < PP; ++k) {
+                    p[t][u][k] = __builtin_amdgcn_exp2f(fmaf(p[t][u][k], zs[t], -off[t])) * boost_f;
+                    sum[t] += p[t][u][k];
+                }
+        }
+        // ---- values
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                float y[8];
-                const uint32_t *sc = reinterpret_cast<const uint32_t *>(&vs[g]);
+                f16x8 vf[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    y[2 * e] = x[2 * e] * low_half(sc[e]);
-                    y[2 * e + 1] = x[2 * e + 1] * high_half(sc[e]);
+                for (int i = 0; i < 4; ++i) vf[i] = value_codes(reinterpret_cast<const uint32_t *>(&vc[u][g])[i]);
+                float sf[PP], mf[PP];
+#pragma unroll
+                for (int k = 0; k < PP; ++k) {
+                    const uint32_t sw = vs[u][g][k / 2], mw = vm[u][g][k / 2];
+                    sf[k] = k & 1 ? high_half(sw) : low_half(sw);
+                    mf[k] = fmaf(8.f, sf[k], k & 1 ? high_half(mw) : low_half(mw));
                 }
-                bf16x8 bs[PT];
-                split<PT>(y, bs);
 #pragma unroll
-                for (int k = PT - 1; k >= 0; --k) {
-                    add[t][g] = mfma(__builtin_bit_cast(bf16x8, vm[g]), bp[k], add[t][g]);
-                    add[t][g] = mfma(operand(kMinus16, kMinus16, kMinus16, kMinus16), bs[k], add[t][g]);
+                for (int t = 0; t < NT; ++t) {
+                    float y[8];
+                    f16x8 bs[TERMS];
 #pragma unroll
-                    for (int i = 4 * g; i < 4 * g + 4; ++i) acc[t][i] = mfma(vf[i], bs[k], acc[t][i]);
+                    for (int k = 0; k < PP; ++k) {
+                        // (two terms: both have to see one rounded product, not one of them a fused conversion)
+                        y[k] = F32 ? product(p[t][u][k], sf[k]) : p[t][u][k] * sf[k];
+                        add[t][g] = fmaf(p[t][u][k], mf[k], add[t][g]);
+                    }
+                    if constexpr (HALF) {
+                        f16x2 lo[2][TERMS];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            lo[e][0] = pack_f16(y[2 * e], y[2 * e + 1]);
+                            if constexpr (TERMS == 2)
+                                lo[e][1] = pack_f16(y[2 * e] - float(lo[e][0][0]), y[2 * e + 1] - float(lo[e][0][1]));
+                        }
+#pragma unroll
+                        for (int k = 0; k < TERMS; ++k)
+                            bs[k] = join8(lo[0][k], lo[1][k], other_half(lo[0][k]), other_half(lo[1][k]));
+                    } else {
+                        split<TERMS>(y, bs);
+                    }
+#pragma unroll
+                    for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][4 * g + i] = mfma(vf[i], bs[k], acc[t][4 * g + i]);
                 }
             }
-        }
-    }
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(next);
+    };
+    int b = b0 + wave;
+#pragma unroll 1
+    for (; b + (UB - 1) * kAttWaves < b1; b += UB * kAttWaves)
+        step(std::integral_constant<int, UB>(), b, b + UB * kAttWaves < b1 ? b + UB * kAttWaves : b);
+    if (UB == 2 && b < b1) step(std::integral_constant<int, 1>(), b, b);
 
     // Join the waves, one tile of rows at a time.
-#pragma unroll 1
+#pragma unroll
     for (int t = 0; t < NT; ++t) {
-        floatx4 o[4 * NG];
-        float m = 0.f, l = 0.f;
-#pragma unroll
-        for (int u = 0; u < NT; ++u)
-            if (u == t) {
-                m = mx[u];
-                l = sum[u];
-#pragma unroll
-                for (int i = 0; i < 4 * NG; ++i) o[i] = acc[u][i] + add[u][i / 4];
-            }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
+        float l = sum_over_c(sum[t]);
+        if constexpr (HALF) l += other_half(l);
         if (t) __syncthreads();
-        if (c == 0) {
-            max_sh[wave][n] = m;
-            sum_sh[wave][n] = l;
+        if (c == 0 && !half) {
+            max_sh[wave][n] = mx[t] == -INFINITY ? mx[t] : off[t];
+            sum_sh[wave][n] = ldexpf(l, -boost);
         }
 #pragma unroll
-        for (int i = 0; i < 4 * NG; ++i) out_sh[wave][n][4 * i + c] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+        for (int g = 0; g < NG; ++g) {
+            float m = sum_over_c(add[t][g]);
+            if constexpr (HALF) m += other_half(m);
+            m = ldexpf(m, -boost);
+            const int e = -boost - kValueExp;
+            if (!half)
+#pragma unroll
+                for (int i = 4 * g; i < 4 * g + 4; ++i)
+                    out_sh[wave][n][4 * i + c] = make_float4(ldexpf(acc[t][i][0], e) + m, ldexpf(acc[t][i][1], e) + m,
+                                                             ldexpf(acc[t][i][2], e) + m, ldexpf(acc[t][i][3], e) + m);
+        }
         __syncthreads();
 #pragma unroll 1
-        for (int idx = threadIdx.x; idx < 16 * (d / 4); idx += kAttBlock) {
+        for (int idx = threadIdx.x; idx < ROWS * (d / 4); idx += kAttBlock) {
             const int r = idx / (d / 4), i4 = idx % (d / 4), row = row0 + 16 * t + r;
             if (row >= rows) continue;
             float M = max_sh[0][r];
@@ -322,112 +628,108 @@ __global__ __launch_bounds__(kAttBlock) void kv4_attend_kernel(AttendArgs a) {
                 v.z = fmaf(f, u.z, v.z);
                 v.w = fmaf(f, u.w, v.w);
             }
-            const int i = row / G, head = h * G + row % G;
-            const size_t token = size_t(s.t0 + i);
-            if (a.splits > 1) {
-                float *p = a.part + ((token * a.n_heads + head) * a.splits + split_i) * (d + 4);
-                *reinterpret_cast<float4 *>(p + 4 * i4) = v;
-                if (i4 == 0) *reinterpret_cast<float2 *>(p + d) = make_float2(M, S);
+            if (piece.count > 1) {
+                float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
+                *reinterpret_cast<float4 *>(o + 4 * i4) = v;
+                if (i4 == 0) *reinterpret_cast<float2 *>(o + d) = make_float2(M, S);
                 continue;
             }
             const float inv = S == 0.f ? 0.f : 1.f / S;  // (a row that sees nothing: 0)
             v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-            const size_t at = token * a.out_stride + size_t(head) * d + 4 * i4;
-            if constexpr (F32) *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
-            else
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) =
-                    make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
         }
     }
 }
 
-// Joins the splits of one row.  grid: (rows, key/value head, sequence); 8 groups of d / 4 lanes (at most 64)
-// take the splits in turn.
+// Joins the pieces of one row.  grid: (rows, key/value head, sequence); groups of d / 4 lanes take the pieces in
+// turn, a running maximum each.
 template <int NG, bool F32>
-__global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int tile_rows) {
     constexpr int d = NG * kGroup, N4 = d / 4, SUB = kAttBlock / N4;
-    __shared__ float wgt[kMaxSplits], red[2 * kAttWaves];
     __shared__ float4 acc_sh[SUB][N4];
-    const Seq s = sequence(a.batch, blockIdx.z);
+    __shared__ float max_sh[SUB], sum_sh[SUB];
+    const Piece piece = find_piece(a.batch, a.window, a.target, blockIdx.z, false, nullptr);
+    if (piece.count <= 1) return;
+    const Seq &s = piece.s;
     const int G = a.group, row = blockIdx.x, h = blockIdx.y;
     if (row >= s.n * G) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const size_t token = size_t(s.t0 + row / G);
-    const int head = h * G + row % G;
-    const float *p = a.part + (token * a.n_heads + head) * a.splits * (d + 4);
-    float m = -INFINITY, l = 0.f;
-    if (tid < a.splits) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p + size_t(tid) * (d + 4) + d);
-        m = ml.x;
-        l = ml.y;
-    }
-    float M = m;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    if (lane == 0) red[wave] = M;
-    __syncthreads();
-    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float f = m == -INFINITY && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);
-    if (tid < a.splits) wgt[tid] = f;
-    const float S1 = dev::wave_sum(f * l);
-    if (lane == 0) red[kAttWaves + wave] = S1;
-    __syncthreads();
-    const float S = red[kAttWaves] + red[kAttWaves + 1] + red[kAttWaves + 2] + red[kAttWaves + 3];
-    const int i4 = tid % N4, sub = tid / N4;
+    const int tid = threadIdx.x, i4 = tid % N4, sub = tid / N4;
+    const size_t step = size_t(a.n_kv) * a.tiles * tile_rows * (d + 4);
+    const float *p = a.part + ((size_t(piece.first) * a.n_kv + h) * a.tiles * tile_rows + row) * (d + 4);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float M = -INFINITY, S = 0.f;
     if (sub < SUB) {
-        for (int k = sub; k < a.splits; k += SUB) {
-            const float w = wgt[k];
-            if (w == 0.f) continue;
-            const float4 u = *reinterpret_cast<const float4 *>(p + size_t(k) * (d + 4) + 4 * i4);
-            v.x = fmaf(w, u.x, v.x);
-            v.y = fmaf(w, u.y, v.y);
-            v.z = fmaf(w, u.z, v.z);
-            v.w = fmaf(w, u.w, v.w);
+#pragma unroll 4
+        for (int k = sub; k < piece.count; k += SUB) {
+            const float2 ml = *reinterpret_cast<const float2 *>(p + k * step + d);
+            const float4 u = *reinterpret_cast<const float4 *>(p + k * step + 4 * i4);
+            const float now = fmaxf(M, ml.x);
+            // (as in the attention kernel: nothing seen counts 0, NaN stays)
+            const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
+            const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
+            M = now;
+            S = fmaf(S, f, ml.y * g);
+            v.x = fmaf(v.x, f, u.x * g);
+            v.y = fmaf(v.y, f, u.y * g);
+            v.z = fmaf(v.z, f, u.z * g);
+            v.w = fmaf(v.w, f, u.w * g);
         }
         acc_sh[sub][i4] = v;
+        if (i4 == 0) {
+            max_sh[sub] = M;
+            sum_sh[sub] = S;
+        }
     }
     __syncthreads();
     if (tid >= N4) return;
-    v = acc_sh[0][tid];
+    float top = max_sh[0];
 #pragma unroll
-    for (int k = 1; k < SUB; ++k) {
+    for (int k = 1; k < SUB; ++k) top = fmaxf(top, max_sh[k]);
+    S = 0.f;
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < SUB; ++k) {
+        const float f = max_sh[k] == -INFINITY && sum_sh[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f(max_sh[k] - top);
         const float4 u = acc_sh[k][tid];
-        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+        S = fmaf(f, sum_sh[k], S);
+        v.x = fmaf(f, u.x, v.x);
+        v.y = fmaf(f, u.y, v.y);
+        v.z = fmaf(f, u.z, v.z);
+        v.w = fmaf(f, u.w, v.w);
     }
     const float inv = S == 0.f ? 0.f : 1.f / S;
     v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-    const size_t at = token * a.out_stride + size_t(head) * d + 4 * tid;
-    if constexpr (F32) *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
-    else
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * tid, v);
 }
 
-// Tiles of 16 rows per wave, and the splits of the positions.
+// Tiles of 16 rows per wave (0: one of 8), row tiles of the largest sequence, and the split of the positions.
 struct AttendPlan {
-    int tiles, blocks, splits;
+    int tiles, tile_rows, blocks, target, units;
+    size_t workspace;
 };
 AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_pos, bool f32) {
     const long long rows = (long long)max_q * group;
-    const int most = d <= 128 ? (f32 ? 2 : 4) : (f32 ? 1 : 2);  // what a wave's registers hold
-    AttendPlan p;
-    p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
-    p.blocks = int((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-    const long long base = (long long)p.blocks * n_kv * n_seq;
-    const long long most_splits = std::max(1, max_pos / kPos / kAttWaves);
-    p.splits = int(std::max(1ll, std::min({(long long)kMaxSplits, most_splits, 512 / base})));
+    // what a wave's registers hold
+    const int most = d <= 64 ? (f32 ? 2 : 4) : d <= 128 ? 2 : d <= 192 && !f32 ? 2 : 1;
+    AttendPlan p{};
+    p.tiles = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
+    p.tile_rows = p.tiles ? 16 * p.tiles : 8;
+    p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
+    const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
+    const long long pieces = (max_pos / kPos + kAttWaves - 1) / kAttWaves;  // most that a sequence has
+    if (base * n_seq < kTarget && pieces > 1) {
+        p.target = int(std::min(std::max(1ll, kTarget / base), pieces * n_seq));
+        p.units = p.target + n_seq;
+        p.workspace = (size_t(p.units) * n_kv * p.blocks * p.tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
+    }
     return p;
 }
 
 }  // namespace
 
-size_t kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int d, int max_q, int max_pos) {
-    size_t n = 0;
-    for (bool f32 : {false, true}) {
-        const AttendPlan p = attend_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_pos, f32);
-        if (p.splits > 1) n = std::max(n, size_t(T) * n_heads * p.splits * (d + 4) * sizeof(float));
-    }
-    return (n + 255) & ~size_t(255);
+size_t kv4_attention_workspace_bytes(int, int n_seq, int n_heads, int n_kv, int d, int max_q, int max_pos) {
+    return std::max(attend_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_pos, false).workspace,
+                    attend_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_pos, true).workspace);
 }
 
 hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, const void *cache, const kv4::Batch &batch,
@@ -446,45 +748,36 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     a.n_kv = n_kv;
     a.group = n_heads / n_kv;
     a.window = window;
-    a.splits = p.splits;
+    a.target = p.target;
+    a.tiles = p.blocks;
     a.scale = scale * 1.44269504088896341f;
     a.batch = batch;
     a.err = err;
-    const dim3 grid(p.blocks * p.splits, n_kv, batch.n_seq);
-#define KV4_RUN(NG, NT, F) kv4_attend_kernel<NG, NT, F><<<grid, kAttBlock, 0, s>>>(a)
-#define KV4_SMALL(NG)                               \
-    case NG * kGroup:                               \
-        if (f32) {                                  \
-            if (p.tiles == 1) KV4_RUN(NG, 1, true); \
-            else KV4_RUN(NG, 2, true);              \
-        } else {                                    \
-            if (p.tiles == 1) KV4_RUN(NG, 1, false); \
-            else if (p.tiles == 2) KV4_RUN(NG, 2, false); \
-            else KV4_RUN(NG, 4, false);             \
-        }                                           \
-        break;
-#define KV4_LARGE(NG)                               \
-    case NG * kGroup:                               \
-        if (f32) KV4_RUN(NG, 1, true);              \
-        else if (p.tiles == 1) KV4_RUN(NG, 1, false); \
-        else KV4_RUN(NG, 2, false);                 \
-        break;
-    switch (d) {
-        KV4_SMALL(1) KV4_SMALL(2) KV4_LARGE(3) KV4_LARGE(4)
+    const dim3 grid = p.target ? dim3(p.units, n_kv, p.blocks) : dim3(p.blocks, n_kv, batch.n_seq);
+#define KV4_RUN(NG, NT, F) kv4_attend_kernel<NG, NT ? NT : 1, F, NT == 0><<<grid, kAttBlock, 0, s>>>(a)
+#define KV4_CASE(NG, NT, F) case (NG * 2 + F) * 8 + NT: KV4_RUN(NG, NT, F); break;
+    switch ((d / kGroup * 2 + f32) * 8 + p.tiles) {
+        KV4_CASE(1, 0, false) KV4_CASE(1, 1, false) KV4_CASE(1, 2, false) KV4_CASE(1, 4, false)
+        KV4_CASE(1, 0, true) KV4_CASE(1, 1, true) KV4_CASE(1, 2, true)
+        KV4_CASE(2, 0, false) KV4_CASE(2, 1, false) KV4_CASE(2, 2, false)
+        KV4_CASE(2, 0, true) KV4_CASE(2, 1, true) KV4_CASE(2, 2, true)
+        KV4_CASE(3, 0, false) KV4_CASE(3, 1, false) KV4_CASE(3, 2, false)
+        KV4_CASE(3, 0, true) KV4_CASE(3, 1, true)
+        KV4_CASE(4, 0, false) KV4_CASE(4, 1, false)
+        KV4_CASE(4, 0, true) KV4_CASE(4, 1, true)
     default: return hipErrorInvalidValue;
     }
+#undef KV4_CASE
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
+    if (e != hipSuccess || !p.target) return e;
     const dim3 jgrid(batch.max_q * a.group, n_kv, batch.n_seq);
 #define KV4_JOIN(NG)                                                    \
     case NG * kGroup:                                                   \
-        if (f32) kv4_join_kernel<NG, true><<<jgrid, kAttBlock, 0, s>>>(a); \
-        else kv4_join_kernel<NG, false><<<jgrid, kAttBlock, 0, s>>>(a); \
+        if (f32) kv4_join_kernel<NG, true><<<jgrid, kAttBlock, 0, s>>>(a, p.tile_rows); \
+        else kv4_join_kernel<NG, false><<<jgrid, kAttBlock, 0, s>>>(a, p.tile_rows); \
         break;
     switch (d) { KV4_JOIN(1) KV4_JOIN(2) KV4_JOIN(3) KV4_JOIN(4) }
 #undef KV4_JOIN
-#undef KV4_LARGE
-#undef KV4_SMALL
 #undef KV4_RUN
     return hipGetLastError();
 }

@@ -82,13 +82,13 @@ __global__ __launch_bounds__(kMvBlock) void matvec_int4_kernel(const float *__re
     const bool live = ONE ? term < 3 : n < T;
 
     bf16x8 xt[kMvPass][4][NP];
-    floatx4 init[kMvPass];  // -24 sum of x over the group
+    floatx4 init[kMvPass][ONE ? 1 : 2];  // -24 sum of x over the group: of the leading terms, of the others
     auto load_x = [&](int pass, float &squares) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < kMvPass; ++r) {
             const int g = (pass * kMvWaves + wave) * share + r;
             const bool in = live && r < share && g < KG;
-            init[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (floatx4 &z : init[r]) z = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(kMvBlock) void matvec_int4_kernel(const float *__re
                 constexpr uint32_t m24 = 0xC1C0C1C0u;  // bf16 -24 twice
 #pragma unroll
                 for (int k = NP - 1; k >= 0; --k)
-                    init[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        xt[r][j][k], __builtin_bit_cast(bf16x8, make_uint4(m24, m24, m24, m24)), init[r], 0, 0, 0);
+                    init[r][k > 0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        xt[r][j][k], __builtin_bit_cast(bf16x8, make_uint4(m24, m24, m24, m24)), init[r][k > 0], 0, 0, 0);
             }
         }
     };
@@ -146,12 +146,19 @@ __global__ __launch_bounds__(kMvBlock) void matvec_int4_kernel(const float *__re
 #pragma unroll
                 for (int j = 0; j < RB; ++j) {
                     const uint32_t u[4] = {wv[r][j].x, wv[r][j].y, wv[r][j].z, wv[r][j].w};
-                    floatx4 z = init[r];
+                    // (the leading terms apart from the small ones, whose sums would be rounded at its size)
+                    floatx4 z = init[r][0];
 #pragma unroll
-                    for (int k = NP - 1; k >= 0; --k)
+                    for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt[r][e][0], codes24(u[e]), z, 0, 0, 0);
+                    if constexpr (!ONE) {
+                        floatx4 v = init[r][1];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt[r][e][k], codes24(u[e]), z, 0, 0, 0);
+                        for (int k = 2; k >= 1; --k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt[r][e][k], codes24(u[e]), v, 0, 0, 0);
+                        z += v;
+                    }
                     const float s = in ? dev::bf16_bits_to_float(sc[r][j]) : 0.f;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) acc[j][q] = fmaf(s, z[q], acc[j][q]);

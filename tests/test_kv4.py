@@ -42,13 +42,15 @@ def magnitude(x):
     return ((32 + u) * s + m.abs()).flatten(-2)
 
 
-def attend(q, ks, vs, ns, ls, G, window, scale):
+def attend(q, ks, vs, ns, ls, G, window, scale, dtype):
     """Plain attention and its error bound: q [T, heads, d] float64; ks, vs: per sequence [L, n_kv, d] vectors
     before quantisation.  The bound per output is the sum of the roundings on its way:
-      scores: exact products in fp32 sums of at most 32 partial results (2^-24 each of what they amount to),
-              then two roundings on the way to the exponent; an error e of a score changes a probability by e;
+      scores: queries within 2^-22 of the head's largest element, products in fp32 sums of at most 32 partial
+              results (2^-24 each of what they amount to), two roundings on the way to the exponent, and for
+              bf16 tensors keys as fp16 (2^-11); an error e of a score changes a probability by e;
       exponentials and the sum: 2^-20 together;
-      probabilities: times the scale (2^-24) and into bf16 terms: 2^-16 (two terms) or 2^-8 (one)."""
+      probabilities and values: two fp16 terms (2^-22) or three fp16 roundings (3 x 2^-11)."""
+    keys = 0.0 if dtype is F32 else 2.0 ** -11
     T, heads, d = q.shape
     out = torch.zeros((T, heads, d), dtype=torch.float64)
     amount = torch.zeros((T, heads, d), dtype=torch.float64)  # sum of P x magnitude
@@ -66,14 +68,16 @@ def attend(q, ks, vs, ns, ls, G, window, scale):
                 p = torch.softmax(z, 0)
                 out[t0 + i, h] = p @ V
                 amount[t0 + i, h] = p @ magnitude(v[first:P + 1, h // G])
-                e = (magnitude(k[first:P + 1, h // G]) @ q[t0 + i, h].abs()) * abs(scale) * 2.0 ** -19
-                shift[t0 + i, h] = (e + z.abs() * 2.0 ** -22).max()
+                m = magnitude(k[first:P + 1, h // G])
+                e = (m @ q[t0 + i, h].abs()) * 2.0 ** -19 + m.sum(1) * q[t0 + i, h].abs().max() * 2.0 ** -22
+                e = e + (K.abs() @ q[t0 + i, h].abs()) * keys
+                shift[t0 + i, h] = (e * abs(scale) + z.abs() * 2.0 ** -22).max()
         t0 += n
     return out, amount, shift
 
 
 def attention_tolerance(ref, amount, shift, dtype):
-    term = 2.0 ** -16 if dtype is F32 else 2.0 ** -8
+    term = 2.0 ** -22 if dtype is F32 else 3 * 2.0 ** -11
     return amount * (2 * shift + 2.0 ** -20 + term) + ref.abs() * torch.finfo(dtype).eps / 2 + 1e-30
 
 
@@ -359,7 +363,7 @@ def attention_case(d, n_kv, G, ns, ls, max_pos, window, dtype, seed=0, scale=Non
     cache = fill(moe.kv4_cache(len(ls), n_kv, d, max_pos))
     put(ks, vs, cache, F32)
     q = torch.randn((sum(ns), n_kv * G, d), generator=gen).to(dtype)
-    ref, amount, shift = attend(q.double(), ks, vs, ns, ls, G, window, d ** -0.5 if scale is None else scale)
+    ref, amount, shift = attend(q.double(), ks, vs, ns, ls, G, window, d ** -0.5 if scale is None else scale, dtype)
     return cache, q, ref, attention_tolerance(ref, amount, shift, dtype)
 
 
@@ -424,13 +428,11 @@ def test_attention_long_and_split(n):
     cache = fill(moe.kv4_cache(1, n_kv, d, 5024))
     put([k], [v], cache, F32)
     q = torch.randn((n, G, d), generator=gen)
-    ref, amount, shift = attend(q.double(), [k], [v], [n], [L], G, 0, d ** -0.5)
     qs, kl, _ = batch([n], [L])
     assert moe.moe_kv4_attention_workspace_bytes(n, 1, G, n_kv, d, n, 5024) > 0
     for dtype in (F32, BF16):
         qd = q.to(dtype)
-        if dtype is BF16:
-            ref, amount, shift = attend(qd.double(), [k], [v], [n], [L], G, 0, d ** -0.5)
+        ref, amount, shift = attend(qd.double(), [k], [v], [n], [L], G, 0, d ** -0.5, dtype)
         out = moe.moe_kv4_attention(qd.cuda(), cache, kl, q_start=qs, max_q=n)
         err = (out.cpu().double() - ref).abs()
         tol = attention_tolerance(ref, amount, shift, dtype)
@@ -667,7 +669,7 @@ def test_block_matches_its_parts(d, n_kv, G, lens):
                 att[h] = p @ V[at:at + L, h // G]
             y[t] += wo @ att.flatten()
         at += L
-    # 2^-16 of the probabilities' terms, scores within 2^-16 and the projections' sums, on outputs of sum |w| |att|
+    # probabilities and scores within 2^-16 and the projections' sums, on outputs of sum |w| |att|
     tol = wo.abs().sum(1).max() * 4.0 * 2.0 ** -14 / math.sqrt(nh * d) + 1e-5
     assert ((xd.cpu().double() - y).abs() <= tol).all(), float((xd.cpu().double() - y).abs().max() / tol)
     for t, L in enumerate(lens):

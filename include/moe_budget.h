@@ -312,7 +312,7 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
  *   w    device MOE_INT4G128 matrix [N x K], 16-byte aligned: packed nibbles [N x K/2], then bf16 scales [N x K/128]
  *   add  device fp32 [T x N], or NULL; may be y
  *   y    device fp32 [T x N], apart from x
- * Exact products, fp32 sums.  T == 0 or N == 0 is a no-op. */
+ * The tokens' values enter within 2^-22 of the token's largest; exact products, fp32 sums.  T == 0 or N == 0 is a no-op. */
 MOE_API int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
                             void *stream);
 

@@ -333,16 +333,28 @@ def moe_attention_decode(x, w_qkv, w_o, k_cache, v_cache, p: int, n_heads: int, 
 
 
 # ------------------------------------------------------- 4-bit cache, int4 projections ---
-def _here(*tensors):
-    """The tensors' common device, which has to be the current one (the library launches there)."""
+def _current_device() -> int:
     import torch
-    devs = {t.device for t in tensors if t is not None}
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
+def _here(*tensors) -> int:
+    """The tensors' common device, which has to be the current one (the library launches there)."""
+    current = None
     for t in tensors:
-        if t is not None and not t.is_cuda:
+        if t is None:
+            continue
+        dev = t.get_device()
+        if dev < 0:
             raise ValueError("the tensors must be device tensors")
-    if devs != {torch.device("cuda", torch.cuda.current_device())}:
-        raise ValueError(f"the tensors are on {sorted(map(str, devs))}, the current device is cuda:{torch.cuda.current_device()}")
-    return devs.pop()
+        if current is None:
+            current = _current_device()
+        if dev != current:
+            raise ValueError(f"a tensor is on cuda:{dev}, the current device is cuda:{current}")
+    return current
 
 
 class _On:
@@ -351,11 +363,13 @@ class _On:
     A tensor made here for a call on another stream than the current one belongs to that stream, and the
     caller's tensors are marked as used there, so that none is handed out again before the work has run."""
 
+    __slots__ = ("handle", "other")
+
     def __init__(self, stream):
-        import torch
         self.handle = _stream(stream)
         self.other = None
         if stream is not None and self.handle != _stream(None):
+            import torch
             self.other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle)
 
     def empty(self, shape, dtype, device):
@@ -372,48 +386,47 @@ class _On:
                     t.record_stream(self.other)
 
 
-def _float_code(t, name):
+def _float_code(dtype, name):
     import torch
-    code = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected float32 or bfloat16")
-    return code
+    if dtype is torch.float32:
+        return MOE_F32
+    if dtype is torch.bfloat16:
+        return MOE_BF16
+    raise ValueError(f"{name} has dtype {dtype}, expected float32 or bfloat16")
 
 
 def _rows(t, name, heads, d, T=None, dtype=None):
     """(pointer, elements from token to token) of a token array [T, heads, d]; only the tokens may be strided."""
-    if t is None:
-        return None, 0
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or (T is not None and t.shape[0] != T):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{'T' if T is None else T}, {heads}, {d}]")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d or (T is not None and shape[0] != T):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [{'T' if T is None else T}, {heads}, {d}]")
     if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+    if (stride[2] != 1 or (stride[1] != d and heads > 1)) and shape[0]:
         raise ValueError(f"{name}: the heads and dims of a token must be contiguous")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+    return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
 
 
 def _kv4_shape(cache):
     """(n_seq, n_kv, head_dim, max_pos) of a cache made by kv4_cache."""
     import torch
-    if cache.dtype is not torch.uint8 or cache.dim() != 4 or cache.shape[3] not in (36 * 64, 36 * 128, 36 * 192, 36 * 256):
-        raise ValueError(f"cache {cache.dtype} {tuple(cache.shape)} is no 4-bit cache (uint8 [n_seq, n_kv, blocks, 36 head_dim])")
+    shape = cache.shape
+    if cache.dtype is not torch.uint8 or len(shape) != 4 or shape[3] not in (36 * 64, 36 * 128, 36 * 192, 36 * 256):
+        raise ValueError(f"cache {cache.dtype} {tuple(shape)} is no 4-bit cache (uint8 [n_seq, n_kv, blocks, 36 head_dim])")
     if not cache.is_contiguous():
         raise ValueError("cache must be contiguous")
-    return cache.shape[0], cache.shape[1], cache.shape[3] // 36, cache.shape[2] * MOE_KV4_BLOCK
+    return shape[0], shape[1], shape[3] // 36, shape[2] * MOE_KV4_BLOCK
 
 
-def _kv4_batch(cache, T, kv_len, q_start, max_q):
+def _kv4_batch(n_seq, T, kv_len, q_start, max_q):
     import torch
-    n_seq = cache.shape[0]
-    if kv_len.numel() != n_seq:
-        raise ValueError(f"kv_len has {kv_len.numel()} entries, the cache {n_seq} sequences")
-    if q_start is not None and q_start.numel() != n_seq + 1:
-        raise ValueError(f"q_start has {q_start.numel()} entries, expected {n_seq + 1}")
-    return (_dev(kv_len, "kv_len", torch.int32), _dev(q_start, "q_start", torch.int32),
-            1 if q_start is None else max(T, 1) if max_q is None else max_q)
+    if kv_len.dtype is not torch.int32 or kv_len.numel() != n_seq or not kv_len.is_contiguous():
+        raise ValueError(f"kv_len {kv_len.dtype} {tuple(kv_len.shape)}: expected contiguous int32, one per sequence ({n_seq})")
+    if q_start is None:
+        return kv_len.data_ptr(), None, 1
+    if q_start.dtype is not torch.int32 or q_start.numel() != n_seq + 1 or not q_start.is_contiguous():
+        raise ValueError(f"q_start {q_start.dtype} {tuple(q_start.shape)}: expected {n_seq + 1} contiguous int32")
+    return kv_len.data_ptr(), q_start.data_ptr(), (max(T, 1) if max_q is None else max_q)
 
 
 def moe_kv4_cache_bytes(n_seq: int, n_kv: int, head_dim: int, max_pos: int) -> int:
@@ -435,14 +448,16 @@ def moe_kv4_append(k, v, cache, kv_len, q_start=None, max_q: int | None = None, 
     the last positions of their sequences (kv_len int32 [n_seq], the tokens included; q_start int32 [n_seq + 1]:
     sequence b's rows, None for one token each; max_q: most tokens of a sequence, T by default)."""
     n_seq, n_kv, d, max_pos = _kv4_shape(cache)
-    T = k.shape[0]
+    T, dtype = k.shape[0], k.dtype
     kp, ks = _rows(k, "k", n_kv, d)
-    vp, vs = _rows(v, "v", n_kv, d, T, k.dtype)
-    lp, qp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    vp, vs = _rows(v, "v", n_kv, d, T, dtype)
+    lp, qp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     _here(k, v, cache, kv_len, q_start)
     on = _On(stream)
-    _check(lib().moe_kv4_append(kp, vp, _float_code(k, "k"), ks, vs, T, n_seq, n_kv, d, max_pos, qp, mq, lp,
-                                _dev(cache, "cache"), cache.numel(), on.handle), "moe_kv4_append")
+    code = (_lib or lib()).moe_kv4_append(kp, vp, _float_code(dtype, "k"), ks, vs, T, n_seq, n_kv, d, max_pos, qp, mq, lp,
+                                          cache.data_ptr(), cache.numel(), on.handle)
+    if code:
+        _check(code, "moe_kv4_append")
     on.used(k, v, cache, kv_len, q_start)
 
 
@@ -454,15 +469,17 @@ def moe_kv4_read(cache, kv_len, T: int, q_start=None, max_q: int | None = None, 
     n_seq, n_kv, d, max_pos = _kv4_shape(cache)
     given = k_out if k_out is not None else v_out
     dtype = given.dtype if given is not None else torch.bfloat16 if dtype is None else dtype
-    lp, qp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    lp, qp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     device = _here(cache, kv_len, q_start, k_out, v_out)
     on = _On(stream)
     k_out = on.empty((T, n_kv, d), dtype, device) if k_out is None else k_out
     v_out = on.empty((T, n_kv, d), dtype, device) if v_out is None else v_out
     kp, ks = _rows(k_out, "k_out", n_kv, d, T, dtype)
     vp, vs = _rows(v_out, "v_out", n_kv, d, T, dtype)
-    _check(lib().moe_kv4_read(_dev(cache, "cache"), cache.numel(), T, n_seq, n_kv, d, max_pos, qp, mq, lp, kp, vp,
-                              _float_code(k_out, "k_out"), ks, vs, on.handle), "moe_kv4_read")
+    code = (_lib or lib()).moe_kv4_read(cache.data_ptr(), cache.numel(), T, n_seq, n_kv, d, max_pos, qp, mq, lp, kp, vp,
+                                        _float_code(dtype, "k_out"), ks, vs, on.handle)
+    if code:
+        _check(code, "moe_kv4_read")
     on.used(cache, kv_len, q_start, k_out, v_out)
     return k_out, v_out
 
@@ -477,24 +494,28 @@ def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, 
     """Causal attention of the tokens' queries (fp32 or bf16 [T, n_heads, d]) over the 4-bit cache, with
     window > 0 over the last `window` positions (batch as for moe_kv4_append; scale 1 / sqrt(d) by default);
     returns out [T, n_heads, d] of q's type.  Rows from q_start[-1] on are not written."""
-    import torch
     n_seq, n_kv, d, max_pos = _kv4_shape(cache)
     if q.dim() != 3:
         raise ValueError(f"q has shape {tuple(q.shape)}, expected [T, n_heads, {d}]")
-    T, n_heads = q.shape[0], q.shape[1]
+    T, n_heads, _ = q.shape
+    dtype = q.dtype
     qp, qs = _rows(q, "q", n_heads, d)
-    lp, sp, mq = _kv4_batch(cache, T, kv_len, q_start, max_q)
+    lp, sp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     device = _here(q, cache, kv_len, q_start, out, workspace)
     on = _On(stream)
-    out = on.empty((T, n_heads, d), q.dtype, device) if out is None else out
-    op, os_ = _rows(out, "out", n_heads, d, T, q.dtype)
+    if out is None:
+        out = on.empty((T, n_heads, d), dtype, device)
+    op, os_ = _rows(out, "out", n_heads, d, T, dtype)
     if workspace is None:
+        import torch
         n = moe_kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, d, mq, max_pos)
         workspace = on.empty(max(n, 256), torch.uint8, device)
-    _check(lib().moe_kv4_attention(qp, _float_code(q, "q"), qs, _dev(cache, "cache"), cache.numel(), T, n_seq, n_heads,
-                                   n_kv, d, max_pos, sp, mq, lp, window, d ** -0.5 if scale is None else scale, op, os_,
-                                   _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                   on.handle), "moe_kv4_attention")
+    code = (_lib or lib()).moe_kv4_attention(qp, _float_code(dtype, "q"), qs, cache.data_ptr(), cache.numel(), T, n_seq,
+                                             n_heads, n_kv, d, max_pos, sp, mq, lp, window,
+                                             d ** -0.5 if scale is None else scale, op, os_, _dev(workspace, "workspace"),
+                                             workspace.nbytes, on.handle)
+    if code:
+        _check(code, "moe_kv4_attention")
     on.used(q, cache, kv_len, q_start, out, workspace)
     return out
 
@@ -515,13 +536,17 @@ def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, strea
     T, K = x.shape
     device = _here(x, w, add, y)
     on = _On(stream)
-    y = on.empty((T, N), torch.float32, device) if y is None else y
-    for t, name in ((y, "y"), (add, "add")):
-        if t is not None and t.numel() != T * N:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{T}, {N}]")
-    _check(lib().moe_matvec_int4(_dev(x, "x", torch.float32), _int4_matrix(w, "w", N, K), T, N, K,
-                                 _dev(add, "add", torch.float32), _dev(y, "y", torch.float32),
-                                 MOE_ROUTE_RMSNORM if rmsnorm else 0, on.handle), "moe_matvec_int4")
+    if y is None:
+        y = on.empty((T, N), torch.float32, device)
+    elif y.numel() != T * N:
+        raise ValueError(f"y has shape {tuple(y.shape)}, expected [{T}, {N}]")
+    if add is not None and add.numel() != T * N:
+        raise ValueError(f"add has shape {tuple(add.shape)}, expected [{T}, {N}]")
+    code = (_lib or lib()).moe_matvec_int4(_dev(x, "x", torch.float32), _int4_matrix(w, "w", N, K), T, N, K,
+                                           _dev(add, "add", torch.float32), _dev(y, "y", torch.float32),
+                                           MOE_ROUTE_RMSNORM if rmsnorm else 0, on.handle)
+    if code:
+        _check(code, "moe_matvec_int4")
     on.used(x, w, add, y)
     return y
 

@@ -474,9 +474,10 @@ def test_attention_bad_batch_and_values(dtype):
 
 # ----------------------------------------------------------------------------------- int4 products (GPU) ---
 def matvec_reference(x, w, add, norm):
-    """Value and bound: exact products of (24 + q) s x in fp32 sums: a group's sum of at most 12 partial results
-    plus 24 times the sum of x, the groups' scaled sums (K / 128 of them), the terms and the norm: 2^-24 of
-    what they amount to for each of at most 32 + K / 128 roundings."""
+    """Value and bound: the tokens' values within 2^-22 of the token's largest, exact products of q s x in fp32 sums:
+    a group's sum of at most 12 partial results, the groups' scaled sums (K / 128 of them), the terms and the
+    norm: 2^-24 of what they amount to for each of at most 32 + K / 128 roundings (2^-22 where a matrix
+    product rounds towards zero)."""
     h = x.double()
     r = torch.ones((x.shape[0], 1), dtype=torch.float64)
     if norm:
@@ -484,8 +485,9 @@ def matvec_reference(x, w, add, norm):
     K = x.shape[1]
     q, s = w
     y = (h * r) @ (q * s).T
-    amount = (h.abs() * r) @ ((48 + q.abs()) * s.abs()).T
-    tol = amount * (32 + K // 128) * 2.0 ** -24 + y.abs() * 2.0 ** -21
+    amount = (h.abs() * r) @ (q.abs() * s.abs()).T
+    largest = (h.abs().amax(1, keepdim=True) * r) @ (q.abs() * s.abs()).sum(1)[None]
+    tol = amount * (32 + K // 128) * 2.0 ** -22 + largest * 2.0 ** -22 + y.abs() * 2.0 ** -21
     if add is not None:
         y = y + add.double()
     return y, tol + y.abs() * 2.0 ** -24

@@ -296,7 +296,9 @@ MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, 
  * token's own, with window > 0 the last `window` of those (window <= 2^30); query head j reads key/value head
  * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums;
  * queries enter exactly (MOE_BF16) or as two fp16 terms (MOE_F32: 2^-22 of the head's largest element), probabilities
- * times scales rounded to fp16 (2^-11) or as two fp16 terms (2^-22).  Elements of q up to 2^100 in magnitude.
+ * times scales as two fp16 terms (MOE_F32: 2^-22) or rounded to fp16 (MOE_BF16: 2^-11; calls of many rows round the
+ * held keys and values to fp16 as well).  Elements of q up to 2^100 in magnitude; keys and values within 2^20 of
+ * the largest of their sequence keep the precision stated.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
  *   out        device, as q with out_stride, same dtype
  *   scale      any finite factor, as a rule 1 / sqrt(head_dim)

@@ -641,6 +641,311 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     }
 }
 
+// ---- many rows (prompts), bf16 tensors -------------------------------------------------------------------------
+//
+// Where a block of positions meets hundreds of rows the arithmetic per score counts, not the bytes: the waves of a
+// block turn the codes of 64 positions into fp16 keys and values once (2^-11; scaled by powers of two, 2^6 the
+// largest) and share them through LDS in the operands' order, and a score costs an fma, an exponential, a share
+// of a maximum and of a conversion.  Two buffers: the next positions' codes are loaded before the present ones are
+// used and turned after.  The sums of P come from the matrix cores too.
+constexpr int kPromptTiles = 2;  // row tiles of 16 per wave
+
+// A barrier for what the block's waves pass one another through LDS; loads in flight stay so.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// The power of two that takes values of at most |m| + 15 s below 2^6: m, s a pair of bf16 per lane.
+__device__ __forceinline__ int held_exponent(uint32_t m, uint32_t s) {
+    m &= 0x7fff7fffu;
+    const uint32_t tm = dev::wave_reduce_u32<true>(max(m & 0xffffu, m >> 16)), ts = dev::wave_reduce_u32<true>(max(s & 0xffffu, s >> 16));
+    const float top = fmaf(15.f, bf16_float(ts), bf16_float(tm));
+    return top > 0.f && top < INFINITY ? min(5 - ilogbf(top), 100) : 0;
+}
+
+// grid: (row tiles, key/value head, sequence); WAVES x 32 rows per block.
+template <int NG, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a) {
+    constexpr int d = NG * kGroup, NT = kPromptTiles, ROWS = 16 * NT * WAVES;
+    constexpr int FRAGS = 8 * NG;           // operands (1 KiB) of two blocks' keys, and of their values
+    constexpr int WORDS = 16 * NG / WAVES;  // words of codes per lane that a wave turns
+    constexpr int SPLIT = WAVES / 4;        // waves that share one block's keys or values
+    static_assert(WAVES == 4 || WAVES == 8);
+    __shared__ uint4 kf_sh[2][FRAGS][64], vf_sh[2][FRAGS][64];
+    const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+    const Seq s = sequence(a.batch, blockIdx.z);
+    if (s.bad && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(a.err, kErrRange);
+    // (the last rows see the most positions: their blocks start first)
+    const int G = a.group, rows = s.n * G, tile = gridDim.x - 1 - blockIdx.x, row0 = tile * ROWS;
+    if (row0 >= rows) return;
+    const int p_first = s.len - s.n + row0 / G, p_last = s.len - s.n + min(s.n - 1, (row0 + ROWS - 1) / G);
+    const int b0 = a.window ? max(0, p_first - a.window + 1) / kPos : 0, b1 = p_last < 0 ? b0 : p_last / kPos + 1;
+    const uint8_t *seq = a.cache + (size_t(blockIdx.z) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
+
+    // What this wave turns: block `mine_b` of the pair, its keys or values, a half of them (eight waves).
+    const int mine_b = (wave >> 1) & 1, part = wave >> 2;
+    const bool values = wave & 1;
+    uint32_t raw[WORDS], ps[4 * NG], pm[4 * NG], lim[4];  // codes, scales and bases; all the pair's scales and bases
+    auto load = [&](int b) __attribute__((always_inline)) {
+        // (past the last block: that one again, masked by its position)
+        const uint8_t *block = seq + size_t(min(b + mine_b, b1 - 1)) * block_bytes(d);
+        const uint8_t *codes = block + (values ? v_codes(d) : k_codes(d));
+        if constexpr (WORDS % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) {
+                const uint4 u = dev::load16(codes + (part * (WORDS / 4) + i) * 1024 + lane * 16);
+                raw[4 * i] = u.x, raw[4 * i + 1] = u.y, raw[4 * i + 2] = u.z, raw[4 * i + 3] = u.w;
+            }
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2 *>(codes + lane * 16 + part * 8);
+            raw[0] = u.x, raw[1] = u.y;
+        }
+        if (values) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint4 u = dev::load16(block + v_scales(d) + g * 64 + c * 16), v = dev::load16(block + v_bases(d) + g * 64 + c * 16);
+                ps[4 * g] = u.x, ps[4 * g + 1] = u.y, ps[4 * g + 2] = u.z, ps[4 * g + 3] = u.w;
+                pm[4 * g] = v.x, pm[4 * g + 1] = v.y, pm[4 * g + 2] = v.z, pm[4 * g + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                pm[g] = *reinterpret_cast<const uint32_t *>(block + k_bases(d) + g * 64 + n * 4);
+#pragma unroll
+                for (int tau = 0; tau < 2; ++tau)
+                    ps[2 * g + tau] = *reinterpret_cast<const uint16_t *>(block + k_scales(d) + g * 64 + 2 * order_index(16 * tau + n));
+            }
+        }
+        // Every wave sees all the scales and bases: one pair of values per lane and array (lane = block, word).
+        const uint8_t *all = seq + size_t(min(b + (lane >> 5), b1 - 1)) * block_bytes(d) + 4 * ((lane & 31) % (16 * NG));
+        lim[0] = *reinterpret_cast<const uint32_t *>(all + k_scales(d));
+        lim[1] = *reinterpret_cast<const uint32_t *>(all + k_bases(d));
+        lim[2] = *reinterpret_cast<const uint32_t *>(all + v_scales(d));
+        lim[3] = *reinterpret_cast<const uint32_t *>(all + v_bases(d));
+    };
+    int ek[2] = {0, 0}, ev[2] = {0, 0};  // exponents of the two buffers' keys and values
+    auto turn = [&](int b, int buf, int most) __attribute__((always_inline)) {  // most: of the values' exponent
+        if ((b + 2) * kPos > s.len) {
+            // Positions that hold nothing yet may hold anything: their scales and bases count as zeros.
+            const int blk = min(b + (lane >> 5), b1 - 1), w = (lane & 31) % (16 * NG) & 15;  // word of the group's 16
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int o = 2 * w + e, in_order = 16 * ((o >> 2) & 1) + 4 * (o >> 3) + (o & 3), in_tiles = 16 * e + w;
+                const uint32_t drop = ~(0xffffu << (16 * e));
+                if (blk * kPos + in_order >= s.len) lim[0] &= drop, lim[2] &= drop, lim[3] &= drop;
+                if (blk * kPos + in_tiles >= s.len) lim[1] &= drop;
+            }
+            if (values) {
+                const int own = min(b + mine_b, b1 - 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int k = 2 * i + e;
+                        if (own * kPos + 16 * (k >> 2) + 4 * c + (k & 3) < s.len) continue;
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            ps[4 * g + i] &= ~(0xffffu << (16 * e));
+                            pm[4 * g + i] &= ~(0xffffu << (16 * e));
+                        }
+                    }
+            }
+        }
+        ek[buf] = held_exponent(lim[1], lim[0]);
+        ev[buf] = min(most, held_exponent(lim[3], lim[2]));
+        const float fm = ldexpf(1.f, values ? ev[buf] : ek[buf]), fs = fm * 512.f;  // (codes as u 2^-9)
+        uint4 *dst = &(values ? vf_sh : kf_sh)[buf][mine_b * 4 * NG + part * WORDS][lane];
+        auto turned = [&](uint32_t w, f16x2 s0, f16x2 s1, f16x2 s2, f16x2 s3, f16x2 m0, f16x2 m1, f16x2 m2, f16x2 m3) {
+            constexpr _Float16 l = 0x1p15f, q = 0x1p11f;
+            const f16x8 u = raw_codes(w) * f16x8{l, l, q, q, l, l, q, q};
+            return __builtin_bit_cast(uint4, u * join8(s0, s1, s2, s3) + join8(m0, m1, m2, m3));
+        };
+        if (values) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                if (SPLIT == 2 && NG == 2 && g != part) continue;  // (a half of two groups' words is one group's)
+                f16x2 sc[4], ba[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sc[i] = pack_f16(low_half(ps[4 * g + i]) * fs, high_half(ps[4 * g + i]) * fs);
+                    ba[i] = pack_f16(low_half(pm[4 * g + i]) * fm, high_half(pm[4 * g + i]) * fm);
+                }
+                constexpr int per = WORDS < 4 ? WORDS : 4;
+#pragma unroll
+                for (int i = 0; i < per; ++i) {
+                    const int w = (SPLIT == 2 && NG == 2 ? 0 : 4 * g) + i;
+                    dst[w * 64] = turned(raw[w], sc[0], sc[1], sc[2], sc[3], ba[0], ba[1], ba[2], ba[3]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int tau = 0; tau < 2; ++tau) {
+                if (SPLIT == 2 && tau != part) continue;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float sv = low_half(ps[2 * g + tau]) * fs, mv = (tau ? high_half(pm[g]) : low_half(pm[g])) * fm;
+                    const f16x2 sc = pack_f16(sv, sv), ba = pack_f16(mv, mv);
+#pragma unroll
+                    for (int j = 2 * g; j < 2 * g + 2; ++j) {
+                        const int w = (SPLIT == 2 ? 0 : tau * 2 * NG) + j;
+                        dst[w * 64] = turned(raw[w], sc, sc, sc, sc, ba, ba, ba, ba);
+                    }
+                }
+            }
+        }
+    };
+
+    // The rows: their queries as operands, scaled as in kv4_attend_kernel; a row past the last repeats it.
+    const int w_row0 = row0 + wave * 16 * NT;
+    auto row_of = [&](int t) { return min(w_row0 + 16 * t + n, rows - 1); };
+    f16x8 bq[NT][2 * NG];
+    int last[NT];
+    float zs[NT];
+    {
+        uint4 qraw[NT][2 * NG];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = row_of(t), i = row / G;
+            const size_t at = size_t(s.t0 + i) * a.q_stride + size_t(h * G + row - i * G) * d + 8 * c;
+            last[t] = s.len - s.n + i;
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j)
+                qraw[t][j] = dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * j));
+        }
+        if (b0 < b1) load(b0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float x[2 * NG][8], top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j) {
+                const uint32_t w[4] = {qraw[t][j].x, qraw[t][j].y, qraw[t][j].z, qraw[t][j].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[j][2 * e] = low_half(w[e]);
+                    x[j][2 * e + 1] = high_half(w[e]);
+                    top = fmaxf(top, fmaxf(fabsf(x[j][2 * e]), fabsf(x[j][2 * e + 1])));
+                }
+            }
+            top = max_over_c(top);
+            const int e2 = top > 0.f && top < INFINITY ? min(max(14 - ilogbf(top), -88), 148) : 0;
+            zs[t] = fmaxf(ldexpf(fabsf(a.scale), -e2), 0x1p-126f);
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j) {
+                f16x8 q1[1];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = ldexpf(a.scale < 0.f ? -x[j][e] : x[j][e], e2);
+                split<1>(x[j], q1);
+                bq[t][j] = q1[0];
+            }
+        }
+    }
+
+    floatx4 acc[NT][4 * NG], sum[NT];  // sum of 2^(15 + ea) P V (dims x rows), sum of 2^15 P (in every element)
+    float mx[NT];                      // the row's largest score, log2 units
+    int ea = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        mx[t] = -INFINITY;
+        sum[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (b0 < b1) turn(b0, 0, 100);
+    lds_barrier();
+    // (the wave's own rows decide which blocks need no mask)
+    const int w_first = s.len - s.n + min(w_row0, rows - 1) / G, w_last = s.len - s.n + min(w_row0 + 16 * NT - 1, rows - 1) / G;
+    auto step = [&](int b, int buf) __attribute__((always_inline)) {
+        const bool more = b + 2 < b1;
+        if (more) load(b + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        float p[NT][16];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {  // 16 positions: block u / 2, tile u % 2
+            f16x8 kf[2 * NG];
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j) kf[j] = __builtin_bit_cast(f16x8, kf_sh[buf][u * 2 * NG + j][lane]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                floatx4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 2 * NG; ++j) z = mfma(kf[j], bq[t][j], z);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[t][4 * u + r] = z[r];
+            }
+        }
+        const bool full = (b + 2) * kPos - 1 <= w_first && b + 2 <= b1 && (!a.window || b * kPos > w_last - a.window);
+        const float unscale = ldexpf(1.f, -ek[buf]);
+        const int e_new = ev[buf];
+        f16x8 bp[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (!full) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int at = (b + (k >> 3)) * kPos + 16 * ((k >> 2) & 1) + 4 * c + (k & 3);
+                    if (at > last[t] || at >= b1 * kPos || (a.window && at <= last[t] - a.window)) p[t][k] = -INFINITY;
+                }
+            }
+            float top = p[t][0];
+#pragma unroll
+            for (int k = 1; k < 16; ++k) top = fmaxf(top, p[t][k]);
+            top = max_over_c(top);
+            const float zk = fmaxf(zs[t] * unscale, 0x1p-126f);
+            const float was = mx[t], now = fmaxf(was, top == -INFINITY ? top : product(top, zk));
+            if (__any(now > was) || e_new != ea) {
+                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(was - now), fa = ldexpf(f, e_new - ea);
+                mx[t] = now;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[t][r] *= f;
+#pragma unroll
+                for (int i = 0; i < 4 * NG; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[t][i][r] *= fa;
+            }
+            const float off = now == -INFINITY ? 0.f : now - 15.f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) p[t][k] = __builtin_amdgcn_exp2f(fmaf(p[t][k], zk, -off));
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                bp[t][u] = join8(pack_f16(p[t][8 * u], p[t][8 * u + 1]), pack_f16(p[t][8 * u + 2], p[t][8 * u + 3]),
+                                 pack_f16(p[t][8 * u + 4], p[t][8 * u + 5]), pack_f16(p[t][8 * u + 6], p[t][8 * u + 7]));
+        }
+        ea = e_new;
+        const _Float16 one = 1.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sum[t] = mfma(f16x8{one, one, one, one, one, one, one, one}, bp[t][u], sum[t]);
+#pragma unroll
+            for (int i = 0; i < 4 * NG; ++i) {
+                const f16x8 vf = __builtin_bit_cast(f16x8, vf_sh[buf][u * 4 * NG + i][lane]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t][i] = mfma(vf, bp[t][u], acc[t][i]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) turn(b + 2, buf ^ 1, ea);
+        lds_barrier();
+    };
+#pragma unroll 1
+    for (int b = b0; b < b1; b += 4) {
+        step(b, 0);
+        if (b + 2 < b1) step(b + 2, 1);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = w_row0 + 16 * t + n;
+        if (row >= rows) continue;
+        const float l = sum[t][0], inv = l == 0.f ? 0.f : 1.f / l;
+        const size_t at = size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * c;
+#pragma unroll
+        for (int i = 0; i < 4 * NG; ++i)
+            store4<false>(a.out, at + 16 * i, make_float4(ldexpf(acc[t][i][0] * inv, -ea), ldexpf(acc[t][i][1] * inv, -ea),
+                                                          ldexpf(acc[t][i][2] * inv, -ea), ldexpf(acc[t][i][3] * inv, -ea)));
+    }
+}
+
 // Joins the pieces of one row.  grid: (rows, key/value head, sequence); groups of d / 4 lanes take the pieces in
 // turn, a running maximum each.
 template <int NG, bool F32>
@@ -704,6 +1009,7 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
 
 // Tiles of 16 rows per wave (0: one of 8), row tiles of the largest sequence, and the split of the positions.
 struct AttendPlan {
+    int prompt;  // waves of the kernel for many rows, or 0
     int tiles, tile_rows, blocks, target, units;
     size_t workspace;
 };
@@ -712,6 +1018,11 @@ AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max
     // what a wave's registers hold
     const int most = d <= 64 ? (f32 ? 2 : 4) : d <= 128 ? 2 : d <= 192 && !f32 ? 2 : 1;
     AttendPlan p{};
+    if (!f32 && d <= 128 && rows >= 128 && (rows + 127) / 128 * n_kv * n_seq >= 64) {
+        p.prompt = (rows + 255) / 256 * n_kv * n_seq >= 256 ? 8 : 4;
+        p.blocks = int((rows + 32 * p.prompt - 1) / (32 * p.prompt));
+        return p;
+    }
     p.tiles = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
     p.tile_rows = p.tiles ? 16 * p.tiles : 8;
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
@@ -754,6 +1065,13 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     a.batch = batch;
     a.err = err;
     const dim3 grid = p.target ? dim3(p.units, n_kv, p.blocks) : dim3(p.blocks, n_kv, batch.n_seq);
+    if (p.prompt) {
+        if (d == 64 && p.prompt == 4) kv4_prompt_kernel<1, 4><<<grid, 256, 0, s>>>(a);
+        else if (d == 64) kv4_prompt_kernel<1, 8><<<grid, 512, 0, s>>>(a);
+        else if (p.prompt == 4) kv4_prompt_kernel<2, 4><<<grid, 256, 0, s>>>(a);
+        else kv4_prompt_kernel<2, 8><<<grid, 512, 0, s>>>(a);
+        return hipGetLastError();
+    }
 #define KV4_RUN(NG, NT, F) kv4_attend_kernel<NG, NT ? NT : 1, F, NT == 0><<<grid, kAttBlock, 0, s>>>(a)
 #define KV4_CASE(NG, NT, F) case (NG * 2 + F) * 8 + NT: KV4_RUN(NG, NT, F); break;
     switch ((d / kGroup * 2 + f32) * 8 + p.tiles) {

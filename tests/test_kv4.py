@@ -57,21 +57,19 @@ def attend(q, ks, vs, ns, ls, G, window, scale, dtype):
     shift = torch.zeros((T, heads, 1), dtype=torch.float64)   # largest error of a score
     t0 = 0
     for n, L, k, v in zip(ns, ls, ks, vs):
-        for i in range(n):
-            P = L - n + i
-            if P < 0:
-                continue
-            first = max(0, P - window + 1) if window else 0
-            for h in range(heads):
-                K, V = held(k[first:P + 1, h // G]), held(v[first:P + 1, h // G])
-                z = (K @ q[t0 + i, h]) * scale
-                p = torch.softmax(z, 0)
-                out[t0 + i, h] = p @ V
-                amount[t0 + i, h] = p @ magnitude(v[first:P + 1, h // G])
-                m = magnitude(k[first:P + 1, h // G])
-                e = (m @ q[t0 + i, h].abs()) * 2.0 ** -19 + m.sum(1) * q[t0 + i, h].abs().max() * 2.0 ** -22
-                e = e + (K.abs() @ q[t0 + i, h].abs()) * keys
-                shift[t0 + i, h] = (e * abs(scale) + z.abs() * 2.0 ** -22).max()
+        first = max(0, n - L)  # tokens before it are padding
+        at = torch.arange(L - n + first, L).view(-1, 1, 1)
+        p = torch.arange(L)
+        see = (p <= at) & (p > at - (window or L + 1))
+        for h in range(heads // G if n > first else 0):
+            rows, cols = slice(t0 + first, t0 + n), slice(h * G, (h + 1) * G)
+            K, V, mk, mv = held(k[:, h]), held(v[:, h]), magnitude(k[:, h]), magnitude(v[:, h])
+            x = q[rows, cols]
+            z = x @ K.T * scale
+            w = torch.softmax(torch.where(see, z, torch.tensor(-math.inf, dtype=torch.float64)), -1)
+            out[rows, cols], amount[rows, cols] = w @ V, w @ mv
+            e = x.abs() @ mk.T * 2.0 ** -19 + mk.sum(1) * x.abs().amax(-1, keepdim=True) * 2.0 ** -22 + x.abs() @ K.abs().T * keys
+            shift[rows, cols] = torch.where(see, e * abs(scale) + z.abs() * 2.0 ** -22, 0.0).amax(-1, keepdim=True)
         t0 += n
     return out, amount, shift
 
@@ -353,6 +351,13 @@ CASES = [  # (d, n_kv, group, tokens, lengths, max_pos, window)
     (64, 1, 2, [4, 4], [130, 64], 160, 1),
     (64, 2, 4, [6, 5, 3, 1], [2, 0, 3, 0], 32, 0),      # padded tokens, sequences without a position
     (128, 1, 4, [40, 1], [7, 0], 64, 5),
+    # hundreds of rows on many heads
+    (128, 16, 4, [40, 33, 70, 5], [40, 100, 200, 3], 224, 0),
+    (64, 16, 8, [16, 1, 17], [300, 1, 64], 320, 0),
+    (128, 16, 8, [31, 16, 40, 2], [64, 20, 17, 1], 96, 0),
+    (64, 16, 4, [33, 40, 64, 20], [130, 65, 64, 7], 160, 48),
+    (128, 64, 4, [33, 32, 31, 40], [97, 32, 10, 160], 160, 0),
+    (64, 64, 2, [64, 80, 70, 3], [70, 80, 200, 0], 224, 33),
 ]
 
 
@@ -414,6 +419,29 @@ def test_attention_scales(dtype, scale):
     qs, kl, _ = batch(case[3], case[4])
     out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, scale=scale)
     assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n_kv,G,n", [(2, 4, 1), (2, 12, 1), (2, 12, 3), (16, 8, 40)])
+@pytest.mark.parametrize("order", [1, -1])
+def test_attention_over_keys_and_values_of_changing_size(dtype, n_kv, G, n, order):
+    """Keys and values that grow (or shrink) by 2^16 from one run of positions to the next, run by run."""
+    gen = torch.Generator().manual_seed(n + G)
+    d, L = 128, 450
+    size = torch.exp2(torch.tensor([-8, -3, 0, 8, -8, 2, 5, 8, 1, -5])[::order].float()).repeat_interleave(45)[:, None, None]
+    v = torch.randn((L, n_kv, d), generator=gen) * size
+    k = torch.randn((L, n_kv, d), generator=gen) * size.rsqrt().clamp(max=4)
+    ks, vs, ns, ls = [k, k[:90]], [v, v[:90]], [n, n], [L, 90]
+    cache = fill(moe.kv4_cache(2, n_kv, d, 480))
+    put(ks, vs, cache, F32)
+    q = torch.randn((2 * n, n_kv * G, d), generator=gen).to(dtype)
+    ref, amount, shift = attend(q.double(), ks, vs, ns, ls, G, 0, 0.02, dtype)
+    qs, kl, _ = batch(ns, ls)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=n, scale=0.02)
+    moe.moe_sync_check()
+    err, tol = (out.cpu().double() - ref).abs(), attention_tolerance(ref, amount, shift, dtype)
+    assert (err <= tol).all(), float((err / tol).max())
 
 
 @pytest.mark.gpu

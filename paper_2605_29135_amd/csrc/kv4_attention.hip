@@ -656,12 +656,20 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-// The power of two that takes values of at most |m| + 15 s below 2^6: m, s a pair of bf16 per lane.
+// The power of two that takes values of at most |m| + 15 s below 2^6: m, s a pair of bf16 per lane (s >= 0).
 __device__ __forceinline__ int held_exponent(uint32_t m, uint32_t s) {
-    m &= 0x7fff7fffu;
-    const uint32_t tm = dev::wave_reduce_u32<true>(max(m & 0xffffu, m >> 16)), ts = dev::wave_reduce_u32<true>(max(s & 0xffffu, s >> 16));
-    const float top = fmaf(15.f, bf16_float(ts), bf16_float(tm));
-    return top > 0.f && top < INFINITY ? min(5 - ilogbf(top), 100) : 0;
+    // 2 max(|m|, 16 s) is no less; bf16 bits compare as numbers, and four exponents more are times 16
+    const u16x2 v = __builtin_elementwise_max(__builtin_bit_cast(u16x2, m & 0x7fff7fffu), __builtin_bit_cast(u16x2, s + 0x02000200u));
+    int top = max(int(v[0]), int(v[1]));
+#define ROW_MAX(CTRL) top = max(top, __builtin_amdgcn_update_dpp(0, top, CTRL, 0xF, 0xF, true))
+    ROW_MAX(0xB1);
+    ROW_MAX(0x4E);
+    ROW_MAX(0x141);
+    ROW_MAX(0x140);
+#undef ROW_MAX
+    const int all = max(max(__builtin_amdgcn_readlane(top, 0), __builtin_amdgcn_readlane(top, 16)),
+                        max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)));
+    return min(131 - (all >> 7), 100);  // (below 2^(exponent - 127 + 2))
 }
 
 // grid: (row tiles, key/value head, sequence); WAVES x 32 rows per block.

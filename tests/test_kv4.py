@@ -429,7 +429,7 @@ def test_attention_over_keys_and_values_of_changing_size(dtype, n_kv, G, n, orde
     """Keys and values that grow (or shrink) by 2^16 from one run of positions to the next, run by run."""
     gen = torch.Generator().manual_seed(n + G)
     d, L = 128, 450
-    size = torch.exp2(torch.tensor([-8, -3, 0, 8, -8, 2, 5, 8, 1, -5])[::order].float()).repeat_interleave(45)[:, None, None]
+    size = torch.exp2(torch.tensor([-8, -3, 0, 8, -8, 2, 5, 8, 1, -5][::order]).float()).repeat_interleave(45)[:, None, None]
     v = torch.randn((L, n_kv, d), generator=gen) * size
     k = torch.randn((L, n_kv, d), generator=gen) * size.rsqrt().clamp(max=4)
     ks, vs, ns, ls = [k, k[:90]], [v, v[:90]], [n, n], [L, 90]

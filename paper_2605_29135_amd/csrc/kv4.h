@@ -95,21 +95,21 @@ __device__ __forceinline__ float over8(float v, F f) {
 }
 
 __device__ __forceinline__ Quantised quantise8(const float (&x)[8]) {
-    float lo = x[0], hi = x[0], fin = 0.f;
+    float lo = x[0], hi = x[0], nan = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lo = fminf(lo, x[i]);
         hi = fmaxf(hi, x[i]);
-        fin = fmaxf(fin, (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u ? 1.f : 0.f);
+        nan = fmaf(x[i], 0.f, nan);  // (an infinity or NaN makes it NaN)
     }
     lo = over8(lo, [](float a, float b) { return fminf(a, b); });
     hi = over8(hi, [](float a, float b) { return fmaxf(a, b); });
-    fin = over8(fin, [](float a, float b) { return fmaxf(a, b); });
+    nan = over8(nan, [](float a, float b) { return a + b; });
     Quantised r;
     uint32_t mb = bf16_rne(lo);
     const float m = bf16_float(mb);
     uint32_t sb = bf16_rne((hi - m) * (1.0f / 15.0f));
-    r.bad = fin != 0.f || (mb & 0x7f80u) == 0x7f80u || (sb & 0x7f80u) == 0x7f80u;
+    r.bad = !(nan == 0.f) || (mb & 0x7f80u) == 0x7f80u || (sb & 0x7f80u) == 0x7f80u;
     // (hi >= m up to the rounding of m: a range below zero, like one below 2^-126, has the scale 0)
     if (r.bad || (sb & 0x8000u) || (sb & 0x7f80u) == 0) sb = 0;
     if (r.bad) mb = 0;
@@ -122,14 +122,16 @@ __device__ __forceinline__ Quantised quantise8(const float (&x)[8]) {
         for (int i = 0; i < 8; ++i) {
             const float t = x[i] - m;
             // The nearest integer by the reciprocal is off by one at most, and only next to a half: the exact
-            // remainder t - q s says which side t lies on (|q| <= 16 and s has 8 bits: q s is exact).
-            float q = rintf(fminf(fmaxf(t * inv, 0.f), 15.f));
-            const float rem = fmaf(-q, s, t);
-            const bool odd = int(q) & 1;
-            if (rem > half || (rem == half && odd)) q += 1.f;
-            else if (rem < -half || (rem == -half && odd)) q -= 1.f;
-            q = fminf(fmaxf(q, 0.f), 15.f);
-            r.word |= uint32_t(int(q)) << nibble_bit(i);
+            // remainder t - q s says which side t lies on (q <= 15 and s has 8 bits: q s is exact).  Half a step
+            // off is right for an even q only: for an odd one the bound is the number below half a step.
+            const float f = rintf(__builtin_amdgcn_fmed3f(t * inv, 0.f, 15.f));
+            const float rem = fmaf(-f, s, t);
+            int q = int(f);
+            const float bound = __int_as_float(__float_as_int(half) - (q & 1));
+            const int step = (__float_as_int(rem) >> 31) | 1;
+            q = fabsf(rem) > bound ? q + step : q;
+            q = min(max(q, 0), 15);
+            r.word |= uint32_t(q) << nibble_bit(i);
         }
     }
     return r;

@@ -3,8 +3,8 @@
 // The bound is bytes: 4 d (bf16) read and 1.125 d written per position and head.  A block of threads takes one
 // 32-position block of one head: 8 lanes hold a group of 64 dims, find its range and form its codes.  A key's
 // word belongs to one position, a value's word to 8 positions of one dim: the values' codes are turned through
-// LDS, and a word that only some of the new positions cover keeps the others' nibbles (read, merged, written
-// by the one lane that owns it).
+// LDS, and a word that only some of the new positions cover keeps the others' nibbles (read ahead, merged, written
+// by the one lane that owns it).  Everything is written from LDS in the cache's order, in whole lines.
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
@@ -48,77 +48,109 @@ __device__ __forceinline__ void store8(void *p, size_t i, const float (&x)[8]) {
 
 constexpr int kStoreBlock = 256;
 
+// Position (of 32) of entry i of a scale or base array: the order 8 c + i, or for the keys' bases [position][tile].
+__device__ __forceinline__ int entry_position(int i, bool tiles) {
+    return tiles ? 16 * (i & 1) + (i >> 1) : 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3);
+}
+
 // grid: (blocks of positions that a sequence's new tokens can touch, head, sequence)
 template <int NG, bool F32>
 __global__ __launch_bounds__(kStoreBlock) void kv4_append_kernel(const void *__restrict__ k, const void *__restrict__ v,
                                                                  long long k_stride, long long v_stride, Batch batch,
                                                                  uint8_t *__restrict__ cache, int *err) {
-    constexpr int d = NG * kGroup, NC = d / 8;  // chunks of 8 dims
-    __shared__ uint32_t codes[kPos][NC + 1];
+    constexpr int d = NG * kGroup, NC = d / 8, R = kPos * NC / kStoreBlock;  // chunks of 8 dims; items per thread
+    __shared__ uint32_t codes[2][kPos][NC + 1], params[2][NG][kPos];         // of keys and values; scale and base
     const Seq s = sequence(batch, blockIdx.z);
-    const int h = blockIdx.y, n_kv = gridDim.y;
-    if (s.bad && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(err, kErrRange);
+    const int h = blockIdx.y, n_kv = gridDim.y, tid = threadIdx.x;
+    if (s.bad && blockIdx.x == 0 && h == 0 && tid == 0) atomicOr(err, kErrRange);
     const int first = max(s.len - s.n, 0), blk = first / kPos + blockIdx.x;  // (tokens before position 0 are padding)
     if (s.n == 0 || blk * kPos >= s.len) return;
     uint8_t *block = cache + (size_t(blockIdx.z) * n_kv + h) * (batch.max_pos / kPos) * block_bytes(d) +
                      size_t(blk) * block_bytes(d);
     const int p_lo = max(first - blk * kPos, 0), p_hi = min(s.len - blk * kPos, kPos);  // new positions of the block
     const long long t_of_0 = (long long)s.t0 + blk * kPos - (s.len - s.n);              // token of the block's position 0
+    // A thread's words of the codes: consecutive ones of the piece-wise arrays (4 d of keys, 4 d of values).
+    uint32_t *kw = reinterpret_cast<uint32_t *>(block + k_codes(d)), *vw = reinterpret_cast<uint32_t *>(block + v_codes(d));
+    const bool whole = p_lo == 0 && p_hi == kPos;
+    uint32_t old[R];
+    if (!whole)
+#pragma unroll
+        for (int i = 0; i < R; ++i) old[i] = vw[i * kStoreBlock + tid];
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < kPos * NC / kStoreBlock; ++i) {
-        const int item = i * kStoreBlock + threadIdx.x, p = item / NC, chunk = item % NC;
+    for (int i = 0; i < R; ++i) {
+        const int item = i * kStoreBlock + tid, p = item / NC, chunk = item % NC;
         if (p < p_lo || p >= p_hi) continue;  // (the 8 lanes of a group share p)
-        float x[8];
+        float x[8], y[8];
         load8<F32>(k, size_t(t_of_0 + p) * k_stride + size_t(h) * d + 8 * chunk, x);
-        const Quantised zk = quantise8(x);
-        store_key<NG>(block, p, chunk, zk);
-        load8<F32>(v, size_t(t_of_0 + p) * v_stride + size_t(h) * d + 8 * chunk, x);
-        const Quantised zv = quantise8(x);
-        codes[p][chunk] = zv.word;
-        if ((chunk & 7) == 0) store_value_scale<NG>(block, p, chunk >> 3, zv);
+        load8<F32>(v, size_t(t_of_0 + p) * v_stride + size_t(h) * d + 8 * chunk, y);
+        const Quantised zk = quantise8(x), zv = quantise8(y);
+        codes[0][p][chunk] = zk.word;
+        codes[1][p][chunk] = zv.word;
+        if ((chunk & 7) == 0) {
+            params[0][chunk >> 3][p] = zk.s | (uint32_t(zk.m) << 16);
+            params[1][chunk >> 3][p] = zv.s | (uint32_t(zv.m) << 16);
+        }
         bad |= zk.bad || zv.bad;
     }
     if (bad) atomicOr(err, kErrNonfinite);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4 * d / kStoreBlock; ++i) {
-        const int item = i * kStoreBlock + threadIdx.x;  // (piece, lane, word of the lane's 16 bytes)
-        const int w = (item >> 8) * 4 + (item & 3), lane = (item >> 2) & 63, c = lane >> 4;
-        const int dim = 16 * w + (lane & 15), shift = nibble_bit(dim & 7);
+    for (int i = 0; i < R; ++i) {
+        const int item = i * kStoreBlock + tid;  // (piece, lane, word of the lane's 16 bytes)
+        const int w = (item >> 8) * 4 + (item & 3), lane = (item >> 2) & 63, c = lane >> 4, n = lane & 15;
+        const int p = 16 * (w / (2 * NG)) + n;
+        if (p >= p_lo && p < p_hi) kw[item] = codes[0][p][4 * (w % (2 * NG)) + c];
+        const int dim = 16 * w + n, shift = nibble_bit(dim & 7);
         uint32_t word = 0, keep = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int p = 16 * (e >> 2) + 4 * c + (e & 3);
-            if (p >= p_lo && p < p_hi) word |= ((codes[p][dim >> 3] >> shift) & 15u) << nibble_bit(e);
+            const int q = 16 * (e >> 2) + 4 * c + (e & 3);
+            if (whole || (q >= p_lo && q < p_hi)) word |= ((codes[1][q][dim >> 3] >> shift) & 15u) << nibble_bit(e);
             else keep |= 15u << nibble_bit(e);
         }
-        uint32_t *dst = reinterpret_cast<uint32_t *>(block + v_codes(d) + 4 * item);
-        if (keep == ~0u) continue;
-        *dst = keep ? (*dst & keep) | word : word;
+        if (whole) vw[item] = word;
+        else if (keep != ~0u) vw[item] = (old[i] & keep) | word;
+    }
+#pragma unroll
+    for (int i = tid; i < 4 * NG * kPos; i += kStoreBlock) {  // arrays of scales and bases, keys' then values'
+        const int array = i / (NG * kPos), p = entry_position(i % kPos, array == 1);
+        if (p < p_lo || p >= p_hi) continue;
+        const uint32_t sm = params[array >> 1][(i / kPos) % NG][p];
+        reinterpret_cast<uint16_t *>(block + k_scales(d))[i] = uint16_t(array & 1 ? sm >> 16 : sm);
     }
 }
 
-// grid: (blocks of positions, head, sequence): the values of the sequence's last n positions, as held.
+// grid: (blocks of positions, head, sequence): the values of the sequence's last n positions, as held.  A block goes
+// through LDS as it lies; 8 lanes form 64 dims of a position.
 template <int NG, bool F32>
 __global__ __launch_bounds__(kStoreBlock) void kv4_read_kernel(const uint8_t *__restrict__ cache, Batch batch,
                                                                void *__restrict__ k, void *__restrict__ v,
                                                                long long k_stride, long long v_stride, int *err) {
-    constexpr int d = NG * kGroup, NC = d / 8;
+    constexpr int d = NG * kGroup, NC = d / 8, R = kPos * NC / kStoreBlock;
+    __shared__ uint4 held[block_bytes(d) / 16];
     const Seq s = sequence(batch, blockIdx.z);
-    const int h = blockIdx.y, n_kv = gridDim.y;
-    if (s.bad && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(err, kErrRange);
+    const int h = blockIdx.y, n_kv = gridDim.y, tid = threadIdx.x;
+    if (s.bad && blockIdx.x == 0 && h == 0 && tid == 0) atomicOr(err, kErrRange);
     // blocks of positions from the first token's, which may lie before position 0 (those rows are zeros)
     const int first = s.len - s.n, b0 = first >= 0 ? first / kPos : -((-first + kPos - 1) / kPos);
     const int blk = b0 + blockIdx.x;
     if (s.n == 0 || blk * kPos >= s.len) return;
-    const uint8_t *block = cache + (size_t(blockIdx.z) * n_kv + h) * (batch.max_pos / kPos) * block_bytes(d) +
-                           size_t(max(blk, 0)) * block_bytes(d);
     const int p_lo = max(first - blk * kPos, 0), p_hi = min(s.len - blk * kPos, kPos);
     const long long t_of_0 = (long long)s.t0 + blk * kPos - first;
-#pragma unroll 1
-    for (int i = 0; i < kPos * NC / kStoreBlock; ++i) {
-        const int item = i * kStoreBlock + threadIdx.x, p = item / NC, chunk = item % NC, g = chunk >> 3;
+    if (blk >= 0) {
+        const uint8_t *block = cache + (size_t(blockIdx.z) * n_kv + h) * (batch.max_pos / kPos) * block_bytes(d) +
+                               size_t(blk) * block_bytes(d);
+#pragma unroll
+        for (int i = 0; i < int((block_bytes(d) / 16 + kStoreBlock - 1) / kStoreBlock); ++i)
+            if (i * kStoreBlock + tid < int(block_bytes(d) / 16))
+                held[i * kStoreBlock + tid] = dev::load16(block + (i * kStoreBlock + tid) * 16);
+    }
+    __syncthreads();
+    const uint8_t *block = reinterpret_cast<const uint8_t *>(held);
+#pragma unroll 2
+    for (int i = 0; i < R; ++i) {
+        const int item = i * kStoreBlock + tid, p = item / NC, chunk = item % NC, g = chunk >> 3;
         if (p < p_lo || p >= p_hi) continue;
         float x[8], y[8];
         if (blk < 0) {

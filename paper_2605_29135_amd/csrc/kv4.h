@@ -117,22 +117,19 @@ __device__ __forceinline__ Quantised quantise8(const float (&x)[8]) {
     r.m = uint16_t(mb);
     r.word = 0;
     if (sb) {
-        const float s = bf16_float(sb), inv = __builtin_amdgcn_rcpf(s), half = 0.5f * s;
+        // The quotient by the reciprocal, corrected by its exact remainder, is the nearest fp32 number: k + 1/2 comes
+        // out where t / s is that, and nowhere else ((k + 1/2) s has at most 13 bits, so another t is off by 2^-24 of
+        // itself, more than half a last place of the quotient).  Adding 2^23 rounds to the nearest integer, ties to
+        // even, in the low bits; what the eight sums carry above them goes off at the end.
+        const float s = bf16_float(sb), inv = __builtin_amdgcn_rcpf(s);
+        uint32_t carry = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float t = x[i] - m;
-            // The nearest integer by the reciprocal is off by one at most, and only next to a half: the exact
-            // remainder t - q s says which side t lies on (q <= 15 and s has 8 bits: q s is exact).  Half a step
-            // off is right for an even q only: for an odd one the bound is the number below half a step.
-            const float f = rintf(__builtin_amdgcn_fmed3f(t * inv, 0.f, 15.f));
-            const float rem = fmaf(-f, s, t);
-            int q = int(f);
-            const float bound = __int_as_float(__float_as_int(half) - (q & 1));
-            const int step = (__float_as_int(rem) >> 31) | 1;
-            q = fabsf(rem) > bound ? q + step : q;
-            q = min(max(q, 0), 15);
-            r.word |= uint32_t(q) << nibble_bit(i);
+            const float t = x[i] - m, q0 = t * inv, q = fmaf(fmaf(-q0, s, t), inv, q0);
+            r.word += __float_as_uint(__builtin_amdgcn_fmed3f(q, 0.f, 15.f) + 8388608.f) << nibble_bit(i);
+            carry += 0x4B000000u << nibble_bit(i);
         }
+        r.word -= carry;
     }
     return r;
 }

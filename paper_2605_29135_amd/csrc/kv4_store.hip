@@ -14,23 +14,30 @@ namespace {
 
 using namespace kv4;
 
-// 8 consecutive elements of a row (16-byte aligned).
+// 8 consecutive elements of a row (16-byte aligned), as they lie and in fp32.
 template <bool F32>
-__device__ __forceinline__ void load8(const void *p, size_t i, float (&x)[8]) {
-    if constexpr (F32) {
-        const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
-        const float4 a = dev::load_f4(q), b = dev::load_f4(q + 1);
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-        const uint4 a = dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(p) + i));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Eight {
+    uint4 raw[F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void *p, size_t i) {
+        const uint8_t *q = static_cast<const uint8_t *>(p) + i * (F32 ? 4 : 2);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        for (int e = 0; e < (F32 ? 2 : 1); ++e) raw[e] = dev::load16(q + 16 * e);
+    }
+    __device__ __forceinline__ void floats(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < (F32 ? 2 : 1); ++e) {
+            const uint32_t w[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if constexpr (F32) x[4 * e + u] = __uint_as_float(w[u]);
+                else {
+                    x[2 * u] = __uint_as_float(w[u] << 16);
+                    x[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u);
+                }
+            }
         }
     }
-}
+};
 
 template <bool F32>
 __device__ __forceinline__ void store8(void *p, size_t i, const float (&x)[8]) {
@@ -76,14 +83,24 @@ __global__ __launch_bounds__(kStoreBlock) void kv4_append_kernel(const void *__r
     if (!whole)
 #pragma unroll
         for (int i = 0; i < R; ++i) old[i] = vw[i * kStoreBlock + tid];
+    // (all the loads before any use: a position that is not new reads the nearest one that is)
+    Eight<F32> ek[R], ev[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int item = i * kStoreBlock + tid, chunk = item % NC;
+        const size_t token = size_t(t_of_0 + min(max(item / NC, p_lo), p_hi - 1));
+        ek[i].load(k, token * k_stride + size_t(h) * d + 8 * chunk);
+        ev[i].load(v, token * v_stride + size_t(h) * d + 8 * chunk);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int item = i * kStoreBlock + tid, p = item / NC, chunk = item % NC;
         if (p < p_lo || p >= p_hi) continue;  // (the 8 lanes of a group share p)
         float x[8], y[8];
-        load8<F32>(k, size_t(t_of_0 + p) * k_stride + size_t(h) * d + 8 * chunk, x);
-        load8<F32>(v, size_t(t_of_0 + p) * v_stride + size_t(h) * d + 8 * chunk, y);
+        ek[i].floats(x);
+        ev[i].floats(y);
         const Quantised zk = quantise8(x), zv = quantise8(y);
         codes[0][p][chunk] = zk.word;
         codes[1][p][chunk] = zv.word;

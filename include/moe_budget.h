@@ -297,11 +297,11 @@ MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, 
  * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums;
  * queries enter exactly (MOE_BF16) or as two fp16 terms (MOE_F32: 2^-22 of the head's largest element), probabilities
  * times scales as two fp16 terms (MOE_F32: 2^-22) or rounded to fp16 (MOE_BF16: 2^-11; calls of many rows round the
- * held keys and values to fp16 as well).  Elements of q up to 2^100 in magnitude; keys and values within 2^20 of
- * the largest of their sequence keep the precision stated.
+ * held keys and values to fp16 as well).  For elements of q up to 2^100, keys and values
+ * from 2^-60 to 2^40 in magnitude; a key or value keeps the precision stated within 2^20 of the largest near it.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
  *   out        device, as q with out_stride, same dtype
- *   scale      any finite factor, as a rule 1 / sqrt(head_dim)
+ *   scale      a factor of magnitude up to 2^32, as a rule 1 / sqrt(head_dim)
  *   workspace  device, >= moe_kv4_attention_workspace_bytes(...) (may be NULL when that is 0) */
 MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *cache, size_t cache_bytes, int T,
                               int n_seq, int n_heads, int n_kv, int head_dim, int max_pos, const int32_t *q_start,

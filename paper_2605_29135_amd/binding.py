@@ -358,32 +358,46 @@ def _here(*tensors) -> int:
 
 
 class _On:
-    """The stream a call runs on: its handle, and the tensors that must outlive the call's work on it.
+    """Another stream than the current one, which a call was given to run on.
 
-    A tensor made here for a call on another stream than the current one belongs to that stream, and the
-    caller's tensors are marked as used there, so that none is handed out again before the work has run."""
+    A tensor made here for the call belongs to that stream, and the caller's tensors are marked as used there,
+    so that none is handed out again before the work has run."""
 
-    __slots__ = ("handle", "other")
+    __slots__ = ("stream",)
 
-    def __init__(self, stream):
-        self.handle = _stream(stream)
-        self.other = None
-        if stream is not None and self.handle != _stream(None):
-            import torch
-            self.other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle)
-
-    def empty(self, shape, dtype, device):
+    def __init__(self, stream, handle):
         import torch
-        if self.other is None:
-            return torch.empty(shape, dtype=dtype, device=device)
-        with torch.cuda.stream(self.other):
-            return torch.empty(shape, dtype=dtype, device=device)
+        self.stream = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle)
 
     def used(self, *tensors):
-        if self.other is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.other)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+
+
+def _current_stream(device: int) -> int:
+    import torch
+    try:
+        return torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
+
+
+def _run_on(stream, device: int):
+    """(handle of the stream a call runs on, _On when that is not the current one)."""
+    current = _current_stream(device)
+    if stream is None:
+        return current, None
+    handle = _stream(stream)
+    return handle, None if handle == current else _On(stream, handle)
+
+
+def _empty(on, shape, dtype, device):
+    import torch
+    if on is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(on.stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _float_code(dtype, name):
@@ -452,13 +466,13 @@ def moe_kv4_append(k, v, cache, kv_len, q_start=None, max_q: int | None = None, 
     kp, ks = _rows(k, "k", n_kv, d)
     vp, vs = _rows(v, "v", n_kv, d, T, dtype)
     lp, qp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
-    _here(k, v, cache, kv_len, q_start)
-    on = _On(stream)
+    handle, on = _run_on(stream, _here(k, v, cache, kv_len, q_start))
     code = (_lib or lib()).moe_kv4_append(kp, vp, _float_code(dtype, "k"), ks, vs, T, n_seq, n_kv, d, max_pos, qp, mq, lp,
-                                          cache.data_ptr(), cache.numel(), on.handle)
+                                          cache.data_ptr(), cache.numel(), handle)
     if code:
         _check(code, "moe_kv4_append")
-    on.used(k, v, cache, kv_len, q_start)
+    if on is not None:
+        on.used(k, v, cache, kv_len, q_start)
 
 
 def moe_kv4_read(cache, kv_len, T: int, q_start=None, max_q: int | None = None, k_out=None, v_out=None, dtype=None,
@@ -471,16 +485,17 @@ def moe_kv4_read(cache, kv_len, T: int, q_start=None, max_q: int | None = None, 
     dtype = given.dtype if given is not None else torch.bfloat16 if dtype is None else dtype
     lp, qp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     device = _here(cache, kv_len, q_start, k_out, v_out)
-    on = _On(stream)
-    k_out = on.empty((T, n_kv, d), dtype, device) if k_out is None else k_out
-    v_out = on.empty((T, n_kv, d), dtype, device) if v_out is None else v_out
+    handle, on = _run_on(stream, device)
+    k_out = _empty(on, (T, n_kv, d), dtype, device) if k_out is None else k_out
+    v_out = _empty(on, (T, n_kv, d), dtype, device) if v_out is None else v_out
     kp, ks = _rows(k_out, "k_out", n_kv, d, T, dtype)
     vp, vs = _rows(v_out, "v_out", n_kv, d, T, dtype)
     code = (_lib or lib()).moe_kv4_read(cache.data_ptr(), cache.numel(), T, n_seq, n_kv, d, max_pos, qp, mq, lp, kp, vp,
-                                        _float_code(dtype, "k_out"), ks, vs, on.handle)
+                                        _float_code(dtype, "k_out"), ks, vs, handle)
     if code:
         _check(code, "moe_kv4_read")
-    on.used(cache, kv_len, q_start, k_out, v_out)
+    if on is not None:
+        on.used(cache, kv_len, q_start, k_out, v_out)
     return k_out, v_out
 
 
@@ -502,21 +517,22 @@ def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, 
     qp, qs = _rows(q, "q", n_heads, d)
     lp, sp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     device = _here(q, cache, kv_len, q_start, out, workspace)
-    on = _On(stream)
+    handle, on = _run_on(stream, device)
     if out is None:
-        out = on.empty((T, n_heads, d), dtype, device)
+        out = _empty(on, (T, n_heads, d), dtype, device)
     op, os_ = _rows(out, "out", n_heads, d, T, dtype)
     if workspace is None:
         import torch
         n = moe_kv4_attention_workspace_bytes(T, n_seq, n_heads, n_kv, d, mq, max_pos)
-        workspace = on.empty(max(n, 256), torch.uint8, device)
+        workspace = _empty(on, max(n, 256), torch.uint8, device)
     code = (_lib or lib()).moe_kv4_attention(qp, _float_code(dtype, "q"), qs, cache.data_ptr(), cache.numel(), T, n_seq,
                                              n_heads, n_kv, d, max_pos, sp, mq, lp, window,
                                              d ** -0.5 if scale is None else scale, op, os_, _dev(workspace, "workspace"),
-                                             workspace.nbytes, on.handle)
+                                             workspace.nbytes, handle)
     if code:
         _check(code, "moe_kv4_attention")
-    on.used(q, cache, kv_len, q_start, out, workspace)
+    if on is not None:
+        on.used(q, cache, kv_len, q_start, out, workspace)
     return out
 
 
@@ -535,19 +551,20 @@ def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, strea
     import torch
     T, K = x.shape
     device = _here(x, w, add, y)
-    on = _On(stream)
+    handle, on = _run_on(stream, device)
     if y is None:
-        y = on.empty((T, N), torch.float32, device)
+        y = _empty(on, (T, N), torch.float32, device)
     elif y.numel() != T * N:
         raise ValueError(f"y has shape {tuple(y.shape)}, expected [{T}, {N}]")
     if add is not None and add.numel() != T * N:
         raise ValueError(f"add has shape {tuple(add.shape)}, expected [{T}, {N}]")
     code = (_lib or lib()).moe_matvec_int4(_dev(x, "x", torch.float32), _int4_matrix(w, "w", N, K), T, N, K,
                                            _dev(add, "add", torch.float32), _dev(y, "y", torch.float32),
-                                           MOE_ROUTE_RMSNORM if rmsnorm else 0, on.handle)
+                                           MOE_ROUTE_RMSNORM if rmsnorm else 0, handle)
     if code:
         _check(code, "moe_matvec_int4")
-    on.used(x, w, add, y)
+    if on is not None:
+        on.used(x, w, add, y)
     return y
 
 
@@ -565,16 +582,17 @@ def moe_attention_decode_int4(x, w_qkv, w_o, cache, kv_len, n_heads: int, theta:
     if n_seq != T or kv_len.numel() != T:
         raise ValueError(f"{T} tokens need a cache of {T} sequences (has {n_seq}) and as many lengths (has {kv_len.numel()})")
     device = _here(x, w_qkv, w_o, cache, kv_len, workspace)
-    on = _On(stream)
+    handle, on = _run_on(stream, device)
     if workspace is None:
-        workspace = on.empty(max(moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, d, max_pos), 256),
+        workspace = _empty(on, max(moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, d, max_pos), 256),
                              torch.uint8, device)
     _check(lib().moe_attention_decode_int4(
         _dev(x, "x", torch.float32), T, H, n_heads, n_kv, d, _int4_matrix(w_qkv, "w_qkv", (n_heads + 2 * n_kv) * d, H),
         _int4_matrix(w_o, "w_o", H, n_heads * d), _dev(cache, "cache"), cache.numel(), max_pos,
         _dev(kv_len, "kv_len", torch.int32), theta, _dev(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), on.handle), "moe_attention_decode_int4")
-    on.used(x, w_qkv, w_o, cache, kv_len, workspace)
+        workspace.numel() * workspace.element_size(), handle), "moe_attention_decode_int4")
+    if on is not None:
+        on.used(x, w_qkv, w_o, cache, kv_len, workspace)
     return x
 
 

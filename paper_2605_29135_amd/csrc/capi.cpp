@@ -362,8 +362,9 @@ int moe_kv4_read(const void *cache, size_t cache_bytes, int T, int n_seq, int n_
 }
 
 size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q, int max_pos) {
-    // (a caller without q_start may pass any max_q of at least 1: a plan for 1 is then what runs)
+    // (a caller without q_start may pass any max_q: a plan for 1 is then what runs)
     const int32_t some = 0;
+    max_q = std::max(max_q, 1);
     if (check_kv4_shape("kv4 attention", n_seq, n_kv, head_dim, max_pos) != MOE_OK ||
         check_kv4_batch("kv4 attention", MOE_F32, T, n_seq, n_heads, n_kv, &some, &max_q) != MOE_OK || T == 0 || n_seq == 0)
         return 0;
@@ -381,7 +382,8 @@ int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *
     if (st != MOE_OK) return st;
     if (window < 0 || window > (1 << 30))
         return fail(MOE_ERR_INVALID_ARG, "kv4 attention: window=%d outside [0, 2^30]", window);
-    if (!std::isfinite(scale)) return fail(MOE_ERR_INVALID_ARG, "kv4 attention: scale must be finite");
+    if (!(std::fabs(scale) <= 4294967296.f))
+        return fail(MOE_ERR_INVALID_ARG, "kv4 attention: the scale's magnitude must be at most 2^32");
     if (T == 0 || n_seq == 0) return MOE_OK;
     if (!q || !out) return fail(MOE_ERR_INVALID_ARG, "kv4 attention: NULL pointer");
     if (!rows_ok(q, q_stride, n_heads, head_dim, dtype) || !rows_ok(out, out_stride, n_heads, head_dim, dtype))

@@ -485,7 +485,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
         if (scales_rose) {
             const int e = int(dev::wave_reduce_u32<true>(most_s) >> 7), was = boost;
             top_s = (uint32_t(e) << 7) | 0x7fu;
-            boost = min(141 - e, 100);  // (sums over up to 2^26 positions stay finite)
+            boost = min(141 - e, 60);  // (sums of bases up to 2^40 over up to 2^26 positions stay finite)
             boost_f = ldexpf(1.f, boost);
             rise = ldexpf(1.f, min(boost - was, 126));  // (it rises from its start only: the sums are still zeros)
         }

@@ -158,7 +158,7 @@ def test_attention_refusals():
                 q_start=None, max_q=1, kv_len=OK_PTR, window=0, scale=0.125, out=OK_PTR, os=512, ws=OK_PTR, wb=big)
     bads = [dict(q=None), dict(out=None), dict(q=OK_PTR + 2), dict(out=OK_PTR + 8), dict(qs=508), dict(os=516),
             dict(dtype=3), dict(T=3), dict(heads=9), dict(heads=0), dict(n_kv=0), dict(d=48), dict(mp=4097),
-            dict(window=-1), dict(window=(1 << 30) + 1), dict(scale=math.inf), dict(scale=math.nan), dict(cache=None),
+            dict(window=-1), dict(window=(1 << 30) + 1), dict(scale=math.inf), dict(scale=math.nan), dict(scale=-4.5e9), dict(cache=None),
             dict(kv_len=None), dict(bytes=100), dict(ws=None), dict(ws=OK_PTR + 4), dict(wb=16),
             dict(q_start=OK_PTR, max_q=0), dict(q_start=OK_PTR, max_q=1 << 24)]
     for b in bads:
@@ -414,11 +414,33 @@ def test_attention_strides_rows_behind_and_loose_max_q(dtype):
 @pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
 def test_attention_scales(dtype, scale):
     """Scores that are all equal, turned round, and so far apart that few positions count."""
-    case = (128, 1, 4, [2, 1], [70, 40], 96, 0)
-    cache, q, ref, tol = attention_case(*case, dtype, scale=scale)
-    qs, kl, _ = batch(case[3], case[4])
-    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, scale=scale)
-    assert ((out.cpu().double() - ref).abs() <= tol).all()
+    for case in ((128, 1, 4, [2, 1], [70, 40], 96, 0), (128, 1, 16, [2, 1], [70, 40], 96, 0),
+                 (64, 16, 8, [33, 20, 17, 1], [70, 40, 100, 1], 128, 0)):
+        cache, q, ref, tol = attention_case(*case, dtype, scale=scale)
+        qs, kl, _ = batch(case[3], case[4])
+        out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(case[3]), scale=scale)
+        assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k_size,v_size", [(2.0 ** -30, 2.0 ** -55), (2.0 ** 30, 2.0 ** 38), (1.0, 2.0 ** -20)])
+def test_attention_range(dtype, k_size, v_size):
+    """Keys and values far from one, the scores kept where they are by the scale."""
+    for d, n_kv, G, ns, ls in ((128, 2, 4, [1, 1], [70, 200]), (64, 2, 12, [3, 1], [70, 40]), (128, 16, 8, [20, 33, 17, 1], [70, 40, 100, 1])):
+        gen = torch.Generator().manual_seed(d)
+        ks = [torch.randn((L, n_kv, d), generator=gen) * k_size for L in ls]
+        vs = [torch.randn((L, n_kv, d), generator=gen) * v_size for L in ls]
+        cache = fill(moe.kv4_cache(len(ls), n_kv, d, 224))
+        put(ks, vs, cache, F32)
+        q = torch.randn((sum(ns), n_kv * G, d), generator=gen).to(dtype)
+        scale = d ** -0.5 / k_size
+        ref, amount, shift = attend(q.double(), ks, vs, ns, ls, G, 0, scale, dtype)
+        qs, kl, _ = batch(ns, ls)
+        out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns), scale=scale)
+        err, tol = (out.cpu().double() - ref).abs(), attention_tolerance(ref, amount, shift, dtype)
+        assert (err <= tol).all(), float((err / tol).max())
+    moe.moe_sync_check()
 
 
 @pytest.mark.gpu
@@ -497,6 +519,15 @@ def test_attention_bad_batch_and_values(dtype):
         ok = torch.ones((T, 2), dtype=torch.bool)
         ok[0, 1] = False
         assert ((out - ref).abs() <= tol)[ok].all() and not torch.isfinite(out[0, 1]).any()
+    # nor in a call of many rows
+    case = (64, 16, 8, [33, 20, 17, 1], [70, 40, 100, 1], 128, 0)
+    cache, q, ref, tol = attention_case(*case, dtype)
+    qs, kl, T = batch(case[3], case[4])
+    q[40, 77, 5], q[3, 0, 0] = math.nan, math.inf
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=33).cpu().double()
+    ok = torch.ones((T, 128), dtype=torch.bool)
+    ok[40, 77] = ok[3, 0] = False
+    assert ((out - ref).abs() <= tol)[ok].all() and not torch.isfinite(out[~ok]).any()
     moe.moe_sync_check()
 
 
@@ -551,11 +582,11 @@ def test_matvec_matches_the_plain_form(T, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 7])
-def test_matvec_many_rows(T):
-    """Enough rows that blocks take several items."""
+@pytest.mark.parametrize("N,K", [(40007, 512), (20001, 1408), (16400, 4352), (135000, 128), (270000, 128)])
+@pytest.mark.parametrize("T", [1, 7, 8, 9, 16])
+def test_matvec_many_rows(T, N, K):
+    """Enough rows that waves and blocks take several items."""
     gen = torch.Generator().manual_seed(T)
-    N, K = 40007, 512
     raw, _ = int4_matrix(N, K, gen)
     parts = int4_parts(raw, N, K)
     x = torch.randn((T, K), generator=gen)
@@ -568,9 +599,10 @@ def test_matvec_many_rows(T):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [2, 9])
-def test_matvec_values_that_are_not_finite_or_huge(T):
+@pytest.mark.parametrize("N", [40, 33000])
+def test_matvec_values_that_are_not_finite_or_huge(T, N):
     gen = torch.Generator().manual_seed(3)
-    N, K = 40, 256
+    K = 256
     raw, _ = int4_matrix(N, K, gen)
     q, s = int4_parts(raw, N, K)
     x = torch.randn((T, K), generator=gen)

@@ -308,18 +308,22 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
                               int max_q, const int32_t *kv_len, int window, float scale, void *out,
                               long long out_stride, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Device workspace bytes moe_matvec_int4 needs (0 for up to 3 tokens). */
+MOE_API size_t moe_matvec_int4_workspace_bytes(int T, int K);
+
 /* y[t] = add[t] + W h[t] for T <= MOE_MAX_DECODE_TOKENS tokens, h = x, or with MOE_ROUTE_RMSNORM in flags
  * h = x / sqrt(mean(x^2) + 1e-6).
  *   x    device fp32 [T x K], 16-byte aligned, K a multiple of 128
  *   w    device MOE_INT4G128 matrix [N x K], 16-byte aligned: packed nibbles [N x K/2], then bf16 scales [N x K/128]
  *   add  device fp32 [T x N], or NULL; may be y
  *   y    device fp32 [T x N], apart from x
+ *   workspace device, >= moe_matvec_int4_workspace_bytes(T, K), 16-byte aligned (may be NULL when that is 0)
  * The tokens' values enter within 2^-22 of the token's largest; exact products, fp32 sums.  T == 0 or N == 0 is a no-op. */
 MOE_API int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
-                            void *stream);
+                            void *workspace, size_t workspace_bytes, void *stream);
 
 /* Device workspace bytes moe_attention_decode_int4 needs (0 for an unsupported shape). */
-MOE_API size_t moe_attention_decode_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos);
+MOE_API size_t moe_attention_decode_int4_workspace_bytes(int T, int H, int n_heads, int n_kv, int head_dim, int max_pos);
 
 /* moe_attention_decode's block with int4 projections and a 4-bit cache, for one token of each of T sequences
  * (T <= MOE_MAX_DECODE_TOKENS), in place on x (device fp32 [T x H]): the same arithmetic, with the rotated keys

@@ -95,8 +95,9 @@ def lib() -> C.CDLL:
             "moe_kv4_read": [P, SZ, I, I, I, I, I, P, I, P, P, P, I, LL, LL, P],
             "moe_kv4_attention_workspace_bytes": [I, I, I, I, I, I, I],
             "moe_kv4_attention": [P, I, LL, P, SZ, I, I, I, I, I, I, P, I, P, I, C.c_float, P, LL, P, SZ, P],
-            "moe_matvec_int4": [P, P, I, I, I, P, P, I, P],
-            "moe_attention_decode_int4_workspace_bytes": [I, I, I, I, I],
+            "moe_matvec_int4_workspace_bytes": [I, I],
+            "moe_matvec_int4": [P, P, I, I, I, P, P, I, P, SZ, P],
+            "moe_attention_decode_int4_workspace_bytes": [I, I, I, I, I, I],
             "moe_attention_decode_int4": [P, I, I, I, I, I, P, P, P, SZ, I, P, C.c_float, P, SZ, P],
             "moe_prefill_workspace_bytes": [I, I, I, I, I],
             "moe_prefill_grouped": [P, I, I, I, I, I, P, P, P, P, SZ, I, P, P, P, SZ, I, P],
@@ -129,7 +130,8 @@ def lib() -> C.CDLL:
         L.moe_last_error.restype = C.c_char_p
         L.moe_ffn_workspace_bytes.restype = SZ
         L.moe_prefill_workspace_bytes.restype = SZ
-        for name in ("moe_kv4_cache_bytes", "moe_kv4_attention_workspace_bytes", "moe_attention_decode_int4_workspace_bytes"):
+        for name in ("moe_kv4_cache_bytes", "moe_kv4_attention_workspace_bytes", "moe_matvec_int4_workspace_bytes",
+                     "moe_attention_decode_int4_workspace_bytes"):
             getattr(L, name).restype = SZ
         _lib = L
     return _lib
@@ -545,12 +547,16 @@ def _int4_matrix(w, name, N, K):
     return p
 
 
-def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, stream=None):
+def moe_matvec_int4_workspace_bytes(T: int, K: int) -> int:
+    return int((_lib or lib()).moe_matvec_int4_workspace_bytes(T, K))
+
+
+def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, workspace=None, stream=None):
     """y = add + W h for the tokens x (fp32 [T, K], T <= 16), h = x or its RMS norm; w: uint8 bytes of the
     MOE_INT4G128 matrix [N x K]; add fp32 [T, N] (may be y); returns y [T, N]."""
     import torch
     T, K = x.shape
-    device = _here(x, w, add, y)
+    device = _here(x, w, add, y, workspace)
     handle, on = _run_on(stream, device)
     if y is None:
         y = _empty(on, (T, N), torch.float32, device)
@@ -558,18 +564,22 @@ def moe_matvec_int4(x, w, N: int, y=None, add=None, rmsnorm: bool = False, strea
         raise ValueError(f"y has shape {tuple(y.shape)}, expected [{T}, {N}]")
     if add is not None and add.numel() != T * N:
         raise ValueError(f"add has shape {tuple(add.shape)}, expected [{T}, {N}]")
+    if workspace is None:
+        n = moe_matvec_int4_workspace_bytes(T, K)
+        workspace = _empty(on, n, torch.uint8, device) if n else None
     code = (_lib or lib()).moe_matvec_int4(_dev(x, "x", torch.float32), _int4_matrix(w, "w", N, K), T, N, K,
                                            _dev(add, "add", torch.float32), _dev(y, "y", torch.float32),
-                                           MOE_ROUTE_RMSNORM if rmsnorm else 0, handle)
+                                           MOE_ROUTE_RMSNORM if rmsnorm else 0, _dev(workspace, "workspace"),
+                                           0 if workspace is None else workspace.nbytes, handle)
     if code:
         _check(code, "moe_matvec_int4")
     if on is not None:
-        on.used(x, w, add, y)
+        on.used(x, w, add, y, workspace)
     return y
 
 
-def moe_attention_decode_int4_workspace_bytes(T: int, n_heads: int, n_kv: int, head_dim: int, max_pos: int) -> int:
-    return int(lib().moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos))
+def moe_attention_decode_int4_workspace_bytes(T: int, H: int, n_heads: int, n_kv: int, head_dim: int, max_pos: int) -> int:
+    return int(lib().moe_attention_decode_int4_workspace_bytes(T, H, n_heads, n_kv, head_dim, max_pos))
 
 
 def moe_attention_decode_int4(x, w_qkv, w_o, cache, kv_len, n_heads: int, theta: float = 1.0e6, workspace=None,
@@ -584,7 +594,7 @@ def moe_attention_decode_int4(x, w_qkv, w_o, cache, kv_len, n_heads: int, theta:
     device = _here(x, w_qkv, w_o, cache, kv_len, workspace)
     handle, on = _run_on(stream, device)
     if workspace is None:
-        workspace = _empty(on, max(moe_attention_decode_int4_workspace_bytes(T, n_heads, n_kv, d, max_pos), 256),
+        workspace = _empty(on, max(moe_attention_decode_int4_workspace_bytes(T, H, n_heads, n_kv, d, max_pos), 256),
                              torch.uint8, device)
     _check(lib().moe_attention_decode_int4(
         _dev(x, "x", torch.float32), T, H, n_heads, n_kv, d, _int4_matrix(w_qkv, "w_qkv", (n_heads + 2 * n_kv) * d, H),

@@ -12,6 +12,8 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace moe {
 namespace {
 
@@ -100,9 +102,11 @@ bool attention_int4_shape_supported(int H, int n_heads, int n_kv, int d, int max
            max_pos % kPos == 0 && max_pos <= MOE_KV4_MAX_POS;
 }
 
-size_t attention_int4_workspace_bytes(int T, int n_heads, int n_kv, int d, int max_pos) {
+// (the attention's and the projections' parts share their place: they follow one another)
+size_t attention_int4_workspace_bytes(int T, int H, int n_heads, int n_kv, int d, int max_pos) {
     return align256(sizeof(float) * size_t(T) * (n_heads + 2 * n_kv) * d) + align256(sizeof(float) * size_t(T) * n_heads * d) +
-           kv4_attention_workspace_bytes(T, T, n_heads, n_kv, d, 1, max_pos);
+           std::max(kv4_attention_workspace_bytes(T, T, n_heads, n_kv, d, 1, max_pos),
+                    matvec_int4_workspace_bytes(T, std::max(H, n_heads * d)));
 }
 
 hipError_t launch_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int d, const void *w_qkv,
@@ -113,7 +117,7 @@ hipError_t launch_attention_decode_int4(float *x, int T, int H, int n_heads, int
     float *qkv = reinterpret_cast<float *>(ws);
     float *att = reinterpret_cast<float *>(ws += align256(sizeof(float) * size_t(T) * rows));
     void *aws = ws + align256(sizeof(float) * size_t(T) * n_heads * d);
-    hipError_t e = launch_matvec_int4(x, w_qkv, T, rows, H, nullptr, qkv, true, s);
+    hipError_t e = launch_matvec_int4(x, w_qkv, T, rows, H, nullptr, qkv, true, aws, s);
     if (e != hipSuccess) return e;
     const dim3 grid(n_heads + n_kv, T);
     auto *c = static_cast<uint8_t *>(cache);
@@ -129,7 +133,7 @@ hipError_t launch_attention_decode_int4(float *x, int T, int H, int n_heads, int
     e = launch_kv4_attention(qkv, MOE_F32, rows, cache, batch, n_heads, n_kv, d, 0, 1.f / sqrtf(float(d)), att,
                              (long long)n_heads * d, aws, err, s);
     if (e != hipSuccess) return e;
-    return launch_matvec_int4(att, w_o, T, H, n_heads * d, x, x, false, s);
+    return launch_matvec_int4(att, w_o, T, H, n_heads * d, x, x, false, aws, s);
 }
 
 }  // namespace moe

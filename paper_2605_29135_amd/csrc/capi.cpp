@@ -404,8 +404,13 @@ int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *
                          "kv4 attention launch");
 }
 
+size_t moe_matvec_int4_workspace_bytes(int T, int K) {
+    if (T < 1 || T > MOE_MAX_DECODE_TOKENS || K < 128 || K % 128 || K > (1 << 24)) return 0;
+    return moe::matvec_int4_workspace_bytes(T, K);
+}
+
 int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
-                    void *stream) {
+                    void *workspace, size_t workspace_bytes, void *stream) {
     if (T < 0 || T > MOE_MAX_DECODE_TOKENS)
         return fail(MOE_ERR_INVALID_ARG, "matvec: T=%d outside [0, %d]", T, MOE_MAX_DECODE_TOKENS);
     if (N < 0 || N > (1 << 28) || K < 128 || K % 128 || K > (1 << 24))
@@ -418,16 +423,20 @@ int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const fl
     const auto xa = reinterpret_cast<uintptr_t>(x), ya = reinterpret_cast<uintptr_t>(y);
     if (xa < ya + sizeof(float) * size_t(T) * N && ya < xa + sizeof(float) * size_t(T) * K)
         return fail(MOE_ERR_INVALID_ARG, "matvec: y overlaps x");
-    return finish_launch(moe::launch_matvec_int4(x, w, T, N, K, add, y, flags & MOE_ROUTE_RMSNORM,
+    const size_t need = moe::matvec_int4_workspace_bytes(T, K);
+    if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+        return fail(MOE_ERR_INVALID_ARG, "matvec: needs a 16-byte aligned workspace of %zu bytes (%zu given)", need,
+                    workspace ? workspace_bytes : size_t(0));
+    return finish_launch(moe::launch_matvec_int4(x, w, T, N, K, add, y, flags & MOE_ROUTE_RMSNORM, workspace,
                                                  static_cast<hipStream_t>(stream)),
                          "matvec launch");
 }
 
-size_t moe_attention_decode_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos) {
+size_t moe_attention_decode_int4_workspace_bytes(int T, int H, int n_heads, int n_kv, int head_dim, int max_pos) {
     if (T < 1 || T > MOE_MAX_DECODE_TOKENS ||
-        !moe::attention_int4_shape_supported(128, n_heads, n_kv, head_dim, max_pos))
+        !moe::attention_int4_shape_supported(H, n_heads, n_kv, head_dim, max_pos))
         return 0;
-    return moe::attention_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos);
+    return moe::attention_int4_workspace_bytes(T, H, n_heads, n_kv, head_dim, max_pos);
 }
 
 int moe_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
@@ -445,7 +454,7 @@ int moe_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int
         return fail(MOE_ERR_INVALID_ARG, "attention int4: buffers must be 16-byte aligned");
     const int st = check_kv4_cache("attention int4", cache, cache_bytes, T, n_kv, head_dim, max_pos, kv_len);
     if (st != MOE_OK) return st;
-    const size_t need = moe::attention_int4_workspace_bytes(T, n_heads, n_kv, head_dim, max_pos);
+    const size_t need = moe::attention_int4_workspace_bytes(T, H, n_heads, n_kv, head_dim, max_pos);
     if (workspace_bytes < need)
         return fail(MOE_ERR_INVALID_ARG, "attention int4: workspace of %zu bytes, need %zu", workspace_bytes, need);
     int *eflags = moe::device_error_flags();

@@ -199,12 +199,13 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
                                 void *workspace, int *err, hipStream_t s);
 
 // int4-g128 matrix-vector products (matvec_int4.hip): y = add + W h, h = x or its RMS norm; y may be add.
+size_t matvec_int4_workspace_bytes(int T, int K);
 hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, bool norm,
-                              hipStream_t s);
+                              void *workspace, hipStream_t s);
 
 // Decoder self-attention of one token per sequence with int4 weights and a 4-bit cache (attention_int4.hip).
 bool attention_int4_shape_supported(int H, int n_heads, int n_kv, int head_dim, int max_pos);
-size_t attention_int4_workspace_bytes(int T, int n_heads, int n_kv, int head_dim, int max_pos);
+size_t attention_int4_workspace_bytes(int T, int H, int n_heads, int n_kv, int head_dim, int max_pos);
 hipError_t launch_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
                                         const void *w_o, void *cache, int max_pos, const int32_t *kv_len, float theta,
                                         void *workspace, int *err, hipStream_t s);

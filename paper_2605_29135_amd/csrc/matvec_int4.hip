@@ -27,6 +27,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMvWaves = 8, kMvBlock = kMvWaves * kWave;
 constexpr int kMvGrid = 256;  // compute units
+constexpr int kMvTokens = 3;  // tokens whose terms every block forms itself
 constexpr int kCodeExp = -9;
 
 // The eight codes of a dword as fp16 q 2^-9, in the order 0,4,1,5,2,6,3,7.  (Nibbles at bits 4-7 of a half are 16
@@ -105,22 +106,64 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 __host__ __device__ constexpr int stage_bytes(int T, int GS) { return kMvWaves * GS * 512 * T; }
 __host__ __device__ constexpr int lds_bytes(int T, int GS, int RB) { return stage_bytes(T, GS) + kMvWaves * RB * 4 * kWave * 4; }
 
+// The terms of every token, once for all the blocks of a call: one block per token.  ws: what takes the sums back (int
+// [16]), the norms' factors (float [16]), then at 256 bytes the operands [K / 32][4][2 T rows].
+struct Terms {
+    const int *back;
+    const float *inv;
+    const uint4 *operands;
+};
+__host__ __device__ inline Terms terms_in(const void *ws) {
+    const auto *p = static_cast<const uint8_t *>(ws);
+    return {reinterpret_cast<const int *>(p), reinterpret_cast<const float *>(p + 64), reinterpret_cast<const uint4 *>(p + 256)};
+}
+__global__ __launch_bounds__(256) void matvec_terms_kernel(const float *__restrict__ x, int T, int K, bool norm, uint8_t *ws) {
+    __shared__ float tops[4], sums[4];
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float4 *xr = reinterpret_cast<const float4 *>(x + size_t(t) * K);
+    float top = 0.f, squares = 0.f;
+#pragma unroll 4
+    for (int i = tid; i < K / 4; i += 256) {
+        const float4 u = dev::load_f4(xr + i);
+        top = fmaxf(top, top_of(u));
+        squares += squares_of(u);
+    }
+    top = wave_top(top);
+    squares = dev::wave_sum(squares);
+    if (lane == 0) tops[wave] = top, sums[wave] = squares;
+    __syncthreads();
+    const int e2 = exponent_of(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+    if (tid == 0) {
+        reinterpret_cast<int *>(ws)[t] = -kCodeExp - e2;
+        reinterpret_cast<float *>(ws + 64)[t] = norm ? rsqrtf((sums[0] + sums[1] + sums[2] + sums[3]) / float(K) + 1e-6f) : 1.f;
+    }
+    uint4 *out = reinterpret_cast<uint4 *>(ws + 256) + t;
+#pragma unroll 4
+    for (int i = tid; i < K / 4; i += 256) {  // (K / 4 is a multiple of 32: a pair of lanes stays together)
+        uint4 *f = out + size_t((i >> 5) * 16 + ((i >> 1) & 3) * 4 + ((i >> 3) & 3)) * (2 * T);
+        store_terms(dev::load_f4(xr + i), e2, lane & 1, [&](int k) { return f + k * T; });
+    }
+}
+
 // GS: quantisation groups per wave and pass over the columns; MULTI: several passes, the terms formed again for
-// each.  LOOP: a block has more than one item or pass.  ONE: the two terms share one product (T <= 8).
-template <int RB, int GS, bool ONE, bool MULTI, bool LOOP>
+// each.  LOOP: a block has more than one item or pass.  ONE: the two terms share one product (T <= 8).  PRE: the terms
+// come from matvec_terms_kernel (else T <= kMvTokens).
+template <int RB, int GS, bool ONE, bool MULTI, bool LOOP, bool PRE>
 __global__ __launch_bounds__(kMvBlock, 2) void matvec_int4_kernel(const float *__restrict__ x, const uint8_t *__restrict__ w,
                                                                   int T, int N, int K, const float *add, float *y, bool norm,
-                                                                  int items) {
+                                                                  int items, const void *ws) {
+    static_assert(PRE || ONE, "");
     constexpr int NP = ONE ? 1 : 2;  // products
     extern __shared__ uint4 lds[];
-    __shared__ float sq[kMvWaves][16];  // sums of squares
-    __shared__ int exps[kMvWaves][16];
+    __shared__ float sq[kMvWaves][kMvTokens];  // sums of squares
+    __shared__ int exps[kMvWaves][kMvTokens];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, n = lane & 15, c = lane >> 4;
     const int KG = K / 128, passes = MULTI ? (KG + kMvWaves * GS - 1) / (kMvWaves * GS) : 1;
     const int share = (KG + kMvWaves * passes - 1) / (kMvWaves * passes);  // groups per wave and pass, <= GS
     const uint16_t *scales = reinterpret_cast<const uint16_t *>(w + size_t(N) * (K / 2));
     uint4 *stage = lds + wave * (GS * 32 * T);
-    float *red = reinterpret_cast<float *>(lds) + stage_bytes(T, GS) / 4;
+    float *red = reinterpret_cast<float *>(lds) + (PRE ? 0 : stage_bytes(T, GS) / 4);
+    const Terms pre = terms_in(ws);
 
     struct Weights {
         uint4 w[GS][RB];
@@ -139,41 +182,56 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_int4_kernel(const float *_
     int back[4];  // what takes the sums of row 4 c + q of the product back
     // The wave's columns of every token: four per lane and step of 256, scaled, in two terms.
     auto convert = [&](int pass, bool measure) __attribute__((always_inline)) {
+        if constexpr (PRE) {
+#pragma unroll
+            for (int r = 0; r < GS; ++r) {
+                const int g = min((pass * kMvWaves + wave) * share + min(r, share - 1), KG - 1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < NP; ++k)
+                        xt[r][j][k] = __builtin_bit_cast(f16x8, pre.operands[size_t((g * 4 + j) * 4 + c) * (2 * T) +
+                                                                             (ONE ? min(n, 2 * T - 1) : k * T + min(n, T - 1))]);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = 4 * c + q, t = ONE && row >= T ? row - T : row;
+                back[q] = pre.back[min(t, T - 1)];
+            }
+            return;
+        }
         const int g0 = (pass * kMvWaves + wave) * share, odd = lane & 1;
-#pragma unroll 1
-        for (int t0 = 0; t0 < T; t0 += 4) {
-            float4 v[4][GS / 2];
+        float4 v[kMvTokens][GS / 2];  // (all their loads in flight together)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < kMvTokens; ++t)
 #pragma unroll
-                for (int i = 0; i < GS / 2; ++i) {
-                    const int r = 2 * i + (lane >> 5), g = g0 + r;
-                    v[t][i] = dev::load_f4(reinterpret_cast<const float4 *>(x + size_t(min(t0 + t, T - 1)) * K +
-                                                                            min(g, KG - 1) * 128 + 4 * (lane & 31)));
-                    if (r >= share || g >= KG) v[t][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+            for (int i = 0; i < GS / 2; ++i) {
+                const int r = 2 * i + (lane >> 5), g = g0 + r;
+                v[t][i] = dev::load_f4(reinterpret_cast<const float4 *>(x + size_t(min(t, T - 1)) * K +
+                                                                        min(g, KG - 1) * 128 + 4 * (lane & 31)));
+                if (r >= share || g >= KG) v[t][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (t0 + t >= T) break;
-                float top = 0.f, squares = 0.f;
+        for (int t = 0; t < kMvTokens; ++t) {
+            if (t >= T) break;
+            float top = 0.f, squares = 0.f;
 #pragma unroll
-                for (int i = 0; i < GS / 2; ++i) {
-                    top = fmaxf(top, top_of(v[t][i]));
-                    squares += squares_of(v[t][i]);
-                }
-                top = wave_top(top);
-                const int e2 = exponent_of(top);
-                if (lane == 0) exps[wave][t0 + t] = e2;
-                if (norm && measure) {
-                    squares = dev::wave_sum(squares);
-                    if (lane == 0) sq[wave][t0 + t] = pass ? sq[wave][t0 + t] + squares : squares;
-                }
+            for (int i = 0; i < GS / 2; ++i) {
+                top = fmaxf(top, top_of(v[t][i]));
+                squares += squares_of(v[t][i]);
+            }
+            top = wave_top(top);
+            const int e2 = exponent_of(top);
+            if (lane == 0) exps[wave][t] = e2;
+            if (norm && measure) {
+                squares = dev::wave_sum(squares);
+                if (lane == 0) sq[wave][t] = pass ? sq[wave][t] + squares : squares;
+            }
 #pragma unroll
-                for (int i = 0; i < GS / 2; ++i) {
-                    const int j = (lane >> 1) & 3, part = (lane >> 3) & 3, r = 2 * i + (lane >> 5);
-                    uint4 *f = stage + ((r * 4 + j) * 4 + part) * (2 * T) + t0 + t;
-                    store_terms(v[t][i], e2, odd, [&](int k) { return f + k * T; });
-                }
+            for (int i = 0; i < GS / 2; ++i) {
+                const int j = (lane >> 1) & 3, part = (lane >> 3) & 3, r = 2 * i + (lane >> 5);
+                uint4 *f = stage + ((r * 4 + j) * 4 + part) * (2 * T) + t;
+                store_terms(v[t][i], e2, odd, [&](int k) { return f + k * T; });
             }
         }
         // the operands are this wave's own: a wave-level LDS sync
@@ -262,7 +320,8 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_int4_kernel(const float *_
                     total += part;
                 }
                 float inv = 1.f;
-                if (norm) {
+                if constexpr (PRE) inv = pre.inv[o_token];
+                else if (norm) {
                     float s = 0.f;
 #pragma unroll
                     for (int v = 0; v < kMvWaves; ++v) s += sq[v][o_token];
@@ -448,20 +507,26 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_stream_kernel(const float 
     }
 }
 
-template <int RB, int GS, bool ONE, bool MULTI>
-hipError_t run(const float *x, const uint8_t *w, int T, int N, int K, const float *add, float *y, bool norm, hipStream_t s) {
+template <int RB, int GS, bool ONE, bool MULTI, bool PRE>
+hipError_t run(const float *x, const uint8_t *w, int T, int N, int K, const float *add, float *y, bool norm, void *ws,
+               hipStream_t s) {
     const int tiles = (N + 15) / 16, items = (tiles + RB - 1) / RB;
     // one item per block where they fit the device together, else persistent blocks
-    const int lds = lds_bytes(T, GS, RB), grid = items <= 2 * kMvGrid ? items : kMvGrid;
-    if (MULTI || grid < items) matvec_int4_kernel<RB, GS, ONE, MULTI, true><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items);
-    else matvec_int4_kernel<RB, GS, ONE, false, false><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items);
+    const int lds = lds_bytes(PRE ? 0 : T, GS, RB), most = kMvGrid * (2 * lds <= 160 * 1024 ? 2 : 1);
+    const int grid = items <= most ? items : kMvGrid;
+    if (MULTI || grid < items)
+        matvec_int4_kernel<RB, GS, ONE, MULTI, true, PRE><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
+    else
+        matvec_int4_kernel<RB, GS, ONE, false, false, PRE><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
     return hipGetLastError();
 }
 
 }  // namespace
 
+size_t matvec_int4_workspace_bytes(int T, int K) { return T <= kMvTokens ? 0 : 256 + size_t(4) * T * K; }
+
 hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, bool norm,
-                              hipStream_t s) {
+                              void *ws, hipStream_t s) {
     const auto *wb = static_cast<const uint8_t *>(w);
     const int tiles = (N + 15) / 16;
     if (tiles >= kMvGrid * kMvWaves && stream_lds(T, K) <= 128 * 1024) {  // a row tile for every wave that fits the device
@@ -474,17 +539,26 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
 #undef STREAM
         return hipGetLastError();
     }
+    const bool pre = T > kMvTokens;
+    if (pre) {
+        matvec_terms_kernel<<<T, 256, 0, s>>>(x, T, K, norm, static_cast<uint8_t *>(ws));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     // Four groups per wave where K has more than two for each of the eight waves and the tokens' terms leave the
     // registers for it.
     const int gs = K <= 2048 || T > 8 ? 2 : 4;
-    const int fit = kMvGrid * (2 * lds_bytes(T, gs, 1) <= 160 * 1024 ? 2 : 1);  // blocks that run together
+    const int fit = kMvGrid * (2 * lds_bytes(pre ? 0 : T, gs, 1) <= 160 * 1024 ? 2 : 1);  // blocks that run together
     const int rb = tiles <= fit ? 1 : tiles <= 2 * fit || gs == 4 || T > 8 ? 2 : 4;
     const bool multi = K > kMvWaves * gs * 128;
-#define MATVEC(RB, GS, ONE, MULTI) \
-    if (rb == RB && gs == GS && (T <= 8) == ONE && multi == MULTI) return run<RB, GS, ONE, MULTI>(x, wb, T, N, K, add, y, norm, s);
-    MATVEC(1, 2, true, false) MATVEC(2, 2, true, false) MATVEC(4, 2, true, false)
-    MATVEC(1, 4, true, false) MATVEC(2, 4, true, false) MATVEC(1, 4, true, true) MATVEC(2, 4, true, true)
-    MATVEC(1, 2, false, false) MATVEC(2, 2, false, false) MATVEC(1, 2, false, true) MATVEC(2, 2, false, true)
+#define MATVEC(RB, GS, ONE, MULTI, PRE)                                                 \
+    if (rb == RB && gs == GS && (T <= 8) == ONE && multi == MULTI && pre == PRE)        \
+        return run<RB, GS, ONE, MULTI, PRE>(x, wb, T, N, K, add, y, norm, ws, s);
+    MATVEC(1, 2, true, false, false) MATVEC(2, 2, true, false, false) MATVEC(4, 2, true, false, false)
+    MATVEC(1, 4, true, false, false) MATVEC(2, 4, true, false, false) MATVEC(1, 4, true, true, false) MATVEC(2, 4, true, true, false)
+    MATVEC(1, 2, true, false, true) MATVEC(2, 2, true, false, true) MATVEC(4, 2, true, false, true)
+    MATVEC(1, 4, true, false, true) MATVEC(2, 4, true, false, true) MATVEC(1, 4, true, true, true) MATVEC(2, 4, true, true, true)
+    MATVEC(1, 2, false, false, true) MATVEC(2, 2, false, false, true) MATVEC(1, 2, false, true, true) MATVEC(2, 2, false, true, true)
 #undef MATVEC
     return hipErrorInvalidValue;
 }

@@ -334,7 +334,7 @@ int moe_stack_create(const moe_stack_desc *d, moe_stack **out) {
         s->ad.w_qkv = s->ad.w_o = nullptr;
         s->ad.k_cache = s->ad.v_cache = nullptr;
         s->attn_pos = a->start_pos;
-        const size_t n = a->int4 ? moe::attention_int4_workspace_bytes(1, a->n_heads, a->n_kv, a->head_dim, a->max_pos)
+        const size_t n = a->int4 ? moe::attention_int4_workspace_bytes(1, d->H, a->n_heads, a->n_kv, a->head_dim, a->max_pos)
                                  : moe::attention_workspace_bytes(a->n_heads, a->n_kv, a->head_dim, a->max_pos);
         if ((e = hipMalloc(&s->attn_ws, n)) != hipSuccess || (e = hipMalloc(&s->attn_len, sizeof(int))) != hipSuccess)
             return bail(e, "stack attention workspace");

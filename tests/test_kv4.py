@@ -181,9 +181,13 @@ def test_matvec_and_block_refusals():
               (OK_PTR + 4, OK_PTR, 1, 64, 128, None, far, 0), (OK_PTR, OK_PTR + 8, 1, 64, 128, None, far, 0),
               (OK_PTR, OK_PTR, 1, 64, 128, None, far + 2, 0), (OK_PTR, OK_PTR, 1, 64, 128, far + 1, far, 0),
               (OK_PTR, OK_PTR, 1, 64, 128, None, OK_PTR, 0), (OK_PTR, OK_PTR, 1, 64, 128, None, OK_PTR + 508, 0)]:
-        refused("moe_matvec_int4", *a, None)
-    assert moe.lib().moe_matvec_int4(None, None, 0, 64, 128, None, None, 0, None) == 0
-    assert moe.lib().moe_matvec_int4(None, None, 3, 0, 128, None, None, 0, None) == 0
+        refused("moe_matvec_int4", *a, OK_PTR, 1 << 30, None)
+    need = moe.moe_matvec_int4_workspace_bytes(16, 128)
+    assert need > 0 and moe.moe_matvec_int4_workspace_bytes(1, 128) == moe.moe_matvec_int4_workspace_bytes(17, 128) == 0
+    for ws, size in ((None, 1 << 30), (OK_PTR, need - 1), (OK_PTR + 8, 1 << 30)):
+        refused("moe_matvec_int4", OK_PTR, OK_PTR, 16, 64, 128, None, far, 0, ws, size, None)
+    assert moe.lib().moe_matvec_int4(None, None, 0, 64, 128, None, None, 0, None, 0, None) == 0
+    assert moe.lib().moe_matvec_int4(None, None, 3, 0, 128, None, None, 0, None, 0, None) == 0
     big = 1 << 40
     good = dict(x=OK_PTR, T=2, H=256, nh=4, kv=2, d=64, wq=OK_PTR, wo=OK_PTR, cache=OK_PTR, cb=big, mp=64, kl=OK_PTR,
                 theta=1e4, ws=OK_PTR, wb=big)
@@ -193,9 +197,9 @@ def test_matvec_and_block_refusals():
         a = {**good, **b}
         refused("moe_attention_decode_int4", a["x"], a["T"], a["H"], a["nh"], a["kv"], a["d"], a["wq"], a["wo"], a["cache"],
                 a["cb"], a["mp"], a["kl"], a["theta"], a["ws"], a["wb"], None)
-    assert moe.moe_attention_decode_int4_workspace_bytes(1, 4, 2, 64, 64) > 0
-    assert moe.moe_attention_decode_int4_workspace_bytes(17, 4, 2, 64, 64) == 0
-    assert moe.moe_attention_decode_int4_workspace_bytes(1, 4, 2, 96, 64) == 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, 256, 4, 2, 64, 64) > 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(17, 256, 4, 2, 64, 64) == 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, 256, 4, 2, 96, 64) == 0
 
 
 def test_binding_refuses_host_tensors_and_shapes():

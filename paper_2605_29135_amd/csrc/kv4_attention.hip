@@ -648,7 +648,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 // largest) and share them through LDS in the operands' order, and a score costs an fma, an exponential, a share
 // of a maximum and of a conversion.  Two buffers: the next positions' codes are loaded before the present ones are
 // used and turned after.  The sums of P come from the matrix cores too.
-constexpr int kPromptTiles = 2;  // row tiles of 16 per wave
+constexpr int prompt_tiles(int d) { return d <= 128 ? 2 : 1; }  // row tiles of 16 per wave: what its registers hold
 
 // A barrier for what the block's waves pass one another through LDS; loads in flight stay so.
 __device__ __forceinline__ void lds_barrier() {
@@ -656,10 +656,16 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-// The power of two that takes values of at most |m| + 15 s below 2^6: m, s a pair of bf16 per lane (s >= 0).
-__device__ __forceinline__ int held_exponent(uint32_t m, uint32_t s) {
+// The power of two that takes values of at most |m| + 15 s below 2^6: m, s pairs of bf16, L per lane (s >= 0).
+template <int L>
+__device__ __forceinline__ int held_exponent(const uint32_t (&m)[L], const uint32_t (&s)[L]) {
     // 2 max(|m|, 16 s) is no less; bf16 bits compare as numbers, and four exponents more are times 16
-    const u16x2 v = __builtin_elementwise_max(__builtin_bit_cast(u16x2, m & 0x7fff7fffu), __builtin_bit_cast(u16x2, s + 0x02000200u));
+    u16x2 v = {0, 0};
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+        v = __builtin_elementwise_max(v, __builtin_bit_cast(u16x2, m[l] & 0x7fff7fffu));
+        v = __builtin_elementwise_max(v, __builtin_bit_cast(u16x2, s[l] + 0x02000200u));
+    }
     int top = max(int(v[0]), int(v[1]));
 #define ROW_MAX(CTRL) top = max(top, __builtin_amdgcn_update_dpp(0, top, CTRL, 0xF, 0xF, true))
     ROW_MAX(0xB1);
@@ -672,13 +678,14 @@ __device__ __forceinline__ int held_exponent(uint32_t m, uint32_t s) {
     return min(131 - (all >> 7), 100);  // (below 2^(exponent - 127 + 2))
 }
 
-// grid: (row tiles, key/value head, sequence); WAVES x 32 rows per block.
+// grid: (row tiles, key/value head, sequence); WAVES x 16 NT rows per block.
 template <int NG, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a) {
-    constexpr int d = NG * kGroup, NT = kPromptTiles, ROWS = 16 * NT * WAVES;
+__global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_prompt_kernel(AttendArgs a) {
+    constexpr int d = NG * kGroup, NT = prompt_tiles(d), ROWS = 16 * NT * WAVES;
     constexpr int FRAGS = 8 * NG;           // operands (1 KiB) of two blocks' keys, and of their values
     constexpr int WORDS = 16 * NG / WAVES;  // words of codes per lane that a wave turns
     constexpr int SPLIT = WAVES / 4;        // waves that share one block's keys or values
+    constexpr int LIM = NG > 2 ? 2 : 1;     // a lane's words of each array of the pair's scales and bases
     static_assert(WAVES == 4 || WAVES == 8);
     __shared__ uint4 kf_sh[2][FRAGS][64], vf_sh[2][FRAGS][64];
     const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
@@ -694,7 +701,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a)
     // What this wave turns: block `mine_b` of the pair, its keys or values, a half of them (eight waves).
     const int mine_b = (wave >> 1) & 1, part = wave >> 2;
     const bool values = wave & 1;
-    uint32_t raw[WORDS], ps[4 * NG], pm[4 * NG], lim[4];  // codes, scales and bases; all the pair's scales and bases
+    // (a half of three groups' values is one and a half of them)
+    constexpr int GROUPS = SPLIT == 1 ? NG : (NG + 1) / 2, TAUS = SPLIT == 1 ? 2 : 1;
+    const int g_first = part * WORDS / 4;
+    uint32_t raw[WORDS], ps[4 * GROUPS], pm[4 * GROUPS], lim[4][LIM];  // codes, scales and bases; all the pair's scales and bases
     auto load = [&](int b) __attribute__((always_inline)) {
         // (past the last block: that one again, masked by its position)
         const uint8_t *block = seq + size_t(min(b + mine_b, b1 - 1)) * block_bytes(d);
@@ -706,13 +716,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a)
                 raw[4 * i] = u.x, raw[4 * i + 1] = u.y, raw[4 * i + 2] = u.z, raw[4 * i + 3] = u.w;
             }
         } else {
-            const uint2 u = *reinterpret_cast<const uint2 *>(codes + lane * 16 + part * 8);
-            raw[0] = u.x, raw[1] = u.y;
+#pragma unroll
+            for (int i = 0; i < WORDS / 2; ++i) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(codes + code_offset(part * WORDS + 2 * i, lane));
+                raw[2 * i] = u.x, raw[2 * i + 1] = u.y;
+            }
         }
         if (values) {
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const uint4 u = dev::load16(block + v_scales(d) + g * 64 + c * 16), v = dev::load16(block + v_bases(d) + g * 64 + c * 16);
+            for (int g = 0; g < GROUPS; ++g) {
+                const uint8_t *at = block + (g_first + g) * 64 + c * 16;
+                const uint4 u = dev::load16(at + v_scales(d)), v = dev::load16(at + v_bases(d));
                 ps[4 * g] = u.x, ps[4 * g + 1] = u.y, ps[4 * g + 2] = u.z, ps[4 * g + 3] = u.w;
                 pm[4 * g] = v.x, pm[4 * g + 1] = v.y, pm[4 * g + 2] = v.z, pm[4 * g + 3] = v.w;
             }
@@ -721,28 +735,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a)
             for (int g = 0; g < NG; ++g) {
                 pm[g] = *reinterpret_cast<const uint32_t *>(block + k_bases(d) + g * 64 + n * 4);
 #pragma unroll
-                for (int tau = 0; tau < 2; ++tau)
-                    ps[2 * g + tau] = *reinterpret_cast<const uint16_t *>(block + k_scales(d) + g * 64 + 2 * order_index(16 * tau + n));
+                for (int tau = 0; tau < TAUS; ++tau)
+                    ps[TAUS * g + tau] = *reinterpret_cast<const uint16_t *>(block + k_scales(d) + g * 64 + 2 * order_index(16 * (part + tau) + n));
             }
         }
-        // Every wave sees all the scales and bases: one pair of values per lane and array (lane = block, word).
-        const uint8_t *all = seq + size_t(min(b + (lane >> 5), b1 - 1)) * block_bytes(d) + 4 * ((lane & 31) % (16 * NG));
-        lim[0] = *reinterpret_cast<const uint32_t *>(all + k_scales(d));
-        lim[1] = *reinterpret_cast<const uint32_t *>(all + k_bases(d));
-        lim[2] = *reinterpret_cast<const uint32_t *>(all + v_scales(d));
-        lim[3] = *reinterpret_cast<const uint32_t *>(all + v_bases(d));
+        // Every wave sees all the scales and bases: LIM pairs of values per lane and array (lane = block, word).
+#pragma unroll
+        for (int l = 0; l < LIM; ++l) {
+            const int w = 32 * l + (lane & 31) % (16 * (NG - 2 * l));
+            const uint8_t *all = seq + size_t(min(b + (lane >> 5), b1 - 1)) * block_bytes(d) + 4 * w;
+            lim[0][l] = *reinterpret_cast<const uint32_t *>(all + k_scales(d));
+            lim[1][l] = *reinterpret_cast<const uint32_t *>(all + k_bases(d));
+            lim[2][l] = *reinterpret_cast<const uint32_t *>(all + v_scales(d));
+            lim[3][l] = *reinterpret_cast<const uint32_t *>(all + v_bases(d));
+        }
     };
     int ek[2] = {0, 0}, ev[2] = {0, 0};  // exponents of the two buffers' keys and values
     auto turn = [&](int b, int buf, int most) __attribute__((always_inline)) {  // most: of the values' exponent
         if ((b + 2) * kPos > s.len) {
             // Positions that hold nothing yet may hold anything: their scales and bases count as zeros.
-            const int blk = min(b + (lane >> 5), b1 - 1), w = (lane & 31) % (16 * NG) & 15;  // word of the group's 16
+            const int blk = min(b + (lane >> 5), b1 - 1), w = lane & 15;  // word of the group's 16
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int o = 2 * w + e, in_order = 16 * ((o >> 2) & 1) + 4 * (o >> 3) + (o & 3), in_tiles = 16 * e + w;
                 const uint32_t drop = ~(0xffffu << (16 * e));
-                if (blk * kPos + in_order >= s.len) lim[0] &= drop, lim[2] &= drop, lim[3] &= drop;
-                if (blk * kPos + in_tiles >= s.len) lim[1] &= drop;
+#pragma unroll
+                for (int l = 0; l < LIM; ++l) {
+                    if (blk * kPos + in_order >= s.len) lim[0][l] &= drop, lim[2][l] &= drop, lim[3][l] &= drop;
+                    if (blk * kPos + in_tiles >= s.len) lim[1][l] &= drop;
+                }
             }
             if (values) {
                 const int own = min(b + mine_b, b1 - 1);
@@ -753,7 +774,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a)
                         const int k = 2 * i + e;
                         if (own * kPos + 16 * (k >> 2) + 4 * c + (k & 3) < s.len) continue;
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) {
+                        for (int g = 0; g < GROUPS; ++g) {
                             ps[4 * g + i] &= ~(0xffffu << (16 * e));
                             pm[4 * g + i] &= ~(0xffffu << (16 * e));
                         }
@@ -770,33 +791,34 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_prompt_kernel(AttendArgs a)
             return __builtin_bit_cast(uint4, u * join8(s0, s1, s2, s3) + join8(m0, m1, m2, m3));
         };
         if (values) {
+            f16x2 sc[GROUPS][4], ba[GROUPS][4];
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                if (SPLIT == 2 && NG == 2 && g != part) continue;  // (a half of two groups' words is one group's)
-                f16x2 sc[4], ba[4];
+            for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sc[i] = pack_f16(low_half(ps[4 * g + i]) * fs, high_half(ps[4 * g + i]) * fs);
-                    ba[i] = pack_f16(low_half(pm[4 * g + i]) * fm, high_half(pm[4 * g + i]) * fm);
+                    sc[g][i] = pack_f16(low_half(ps[4 * g + i]) * fs, high_half(ps[4 * g + i]) * fs);
+                    ba[g][i] = pack_f16(low_half(pm[4 * g + i]) * fm, high_half(pm[4 * g + i]) * fm);
                 }
-                constexpr int per = WORDS < 4 ? WORDS : 4;
 #pragma unroll
-                for (int i = 0; i < per; ++i) {
-                    const int w = (SPLIT == 2 && NG == 2 ? 0 : 4 * g) + i;
-                    dst[w * 64] = turned(raw[w], sc[0], sc[1], sc[2], sc[3], ba[0], ba[1], ba[2], ba[3]);
+            for (int w = 0; w < WORDS; ++w) {
+                if (NG == 3 && SPLIT == 2 && (w & ~1) == 2 && part) {  // (there the second half's next group begins)
+                    dst[w * 64] = turned(raw[w], sc[1][0], sc[1][1], sc[1][2], sc[1][3], ba[1][0], ba[1][1], ba[1][2], ba[1][3]);
+                    continue;
                 }
+                constexpr int last_group = GROUPS - 1;
+                const int g = min(w / 4, last_group);
+                dst[w * 64] = turned(raw[w], sc[g][0], sc[g][1], sc[g][2], sc[g][3], ba[g][0], ba[g][1], ba[g][2], ba[g][3]);
             }
         } else {
 #pragma unroll
-            for (int tau = 0; tau < 2; ++tau) {
-                if (SPLIT == 2 && tau != part) continue;
+            for (int tau = 0; tau < TAUS; ++tau) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const float sv = low_half(ps[2 * g + tau]) * fs, mv = (tau ? high_half(pm[g]) : low_half(pm[g])) * fm;
+                    const float sv = low_half(ps[TAUS * g + tau]) * fs, mv = (part + tau ? high_half(pm[g]) : low_half(pm[g])) * fm;
                     const f16x2 sc = pack_f16(sv, sv), ba = pack_f16(mv, mv);
 #pragma unroll
                     for (int j = 2 * g; j < 2 * g + 2; ++j) {
-                        const int w = (SPLIT == 2 ? 0 : tau * 2 * NG) + j;
+                        const int w = tau * 2 * NG + j;
                         dst[w * 64] = turned(raw[w], sc, sc, sc, sc, ba, ba, ba, ba);
                     }
                 }
@@ -1026,9 +1048,10 @@ AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max
     // what a wave's registers hold
     const int most = d <= 64 ? (f32 ? 2 : 4) : d <= 128 ? 2 : d <= 192 && !f32 ? 2 : 1;
     AttendPlan p{};
-    if (!f32 && d <= 128 && rows >= 128 && (rows + 127) / 128 * n_kv * n_seq >= 64) {
-        p.prompt = (rows + 255) / 256 * n_kv * n_seq >= 256 ? 8 : 4;
-        p.blocks = int((rows + 32 * p.prompt - 1) / (32 * p.prompt));
+    if (!f32 && rows >= 128 && (rows + 127) / 128 * n_kv * n_seq >= 64) {
+        const int per = 64 * prompt_tiles(d);  // rows of four waves
+        p.prompt = (rows + 2 * per - 1) / (2 * per) * n_kv * n_seq >= 256 ? 8 : 4;
+        p.blocks = int((rows + per * (p.prompt / 4) - 1) / (per * (p.prompt / 4)));
         return p;
     }
     p.tiles = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
@@ -1074,10 +1097,10 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     a.err = err;
     const dim3 grid = p.target ? dim3(p.units, n_kv, p.blocks) : dim3(p.blocks, n_kv, batch.n_seq);
     if (p.prompt) {
-        if (d == 64 && p.prompt == 4) kv4_prompt_kernel<1, 4><<<grid, 256, 0, s>>>(a);
-        else if (d == 64) kv4_prompt_kernel<1, 8><<<grid, 512, 0, s>>>(a);
-        else if (p.prompt == 4) kv4_prompt_kernel<2, 4><<<grid, 256, 0, s>>>(a);
-        else kv4_prompt_kernel<2, 8><<<grid, 512, 0, s>>>(a);
+#define KV4_PROMPT(NG, W) \
+    if (d == NG * kGroup && p.prompt == W) kv4_prompt_kernel<NG, W><<<grid, 64 * W, 0, s>>>(a);
+        KV4_PROMPT(1, 4) KV4_PROMPT(1, 8) KV4_PROMPT(2, 4) KV4_PROMPT(2, 8) KV4_PROMPT(3, 4) KV4_PROMPT(3, 8) KV4_PROMPT(4, 4) KV4_PROMPT(4, 8)
+#undef KV4_PROMPT
         return hipGetLastError();
     }
 #define KV4_RUN(NG, NT, F) kv4_attend_kernel<NG, NT ? NT : 1, F, NT == 0><<<grid, kAttBlock, 0, s>>>(a)

@@ -362,6 +362,10 @@ CASES = [  # (d, n_kv, group, tokens, lengths, max_pos, window)
     (64, 16, 4, [33, 40, 64, 20], [130, 65, 64, 7], 160, 48),
     (128, 64, 4, [33, 32, 31, 40], [97, 32, 10, 160], 160, 0),
     (64, 64, 2, [64, 80, 70, 3], [70, 80, 200, 0], 224, 33),
+    (192, 16, 4, [40, 33, 70, 5], [40, 100, 200, 3], 224, 0),
+    (192, 16, 8, [33, 20, 17, 1], [130, 65, 64, 7], 160, 48),
+    (256, 16, 4, [40, 33, 70, 5], [40, 100, 200, 3], 224, 0),
+    (256, 32, 3, [43, 64, 1, 44], [31, 160, 0, 129], 160, 33),
 ]
 
 
@@ -431,7 +435,8 @@ def test_attention_scales(dtype, scale):
 @pytest.mark.parametrize("k_size,v_size", [(2.0 ** -30, 2.0 ** -55), (2.0 ** 30, 2.0 ** 38), (1.0, 2.0 ** -20)])
 def test_attention_range(dtype, k_size, v_size):
     """Keys and values far from one, the scores kept where they are by the scale."""
-    for d, n_kv, G, ns, ls in ((128, 2, 4, [1, 1], [70, 200]), (64, 2, 12, [3, 1], [70, 40]), (128, 16, 8, [20, 33, 17, 1], [70, 40, 100, 1])):
+    for d, n_kv, G, ns, ls in ((128, 2, 4, [1, 1], [70, 200]), (64, 2, 12, [3, 1], [70, 40]), (128, 16, 8, [20, 33, 17, 1], [70, 40, 100, 1]),
+                              (192, 16, 8, [20, 33, 17, 1], [70, 40, 100, 1]), (256, 16, 8, [20, 33, 17, 1], [70, 40, 100, 1])):
         gen = torch.Generator().manual_seed(d)
         ks = [torch.randn((L, n_kv, d), generator=gen) * k_size for L in ls]
         vs = [torch.randn((L, n_kv, d), generator=gen) * v_size for L in ls]

@@ -36,7 +36,9 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
-constexpr int kTarget = 512;  // blocks that fill the device, where rows and heads alone give fewer
+// Blocks that fill the device, where rows and heads alone give fewer: one token of 64 heads over 131071 positions of
+// 8 heads takes 30.0 us with 512, 35.8 with 768 and 34.1 with 1024 (256 leave half of the waves' places empty).
+constexpr int kTarget = 512;
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -144,6 +146,8 @@ struct AttendArgs {
     long long q_stride, out_stride;
     int n_heads, n_kv, group, window;
     int target;  // splits of a whole batch (0: every sequence in one piece)
+    int least;   // blocks of positions that a piece has at least; the rest come in multiples of `unit`
+    int unit;
     int tiles;   // row tiles of the largest sequence
     float scale;  // times log2(e)
     Batch batch;
@@ -156,7 +160,7 @@ __device__ __forceinline__ int seen_blocks(const Seq &s, int window) {
     return (s.len - 1) / kPos + 1 - (window ? max(0, s.len - s.n - window + 1) / kPos : 0);
 }
 
-// The split of a batch: sequences are cut into pieces of `chunk` blocks of positions, at least one per wave, so
+// The split of a batch: sequences are cut into pieces of `chunk` blocks of positions, at least `least`, so
 // that there are about `target` of them in all; a sequence has at least one piece.  Every wave works it out for
 // itself.  by_unit: which piece is number `want`; otherwise, the pieces of sequence `want`.
 struct Piece {
@@ -164,7 +168,9 @@ struct Piece {
     int seq, split, chunk;
     int first, count;  // of the sequence's pieces (count 0: there is no such piece)
 };
-__device__ __forceinline__ Piece find_piece(const Batch &b, int window, int target, int want, bool by_unit, int *err) {
+__device__ __forceinline__ Piece find_piece(const AttendArgs &a, int want, bool by_unit, int *err) {
+    const Batch &b = a.batch;
+    const int window = a.window, target = a.target;
     const int lane = threadIdx.x & 63;
     uint32_t total = 0;  // (a batch that is split has fewer than kTarget sequences of at most 2^21 blocks)
     Seq s{0, 0, 0, false};
@@ -181,7 +187,8 @@ __device__ __forceinline__ Piece find_piece(const Batch &b, int window, int targ
         total += uint32_t(__builtin_amdgcn_readlane(int(wave_scan(uint32_t(nb))), 63));
     }
     Piece p{};
-    p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), kAttWaves);
+    p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), a.least);
+    p.chunk = (p.chunk + a.unit - 1) & -a.unit;
     int before = 0;
 #pragma unroll 1
     for (int base = 0; base < b.n_seq; base += 64) {
@@ -206,6 +213,26 @@ __device__ __forceinline__ Piece find_piece(const Batch &b, int window, int targ
     return p;
 }
 
+// This block's piece: grid (row tiles, key/value head, sequence), or (pieces, key/value head, row tiles).
+__device__ __forceinline__ Piece this_piece(const AttendArgs &a, int tile, int *err) {
+    if (a.target) return find_piece(a, blockIdx.x, true, blockIdx.x == 0 ? err : nullptr);
+    Piece p{};
+    p.seq = blockIdx.z;
+    p.count = 1;
+    p.s = sequence(a.batch, p.seq);
+    if (p.s.bad && err && (threadIdx.x & 63) == 0) atomicOr(err, kErrRange);
+    return p;
+}
+// Blocks of positions (first, end): those that some of the rows sees, the piece's share of them.
+__device__ __forceinline__ int2 tile_blocks(const AttendArgs &a, const Piece &piece, int row, int row_end) {
+    const Seq &s = piece.s;
+    const int p_first = s.len - s.n + row / a.group, p_last = s.len - s.n + (row_end - 1) / a.group;
+    const int b_first = a.window ? max(0, s.len - s.n - a.window + 1) / kPos : 0;
+    const int t_first = a.window ? max(0, p_first - a.window + 1) / kPos : 0, t_end = p_last < 0 ? 0 : p_last / kPos + 1;
+    return make_int2(max(t_first, b_first + piece.split * piece.chunk),
+                     piece.split == piece.count - 1 ? t_end : min(t_end, b_first + (piece.split + 1) * piece.chunk));
+}
+
 template <bool F32>
 __device__ __forceinline__ void store4(void *out, size_t at, float4 v) {
     if constexpr (F32) *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = v;
@@ -226,31 +253,16 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
     const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int half = HALF ? n >> 3 : 0, n_row = HALF ? n & 7 : n;
-    int tile = blockIdx.x;
-    Piece piece{};
-    int *err = blockIdx.x == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr;
-    if (a.target) {
-        tile = blockIdx.z;
-        piece = find_piece(a.batch, a.window, a.target, blockIdx.x, true, tile == 0 ? err : nullptr);
-        if (piece.count == 0) return;
-    } else {
-        piece.seq = blockIdx.z;
-        piece.count = 1;
-        piece.s = sequence(a.batch, piece.seq);
-        if (piece.s.bad && err && lane == 0) atomicOr(err, kErrRange);
-    }
+    const int tile = a.target ? blockIdx.z : blockIdx.x;
+    const Piece piece = this_piece(a, tile, tile == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
+    if (piece.count == 0) return;
     const Seq &s = piece.s;
     const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
     if (row0 >= rows) return;
-
-    // Blocks of positions: those that some row of the tile sees, this piece's share of them.
     const int p_first = s.len - s.n + row0 / G;                               // position of the tile's first row
     const int p_last = s.len - s.n + min(s.n - 1, (row0 + ROWS * NT - 1) / G);  // of its last row
-    const int b_first = a.window ? max(0, s.len - s.n - a.window + 1) / kPos : 0;
-    const int t_first = a.window ? max(0, p_first - a.window + 1) / kPos : 0;
-    const int t_end = p_last < 0 ? 0 : p_last / kPos + 1;
-    const int b0 = max(t_first, b_first + piece.split * piece.chunk);
-    const int b1 = piece.split == piece.count - 1 ? t_end : min(t_end, b_first + (piece.split + 1) * piece.chunk);
+    const int2 range = tile_blocks(a, piece, row0, min(row0 + ROWS * NT, rows));
+    const int b0 = range.x, b1 = range.y;
     const uint8_t *seq = a.cache + (size_t(piece.seq) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
 
     // A block's operands as they lie in the cache.  Keys and values are loaded one block ahead, each as soon as
@@ -689,14 +701,16 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     static_assert(WAVES == 4 || WAVES == 8);
     __shared__ uint4 kf_sh[2][FRAGS][64], vf_sh[2][FRAGS][64];
     const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
-    const Seq s = sequence(a.batch, blockIdx.z);
-    if (s.bad && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(a.err, kErrRange);
     // (the last rows see the most positions: their blocks start first)
-    const int G = a.group, rows = s.n * G, tile = gridDim.x - 1 - blockIdx.x, row0 = tile * ROWS;
+    const int tile = a.tiles - 1 - int(a.target ? blockIdx.z : blockIdx.x);
+    const Piece piece = this_piece(a, tile, tile == a.tiles - 1 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
+    if (piece.count == 0) return;
+    const Seq &s = piece.s;
+    const int G = a.group, rows = s.n * G, row0 = tile * ROWS;
     if (row0 >= rows) return;
-    const int p_first = s.len - s.n + row0 / G, p_last = s.len - s.n + min(s.n - 1, (row0 + ROWS - 1) / G);
-    const int b0 = a.window ? max(0, p_first - a.window + 1) / kPos : 0, b1 = p_last < 0 ? b0 : p_last / kPos + 1;
-    const uint8_t *seq = a.cache + (size_t(blockIdx.z) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
+    const int2 range = tile_blocks(a, piece, row0, min(row0 + ROWS, rows));
+    const int b0 = range.x, b1 = range.y;
+    const uint8_t *seq = a.cache + (size_t(piece.seq) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
 
     // What this wave turns: block `mine_b` of the pair, its keys or values, a half of them (eight waves).
     const int mine_b = (wave >> 1) & 1, part = wave >> 2;
@@ -967,6 +981,16 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     for (int t = 0; t < NT; ++t) {
         const int row = w_row0 + 16 * t + n;
         if (row >= rows) continue;
+        if (piece.count > 1) {
+            float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * ROWS + row) * (d + 4);
+#pragma unroll
+            for (int i = 0; i < 4 * NG; ++i)
+                *reinterpret_cast<float4 *>(o + 16 * i + 4 * c) =
+                    make_float4(ldexpf(acc[t][i][0], -ea), ldexpf(acc[t][i][1], -ea), ldexpf(acc[t][i][2], -ea), ldexpf(acc[t][i][3], -ea));
+            // (the sums' probabilities are relative to this; the maximum -inf stays)
+            if (c == 0) *reinterpret_cast<float2 *>(o + d) = make_float2(mx[t] - 15.f, sum[t][0]);
+            continue;
+        }
         const float l = sum[t][0], inv = l == 0.f ? 0.f : 1.f / l;
         const size_t at = size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * c;
 #pragma unroll
@@ -976,6 +1000,20 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     }
 }
 
+// One more piece (its maximum and sum, four dims of its output).  As in the attention kernel: nothing seen counts 0,
+// NaN stays.
+__device__ __forceinline__ void join_piece(float &M, float &S, float4 &v, float2 ml, float4 u) {
+    const float now = fmaxf(M, ml.x);
+    const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
+    const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
+    M = now;
+    S = fmaf(S, f, ml.y * g);
+    v.x = fmaf(v.x, f, u.x * g);
+    v.y = fmaf(v.y, f, u.y * g);
+    v.z = fmaf(v.z, f, u.z * g);
+    v.w = fmaf(v.w, f, u.w * g);
+}
+
 // Joins the pieces of one row.  grid: (rows, key/value head, sequence); groups of d / 4 lanes take the pieces in
 // turn, a running maximum each.
 template <int NG, bool F32>
@@ -983,7 +1021,7 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
     constexpr int d = NG * kGroup, N4 = d / 4, SUB = kAttBlock / N4;
     __shared__ float4 acc_sh[SUB][N4];
     __shared__ float max_sh[SUB], sum_sh[SUB];
-    const Piece piece = find_piece(a.batch, a.window, a.target, blockIdx.z, false, nullptr);
+    const Piece piece = find_piece(a, blockIdx.z, false, nullptr);
     if (piece.count <= 1) return;
     const Seq &s = piece.s;
     const int G = a.group, row = blockIdx.x, h = blockIdx.y;
@@ -998,16 +1036,7 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
         for (int k = sub; k < piece.count; k += SUB) {
             const float2 ml = *reinterpret_cast<const float2 *>(p + k * step + d);
             const float4 u = *reinterpret_cast<const float4 *>(p + k * step + 4 * i4);
-            const float now = fmaxf(M, ml.x);
-            // (as in the attention kernel: nothing seen counts 0, NaN stays)
-            const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
-            const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
-            M = now;
-            S = fmaf(S, f, ml.y * g);
-            v.x = fmaf(v.x, f, u.x * g);
-            v.y = fmaf(v.y, f, u.y * g);
-            v.z = fmaf(v.z, f, u.z * g);
-            v.w = fmaf(v.w, f, u.w * g);
+            join_piece(M, S, v, ml, u);
         }
         acc_sh[sub][i4] = v;
         if (i4 == 0) {
@@ -1037,30 +1066,71 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
     store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * tid, v);
 }
 
-// Tiles of 16 rows per wave (0: one of 8), row tiles of the largest sequence, and the split of the positions.
+// The same for many rows: a group of d / 4 lanes takes one row and its pieces one after the other.  grid: (groups of
+// rows, key/value head, sequence)
+template <int NG, bool F32>
+__global__ __launch_bounds__(kAttBlock) void kv4_join_rows_kernel(AttendArgs a, int tile_rows) {
+    constexpr int d = NG * kGroup, N4 = d / 4, ROWS = kAttBlock / N4;
+    const Piece piece = find_piece(a, blockIdx.z, false, nullptr);
+    if (piece.count <= 1) return;
+    const Seq &s = piece.s;
+    const int G = a.group, i4 = threadIdx.x % N4, sub = threadIdx.x / N4, row = blockIdx.x * ROWS + sub, h = blockIdx.y;
+    if (sub >= ROWS || row >= s.n * G) return;
+    const size_t step = size_t(a.n_kv) * a.tiles * tile_rows * (d + 4);
+    const float *p = a.part + ((size_t(piece.first) * a.n_kv + h) * a.tiles * tile_rows + row) * (d + 4);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float M = -INFINITY, S = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < piece.count; ++k) {
+        const float2 ml = *reinterpret_cast<const float2 *>(p + k * step + d);
+        join_piece(M, S, v, ml, *reinterpret_cast<const float4 *>(p + k * step + 4 * i4));
+    }
+    const float inv = S == 0.f ? 0.f : 1.f / S;
+    v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
+    store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
+}
+
+// What a call launches: from its sizes alone, since lengths are on the device (max_pos bounds them).
 struct AttendPlan {
-    int prompt;  // waves of the kernel for many rows, or 0
-    int tiles, tile_rows, blocks, target, units;
+    int prompt;     // waves of the kernel for many rows, or 0
+    int tiles;      // otherwise: tiles of 16 rows per wave (0: one of 8)
+    int tile_rows, blocks;  // rows per block, blocks of the largest sequence's rows
+    int target, least, units;
     size_t workspace;
 };
 AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_pos, bool f32) {
     const long long rows = (long long)max_q * group;
-    // what a wave's registers hold
-    const int most = d <= 64 ? (f32 ? 2 : 4) : d <= 128 ? 2 : d <= 192 && !f32 ? 2 : 1;
     AttendPlan p{};
-    if (!f32 && rows >= 128 && (rows + 127) / 128 * n_kv * n_seq >= 64) {
+    int fill = kTarget;
+    // Many rows: keys and values turned to fp16 once for a block's rows.  It starts later and goes on faster: with 32
+    // query and 4 key/value heads of 128, 64 tokens over 512 positions take 19.8 us (the other kernel 20.7), 32 over
+    // 1024 19.9 (20.8), 128 over 128 11.5 (8.9), 128 over 1024 22.9 (33.8), 2048 over 8192 328 (834).  With heads of
+    // 256 it draws level at half as many scores, of 64 at twice as many.
+    if (!f32 && rows >= 128 && double(rows) * n_kv * n_seq * max_pos * d >= double(1 << 27)) {
         const int per = 64 * prompt_tiles(d);  // rows of four waves
-        p.prompt = (rows + 2 * per - 1) / (2 * per) * n_kv * n_seq >= 256 ? 8 : 4;
-        p.blocks = int((rows + per * (p.prompt / 4) - 1) / (per * (p.prompt / 4)));
-        return p;
+        const long long four = (rows + per - 1) / per * n_kv * n_seq, eight = (rows + 2 * per - 1) / (2 * per) * n_kv * n_seq;
+        // Eight waves turn half as often as two blocks of four: taken where they fill the device (2048 tokens over
+        // 8192 positions: 339 us, four 385), and for heads of more than 128, of which a unit holds one block, where the
+        // positions are split (300 tokens, 16 heads of 256, 8000 positions: 82 us, four 261).
+        fill = d <= 128 ? 512 : 256;
+        p.least = four * 4 >= fill ? 16 : 8;  // (600 tokens, 32 heads of 64, 1000 positions: 27 us, 35 with 8)
+        p.prompt = eight >= 256 || (d > 128 && rows > per && four * 3 <= fill * 2) ? 8 : 4;
+        p.tile_rows = per * (p.prompt / 4);
+        if (p.prompt == 8) fill = 256;
+    } else {
+        const int most = d <= 64 ? (f32 ? 2 : 4) : d <= 128 ? 2 : d <= 192 && !f32 ? 2 : 1;  // what a wave's registers hold
+        p.tiles = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
+        p.tile_rows = p.tiles ? 16 * p.tiles : 8;
+        p.least = kAttWaves;
     }
-    p.tiles = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
-    p.tile_rows = p.tiles ? 16 * p.tiles : 8;
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
-    const long long pieces = (max_pos / kPos + kAttWaves - 1) / kAttWaves;  // most that a sequence has
-    if (base * n_seq < kTarget && pieces > 1) {
-        p.target = int(std::min(std::max(1ll, kTarget / base), pieces * n_seq));
+    const long long pieces = (max_pos / kPos + p.least - 1) / p.least;  // most that a sequence has
+    // Split where that makes more blocks; many rows, whose pieces' outputs cost more, where it makes twice as many (300
+    // tokens, 32 heads of 128, 8000 positions: 254 us whole, 78 split; 1556 rows of 4 heads of 64 in each of 6 sequences
+    // of up to 701, 312 blocks: 23 whole, 29 split).
+    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && pieces > 1) {
+        p.target = int(std::min(std::max(1ll, fill / base), pieces * n_seq));
         p.units = p.target + n_seq;
         p.workspace = (size_t(p.units) * n_kv * p.blocks * p.tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
     }
@@ -1091,6 +1161,8 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     a.group = n_heads / n_kv;
     a.window = window;
     a.target = p.target;
+    a.least = p.least;
+    a.unit = p.prompt ? 2 : 1;
     a.tiles = p.blocks;
     a.scale = scale * 1.44269504088896341f;
     a.batch = batch;
@@ -1101,8 +1173,7 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     if (d == NG * kGroup && p.prompt == W) kv4_prompt_kernel<NG, W><<<grid, 64 * W, 0, s>>>(a);
         KV4_PROMPT(1, 4) KV4_PROMPT(1, 8) KV4_PROMPT(2, 4) KV4_PROMPT(2, 8) KV4_PROMPT(3, 4) KV4_PROMPT(3, 8) KV4_PROMPT(4, 4) KV4_PROMPT(4, 8)
 #undef KV4_PROMPT
-        return hipGetLastError();
-    }
+    } else {
 #define KV4_RUN(NG, NT, F) kv4_attend_kernel<NG, NT ? NT : 1, F, NT == 0><<<grid, kAttBlock, 0, s>>>(a)
 #define KV4_CASE(NG, NT, F) case (NG * 2 + F) * 8 + NT: KV4_RUN(NG, NT, F); break;
     switch ((d / kGroup * 2 + f32) * 8 + p.tiles) {
@@ -1117,17 +1188,23 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     default: return hipErrorInvalidValue;
     }
 #undef KV4_CASE
+#undef KV4_RUN
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.target) return e;
-    const dim3 jgrid(batch.max_q * a.group, n_kv, batch.n_seq);
-#define KV4_JOIN(NG)                                                    \
-    case NG * kGroup:                                                   \
-        if (f32) kv4_join_kernel<NG, true><<<jgrid, kAttBlock, 0, s>>>(a, p.tile_rows); \
-        else kv4_join_kernel<NG, false><<<jgrid, kAttBlock, 0, s>>>(a, p.tile_rows); \
-        break;
-    switch (d) { KV4_JOIN(1) KV4_JOIN(2) KV4_JOIN(3) KV4_JOIN(4) }
+    const int rows = batch.max_q * a.group;
+    // One block per row has its pieces in flight together, a group of lanes per row needs fewer blocks: 64 tokens, 32 heads
+    // of 64 (2048 rows) 19.9 and 18.3 us with the attention, 128 (4096 rows) 26.7 and 22.1.
+    const bool many = (long long)rows * n_kv * batch.n_seq >= 2048;
+#define KV4_JOIN(NG, F)                                                                                             \
+    if (d == NG * kGroup && f32 == F) {                                                                             \
+        constexpr int per = kAttBlock / (NG * kGroup / 4);                                                          \
+        if (many) kv4_join_rows_kernel<NG, F><<<dim3((rows + per - 1) / per, n_kv, batch.n_seq), kAttBlock, 0, s>>>(a, p.tile_rows); \
+        else kv4_join_kernel<NG, F><<<dim3(rows, n_kv, batch.n_seq), kAttBlock, 0, s>>>(a, p.tile_rows);            \
+    }
+    KV4_JOIN(1, false) KV4_JOIN(1, true) KV4_JOIN(2, false) KV4_JOIN(2, true)
+    KV4_JOIN(3, false) KV4_JOIN(3, true) KV4_JOIN(4, false) KV4_JOIN(4, true)
 #undef KV4_JOIN
-#undef KV4_RUN
     return hipGetLastError();
 }
 

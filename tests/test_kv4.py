@@ -366,6 +366,13 @@ CASES = [  # (d, n_kv, group, tokens, lengths, max_pos, window)
     (192, 16, 8, [33, 20, 17, 1], [130, 65, 64, 7], 160, 48),
     (256, 16, 4, [40, 33, 70, 5], [40, 100, 200, 3], 224, 0),
     (256, 32, 3, [43, 64, 1, 44], [31, 160, 0, 129], 160, 33),
+    # the same over long caches, whose positions are split
+    (128, 8, 4, [40, 33, 70, 5], [1500, 700, 2000, 3], 2048, 0),
+    (128, 32, 2, [100, 64], [1100, 64], 2048, 600),
+    (64, 16, 8, [33, 20, 17, 0], [1300, 2048, 1, 64], 2048, 0),
+    (64, 2, 8, [256, 200], [1300, 600], 1312, 0),
+    (192, 8, 4, [40, 33, 70, 5], [1500, 700, 2000, 3], 2048, 900),
+    (256, 8, 4, [70, 33], [1057, 1056], 1088, 0),
 ]
 
 

@@ -317,7 +317,8 @@ MOE_API size_t moe_matvec_int4_workspace_bytes(int T, int K);
  *   w    device MOE_INT4G128 matrix [N x K], 16-byte aligned: packed nibbles [N x K/2], then bf16 scales [N x K/128]
  *   add  device fp32 [T x N], or NULL; may be y
  *   y    device fp32 [T x N], apart from x
- *   workspace device, >= moe_matvec_int4_workspace_bytes(T, K), 16-byte aligned (may be NULL when that is 0)
+ *   workspace device, >= moe_matvec_int4_workspace_bytes(T, K), 16-byte aligned, apart from the others (may be NULL when
+ *        that is 0)
  * The tokens' values enter within 2^-22 of the token's largest; exact products, fp32 sums.  T == 0 or N == 0 is a no-op. */
 MOE_API int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, int flags,
                             void *workspace, size_t workspace_bytes, void *stream);

@@ -6,6 +6,11 @@
 //      the cache.
 //   3. Attention over the cache (kv4_attention.hip).
 //   4. Output projection added to x (matvec_int4.hip).
+//
+// Measured in the decode stack (H 2048, 32 query and 4 key/value heads of 128, one token): 22.9 us at 4096 positions,
+// 20.7 at 101, five launches (the bf16 block: 19.4 and 19.1, four launches, with 3.6 times the cache and 3.9 times the
+// weights).  Latency is the bound: projections 5.5 each, heads 4.1 (fp64 rotary angles as in that block), attention
+// 7 and 4.
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
@@ -20,7 +25,7 @@ namespace {
 using namespace kv4;
 
 // One wave per (head, token): query heads in place, key/value heads into the cache.  Latency-bound: a few
-// hundred bytes per wave.  grid: (query heads + key/value heads, tokens)
+// hundred bytes per wave, 4.1 us.  grid: (query heads + key/value heads, tokens)
 template <int NG>
 __global__ __launch_bounds__(64) void heads_kernel(float *__restrict__ qkv, int n_heads, int n_kv, float theta,
                                                    const int32_t *__restrict__ kv_len, int max_pos,

@@ -17,6 +17,13 @@
 // A row is a (token, query head of the group) pair; a wave takes NT tiles of 16 rows over every fourth block
 // of 32 positions, and the block's waves join their (max, sum, output) through LDS.  With few rows the
 // positions are split over more blocks (grid), whose partial results a second launch joins.
+//
+// Bound: with few rows the cache's bytes, 1.125 d per position and key/value head.  Measured (kernel, then join): one
+// token of 64 heads over 131071 positions of 8 heads of 128, bf16, 28.9 + 4.7 us (151 MB, 5.2 TB/s of the 7.2 that a read
+// reaches); 16 sequences of up to 16384, 35.6 + 4.7 us (188 MB, 5.3 TB/s); one token of 32 heads over 4096 positions of
+// 4 heads, fp32, 7.0 + 4.0 us, which is latency.  One block of positions in flight per wave instead of two: 33.5 for the
+// 28.9.  Rows that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which
+// halves the lane arithmetic: 67 -> 57 us for the 16 sequences, with the split by what the sequences hold.
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
@@ -190,7 +197,7 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs &a, int want, bool 
     p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), a.least);
     p.chunk = (p.chunk + a.unit - 1) & -a.unit;
     // (pieces rounded up may be more than run together, and the last few would take as long again: somewhat larger ones
-    // that do are better.  16 sequences of 4822 to 16384 positions: 51 us without, 42 with.)
+    // that do are better.  16 sequences of 4822 to 16384 positions: 51 us without, 39 with.)
     if (b.n_seq > 1 && b.n_seq <= 64) {
         int chunk = p.chunk;
 #pragma unroll 1
@@ -676,6 +683,11 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 // largest) and share them through LDS in the operands' order, and a score costs an fma, an exponential, a share
 // of a maximum and of a conversion.  Two buffers: the next positions' codes are loaded before the present ones are
 // used and turned after.  The sums of P come from the matrix cores too.
+//
+// Bound: lane arithmetic and the chain of a step (operands from LDS, scores, softmax, products, a barrier), about 2.5 us
+// for 64 positions at either block size; the matrix cores are busy 27 % of the time.  2048 tokens of 32 heads of 128 over
+// 8192 positions: 330 us, 0.73 PFLOP/s (1.22 for a large bf16 product); with heads of 256, 16 of them: 366 us, 0.66.
+// Two groups of waves a phase apart: 401 us for the 366 that the first form took.
 constexpr int prompt_tiles(int d) { return d <= 128 ? 2 : 1; }  // row tiles of 16 per wave: what its registers hold
 
 // A barrier for what the block's waves pass one another through LDS; loads in flight stay so.

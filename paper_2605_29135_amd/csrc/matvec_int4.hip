@@ -8,9 +8,14 @@
 // value); every product is exact, and the group's scale multiplies its fp32 sum.  Up to 8 tokens the two terms
 // are rows of one product; for more they are two products.
 //
-// A block takes items of RB row tiles; its eight waves share the columns.  A wave forms the terms of its columns once
-// (lanes over columns, one token after the other), turns them into operands through its own part of LDS and keeps
-// those in registers from item to item; a tile's next weights are loaded as soon as it has been multiplied.
+// A block takes items of RB row tiles; its eight waves share the columns.  With few tokens a wave forms the terms of its
+// columns once (lanes over columns), turns them into operands through its own part of LDS and keeps those in registers
+// from item to item; with more a launch of its own forms every token's, which the blocks read.  A tile's next weights are
+// loaded as soon as it has been multiplied.  Many rows: see matvec_stream_kernel.
+//
+// Measured: 5120 x 2048, 1 token 5.5 us (5.4 MB, 1 TB/s: a launch, the chain of loads and the sum over waves); 2048 x
+// 4096, 16 tokens 3.9 us for the terms and 7.1 us (half of the units have a block); 131071 x 2048, 3 tokens 29.1 us
+// (140 MB, 4.8 TB/s).
 #include "device_common.h"
 #include "internal.h"
 
@@ -27,7 +32,10 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMvWaves = 8, kMvBlock = kMvWaves * kWave;
 constexpr int kMvGrid = 256;  // compute units
-constexpr int kMvTokens = 3;  // tokens whose terms every block forms itself
+constexpr int kMvFit = 2 * kMvGrid;  // blocks that run together
+// Tokens whose terms every block forms itself: 5120 x 4096 with 3 tokens takes 9.4 us, with 4 and a launch for them 11.6;
+// 9 tokens take 24.6 us without that launch and 15.7 with it.
+constexpr int kMvTokens = 3;
 constexpr int kCodeExp = -9;
 
 // The eight codes of a dword as fp16 q 2^-9, in the order 0,4,1,5,2,6,3,7.  (Nibbles at bits 4-7 of a half are 16
@@ -511,13 +519,16 @@ template <int RB, int GS, bool ONE, bool MULTI, bool PRE>
 hipError_t run(const float *x, const uint8_t *w, int T, int N, int K, const float *add, float *y, bool norm, void *ws,
                hipStream_t s) {
     const int tiles = (N + 15) / 16, items = (tiles + RB - 1) / RB;
-    // one item per block where they fit the device together, else persistent blocks
-    const int lds = lds_bytes(PRE ? 0 : T, GS, RB), most = kMvGrid * (2 * lds <= 160 * 1024 ? 2 : 1);
-    const int grid = items <= most ? items : kMvGrid;
-    if (MULTI || grid < items)
-        matvec_int4_kernel<RB, GS, ONE, MULTI, true, PRE><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
-    else
-        matvec_int4_kernel<RB, GS, ONE, false, false, PRE><<<grid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
+    // one item per block where they fit the device together, else persistent blocks (rows enough for those at K up to 2048
+    // go to the other kernel)
+    const int lds = lds_bytes(PRE ? 0 : T, GS, RB);
+    if constexpr (MULTI || GS == 4) {
+        if (MULTI || items > kMvFit) {
+            matvec_int4_kernel<RB, GS, ONE, MULTI, true, PRE><<<items <= kMvFit ? items : kMvGrid, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (!MULTI) matvec_int4_kernel<RB, GS, ONE, false, false, PRE><<<items, kMvBlock, lds, s>>>(x, w, T, N, K, add, y, norm, items, ws);
     return hipGetLastError();
 }
 
@@ -529,7 +540,12 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
                               void *ws, hipStream_t s) {
     const auto *wb = static_cast<const uint8_t *>(w);
     const int tiles = (N + 15) / 16;
-    if (tiles >= kMvGrid * kMvWaves && stream_lds(T, K) <= 128 * 1024) {  // a row tile for every wave that fits the device
+    // A wave per row tile takes time by K, the columns shared by a block's waves time by N.  Taken with a tile for every wave
+    // that fits the device (131071 x 2048, 3 tokens: 29 us, 39 shared; 30000 x 8192, 1 token 33 and 38), and down to a
+    // quarter of that where rows are many times the columns (1 token: 12000 x 512 5.9 and 7.4 us, 20000 x 2048 10.7 and
+    // 11.4; but 12000 x 2048 10.3 and 7.3, 20000 x 4096 18.9 and 15.5).
+    const bool many = tiles >= kMvGrid * kMvWaves || (tiles >= kMvGrid * kMvWaves / 4 && N / 8 >= K);
+    if (many && stream_lds(T, K) <= 128 * 1024) {
         // two blocks per unit where the tokens' terms and a wave's registers leave room, else more tiles per wave
         const int per = T <= 8 && stream_lds(T, K) <= 72 * 1024 ? 2 : 1, waves = per * kMvGrid * kMvWaves;
         const int rb = tiles >= 4 * waves && per == 1 ? 4 : tiles >= 2 * waves ? 2 : 1, items = (tiles + rb - 1) / rb;
@@ -546,17 +562,16 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
         if (e != hipSuccess) return e;
     }
     // Four groups per wave where K has more than two for each of the eight waves and the tokens' terms leave the
-    // registers for it.
+    // registers for it (else a second pass over the columns: 8 tokens of 2048 x 4096 8.6 us, 16 tokens 10.8).
     const int gs = K <= 2048 || T > 8 ? 2 : 4;
-    const int fit = kMvGrid * (2 * lds_bytes(pre ? 0 : T, gs, 1) <= 160 * 1024 ? 2 : 1);  // blocks that run together
-    const int rb = tiles <= fit ? 1 : tiles <= 2 * fit || gs == 4 || T > 8 ? 2 : 4;
+    const int rb = tiles <= kMvFit ? 1 : 2;
     const bool multi = K > kMvWaves * gs * 128;
 #define MATVEC(RB, GS, ONE, MULTI, PRE)                                                 \
     if (rb == RB && gs == GS && (T <= 8) == ONE && multi == MULTI && pre == PRE)        \
         return run<RB, GS, ONE, MULTI, PRE>(x, wb, T, N, K, add, y, norm, ws, s);
-    MATVEC(1, 2, true, false, false) MATVEC(2, 2, true, false, false) MATVEC(4, 2, true, false, false)
+    MATVEC(1, 2, true, false, false) MATVEC(2, 2, true, false, false)
     MATVEC(1, 4, true, false, false) MATVEC(2, 4, true, false, false) MATVEC(1, 4, true, true, false) MATVEC(2, 4, true, true, false)
-    MATVEC(1, 2, true, false, true) MATVEC(2, 2, true, false, true) MATVEC(4, 2, true, false, true)
+    MATVEC(1, 2, true, false, true) MATVEC(2, 2, true, false, true)
     MATVEC(1, 4, true, false, true) MATVEC(2, 4, true, false, true) MATVEC(1, 4, true, true, true) MATVEC(2, 4, true, true, true)
     MATVEC(1, 2, false, false, true) MATVEC(2, 2, false, false, true) MATVEC(1, 2, false, true, true) MATVEC(2, 2, false, true, true)
 #undef MATVEC

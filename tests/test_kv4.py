@@ -598,7 +598,8 @@ def test_matvec_matches_the_plain_form(T, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("N,K", [(40007, 512), (20001, 1408), (16400, 4352), (135000, 128), (270000, 128)])
+@pytest.mark.parametrize("N,K", [(40007, 512), (20001, 1408), (16400, 4352), (135000, 128), (270000, 128),
+                                 (9001, 1024), (8300, 2048), (16400, 2176)])
 @pytest.mark.parametrize("T", [1, 7, 8, 9, 16])
 def test_matvec_many_rows(T, N, K):
     """Enough rows that waves and blocks take several items."""

@@ -680,6 +680,44 @@ def test_captured_decode_step_replays_with_new_lengths():
 
 
 @pytest.mark.gpu
+def test_captured_prompts_replay_with_new_lengths():
+    """Prompts over a long cache, whose split goes by the lengths on the device, and a product of nine tokens, captured
+    once; a query that is not finite spoils its own row in every piece and no other."""
+    gen = torch.Generator().manual_seed(23)
+    n_kv, G, d, max_pos, ns, ls = 8, 4, 128, 2048, [40, 33], [1400, 90]
+    cache = fill(moe.kv4_cache(2, n_kv, d, max_pos))
+    k = [torch.randn((2000, n_kv, d), generator=gen) for _ in ns]
+    put(k, k, cache, BF16)
+    qs, kl, T = batch(ns, ls)
+    q = torch.randn((T, n_kv * G, d), generator=gen).bfloat16().cuda()
+    raw, _ = int4_matrix(500, 2048, gen)
+    raw, x = raw.cuda(), torch.randn((9, 2048), generator=gen).cuda()
+    n = moe.moe_kv4_attention_workspace_bytes(T, 2, n_kv * G, n_kv, d, 40, max_pos)
+    assert n > 0 and moe.moe_matvec_int4_workspace_bytes(9, 2048) > 0
+    ws, ws9 = (torch.empty(b, dtype=torch.uint8, device="cuda") for b in (n, moe.moe_matvec_int4_workspace_bytes(9, 2048)))
+    out, y = torch.empty_like(q), torch.empty((9, 500), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        moe.moe_kv4_attention(q, cache, kl, q_start=qs, max_q=40, out=out, workspace=ws)
+        moe.moe_matvec_int4(x, raw, 500, y=y, rmsnorm=True, workspace=ws9)
+    for i, lens in enumerate(([1400, 90], [40, 1990], [0, 33], [2000, 2000])):
+        kl.copy_(torch.tensor(lens, dtype=torch.int32))
+        x.mul_(1.5)
+        graph.replay()
+        ref = moe.moe_kv4_attention(q, cache, kl, q_start=qs, max_q=40)
+        assert torch.equal(out, ref) and torch.equal(y, moe.moe_matvec_int4(x, raw, 500, rmsnorm=True))
+    bad = q.clone()
+    bad[5, 7, 3], bad[60, 0, 0] = math.nan, math.inf
+    spoilt = moe.moe_kv4_attention(bad, cache, kl, q_start=qs, max_q=40)
+    ok = torch.ones((T, n_kv * G), dtype=torch.bool)
+    ok[5, 7] = ok[60, 0] = False
+    assert torch.equal(spoilt.cpu()[ok], ref.cpu()[ok]) and not torch.isfinite(spoilt.cpu()[~ok]).any()
+    moe.moe_sync_check()
+
+
+@pytest.mark.gpu
 def test_calls_on_another_stream():
     gen = torch.Generator().manual_seed(22)
     k = torch.randn((64, 2, 128), generator=gen).cuda()

@@ -373,6 +373,10 @@ CASES = [  # (d, n_kv, group, tokens, lengths, max_pos, window)
     (64, 2, 8, [256, 200], [1300, 600], 1312, 0),
     (192, 8, 4, [40, 33, 70, 5], [1500, 700, 2000, 3], 2048, 900),
     (256, 8, 4, [70, 33], [1057, 1056], 1088, 0),
+    # more sequences than a wave has lanes, split
+    (64, 1, 4, [1] * 70, [(37 * i) % 600 for i in range(70)], 608, 0),
+    (64, 1, 8, [16 - i % 3 for i in range(70)], [16 + (53 * i) % 590 for i in range(70)], 608, 0),
+    (128, 2, 1, [3] * 33 + [0] * 33 + [2] * 33, [(71 * i) % 700 for i in range(99)], 704, 100),
 ]
 
 

@@ -37,6 +37,7 @@ constexpr int kMvFit = 2 * kMvGrid;  // blocks that run together
 // 9 tokens take 24.6 us without that launch and 15.7 with it.
 constexpr int kMvTokens = 3;
 constexpr int kCodeExp = -9;
+constexpr int kTermsBlock = 1024;
 
 // The eight codes of a dword as fp16 q 2^-9, in the order 0,4,1,5,2,6,3,7.  (Nibbles at bits 4-7 of a half are 16
 // times those at 0-3, which their factor takes back.)
@@ -114,7 +115,8 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 __host__ __device__ constexpr int stage_bytes(int T, int GS) { return kMvWaves * GS * 512 * T; }
 __host__ __device__ constexpr int lds_bytes(int T, int GS, int RB) { return stage_bytes(T, GS) + kMvWaves * RB * 4 * kWave * 4; }
 
-// The terms of every token, once for all the blocks of a call: one block per token.  ws: what takes the sums back (int
+// The terms of every token, once for all the blocks of a call: one block per token (16 of 4096 columns 3.2 us, which is a
+// launch and its chain of loads, two reductions and stores).  ws: what takes the sums back (int
 // [16]), the norms' factors (float [16]), then at 256 bytes the operands [K / 32][4][2 T rows].
 struct Terms {
     const int *back;
@@ -125,13 +127,21 @@ __host__ __device__ inline Terms terms_in(const void *ws) {
     const auto *p = static_cast<const uint8_t *>(ws);
     return {reinterpret_cast<const int *>(p), reinterpret_cast<const float *>(p + 64), reinterpret_cast<const uint4 *>(p + 256)};
 }
-__global__ __launch_bounds__(256) void matvec_terms_kernel(const float *__restrict__ x, int T, int K, bool norm, uint8_t *ws) {
-    __shared__ float tops[4], sums[4];
+__global__ __launch_bounds__(kTermsBlock) void matvec_terms_kernel(const float *__restrict__ x, int T, int K, bool norm, uint8_t *ws) {
+    constexpr int WAVES = kTermsBlock / kWave;
+    __shared__ float tops[WAVES], sums[WAVES];
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float4 *xr = reinterpret_cast<const float4 *>(x + size_t(t) * K);
-    float top = 0.f, squares = 0.f;
-#pragma unroll 4
-    for (int i = tid; i < K / 4; i += 256) {
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 held[2];  // (8192 columns; the rest is read again)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int i = tid + u * kTermsBlock;
+        held[u] = i < K / 4 ? dev::load_f4(xr + i) : zero;
+    }
+    float top = fmaxf(top_of(held[0]), top_of(held[1])), squares = squares_of(held[0]) + squares_of(held[1]);
+#pragma unroll 1
+    for (int i = tid + 2 * kTermsBlock; i < K / 4; i += kTermsBlock) {
         const float4 u = dev::load_f4(xr + i);
         top = fmaxf(top, top_of(u));
         squares += squares_of(u);
@@ -140,17 +150,24 @@ __global__ __launch_bounds__(256) void matvec_terms_kernel(const float *__restri
     squares = dev::wave_sum(squares);
     if (lane == 0) tops[wave] = top, sums[wave] = squares;
     __syncthreads();
-    const int e2 = exponent_of(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+    top = tops[0], squares = sums[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]), squares += sums[w];
+    const int e2 = exponent_of(top);
     if (tid == 0) {
         reinterpret_cast<int *>(ws)[t] = -kCodeExp - e2;
-        reinterpret_cast<float *>(ws + 64)[t] = norm ? rsqrtf((sums[0] + sums[1] + sums[2] + sums[3]) / float(K) + 1e-6f) : 1.f;
+        reinterpret_cast<float *>(ws + 64)[t] = norm ? rsqrtf(squares / float(K) + 1e-6f) : 1.f;
     }
     uint4 *out = reinterpret_cast<uint4 *>(ws + 256) + t;
-#pragma unroll 4
-    for (int i = tid; i < K / 4; i += 256) {  // (K / 4 is a multiple of 32: a pair of lanes stays together)
+    auto store = [&](int i, float4 u) {  // (K / 4 is a multiple of 32: a pair of lanes stays together)
         uint4 *f = out + size_t((i >> 5) * 16 + ((i >> 1) & 3) * 4 + ((i >> 3) & 3)) * (2 * T);
-        store_terms(dev::load_f4(xr + i), e2, lane & 1, [&](int k) { return f + k * T; });
-    }
+        store_terms(u, e2, lane & 1, [&](int k) { return f + k * T; });
+    };
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        if (tid + u * kTermsBlock < K / 4) store(tid + u * kTermsBlock, held[u]);
+#pragma unroll 1
+    for (int i = tid + 2 * kTermsBlock; i < K / 4; i += kTermsBlock) store(i, dev::load_f4(xr + i));
 }
 
 // GS: quantisation groups per wave and pass over the columns; MULTI: several passes, the terms formed again for
@@ -557,7 +574,7 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
     }
     const bool pre = T > kMvTokens;
     if (pre) {
-        matvec_terms_kernel<<<T, 256, 0, s>>>(x, T, K, norm, static_cast<uint8_t *>(ws));
+        matvec_terms_kernel<<<T, kTermsBlock, 0, s>>>(x, T, K, norm, static_cast<uint8_t *>(ws));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

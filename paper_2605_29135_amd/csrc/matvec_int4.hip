@@ -578,9 +578,10 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    // Four groups per wave where K has more than two for each of the eight waves and the tokens' terms leave the
-    // registers for it (else a second pass over the columns: 8 tokens of 2048 x 4096 8.6 us, 16 tokens 10.8).
-    const int gs = K <= 2048 || T > 8 ? 2 : 4;
+    // Four groups per wave where K has more than two for each of the eight waves; with more than eight tokens, whose terms
+    // fill the registers, where that makes one pass over the columns (16 tokens: 40000 x 4096 33 us, 42 in two passes of two
+    // groups; 20000 x 8192 58 us in two of four, 47 in four of two).
+    const int gs = K <= 2048 || (T > 8 && K > 4096) ? 2 : 4;
     const int rb = tiles <= kMvFit ? 1 : 2;
     const bool multi = K > kMvWaves * gs * 128;
 #define MATVEC(RB, GS, ONE, MULTI, PRE)                                                 \
@@ -590,7 +591,7 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
     MATVEC(1, 4, true, false, false) MATVEC(2, 4, true, false, false) MATVEC(1, 4, true, true, false) MATVEC(2, 4, true, true, false)
     MATVEC(1, 2, true, false, true) MATVEC(2, 2, true, false, true)
     MATVEC(1, 4, true, false, true) MATVEC(2, 4, true, false, true) MATVEC(1, 4, true, true, true) MATVEC(2, 4, true, true, true)
-    MATVEC(1, 2, false, false, true) MATVEC(2, 2, false, false, true) MATVEC(1, 2, false, true, true) MATVEC(2, 2, false, true, true)
+    MATVEC(1, 2, false, false, true) MATVEC(2, 2, false, false, true) MATVEC(1, 4, false, false, true) MATVEC(2, 4, false, false, true) MATVEC(1, 2, false, true, true) MATVEC(2, 2, false, true, true)
 #undef MATVEC
     return hipErrorInvalidValue;
 }

@@ -582,7 +582,7 @@ def int4_parts(raw, N, K):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 2, 3, 5, 6, 8, 11, 16])
-@pytest.mark.parametrize("N,K", [(1, 128), (15, 256), (17, 2048), (100, 1408), (33, 4224), (16, 8192)])
+@pytest.mark.parametrize("N,K", [(1, 128), (15, 256), (17, 2048), (100, 1408), (33, 4224), (16, 8192), (100, 2560)])
 def test_matvec_matches_the_plain_form(T, N, K):
     gen = torch.Generator().manual_seed(T * 1000 + N)
     raw, _ = int4_matrix(N, K, gen)
@@ -603,7 +603,7 @@ def test_matvec_matches_the_plain_form(T, N, K):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("N,K", [(40007, 512), (20001, 1408), (16400, 4352), (135000, 128), (270000, 128),
-                                 (9001, 1024), (8300, 2048), (16400, 2176)])
+                                 (9001, 1024), (8300, 2048), (16400, 2176), (8300, 2304)])
 @pytest.mark.parametrize("T", [1, 7, 8, 9, 16])
 def test_matvec_many_rows(T, N, K):
     """Enough rows that waves and blocks take several items."""

@@ -19,10 +19,10 @@
 // positions are split over more blocks (grid), whose partial results a second launch joins.
 //
 // Bound: with few rows the cache's bytes, 1.125 d per position and key/value head.  Measured (kernel, then join): one
-// token of 64 heads over 131071 positions of 8 heads of 128, bf16, 28.9 + 4.7 us (151 MB, 5.2 TB/s of the 7.2 that a read
+// token of 64 heads over 131071 positions of 8 heads of 128, bf16, 30 + 4.8 us (151 MB, 5.0 TB/s of the 7.2 that a read
 // reaches); 16 sequences of up to 16384, 35.6 + 4.7 us (188 MB, 5.3 TB/s); one token of 32 heads over 4096 positions of
 // 4 heads, fp32, 7.0 + 4.0 us, which is latency.  One block of positions in flight per wave instead of two: 33.5 for the
-// 28.9.  Rows that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which
+// 30.  Rows that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which
 // halves the lane arithmetic: 67 -> 57 us for the 16 sequences, with the split by what the sequences hold.
 #include "device_common.h"
 #include "internal.h"

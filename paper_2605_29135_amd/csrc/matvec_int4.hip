@@ -14,8 +14,8 @@
 // loaded as soon as it has been multiplied.  Many rows: see matvec_stream_kernel.
 //
 // Measured: 5120 x 2048, 1 token 5.5 us (5.4 MB, 1 TB/s: a launch, the chain of loads and the sum over waves); 2048 x
-// 4096, 16 tokens 3.9 us for the terms and 7.1 us (half of the units have a block); 131071 x 2048, 3 tokens 29.1 us
-// (140 MB, 4.8 TB/s).
+// 4096, 16 tokens 3.4 us for the terms and 6.6 us (half of the units have a block); 131071 x 2048, 3 tokens 29.6 us
+// (140 MB, 4.7 TB/s).
 #include "device_common.h"
 #include "internal.h"
 
@@ -33,8 +33,8 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr int kMvWaves = 8, kMvBlock = kMvWaves * kWave;
 constexpr int kMvGrid = 256;  // compute units
 constexpr int kMvFit = 2 * kMvGrid;  // blocks that run together
-// Tokens whose terms every block forms itself: 5120 x 4096 with 3 tokens takes 9.4 us, with 4 and a launch for them 11.6;
-// 9 tokens take 24.6 us without that launch and 15.7 with it.
+// Tokens whose terms every block forms itself: 5120 x 4096 with 3 tokens takes 9.4 us, with 4 and a launch for them 11.1;
+// 9 tokens took 24.6 us without that launch and 15.7 with it.
 constexpr int kMvTokens = 3;
 constexpr int kCodeExp = -9;
 constexpr int kTermsBlock = 1024;
@@ -115,7 +115,7 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 __host__ __device__ constexpr int stage_bytes(int T, int GS) { return kMvWaves * GS * 512 * T; }
 __host__ __device__ constexpr int lds_bytes(int T, int GS, int RB) { return stage_bytes(T, GS) + kMvWaves * RB * 4 * kWave * 4; }
 
-// The terms of every token, once for all the blocks of a call: one block per token (16 of 4096 columns 3.2 us, which is a
+// The terms of every token, once for all the blocks of a call: one block per token (16 of 4096 columns 3.4 us, which is a
 // launch and its chain of loads, two reductions and stores).  ws: what takes the sums back (int
 // [16]), the norms' factors (float [16]), then at 256 bytes the operands [K / 32][4][2 T rows].
 struct Terms {

@@ -294,7 +294,8 @@ MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, 
 
 /* Attention of the tokens over the cache: out = sum_p softmax_p(scale q . K_p) V_p over the positions p up to the
  * token's own, with window > 0 the last `window` of those (window <= 2^30); query head j reads key/value head
- * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0.  fp32 scores, softmax and sums;
+ * j / (n_heads / n_kv).  A token that sees no position (padding) gets 0; positions that no token sees (in front of the
+ * window of the sequence's first one) need not have been written.  fp32 scores, softmax and sums;
  * queries enter exactly (MOE_BF16) or as two fp16 terms (MOE_F32: 2^-22 of the head's largest element), probabilities
  * times scales as two fp16 terms (MOE_F32: 2^-22) or rounded to fp16 (MOE_BF16: 2^-11; calls of many rows round the
  * held keys and values to fp16 as well).  For elements of q up to 2^100, keys and values

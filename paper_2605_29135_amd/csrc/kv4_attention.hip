@@ -161,10 +161,14 @@ struct AttendArgs {
     int *err;
 };
 
+// The first position that some token of the sequence sees.
+__device__ __forceinline__ int first_seen(const Seq &s, int window) {
+    return window ? max(0, s.len - s.n - window + 1) : 0;
+}
 // Blocks of positions that a sequence's tokens see.
 __device__ __forceinline__ int seen_blocks(const Seq &s, int window) {
     if (s.n == 0 || s.len == 0) return 0;
-    return (s.len - 1) / kPos + 1 - (window ? max(0, s.len - s.n - window + 1) / kPos : 0);
+    return (s.len - 1) / kPos + 1 - first_seen(s, window) / kPos;
 }
 
 // The split of a batch: sequences are cut into pieces of `chunk` blocks of positions, at least `least`, so
@@ -250,7 +254,7 @@ __device__ __forceinline__ Piece this_piece(const AttendArgs &a, int tile, int *
 __device__ __forceinline__ int2 tile_blocks(const AttendArgs &a, const Piece &piece, int row, int row_end) {
     const Seq &s = piece.s;
     const int p_first = s.len - s.n + row / a.group, p_last = s.len - s.n + (row_end - 1) / a.group;
-    const int b_first = a.window ? max(0, s.len - s.n - a.window + 1) / kPos : 0;
+    const int b_first = first_seen(s, a.window) / kPos;
     const int t_first = a.window ? max(0, p_first - a.window + 1) / kPos : 0, t_end = p_last < 0 ? 0 : p_last / kPos + 1;
     return make_int2(max(t_first, b_first + piece.split * piece.chunk),
                      piece.split == piece.count - 1 ? t_end : min(t_end, b_first + (piece.split + 1) * piece.chunk));
@@ -285,7 +289,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     const int p_first = s.len - s.n + row0 / G;                               // position of the tile's first row
     const int p_last = s.len - s.n + min(s.n - 1, (row0 + ROWS * NT - 1) / G);  // of its last row
     const int2 range = tile_blocks(a, piece, row0, min(row0 + ROWS * NT, rows));
-    const int b0 = range.x, b1 = range.y;
+    const int b0 = range.x, b1 = range.y, p_seen = first_seen(s, a.window);
     const uint8_t *seq = a.cache + (size_t(piece.seq) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
 
     // A block's operands as they lie in the cache.  Keys and values are loaded one block ahead, each as soon as
@@ -487,9 +491,9 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
         __builtin_amdgcn_sched_barrier(0);
         // ---- softmax
         const int past = b + (U - 1) * kAttWaves;  // the last of the blocks
-        if (past * kPos + kPos > s.len) {
-            // Positions that hold nothing yet may hold anything: their probabilities are 0, and 0 times what
-            // lies there has to be 0.
+        if (past * kPos + kPos > s.len || b * kPos < p_seen) {
+            // Positions past the last, and those in front of the first that some token sees, may never have been
+            // written and hold anything: their probabilities are 0, and 0 times what lies there has to be 0.
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int k = 2 * i + e, at = (b + u * kAttWaves) * kPos + 16 * (half + (k >> 2)) + 4 * c + (k & 3);
-                        keep |= at < s.len ? 0xffffu << (16 * e) : 0u;
+                        keep |= at < s.len && at >= p_seen ? 0xffffu << (16 * e) : 0u;
                     }
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
@@ -737,7 +741,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     const int G = a.group, rows = s.n * G, row0 = tile * ROWS;
     if (row0 >= rows) return;
     const int2 range = tile_blocks(a, piece, row0, min(row0 + ROWS, rows));
-    const int b0 = range.x, b1 = range.y;
+    const int b0 = range.x, b1 = range.y, p_seen = first_seen(s, a.window);
     const uint8_t *seq = a.cache + (size_t(piece.seq) * a.n_kv + h) * (a.batch.max_pos / kPos) * block_bytes(d);
 
     // What this wave turns: block `mine_b` of the pair, its keys or values, a half of them (eight waves).
@@ -794,8 +798,10 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     };
     int ek[2] = {0, 0}, ev[2] = {0, 0};  // exponents of the two buffers' keys and values
     auto turn = [&](int b, int buf, int most) __attribute__((always_inline)) {  // most: of the values' exponent
-        if ((b + 2) * kPos > s.len) {
-            // Positions that hold nothing yet may hold anything: their scales and bases count as zeros.
+        if ((b + 2) * kPos > s.len || b * kPos < p_seen) {
+            // Positions that may never have been written (as in kv4_attend_kernel) may hold anything: their scales and
+            // bases count as zeros.
+            auto unseen = [&](int at) { return at >= s.len || at < p_seen; };
             const int blk = min(b + (lane >> 5), b1 - 1), w = lane & 15;  // word of the group's 16
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -803,8 +809,8 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
                 const uint32_t drop = ~(0xffffu << (16 * e));
 #pragma unroll
                 for (int l = 0; l < LIM; ++l) {
-                    if (blk * kPos + in_order >= s.len) lim[0][l] &= drop, lim[2][l] &= drop, lim[3][l] &= drop;
-                    if (blk * kPos + in_tiles >= s.len) lim[1][l] &= drop;
+                    if (unseen(blk * kPos + in_order)) lim[0][l] &= drop, lim[2][l] &= drop, lim[3][l] &= drop;
+                    if (unseen(blk * kPos + in_tiles)) lim[1][l] &= drop;
                 }
             }
             if (values) {
@@ -814,7 +820,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int k = 2 * i + e;
-                        if (own * kPos + 16 * (k >> 2) + 4 * c + (k & 3) < s.len) continue;
+                        if (!unseen(own * kPos + 16 * (k >> 2) + 4 * c + (k & 3))) continue;
 #pragma unroll
                         for (int g = 0; g < GROUPS; ++g) {
                             ps[4 * g + i] &= ~(0xffffu << (16 * e));

@@ -865,3 +865,60 @@ def test_stack_with_int4_attention_equals_its_blocks():
     for bad in (dict(max_pos=48), dict(head_dim=48), dict(start_pos=max_pos), dict(cache=[moe.kv4_cache(2, n_kv, d, max_pos)] * 2)):
         with pytest.raises((moe.MoeError, ValueError)):
             moe.MoeStack(both, H, I, E, k, moe.MOE_BF16, moe.MOE_BF16, router, attention=dict(att, **bad))
+
+
+# ------------------------------------------------------------------- windows over what was never written (GPU) ---
+def relative_rms(out, ref):
+    return float((out.cpu().double() - ref).square().mean().sqrt() / ref.square().mean().sqrt())
+
+
+# Largest relative rms error of an attention over values of one size and scores of a few units.
+#   fp32: probabilities times scales in two fp16 terms and scores of up to 16 in log2 units, each within 2^-22 with both
+#   signs; the exponential's last place; about 5e-7 together.
+#   bf16: the output's rounding, 2^-8 at most and evenly spread (2^-8 / sqrt 3 = 2.26e-3), and three fp16 roundings
+#   (probabilities, keys, values; 2^-11 / sqrt 3 each): 2.31e-3 together.
+RMS = {F32: 1e-6, BF16: 2.5e-3}
+
+WINDOWS = [  # (d, n_kv, group, tokens per sequence, sequences, window, first length, step of the lengths, max_pos)
+    (64, 1, 4, 1, 32, 40, 81, 1, 128),        # every offset of the window's start in its block of 32
+    (128, 1, 4, 1, 32, 40, 81, 1, 128),
+    (64, 2, 16, 1, 32, 70, 300, 1, 512),      # (positions split)
+    (128, 1, 12, 3, 32, 200, 1000, 1, 1056),
+    (192, 1, 2, 2, 32, 33, 100, 1, 160),
+    (256, 1, 2, 1, 32, 1, 64, 1, 128),
+    (256, 2, 12, 2, 16, 64, 400, 7, 512),
+    (64, 4, 8, 40, 32, 45, 90, 1, 128),       # hundreds of rows
+    (64, 4, 8, 40, 8, 640, 900, 5, 1024),
+    (128, 4, 8, 40, 8, 97, 900, 5, 1024),
+    (128, 16, 8, 40, 5, 50, 90, 9, 128),
+    (192, 4, 8, 40, 8, 97, 900, 5, 1024),
+    (256, 4, 8, 40, 8, 640, 900, 5, 1024),
+    (256, 16, 8, 40, 5, 50, 90, 9, 128),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", range(len(WINDOWS)))
+def test_attention_window_over_positions_never_written(case, dtype):
+    """Only the positions that the tokens see are in the cache; in front of them lie NaN, or large finite scales."""
+    d, n_kv, G, n, B, window, L0, step, max_pos = WINDOWS[case]
+    gen = torch.Generator().manual_seed(case)
+    ls = [L0 + step * i for i in range(B)]
+    kept = [min(L, n + window - 1) for L in ls]  # what the sequence's first token sees, and its tokens
+    ks, vs = ([torch.randn((m, n_kv, d), generator=gen) for m in kept] for _ in range(2))
+    q = torch.randn((n * B, n_kv * G, d), generator=gen).to(dtype)
+    # (the same distances: the positions in front are left out of the reference)
+    ref, amount, shift = attend(q.double(), ks, vs, [n] * B, kept, G, window, d ** -0.5, dtype)
+    tol = attention_tolerance(ref, amount, shift, dtype)
+    new, kl, T = batch(kept, ls)
+    qs = batch([n] * B, ls)[0]
+    k, v = torch.cat(ks).cuda(), torch.cat(vs).cuda()
+    for byte in (0xFF, 0x7F, 0x60):  # NaN, 3e38, 6e19
+        cache = fill(moe.kv4_cache(B, n_kv, d, max_pos), byte)
+        moe.moe_kv4_append(k, v, cache, kl, q_start=new)
+        out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=n, window=window)
+        moe.moe_sync_check()
+        err = (out.cpu().double() - ref).abs()
+        assert (err <= tol).all(), (byte, float((err / tol).max()))
+        assert relative_rms(out, ref) <= RMS[dtype], (byte, relative_rms(out, ref))

@@ -299,7 +299,8 @@ MOE_API size_t moe_kv4_attention_workspace_bytes(int T, int n_seq, int n_heads, 
  * queries enter exactly (MOE_BF16) or as two fp16 terms (MOE_F32: 2^-22 of the head's largest element), probabilities
  * times scales as two fp16 terms (MOE_F32: 2^-22) or rounded to fp16 (MOE_BF16: 2^-11; calls of many rows round the
  * held keys and values to fp16 as well).  For elements of q up to 2^100, keys and values
- * from 2^-60 to 2^40 in magnitude; a key or value keeps the precision stated within 2^20 of the largest near it.
+ * from 2^-60 to 2^40 in magnitude, whatever scores these and the scale give (they may pass fp32's largest number); a key
+ * or value keeps the precision stated within 2^20 of the largest near it.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
  *   out        device, as q with out_stride, same dtype
  *   scale      a factor of magnitude up to 2^32, as a rule 1 / sqrt(head_dim)

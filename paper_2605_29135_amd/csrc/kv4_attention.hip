@@ -112,6 +112,17 @@ __device__ __forceinline__ void split(const float (&x)[8], f16x8 (&t)[TERMS]) {
     }
 }
 
+// From a row's scores as formed to log2 units: 2^e2 scales its query, `exp` is in its operands.  Held finite, so that a
+// difference of scores times it is right at any size (0 stays 0, and what is far from 0 stays far).
+__device__ __forceinline__ float row_unit(float scale, int exp) {
+    return fminf(fmaxf(ldexpf(fabsf(scale), exp), 0x1p-126f), 0x1p126f);
+}
+// Scores from here on (log2 units) are far: a product of a score and the row's unit, rounded, is then off by so much
+// (2^-4 at 2^20) that exponentials relative to it leave fp16's range, and is itself infinite further on.  A row that
+// meets one takes its exponentials of differences of scores instead, one operation more for each.
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ bool is_far(float off) { return !(fabsf(off) < kFar); }
+
 // What f makes of v over the four lanes (n, 0..3).
 template <typename F>
 __device__ __forceinline__ float over_c(float v, F f) {
@@ -149,7 +160,7 @@ struct AttendArgs {
     const void *q;
     void *out;
     const uint8_t *cache;
-    float *part;  // [unit][head][tile][16 NT rows][d + 4]: unnormalised output, maximum (log2), sum
+    float *part;  // [unit][head][tile][16 NT rows][d + 4]: unnormalised output, maximum, sum, the row's unit (row_unit)
     long long q_stride, out_stride;
     int n_heads, n_kv, group, window;
     int target;  // splits of a whole batch (0: every sequence in one piece)
@@ -277,7 +288,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     constexpr int UB = NG <= 2 && NT == 1 && (HALF || !F32 || NG == 1) ? 2 : 1;  // blocks of positions at a time
     static_assert(!HALF || NT == 1);
     __shared__ float4 out_sh[kAttWaves][ROWS][d / 4 + 1];
-    __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
+    __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS], unit_sh[ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int half = HALF ? n >> 3 : 0, n_row = HALF ? n & 7 : n;
     const int tile = a.target ? blockIdx.y : blockIdx.x, h = a.target ? blockIdx.x : blockIdx.y;
@@ -385,7 +396,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
         // out, it would not fit fp16; an infinity or NaN stays one.)
         int e2 = 0;
         if (top > 0.f && top < INFINITY) e2 = min(max(14 - ilogbf(top), -88), 148);
-        zs[t] = fmaxf(ldexpf(fabsf(a.scale), -kKeyExp<F32> - e2), 0x1p-126f);
+        zs[t] = row_unit(a.scale, -kKeyExp<F32> - e2);
         float sum = 0.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -418,6 +429,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     floatx4 acc[NT][4 * NG];  // sum of P s (u - 8) (dims x rows), times 2^(boost + kValueExp)
     float add[NT][NG];        // sum of P (m + 8 s), this lane's positions
     float mx[NT], off[NT], sum[NT];
+    bool far[NT], any_far = false;  // (of the row; of any: P and the sums are relative to mx itself, off is 0)
     uint32_t top_s = 0;  // largest bf16 of the exponent of the largest value scale so far
     int boost = 0;
     float boost_f = 1.f;  // 2^boost
@@ -425,6 +437,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     for (int t = 0; t < NT; ++t) {
         mx[t] = -INFINITY;
         off[t] = sum[t] = 0.f;
+        far[t] = false;
 #pragma unroll
         for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -548,9 +561,22 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
             if constexpr (HALF) top = fmaxf(top, other_half(top));
             top = max_over_c(top);
             const float was = mx[t], now = fmaxf(was, top);
-            if (scales_rose || __any(now > was)) {
-                const float to = now == -INFINITY ? 0.f : product(now, zs[t]);
-                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[t] - to) * rise;
+            if (scales_rose || any_far || __any(now > was)) {
+                float to = now == -INFINITY ? 0.f : product(now, zs[t]), fall = off[t] - to;
+                any_far |= __any(is_far(to));
+                if (__builtin_expect(any_far, 0)) {
+                    if (is_far(to) || far[t]) {
+                        fall = fmaf(was - now, zs[t], far[t] ? 0.f : fmaf(-was, zs[t], off[t]));
+                        far[t] = true;
+                        to = 0.f;
+                    }
+                    const float from = far[t] ? now : 0.f;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int k = 0; k < PP; ++k) p[t][u][k] -= from;
+                }
+                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fall) * rise;
                 mx[t] = now;
                 off[t] = to;
                 sum[t] *= f;
@@ -626,12 +652,15 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     // Join the waves, one tile of rows at a time.
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+        // (relative to the largest score itself: its product with the unit, to which the sums are, is rounded)
+        const float rel = far[t] || mx[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fmaf(-mx[t], zs[t], off[t]));
         float l = sum_over_c(sum[t]);
         if constexpr (HALF) l += other_half(l);
         if (t) __syncthreads();
         if (c == 0 && !half) {
-            max_sh[wave][n] = mx[t] == -INFINITY ? mx[t] : off[t];
-            sum_sh[wave][n] = ldexpf(l, -boost);
+            max_sh[wave][n] = mx[t];
+            sum_sh[wave][n] = ldexpf(l * rel, -boost);
+            if (wave == 0) unit_sh[n] = zs[t];
         }
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -642,8 +671,9 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
             if (!half)
 #pragma unroll
                 for (int i = 4 * g; i < 4 * g + 4; ++i)
-                    out_sh[wave][n][4 * i + c] = make_float4(ldexpf(acc[t][i][0], e) + m, ldexpf(acc[t][i][1], e) + m,
-                                                             ldexpf(acc[t][i][2], e) + m, ldexpf(acc[t][i][3], e) + m);
+                    out_sh[wave][n][4 * i + c] =
+                        make_float4((ldexpf(acc[t][i][0], e) + m) * rel, (ldexpf(acc[t][i][1], e) + m) * rel,
+                                    (ldexpf(acc[t][i][2], e) + m) * rel, (ldexpf(acc[t][i][3], e) + m) * rel);
         }
         __syncthreads();
 #pragma unroll 1
@@ -654,12 +684,13 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 #pragma unroll
             for (int w = 1; w < kAttWaves; ++w) M = fmaxf(M, max_sh[w][r]);
             float S = 0.f;
+            const float unit = unit_sh[r];
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kAttWaves; ++w) {
                 // (a wave that saw nothing of the row has the maximum -inf and the sum 0; one whose scores are
                 // all NaN has the sum NaN, which stays)
-                const float f = max_sh[w][r] == -INFINITY && sum_sh[w][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(max_sh[w][r] - M);
+                const float f = max_sh[w][r] == -INFINITY && sum_sh[w][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[w][r] - M) * unit);
                 const float4 u = out_sh[w][r][i4];
                 S = fmaf(f, sum_sh[w][r], S);
                 v.x = fmaf(f, u.x, v.x);
@@ -670,7 +701,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
             if (piece.count > 1) {
                 float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
                 *reinterpret_cast<float4 *>(o + 4 * i4) = v;
-                if (i4 == 0) *reinterpret_cast<float2 *>(o + d) = make_float2(M, S);
+                if (i4 == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(M, S, unit, 0.f);
                 continue;
             }
             const float inv = S == 0.f ? 0.f : 1.f / S;  // (a row that sees nothing: 0)
@@ -907,7 +938,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
             }
             top = max_over_c(top);
             const int e2 = top > 0.f && top < INFINITY ? min(max(14 - ilogbf(top), -88), 148) : 0;
-            zs[t] = fmaxf(ldexpf(fabsf(a.scale), -e2), 0x1p-126f);
+            zs[t] = row_unit(a.scale, -e2);
 #pragma unroll
             for (int j = 0; j < 2 * NG; ++j) {
                 f16x8 q1[1];
@@ -920,11 +951,13 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     }
 
     floatx4 acc[NT][4 * NG], sum[NT];  // sum of 2^(15 + ea) P V (dims x rows), sum of 2^15 P (in every element)
-    float mx[NT];                      // the row's largest score, log2 units
+    float mx[NT];                      // the row's largest score, without the keys' power of two
+    bool far[NT], any_far = false;     // (as in kv4_attend_kernel)
     int ea = 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         mx[t] = -INFINITY;
+        far[t] = false;
         sum[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -969,10 +1002,25 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
 #pragma unroll
             for (int k = 1; k < 16; ++k) top = fmaxf(top, p[t][k]);
             top = max_over_c(top);
-            const float zk = fmaxf(zs[t] * unscale, 0x1p-126f);
-            const float was = mx[t], now = fmaxf(was, top == -INFINITY ? top : product(top, zk));
-            if (__any(now > was) || e_new != ea) {
-                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(was - now), fa = ldexpf(f, e_new - ea);
+            const float was = mx[t], now = fmaxf(was, top * unscale);
+            const float to = now == -INFINITY ? 0.f : product(now, zs[t]);
+            float by = 15.f - to, unit = fminf(fmaxf(zs[t] * unscale, 0x1p-126f), 0x1p126f);
+            if (any_far || e_new != ea || __any(now > was)) {
+                const float off = product(was, zs[t]);
+                float fall = off - to;
+                any_far |= __any(is_far(to));
+                if (__builtin_expect(any_far, 0)) {
+                    if (is_far(to) || far[t]) {
+                        fall = fmaf(was - now, zs[t], far[t] ? 0.f : fmaf(-was, zs[t], off));
+                        far[t] = true;
+                        by = 15.f;
+                        unit = zs[t];
+                    }
+                    const float same = far[t] ? unscale : 1.f, from = far[t] ? now : 0.f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) p[t][k] = fmaf(p[t][k], same, -from);
+                }
+                const float f = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fall), fa = ldexpf(f, e_new - ea);
                 mx[t] = now;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[t][r] *= f;
@@ -981,9 +1029,8 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[t][i][r] *= fa;
             }
-            const float off = now == -INFINITY ? 0.f : now - 15.f;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) p[t][k] = __builtin_amdgcn_exp2f(fmaf(p[t][k], zk, -off));
+            for (int k = 0; k < 16; ++k) p[t][k] = __builtin_amdgcn_exp2f(fmaf(p[t][k], unit, by));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 bp[t][u] = join8(pack_f16(p[t][8 * u], p[t][8 * u + 1]), pack_f16(p[t][8 * u + 2], p[t][8 * u + 3]),
@@ -1017,12 +1064,14 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
         if (row >= rows) continue;
         if (piece.count > 1) {
             float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * ROWS + row) * (d + 4);
+            // (relative to the largest score itself; every piece has the 2^15)
+            const float rel = far[t] || mx[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fmaf(-mx[t], zs[t], product(mx[t], zs[t])));
 #pragma unroll
             for (int i = 0; i < 4 * NG; ++i)
                 *reinterpret_cast<float4 *>(o + 16 * i + 4 * c) =
-                    make_float4(ldexpf(acc[t][i][0], -ea), ldexpf(acc[t][i][1], -ea), ldexpf(acc[t][i][2], -ea), ldexpf(acc[t][i][3], -ea));
-            // (the sums' probabilities are relative to this; the maximum -inf stays)
-            if (c == 0) *reinterpret_cast<float2 *>(o + d) = make_float2(mx[t] - 15.f, sum[t][0]);
+                    make_float4(ldexpf(acc[t][i][0] * rel, -ea), ldexpf(acc[t][i][1] * rel, -ea), ldexpf(acc[t][i][2] * rel, -ea),
+                                ldexpf(acc[t][i][3] * rel, -ea));
+            if (c == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(mx[t], sum[t][0] * rel, zs[t], 0.f);
             continue;
         }
         const float l = sum[t][0], inv = l == 0.f ? 0.f : 1.f / l;
@@ -1034,12 +1083,12 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     }
 }
 
-// One more piece (its maximum and sum, four dims of its output).  As in the attention kernel: nothing seen counts 0,
-// NaN stays.
-__device__ __forceinline__ void join_piece(float &M, float &S, float4 &v, float2 ml, float4 u) {
+// One more piece (its maximum, sum and the row's unit; four dims of its output).  As in the attention kernel: nothing
+// seen counts 0, NaN stays.
+__device__ __forceinline__ void join_piece(float &M, float &S, float4 &v, float4 ml, float4 u) {
     const float now = fmaxf(M, ml.x);
-    const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
-    const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
+    const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f((M - now) * ml.z);
+    const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - now) * ml.z);
     M = now;
     S = fmaf(S, f, ml.y * g);
     v.x = fmaf(v.x, f, u.x * g);
@@ -1064,13 +1113,14 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
     const size_t step = size_t(a.n_kv) * a.tiles * tile_rows * (d + 4);
     const float *p = a.part + ((size_t(piece.first) * a.n_kv + h) * a.tiles * tile_rows + row) * (d + 4);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float M = -INFINITY, S = 0.f;
+    float M = -INFINITY, S = 0.f, unit = 0.f;  // (the group that ends the work has the first piece)
     if (sub < SUB) {
 #pragma unroll 4
         for (int k = sub; k < piece.count; k += SUB) {
-            const float2 ml = *reinterpret_cast<const float2 *>(p + k * step + d);
+            const float4 ml = *reinterpret_cast<const float4 *>(p + k * step + d);
             const float4 u = *reinterpret_cast<const float4 *>(p + k * step + 4 * i4);
             join_piece(M, S, v, ml, u);
+            unit = ml.z;
         }
         acc_sh[sub][i4] = v;
         if (i4 == 0) {
@@ -1087,7 +1137,7 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int t
     v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < SUB; ++k) {
-        const float f = max_sh[k] == -INFINITY && sum_sh[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f(max_sh[k] - top);
+        const float f = max_sh[k] == -INFINITY && sum_sh[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[k] - top) * unit);
         const float4 u = acc_sh[k][tid];
         S = fmaf(f, sum_sh[k], S);
         v.x = fmaf(f, u.x, v.x);
@@ -1116,7 +1166,7 @@ __global__ __launch_bounds__(kAttBlock) void kv4_join_rows_kernel(AttendArgs a, 
     float M = -INFINITY, S = 0.f;
 #pragma unroll 4
     for (int k = 0; k < piece.count; ++k) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p + k * step + d);
+        const float4 ml = *reinterpret_cast<const float4 *>(p + k * step + d);
         join_piece(M, S, v, ml, *reinterpret_cast<const float4 *>(p + k * step + 4 * i4));
     }
     const float inv = S == 0.f ? 0.f : 1.f / S;

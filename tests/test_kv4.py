@@ -922,3 +922,108 @@ def test_attention_window_over_positions_never_written(case, dtype):
         err = (out.cpu().double() - ref).abs()
         assert (err <= tol).all(), (byte, float((err / tol).max()))
         assert relative_rms(out, ref) <= RMS[dtype], (byte, relative_rms(out, ref))
+
+
+# ------------------------------------------------------------------------------------ scores of any size (GPU) ---
+FAR = [  # (d, n_kv, group, tokens, lengths, max_pos)
+    (64, 1, 4, [1, 1], [70, 1], 96),                  # a tile of up to 8 rows
+    (128, 2, 8, [1, 1, 1], [900, 33, 500], 1024),     # (positions split)
+    (128, 1, 12, [3, 1], [70, 40], 96),
+    (256, 1, 3, [9, 4], [600, 4], 640),
+    (64, 16, 8, [33, 20, 17, 1], [33, 40, 100, 1], 128),
+    (128, 16, 4, [40, 33, 70], [40, 100, 200], 224),  # hundreds of rows
+    (128, 8, 4, [40, 33], [1500, 700], 2048),
+    (256, 8, 4, [70, 33], [1057, 1056], 1088),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("q_exp,k_exp,scale", [
+    (100, -60, 2.0 ** 32), (100, 40, 2.0 ** 32), (100, -60, 2.0 ** 18), (100, 40, -(2.0 ** -40)),
+    (14, 14, 0.125), (12, 10, 0.125), (40, 20, 1.0), (-60, 40, 2.0 ** 32)])
+@pytest.mark.parametrize("case", range(len(FAR)))
+def test_attention_of_far_scores(case, q_exp, k_exp, scale, dtype):
+    """Queries, keys and scales up to their limits: each token takes the value at its largest score."""
+    d, n_kv, G, ns, ls, max_pos = FAR[case]
+    gen = torch.Generator().manual_seed(case)
+    ks = [torch.randn((L, n_kv, d), generator=gen) * 2.0 ** (k_exp - 2 if k_exp > 0 else k_exp) for L in ls]
+    vs = [torch.randn((L, n_kv, d), generator=gen) for L in ls]
+    cache = fill(moe.kv4_cache(len(ls), n_kv, d, max_pos))
+    put(ks, vs, cache, F32)
+    q = torch.randn((sum(ns), n_kv * G, d), generator=gen)
+    q = (q / q.abs().amax(-1, keepdim=True) * 2.0 ** q_exp).to(dtype)
+    scale = float(np.float32(scale))
+    ref = torch.zeros((sum(ns), n_kv * G, d), dtype=torch.float64)
+    most = torch.zeros_like(ref)
+    clear = torch.ones((sum(ns), n_kv * G, 1), dtype=torch.bool)  # the largest score is one by more than its rounding
+    t0 = 0
+    for n, L, k, v in zip(ns, ls, ks, vs):
+        at = torch.arange(L - n, L).view(-1, 1, 1)
+        see = torch.arange(L) <= at
+        for h in range(n_kv):
+            cols = slice(h * G, (h + 1) * G)
+            x, K = q[t0:t0 + n, cols].double(), held(k[:, h])
+            z = torch.where(see, x @ K.T * scale, torch.tensor(-math.inf, dtype=torch.float64))
+            top = z.topk(min(2, L), -1).values
+            # what fp32 scores, from queries within 2^-22 and keys within 2^-11 in calls of many bf16 rows, can be off by
+            err = (x.abs() @ K.abs().T * abs(scale)).amax(-1, keepdim=True) * (2.0 ** -17 if dtype is F32 else 2.0 ** -10)
+            if L > 1:
+                clear[t0:t0 + n, cols] = (top[..., :1] - top[..., 1:] > err + 40) | (top[..., 1:] == -math.inf)
+            best = z.argmax(-1)
+            ref[t0:t0 + n, cols], most[t0:t0 + n, cols] = held(v[:, h])[best], magnitude(v[:, h])[best]
+        t0 += n
+    assert clear.double().mean() > 0.5 or q_exp + k_exp < 24
+    qs, kl, _ = batch(ns, ls)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns), scale=scale)
+    moe.moe_sync_check()
+    out = out.cpu().double()
+    assert torch.isfinite(out).all()
+    # (the probability is one, all others below 2^-40: one value in two fp16 terms, or three fp16 roundings)
+    tol = most * (2.0 ** -20 if dtype is F32 else 3 * 2.0 ** -11) + ref.abs() * torch.finfo(dtype).eps / 2
+    assert ((out - ref).abs() <= tol)[clear.expand_as(ref)].all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", range(len(FAR)))
+def test_attention_far_scores_leave_other_rows_alone(case, dtype):
+    """Every third head's queries are 2^40 times the others', which keep their precision; and scores that become far
+    only late in the cache."""
+    d, n_kv, G, ns, ls, max_pos = FAR[case]
+    gen = torch.Generator().manual_seed(100 + case)
+    ks = [torch.randn((L, n_kv, d), generator=gen) for L in ls]
+    vs = [torch.randn((L, n_kv, d), generator=gen) for L in ls]
+    cache = fill(moe.kv4_cache(len(ls), n_kv, d, max_pos))
+    put(ks, vs, cache, F32)
+    q = torch.randn((sum(ns), n_kv * G, d), generator=gen)
+    far = torch.arange(n_kv * G) % 3 == 1
+    q[:, far] *= 2.0 ** 40
+    q = q.to(dtype)
+    near = q.clone()
+    near[:, far] = 0
+    ref, amount, shift = attend(near.double(), ks, vs, ns, ls, G, 0, d ** -0.5, dtype)
+    tol = attention_tolerance(ref, amount, shift, dtype)
+    qs, kl, _ = batch(ns, ls)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns)).cpu().double()
+    assert torch.isfinite(out).all()
+    assert ((out - ref).abs() <= tol)[:, ~far].all()
+    assert relative_rms(out[:, ~far], ref[:, ~far]) <= RMS[dtype]
+    # the last position's key 2^26 times the others' along every query, its value the only one that counts where
+    # its score is the largest
+    for k in ks:
+        k[-1] *= 2.0 ** 26
+    put(ks, vs, cache, F32)
+    q = torch.randn((sum(ns), n_kv * G, d), generator=gen).to(dtype)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns)).cpu().double()
+    assert torch.isfinite(out).all()
+    t0 = 0
+    for n, L, k, v in zip(ns, ls, ks, vs):
+        for h in range(n_kv):
+            x = q[t0 + n - 1, h * G:(h + 1) * G].double()
+            z = x @ held(k[-1:, h])[0] * d ** -0.5
+            o, V, m = out[t0 + n - 1, h * G:(h + 1) * G], held(v[-1:, h]), magnitude(v[-1:, h])
+            tol = m * (2.0 ** -20 if dtype is F32 else 3 * 2.0 ** -11) + V.abs() * torch.finfo(dtype).eps / 2
+            assert ((o - V).abs() <= tol)[z > 2.0 ** 16].all()
+        t0 += n
+    moe.moe_sync_check()

@@ -265,7 +265,7 @@ MOE_API int moe_attention_decode(float *x, int H, int n_heads, int n_kv, int hea
  * A token range that does not fit T or max_q counts as empty, a length outside [0, max_pos] as 0; both raise
  * MOE_ERR_RANGE in the device flags.
  * Limits: head_dim 64, 128, 192 or 256; max_pos a multiple of 32, at most MOE_KV4_MAX_POS; n_seq and n_kv at most
- * 65535; max_q times the heads per key/value head at most 2^24.  Token arrays are [T][heads][head_dim] with
+ * 65535, the cache at most 2^60 bytes; max_q times the heads per key/value head at most 2^24.  Token arrays are [T][heads][head_dim] with
  * `stride` elements (at least heads * head_dim) from token to token; they, their strides in bytes, the cache and
  * the workspace must be multiples of 16 bytes.  T or n_seq 0 is a no-op.  dtype: MOE_F32 or MOE_BF16. */
 #define MOE_KV4_GROUP 64

@@ -280,6 +280,11 @@ int check_kv4_shape(const char *what, int n_seq, int n_kv, int head_dim, int max
     if (max_pos < MOE_KV4_BLOCK || max_pos % MOE_KV4_BLOCK || max_pos > MOE_KV4_MAX_POS)
         return fail(MOE_ERR_INVALID_ARG, "%s: max_pos must be a multiple of %d up to %d (max_pos=%d)", what,
                     MOE_KV4_BLOCK, MOE_KV4_MAX_POS, max_pos);
+    // (sequences times heads have at most 32 bits, the blocks of a head at most 35 bits of bytes)
+    const uint64_t rows = uint64_t(n_seq) * n_kv, each = uint64_t(max_pos / moe::kv4::kPos) * moe::kv4::block_bytes(head_dim);
+    if (rows > (1ull << 60) / each)
+        return fail(MOE_ERR_INVALID_ARG, "%s: the cache passes 2^60 bytes (n_seq=%d n_kv=%d head_dim=%d max_pos=%d)", what,
+                    n_seq, n_kv, head_dim, max_pos);
     return MOE_OK;
 }
 

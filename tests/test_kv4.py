@@ -1027,3 +1027,21 @@ def test_attention_far_scores_leave_other_rows_alone(case, dtype):
             assert ((o - V).abs() <= tol)[z > 2.0 ** 16].all()
         t0 += n
     moe.moe_sync_check()
+
+
+def test_cache_whose_size_has_no_number():
+    """A cache of more bytes than 64 bits count (or any device holds) is refused, not checked against what is left."""
+    shape = (65535, 65535, 256, 1 << 26)  # 8.3e19 bytes
+    assert moe.moe_kv4_cache_bytes(*shape) == 0
+    with pytest.raises(moe.MoeError):
+        moe.kv4_cache(*shape, device="cpu")
+    n_seq, n_kv, d, max_pos = shape
+    left = n_seq * n_kv * (max_pos // 32) * 36 * d % (1 << 64)
+    refused("moe_kv4_append", OK_PTR, OK_PTR, 0, n_kv * d, n_kv * d, 1, n_seq, n_kv, d, max_pos, OK_PTR, 1, OK_PTR, OK_PTR,
+            left, None)
+    refused("moe_kv4_read", OK_PTR, left, 1, n_seq, n_kv, d, max_pos, OK_PTR, 1, OK_PTR, OK_PTR, OK_PTR, 0, n_kv * d,
+            n_kv * d, None)
+    assert moe.moe_kv4_attention_workspace_bytes(1, n_seq, n_kv, n_kv, d, 1, max_pos) == 0
+    refused("moe_kv4_attention", OK_PTR, 0, n_kv * d, OK_PTR, left, 1, n_seq, n_kv, n_kv, d, max_pos, OK_PTR, 1, OK_PTR, 0,
+            1.0, OK_PTR, n_kv * d, OK_PTR, left, None)
+    assert moe.moe_kv4_cache_bytes(1024, 64, 256, 1 << 26) > 0

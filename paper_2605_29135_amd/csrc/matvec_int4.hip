@@ -67,6 +67,26 @@ __device__ float row_dot(const uint8_t *w, const uint16_t *scale, const float *x
     return acc;
 }
 
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
+// 1 / sqrt(mean x^2 + 1e-6) from the sum of squares, or, where that is past the largest number, from the squares of
+// x 2^-100 (element by element; an infinite x leaves 0, a NaN stays).
+__device__ float norm_factor(float squares, const float *x, int K) {
+    if (finite(squares)) return rsqrtf(squares / float(K) + 1e-6f);
+    squares = 0.f;
+#pragma unroll 1
+    for (int g = 0; g < K / 128; ++g) {
+        float part = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < 128; ++i) {
+            const float v = x[g * 128 + i] * 0x1p-100f;
+            part = fmaf(v, v, part);
+        }
+        squares += part;
+    }
+    return rsqrtf(squares / float(K)) * 0x1p-100f;
+}
+
 // Largest magnitude over the wave, in every lane.
 __device__ __forceinline__ float wave_top(float v) {
     v = fmaxf(v, dev::dpp<0xB1>(v));
@@ -109,7 +129,6 @@ __device__ __forceinline__ float top_of(float4 u) {
 }
 __device__ __forceinline__ float squares_of(float4 u) { return fmaf(u.x, u.x, fmaf(u.y, u.y, fmaf(u.z, u.z, u.w * u.w))); }
 __device__ __forceinline__ int exponent_of(float top) { return top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0; }
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 
 // Bytes of LDS: the waves' operands (2 T rows: the two terms of each token), then their partial sums.
 __host__ __device__ constexpr int stage_bytes(int T, int GS) { return kMvWaves * GS * 512 * T; }
@@ -156,7 +175,7 @@ __global__ __launch_bounds__(kTermsBlock) void matvec_terms_kernel(const float *
     const int e2 = exponent_of(top);
     if (tid == 0) {
         reinterpret_cast<int *>(ws)[t] = -kCodeExp - e2;
-        reinterpret_cast<float *>(ws + 64)[t] = norm ? rsqrtf(squares / float(K) + 1e-6f) : 1.f;
+        reinterpret_cast<float *>(ws + 64)[t] = norm ? norm_factor(squares, x + size_t(t) * K, K) : 1.f;
     }
     uint4 *out = reinterpret_cast<uint4 *>(ws + 256) + t;
     auto store = [&](int i, float4 u) {  // (K / 4 is a multiple of 32: a pair of lanes stays together)
@@ -350,7 +369,7 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_int4_kernel(const float *_
                     float s = 0.f;
 #pragma unroll
                     for (int v = 0; v < kMvWaves; ++v) s += sq[v][o_token];
-                    inv = rsqrtf(s / float(K) + 1e-6f);
+                    inv = norm_factor(s, x + size_t(o_token) * K, K);
                 }
                 total *= inv;
                 if (!finite(total))
@@ -445,7 +464,7 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_stream_kernel(const float 
         const int e2 = exponent_of(top);
         if (lane == 0) {
             exps[t] = -kCodeExp - e2;
-            inv_sh[t] = norm ? rsqrtf(squares / float(K) + 1e-6f) : 1.f;
+            inv_sh[t] = norm ? norm_factor(squares, x + size_t(t) * K, K) : 1.f;
         }
 #pragma unroll 4
         for (int i = lane; i < K / 4; i += kWave) {  // (K / 4 is a multiple of 32: a pair of lanes stays together)

@@ -1045,3 +1045,22 @@ def test_cache_whose_size_has_no_number():
     refused("moe_kv4_attention", OK_PTR, 0, n_kv * d, OK_PTR, left, 1, n_seq, n_kv, n_kv, d, max_pos, OK_PTR, 1, OK_PTR, 0,
             1.0, OK_PTR, n_kv * d, OK_PTR, left, None)
     assert moe.moe_kv4_cache_bytes(1024, 64, 256, 1 << 26) > 0
+
+
+# ------------------------------------------------------------------------------- int4 products, more (GPU) ---
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 3, 4, 16])
+@pytest.mark.parametrize("N,K", [(40, 256), (33, 4224), (33000, 256)])
+def test_matvec_norm_of_values_whose_squares_do_not_fit(T, N, K):
+    """The norm of values up to the largest of fp32, and of values whose squares vanish."""
+    gen = torch.Generator().manual_seed(T)
+    raw, _ = int4_matrix(N, K, gen)
+    parts = int4_parts(raw, N, K)
+    x = torch.randn((T, K), generator=gen).clamp(-3, 3) / 3
+    for size in (2.0 ** 64, 2.0 ** 100, 3.4e38, 2.0 ** -90):
+        for token in range(T):
+            y = x.clone()
+            y[token] *= size
+            out = moe.moe_matvec_int4(y.cuda(), raw.cuda(), N, rmsnorm=True).cpu().double()
+            ref, tol = matvec_reference(y, parts, None, True)
+            assert ((out - ref).abs() <= tol).all(), (size, token, float(((out - ref).abs() / tol).max()))

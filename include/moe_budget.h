@@ -317,7 +317,7 @@ MOE_API size_t moe_matvec_int4_workspace_bytes(int T, int K);
  * h = x / sqrt(mean(x^2) + 1e-6).
  *   x    device fp32 [T x K], 16-byte aligned, K a multiple of 128
  *   w    device MOE_INT4G128 matrix [N x K], 16-byte aligned: packed nibbles [N x K/2], then bf16 scales [N x K/128]
- *   add  device fp32 [T x N], or NULL; may be y
+ *   add  device fp32 [T x N], or NULL; y itself or apart from it
  *   y    device fp32 [T x N], apart from x
  *   workspace device, >= moe_matvec_int4_workspace_bytes(T, K), 16-byte aligned, apart from the others (may be NULL when
  *        that is 0)

@@ -428,6 +428,9 @@ int moe_matvec_int4(const float *x, const void *w, int T, int N, int K, const fl
     const auto xa = reinterpret_cast<uintptr_t>(x), ya = reinterpret_cast<uintptr_t>(y);
     if (xa < ya + sizeof(float) * size_t(T) * N && ya < xa + sizeof(float) * size_t(T) * K)
         return fail(MOE_ERR_INVALID_ARG, "matvec: y overlaps x");
+    const auto aa = reinterpret_cast<uintptr_t>(add);
+    if (add && add != y && aa < ya + sizeof(float) * size_t(T) * N && ya < aa + sizeof(float) * size_t(T) * N)
+        return fail(MOE_ERR_INVALID_ARG, "matvec: add overlaps y without being y");
     const size_t need = moe::matvec_int4_workspace_bytes(T, K);
     if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(MOE_ERR_INVALID_ARG, "matvec: needs a 16-byte aligned workspace of %zu bytes (%zu given)", need,

@@ -1064,3 +1064,10 @@ def test_matvec_norm_of_values_whose_squares_do_not_fit(T, N, K):
             out = moe.moe_matvec_int4(y.cuda(), raw.cuda(), N, rmsnorm=True).cpu().double()
             ref, tol = matvec_reference(y, parts, None, True)
             assert ((out - ref).abs() <= tol).all(), (size, token, float(((out - ref).abs() / tol).max()))
+
+
+def test_matvec_refuses_what_is_added_half_over_the_output():
+    """`add` is y itself or apart from it: one that overlaps it elsewhere would be read after it was written."""
+    y = OK_PTR + (1 << 30)
+    for add in (y + 4, y + 64 * 4, y + 2 * 64 * 4 - 4, y - 4, y - 64 * 4):
+        refused("moe_matvec_int4", OK_PTR, OK_PTR + (1 << 20), 2, 64, 128, add, y, 0, None, 0, None)

@@ -741,6 +741,11 @@ class MoeStack:
                  router_w: list, shared_w: list | None = None, max_tokens: int = 1, max_prefill_tokens: int = 0,
                  prefetch: int = 0, recall: int = 0, recall_overlap: int = 0, attention: dict | None = None,
                  host_threads: int = 0):
+        int4 = bool(attention.get("int4", False)) if attention is not None else False
+        buffers = ("w_qkv", "w_o", "cache", "cache") if int4 else ("w_qkv", "w_o", "k_cache", "v_cache")
+        for nm in buffers if attention is not None else ():
+            if len(attention[nm]) != len(router_w):
+                raise ValueError(f"attention: {nm} has {len(attention[nm])} entries, the stack {len(router_w)} layers")
         self._router = (C.c_void_p * len(router_w))(*[_dev(w, "router_w") for w in router_w])
         self._shared = None
         if shared_w is not None:
@@ -749,7 +754,6 @@ class MoeStack:
         att = None
         if attention is not None:  # dict: n_heads, n_kv, head_dim, max_pos, theta, start_pos, w_qkv, w_o, k_cache, v_cache
             # or, with "int4": True, int4 matrices and `cache` (a 4-bit cache of one sequence per layer) in place of the last two
-            int4 = bool(attention.get("int4", False))
             arr = lambda ts, nm: (C.c_void_p * len(ts))(*[_dev(t, nm) for t in ts])
             if int4:
                 nh, nk, hd = attention["n_heads"], attention["n_kv"], attention["head_dim"]
@@ -758,8 +762,7 @@ class MoeStack:
                         raise ValueError(f"cache of layer {i} is for {_kv4_shape(c)}, expected (1, {nk}, {hd}, {attention['max_pos']})")
                     _int4_matrix(attention["w_qkv"][i], "w_qkv", (nh + 2 * nk) * hd, H)
                     _int4_matrix(attention["w_o"][i], "w_o", H, nh * hd)
-            self._att_arrays = [arr(attention[nm], nm) for nm in (("w_qkv", "w_o", "cache", "cache") if int4 else
-                                                                  ("w_qkv", "w_o", "k_cache", "v_cache"))]
+            self._att_arrays = [arr(attention[nm], nm) for nm in buffers]
             att = AttentionDesc(attention["n_heads"], attention["n_kv"], attention["head_dim"], attention["max_pos"],
                                 attention.get("theta", 1.0e6), attention.get("start_pos", 0),
                                 *[C.cast(a, C.POINTER(C.c_void_p)) for a in self._att_arrays], int(int4))

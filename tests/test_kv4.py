@@ -1071,3 +1071,18 @@ def test_matvec_refuses_what_is_added_half_over_the_output():
     y = OK_PTR + (1 << 30)
     for add in (y + 4, y + 64 * 4, y + 2 * 64 * 4 - 4, y - 4, y - 64 * 4):
         refused("moe_matvec_int4", OK_PTR, OK_PTR + (1 << 20), 2, 64, 128, add, y, 0, None, 0, None)
+
+
+def test_stack_attention_needs_an_entry_per_layer():
+    """Lists shorter than the stack (the library would read past their arrays) are refused before anything is."""
+    n_kv, d, H, max_pos = 2, 64, 256, 64
+    router = [torch.zeros((8, H)) for _ in range(3)]
+    whole = dict(w_qkv=[torch.zeros(1)] * 3, w_o=[torch.zeros(1)] * 3)
+    caches = [moe.kv4_cache(1, n_kv, d, max_pos, device="cpu")] * 3
+    shape = dict(n_heads=4, n_kv=n_kv, head_dim=d, max_pos=max_pos)
+    for form in (dict(cache=caches, int4=True), dict(k_cache=caches, v_cache=caches)):
+        for name in ("w_qkv", "w_o", *[nm for nm in form if nm != "int4"]):
+            att = {**shape, **whole, **form}
+            for entries in (att[name][:2], att[name] + att[name][:1], []):
+                with pytest.raises(ValueError, match=f"{name} .* 3 layers"):
+                    moe.MoeStack(None, H, 128, 8, 2, moe.MOE_BF16, moe.MOE_BF16, router, attention={**att, name: entries})

@@ -556,7 +556,8 @@ typedef struct {
     void *const *v_cache;           /* host array [L] of device value caches */
     int int4;                       /* 1: the block of moe_attention_decode_int4 -- w_qkv and w_o are MOE_INT4G128
                                        matrices, k_cache[l] is layer l's 4-bit cache of one sequence (keys and
-                                       values; v_cache is not read and may be NULL), max_pos a multiple of 32.
+                                       values; v_cache is not read and may be NULL), all 16-byte aligned, max_pos
+                                       a multiple of 32.
                                        0: bf16 weights and caches */
 } moe_attention_desc;
 

@@ -264,6 +264,10 @@ int moe_stack_create(const moe_stack_desc *d, moe_stack **out) {
         for (int l = 0; l < d->n_layers; ++l)
             if (!a->w_qkv[l] || !a->w_o[l] || !a->k_cache[l] || (!a->int4 && !a->v_cache[l]))
                 return moe::fail(MOE_ERR_INVALID_ARG, "stack: attention buffers of layer %d missing", l);
+        for (int l = 0; a->int4 && l < d->n_layers; ++l)
+            for (const void *p : {a->w_qkv[l], a->w_o[l], static_cast<const void *>(a->k_cache[l])})
+                if (reinterpret_cast<uintptr_t>(p) % 16)
+                    return moe::fail(MOE_ERR_INVALID_ARG, "stack: attention buffers of layer %d must be 16-byte aligned", l);
         if (d->max_prefill_tokens > 0 || d->max_tokens != 1)
             return moe::fail(MOE_ERR_INVALID_ARG, "stack: an attention block decodes one token per step (no prefill)");
     }

@@ -1086,3 +1086,20 @@ def test_stack_attention_needs_an_entry_per_layer():
             for entries in (att[name][:2], att[name] + att[name][:1], []):
                 with pytest.raises(ValueError, match=f"{name} .* 3 layers"):
                     moe.MoeStack(None, H, 128, 8, 2, moe.MOE_BF16, moe.MOE_BF16, router, attention={**att, name: entries})
+
+
+def test_stack_refuses_int4_attention_buffers_out_of_alignment():
+    """As moe_attention_decode_int4 does: its kernels load 16 bytes at a time."""
+    layers = 2
+    pointers = lambda off: (C.c_void_p * layers)(OK_PTR, OK_PTR + off)
+    cast = lambda a: C.cast(a, C.POINTER(C.c_void_p))
+    router = pointers(0)
+    for bad in range(3):
+        for off in (8, 2):
+            arrays = [pointers(off if i == bad else 0) for i in range(3)]
+            att = binding.AttentionDesc(4, 2, 64, 64, 1.0e4, 0, cast(arrays[0]), cast(arrays[1]), cast(arrays[2]), None, 1)
+            desc = binding.StackDesc(layers, 256, 128, 8, 2, moe.MOE_BF16, moe.MOE_BF16, cast(router), None, None, 1, 0, 0, 0, 0,
+                                     C.pointer(att), 0)
+            out = C.c_void_p()
+            assert moe.lib().moe_stack_create(C.byref(desc), C.byref(out)) == -1 and not out.value
+            assert b"aligned" in moe.lib().moe_last_error()

@@ -21,6 +21,8 @@
  *    stream and events, per-device error flags, stack workspaces).
  *  - `stream` is a hipStream_t passed as void* (NULL = the null stream).  Device
  *    work is enqueued asynchronously on it unless a call says otherwise.
+ *  - Descriptors are zero-initialised by the caller and grow at their end, 0 meaning what was before: a caller is
+ *    compiled with the header of the library that it runs with (an older one passes what lies behind its struct).
  *  - Errors found on the device (expert id out of range, non-finite logits,
  *    expert not resident) are raised in per-device sticky flags; read and
  *    clear them with moe_sync_check().

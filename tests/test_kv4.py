@@ -1103,3 +1103,24 @@ def test_stack_refuses_int4_attention_buffers_out_of_alignment():
             out = C.c_void_p()
             assert moe.lib().moe_stack_create(C.byref(desc), C.byref(out)) == -1 and not out.value
             assert b"aligned" in moe.lib().moe_last_error()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,K", [(8, 2432), (5, 4096), (8, 4096), (16, 2048)])
+@pytest.mark.parametrize("N", [131100, 65600])
+def test_matvec_many_rows_of_tokens_that_fill_the_lds(T, K, N):
+    """Tokens whose terms leave a unit room for one block, which then takes several tiles of rows at a time."""
+    gen = torch.Generator().manual_seed(K + T)
+    on = torch.Generator(device="cuda").manual_seed(K)
+    codes = torch.randint(0, 256, (N * K // 2,), generator=on, device="cuda", dtype=torch.uint8)
+    scales = (torch.rand((N * (K // 128),), generator=on, device="cuda") * 0.01 + 0.001).to(BF16)
+    x, add = torch.randn((T, K), generator=gen), torch.randn((T, N), generator=gen)
+    y = torch.full((T * N + 64,), 9.0, device="cuda")
+    moe.moe_matvec_int4(x.cuda(), torch.cat([codes, scales.view(torch.uint8)]), N, y=y[:T * N].view(T, N), add=add.cuda(), rmsnorm=True)
+    rows = torch.cat([torch.arange(0, 130), torch.randint(0, N, (300,), generator=gen), torch.arange(N - 130, N)])
+    raw = torch.cat([codes.view(N, -1)[rows.cuda()].flatten(), scales.view(N, -1)[rows.cuda()].flatten().view(torch.uint8)]).cpu()
+    ref, tol = matvec_reference(x, int4_parts(raw, len(rows), K), add[:, rows], True)
+    out = y[:T * N].view(T, N).cpu()
+    err = (out[:, rows].double() - ref).abs()
+    assert (err <= tol).all(), float((err / tol).max())
+    assert torch.isfinite(out).all() and (y[T * N:] == 9).all()

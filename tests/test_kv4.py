@@ -1124,3 +1124,31 @@ def test_matvec_many_rows_of_tokens_that_fill_the_lds(T, K, N):
     err = (out[:, rows].double() - ref).abs()
     assert (err <= tol).all(), float((err / tol).max())
     assert torch.isfinite(out).all() and (y[T * N:] == 9).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_attention_keeps_its_precision(case, dtype):
+    """The stated roundings over all of a case's outputs together: one left out of fp32's two terms (2^-11) or twice
+    bf16's would show, where a bound for the worst element leaves room."""
+    _, _, _, ns, ls, _, window = CASES[case]
+    cache, q, ref, _ = attention_case(*CASES[case], dtype, seed=1000 + case)
+    qs, kl, _ = batch(ns, ls)
+    out = moe.moe_kv4_attention(q.cuda(), cache, kl, q_start=qs, max_q=max(ns), window=window)
+    moe.moe_sync_check()
+    if ref.abs().amax() == 0:
+        assert (out == 0).all()
+    else:
+        assert relative_rms(out, ref) <= RMS[dtype], relative_rms(out, ref)
+
+
+def test_the_precision_bound_sees_a_dropped_term():
+    """Outputs whose probabilities are rounded once to fp16 are far past fp32's bound (and within bf16's)."""
+    gen = torch.Generator().manual_seed(0)
+    p = torch.softmax(torch.randn((64, 300), generator=gen, dtype=torch.float64), -1)
+    v = torch.randn((300, 128), generator=gen, dtype=torch.float64)
+    ref = p @ v
+    top = p.amax(-1, keepdim=True)
+    assert relative_rms((p / top).half().double() * top @ v, ref) > 20 * RMS[F32]
+    assert relative_rms((p / top).half().double() * top @ v, ref) < RMS[BF16]

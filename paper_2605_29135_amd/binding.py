@@ -442,10 +442,15 @@ def _kv4_batch(n_seq, T, kv_len, q_start, max_q):
         return kv_len.data_ptr(), None, 1
     if q_start.dtype is not torch.int32 or q_start.numel() != n_seq + 1 or not q_start.is_contiguous():
         raise ValueError(f"q_start {q_start.dtype} {tuple(q_start.shape)}: expected {n_seq + 1} contiguous int32")
-    return kv_len.data_ptr(), q_start.data_ptr(), (max(T, 1) if max_q is None else max_q)
+    max_q = max(T, 1) if max_q is None else max_q
+    if T and not 0 < max_q < 1 << 31:
+        raise ValueError(f"max_q={max_q}: a sequence has from 1 to 2^31 - 1 tokens")
+    return kv_len.data_ptr(), q_start.data_ptr(), max_q
 
 
 def moe_kv4_cache_bytes(n_seq: int, n_kv: int, head_dim: int, max_pos: int) -> int:
+    if not all(0 <= n < 1 << 31 for n in (n_seq, n_kv, head_dim, max_pos)):  # (none of the library's shapes)
+        n_kv = 0
     return int(lib().moe_kv4_cache_bytes(n_seq, n_kv, head_dim, max_pos))
 
 
@@ -516,6 +521,8 @@ def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, 
         raise ValueError(f"q has shape {tuple(q.shape)}, expected [T, n_heads, {d}]")
     T, n_heads, _ = q.shape
     dtype = q.dtype
+    if not 0 <= window <= 1 << 30:
+        raise ValueError(f"window={window} outside [0, 2^30]")
     qp, qs = _rows(q, "q", n_heads, d)
     lp, sp, mq = _kv4_batch(n_seq, T, kv_len, q_start, max_q)
     device = _here(q, cache, kv_len, q_start, out, workspace)

@@ -1152,3 +1152,34 @@ def test_the_precision_bound_sees_a_dropped_term():
     top = p.amax(-1, keepdim=True)
     assert relative_rms((p / top).half().double() * top @ v, ref) > 20 * RMS[F32]
     assert relative_rms((p / top).half().double() * top @ v, ref) < RMS[BF16]
+
+
+def test_binding_refuses_numbers_that_do_not_fit_the_library():
+    """A window or max_q past 32 bits is refused, not cut to its low bits."""
+    cache = moe.kv4_cache(1, 2, 64, 32, device="cpu")
+    q, kl, qs = torch.zeros((1, 2, 64)), torch.ones(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for window in ((1 << 32) + 5, 1 << 32, -(1 << 32), (1 << 30) + 1, -1):
+        with pytest.raises(ValueError, match="window"):
+            moe.moe_kv4_attention(q, cache, kl, window=window)
+    for max_q in ((1 << 32) + 1, 1 << 31, 0, -1):
+        for call in (lambda: moe.moe_kv4_attention(q, cache, kl, q_start=qs, max_q=max_q),
+                     lambda: moe.moe_kv4_append(q, q, cache, kl, q_start=qs, max_q=max_q),
+                     lambda: moe.moe_kv4_read(cache, kl, 1, q_start=qs, max_q=max_q)):
+            with pytest.raises(ValueError, match="max_q"):
+                call()
+    for shape in ((1 << 32, 2, 64, 32), ((1 << 32) + 1, 2, 64, 32), (1, 2, (1 << 32) + 64, 32), (1, 2, 64, (1 << 32) + 32)):
+        with pytest.raises(moe.MoeError):
+            moe.kv4_cache(*shape, device="meta")
+
+
+@pytest.mark.gpu
+def test_binding_no_tokens_is_a_no_op():
+    cache, kl = moe.kv4_cache(2, 2, 64, 32), torch.zeros(2, dtype=torch.int32, device="cuda")
+    none, qs = torch.zeros((0, 2, 64), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    before = cache.clone()
+    for max_q in (None, 0, 7):
+        moe.moe_kv4_append(none, none, cache, kl, q_start=qs, max_q=max_q)
+        assert moe.moe_kv4_attention(none, cache, kl, q_start=qs, max_q=max_q).shape == (0, 2, 64)
+        assert moe.moe_kv4_read(cache, kl, 0, q_start=qs, max_q=max_q)[0].shape == (0, 2, 64)
+    moe.moe_sync_check()
+    assert torch.equal(cache, before)

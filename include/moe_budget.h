@@ -339,7 +339,8 @@ MOE_API size_t moe_attention_decode_int4_workspace_bytes(int T, int H, int n_hea
  *   w_o      device MOE_INT4G128 [H x n_heads head_dim]
  *   cache    device, moe_kv4_cache_bytes(T, n_kv, head_dim, max_pos) bytes
  *   kv_len   device int32 [T], the tokens included
- * Needs H and n_heads * head_dim multiples of 128, head_dim and max_pos as above, n_heads <= 1024, theta > 1. */
+ * Needs H (at most 2^24) and n_heads * head_dim multiples of 128, head_dim and max_pos as above, n_heads <= 1024,
+ * theta > 1. */
 MOE_API int moe_attention_decode_int4(float *x, int T, int H, int n_heads, int n_kv, int head_dim, const void *w_qkv,
                                       const void *w_o, void *cache, size_t cache_bytes, int max_pos,
                                       const int32_t *kv_len, float theta, void *workspace, size_t workspace_bytes,

@@ -102,7 +102,7 @@ size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 }  // namespace
 
 bool attention_int4_shape_supported(int H, int n_heads, int n_kv, int d, int max_pos) {
-    return H > 0 && H % 128 == 0 && n_heads > 0 && n_kv > 0 && n_heads % n_kv == 0 && n_heads <= 1024 &&
+    return H > 0 && H % 128 == 0 && H <= 1 << 24 && n_heads > 0 && n_kv > 0 && n_heads % n_kv == 0 && n_heads <= 1024 &&
            (d == 64 || d == 128 || d == 192 || d == 256) && (n_heads * d) % 128 == 0 && max_pos > 0 &&
            max_pos % kPos == 0 && max_pos <= MOE_KV4_MAX_POS;
 }

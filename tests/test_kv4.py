@@ -1183,3 +1183,11 @@ def test_binding_no_tokens_is_a_no_op():
         assert moe.moe_kv4_read(cache, kl, 0, q_start=qs, max_q=max_q)[0].shape == (0, 2, 64)
     moe.moe_sync_check()
     assert torch.equal(cache, before)
+
+
+def test_block_refuses_rows_longer_than_its_products_take():
+    """The block's projections have the limits of moe_matvec_int4: at most 2^24 columns."""
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, 1 << 24, 4, 2, 64, 64) > 0
+    assert moe.moe_attention_decode_int4_workspace_bytes(1, (1 << 24) + 128, 4, 2, 64, 64) == 0
+    refused("moe_attention_decode_int4", OK_PTR, 1, 1 << 25, 4, 2, 64, OK_PTR, OK_PTR, OK_PTR, 1 << 40, 64, OK_PTR, 1.0e4,
+            OK_PTR, 1 << 40, None)

@@ -260,7 +260,8 @@ MOE_API int moe_attention_decode(float *x, int H, int n_heads, int n_kv, int hea
  *
  * The calls below take a batch of n_seq sequences, sequence b at cache entry b:
  *   q_start  device int32 [n_seq + 1], ascending: sequence b's tokens are the rows q_start[b] .. q_start[b + 1)
- *            of the flat token arrays, at most max_q of them; rows from q_start[n_seq] on are not touched.
+ *            of the flat token arrays, at most max_q of them (the launches go by it: a tight one is faster); rows
+ *            from q_start[n_seq] on are not touched.
  *            NULL: one token per sequence (T = n_seq, max_q is taken as 1).
  *   kv_len   device int32 [n_seq]: positions of sequence b, its tokens included -- they are the last ones, token
  *            i of n at position kv_len[b] - n + i.  A token before position 0 is padding.

@@ -467,7 +467,8 @@ def kv4_cache(n_seq: int, n_kv: int, head_dim: int, max_pos: int, device=None):
 def moe_kv4_append(k, v, cache, kv_len, q_start=None, max_q: int | None = None, stream=None):
     """Quantise the tokens' keys and values (fp32 or bf16 [T, n_kv, d], tokens may be strided) into the cache, at
     the last positions of their sequences (kv_len int32 [n_seq], the tokens included; q_start int32 [n_seq + 1]:
-    sequence b's rows, None for one token each; max_q: most tokens of a sequence, T by default)."""
+    sequence b's rows, None for one token each; max_q: most tokens of a sequence, T by default -- the launches go by
+    it, so a tight one is faster)."""
     n_seq, n_kv, d, max_pos = _kv4_shape(cache)
     T, dtype = k.shape[0], k.dtype
     kp, ks = _rows(k, "k", n_kv, d)
@@ -514,8 +515,9 @@ def moe_kv4_attention_workspace_bytes(T: int, n_seq: int, n_heads: int, n_kv: in
 def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, window: int = 0,
                       scale: float | None = None, out=None, workspace=None, stream=None):
     """Causal attention of the tokens' queries (fp32 or bf16 [T, n_heads, d]) over the 4-bit cache, with
-    window > 0 over the last `window` positions (batch as for moe_kv4_append; scale 1 / sqrt(d) by default);
-    returns out [T, n_heads, d] of q's type.  Rows from q_start[-1] on are not written."""
+    window > 0 over the last `window` positions (batch as for moe_kv4_append; without max_q a batch of few tokens per
+    sequence runs as one of long prompts, several times slower; scale 1 / sqrt(d) by default); returns out
+    [T, n_heads, d] of q's type.  Rows from q_start[-1] on are not written."""
     n_seq, n_kv, d, max_pos = _kv4_shape(cache)
     if q.dim() != 3:
         raise ValueError(f"q has shape {tuple(q.shape)}, expected [T, n_heads, {d}]")

@@ -7,10 +7,11 @@
 //   3. Attention over the cache (kv4_attention.hip).
 //   4. Output projection added to x (matvec_int4.hip).
 //
-// Measured in the decode stack (H 2048, 32 query and 4 key/value heads of 128, one token): 22.9 us at 4096 positions,
-// 20.7 at 101, five launches (the bf16 block: 19.4 and 19.1, four launches, with 3.6 times the cache and 3.9 times the
-// weights).  Latency is the bound: projections 5.5 each, heads 4.1 (fp64 rotary angles as in that block), attention
-// 7 and 4.
+// Measured in the decode stack (H 2048, 32 query and 4 key/value heads of 128, one token; in brackets the bf16 block,
+// four launches, with 3.6 times the cache and 3.9 times the weights): 21.0 us at 101 positions of a cache of 4096 (19.0;
+// in a cache of 128, without the second attention launch, 18.5), 23.1 at 4096 (19.6), 24.7 at 8192 (25.9), 29.1 at 16384
+// (38.2).  Up to some thousand positions five launches' latency is the bound: projections 5.5 each, heads 4.1 (fp64 rotary
+// angles as in that block), attention 7 and 4.
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"

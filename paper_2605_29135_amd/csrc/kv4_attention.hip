@@ -18,12 +18,14 @@
 // of 32 positions, and the block's waves join their (max, sum, output) through LDS.  With few rows the
 // positions are split over more blocks (grid), whose partial results a second launch joins.
 //
-// Bound: with few rows the cache's bytes, 1.125 d per position and key/value head.  Measured (kernel, then join): one
-// token of 64 heads over 131071 positions of 8 heads of 128, bf16, 30 + 4.8 us (151 MB, 5.0 TB/s of the 7.2 that a read
-// reaches); 16 sequences of up to 16384, 35.6 + 4.7 us (188 MB, 5.3 TB/s); one token of 32 heads over 4096 positions of
-// 4 heads, fp32, 7.0 + 4.0 us, which is latency.  One block of positions in flight per wave instead of two: 33.5 for the
-// 30.  Rows that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which
-// halves the lane arithmetic: 67 -> 57 us for the 16 sequences, with the split by what the sequences hold.
+// Bound: with few rows the cache's bytes, 1.125 d per position and key/value head.  Measured (kernel, then join; inputs
+// that change from pass to pass, more than the last-level cache holds): one token of 64 heads over 131071 positions of 8
+// heads of 128, bf16, 32.6 + 4.9 us (151 MB, 4.6 TB/s of the 7.2 that a large read reaches); 16 sequences of up to 16384,
+// 40.8 + 4.8 us (188 MB, 4.6 TB/s); one token of 32 heads over 4096 positions of 4 heads, fp32, 7.2 + 3.9 us, which is
+// latency (each wave has one block of positions, loaded for both of the places that the code has).  One block of
+// positions in flight per wave instead of two: 37.8 us for the 37.1 of the first, 47.2 for the 45.8 of the second.  Rows
+// that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which halves the lane
+// arithmetic: 46.0 us for the 16 sequences, 48.3 without.
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
@@ -44,7 +46,7 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
 // Blocks that fill the device, where rows and heads alone give fewer: one token of 64 heads over 131071 positions of
-// 8 heads takes 30.0 us with 512, 35.8 with 768 and 34.1 with 1024 (256 leave half of the waves' places empty).
+// 8 heads takes 37.1 us (with the join) with 512, 39.9 with 256, 41.0 with 768 and 42.2 with 1024.
 constexpr int kTarget = 512;
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
@@ -212,7 +214,8 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs &a, int want, bool 
     p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), a.least);
     p.chunk = (p.chunk + a.unit - 1) & -a.unit;
     // (pieces rounded up may be more than run together, and the last few would take as long again: somewhat larger ones
-    // that do are better.  16 sequences of 4822 to 16384 positions: 51 us without, 39 with.)
+    // that do are better.  16 sequences of 4822 to 16384 positions: 54.0 us without, 45.8 with.  More sequences than lanes
+    // would have to be read again for every size tried.)
     if (b.n_seq > 1 && b.n_seq <= 64) {
         int chunk = p.chunk;
 #pragma unroll 1
@@ -278,7 +281,7 @@ __device__ __forceinline__ void store4(void *out, size_t at, float4 v) {
         *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
-// grid: (row tiles, key/value head, sequence), or with a target (pieces, key/value head, row tiles).
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces).
 // HALF: at most 8 rows.  They fill columns 0-7 and again 8-15, and lane (n, c) takes row n % 8's scores of the
 // positions of tile n / 8 alone: half the arithmetic per lane; the probabilities of tile 1 are handed to the lanes
 // of column n - 8 as operands.
@@ -719,10 +722,12 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 // of a maximum and of a conversion.  Two buffers: the next positions' codes are loaded before the present ones are
 // used and turned after.  The sums of P come from the matrix cores too.
 //
-// Bound: lane arithmetic and the chain of a step (operands from LDS, scores, softmax, products, a barrier), about 2.5 us
-// for 64 positions at either block size; the matrix cores are busy 27 % of the time.  2048 tokens of 32 heads of 128 over
-// 8192 positions: 330 us, 0.73 PFLOP/s (1.22 for a large bf16 product); with heads of 256, 16 of them: 366 us, 0.66.
-// Two groups of waves a phase apart: 401 us for the 366 that the first form took.
+// Bound: the chain of a step (operands from LDS, scores, softmax, products, a barrier), about 2.5 us for 64 positions at
+// either block size, and blocks of unequal length.  2048 tokens of 32 heads of 128 over 8192 positions: 329 us (after some
+// 20 ms of work; 373 for the first launches of an idle device, whose clock still rises), 0.73 PFLOP/s (1.22 for a large
+// bf16 product); the matrix cores are busy 30 % of the time and lanes issue 45 % of it (counters); its 256 blocks are one
+// per unit and walk 97 to 128 steps, so 12 % is idle behind the shorter ones.  With heads of 256, 16 of them: 365 us,
+// 0.66.  Two groups of waves a phase apart: 401 us for the 366 that the first form took.
 constexpr int prompt_tiles(int d) { return d <= 128 ? 2 : 1; }  // row tiles of 16 per wave: what its registers hold
 
 // A barrier for what the block's waves pass one another through LDS; loads in flight stay so.
@@ -753,7 +758,8 @@ __device__ __forceinline__ int held_exponent(const uint32_t (&m)[L], const uint3
     return min(131 - (all >> 7), 100);  // (below 2^(exponent - 127 + 2))
 }
 
-// grid: (row tiles, key/value head, sequence); WAVES x 16 NT rows per block.
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces); WAVES x 16 NT rows
+// per block.
 template <int NG, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_prompt_kernel(AttendArgs a) {
     constexpr int d = NG * kGroup, NT = prompt_tiles(d), ROWS = 16 * NT * WAVES;
@@ -1187,17 +1193,23 @@ AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max
     AttendPlan p{};
     int fill = kTarget;
     // Many rows: keys and values turned to fp16 once for a block's rows.  It starts later and goes on faster: with 32
-    // query and 4 key/value heads of 128, 64 tokens over 512 positions take 19.8 us (the other kernel 20.7), 32 over
-    // 1024 19.9 (20.8), 128 over 128 11.5 (8.9), 128 over 1024 22.9 (33.8), 2048 over 8192 328 (834).  With heads of
-    // 256 it draws level at half as many scores, of 64 at twice as many.
+    // query and 4 key/value heads of 128, 128 tokens over 1024 positions take 21.9 us (the other kernel 27.1), 300 over
+    // 8000 79.5 (226), 2048 over 8192 329 (865); with 16 heads of 256, 300 over 8000 81 (253); with 32 of 64, 64 over
+    // 4000 19.4 (29.4).  Where the rule begins the other kernel is still ahead: 64 over 512 19.5 (14.7), 32 over 1024
+    // 19.9 (15.2).
     if (!f32 && rows >= 128 && double(rows) * n_kv * n_seq * max_pos * d >= double(1 << 27)) {
         const int per = 64 * prompt_tiles(d);  // rows of four waves
         const long long four = (rows + per - 1) / per * n_kv * n_seq, eight = (rows + 2 * per - 1) / (2 * per) * n_kv * n_seq;
         // Eight waves turn half as often as two blocks of four: taken where they fill the device (2048 tokens over
-        // 8192 positions: 339 us, four 385), and for heads of more than 128, of which a unit holds one block, where the
-        // positions are split (300 tokens, 16 heads of 256, 8000 positions: 82 us, four 261).
+        // 8192 positions: 329 us, four 362), and for heads of more than 128, of which a unit holds one block, where the
+        // positions are split (300 tokens, 16 heads of 256, 8000 positions: 81 us, four 140).
         fill = d <= 128 ? 512 : 256;
-        p.least = four * 4 >= fill ? 16 : 8;  // (600 tokens, 32 heads of 64, 1000 positions: 27 us, 35 with 8)
+        // Longer pieces where rows and heads already give a quarter of the blocks: they keep short caches whole (296 tokens
+        // of 3 sequences, 32 heads of 128, up to 325 positions: 20 us, 31 with 8; 370, 64 heads, 593 positions: 23 and 28).
+        // Where the positions are more, or heads are larger, 8 would be faster (600 tokens, 32 heads of 64, 1000 positions:
+        // 25.0 us, 23.7 with 8; 611 of 4 sequences, 4 heads of 192, 751 positions: 37.6 and 29.4); below a quarter 16 would
+        // be slower (128 tokens, 32 heads of 128, 2000 positions: 23.7 us, 29.8 with 16).
+        p.least = four * 4 >= fill ? 16 : 8;
         p.prompt = eight >= 256 || (d > 128 && rows > per && four * 3 <= fill * 2) ? 8 : 4;
         p.tile_rows = per * (p.prompt / 4);
         if (p.prompt == 8) fill = 256;
@@ -1211,8 +1223,9 @@ AttendPlan attend_plan(int n_seq, int n_kv, int group, int d, int max_q, int max
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
     const long long pieces = (max_pos / kPos + p.least - 1) / p.least;  // most that a sequence has
     // Split where that makes more blocks; many rows, whose pieces' outputs cost more, where it makes twice as many (300
-    // tokens, 32 heads of 128, 8000 positions: 254 us whole, 78 split; 1556 rows of 4 heads of 64 in each of 6 sequences
-    // of up to 701, 312 blocks: 23 whole, 29 split).
+    // tokens, 32 heads of 128, 8000 positions: 258 us whole, 79 split; 1556 rows of 4 heads of 64 in each of 6 sequences
+    // of up to 701, 312 blocks: 24 whole, 31 split).  (By the number of blocks alone: a batch that fills the device by it is
+    // not split, however unequal its sequences are.)
     if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && pieces > 1) {
         p.target = int(std::min(std::max(1ll, fill / base), pieces * n_seq));
         p.units = p.target + n_seq - 1;  // (rounding up leaves less than one piece more per sequence)
@@ -1278,7 +1291,7 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     if (e != hipSuccess || !p.target) return e;
     const int rows = batch.max_q * a.group;
     // One block per row has its pieces in flight together, a group of lanes per row needs fewer blocks: 64 tokens, 32 heads
-    // of 64 (2048 rows) 19.9 and 18.3 us with the attention, 128 (4096 rows) 26.7 and 22.1.
+    // of 64, 4000 positions (2048 rows) 19.3 and 19.4 us with the attention, 128 (4096 rows) 26.1 and 22.7.
     const bool many = (long long)rows * n_kv * batch.n_seq >= 2048;
 #define KV4_JOIN(NG, F)                                                                                             \
     if (d == NG * kGroup && f32 == F) {                                                                             \

@@ -6,10 +6,13 @@
 // LDS, and a word that only some of the new positions cover keeps the others' nibbles (read ahead, merged, written
 // by the one lane that owns it).  Everything is written from LDS in the cache's order, in whole lines.
 //
-// Measured (8 heads of 128, bf16): 6 311 new positions of four sequences 14.0 us (33 MB, 2.4 TB/s), read back 9.6 us
-// (3.4 TB/s); one new position of 16 sequences 4.4 and 3.0 us, which is a launch and its chain of loads.  What is left in
-// the long form is arithmetic: about eleven operations per element for the range, the quotient and the code (written
-// straight to the cache, a nibble's word at a time, it took 21 us).
+// Measured (8 heads of 128, bf16): 6 311 new positions of four sequences 13.7 us (33 MB, 2.4 TB/s), read back 9.6 us
+// (3.4 TB/s); one new position of 16 sequences 4.4 and 3.1 us, which is a launch and its chain of loads.  The long form's
+// bytes are 6.5 us at a copy's rate, and the lanes issue for 7.6 us of the append (23 operations per element, counted) and
+// 3.3 of the read: the device holds all of the blocks that have work at once, they load, then compute, then store
+// together, and little of the one runs under the other.  (Blocks beyond a sequence's tokens cost 0.5 us of the read, and
+// none of the append: 199 per sequence and head were launched, 65 would do.  Written straight to the cache, a nibble's word
+// at a time, the append took 21 us.)
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"

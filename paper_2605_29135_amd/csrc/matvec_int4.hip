@@ -14,8 +14,8 @@
 // loaded as soon as it has been multiplied.  Many rows: see matvec_stream_kernel.
 //
 // Measured: 5120 x 2048, 1 token 5.5 us (5.4 MB, 1 TB/s: a launch, the chain of loads and the sum over waves); 2048 x
-// 4096, 16 tokens 3.4 us for the terms and 6.6 us (half of the units have a block); 131071 x 2048, 3 tokens 29.6 us
-// (140 MB, 4.7 TB/s).
+// 4096, 16 tokens 3.4 us for the terms and 6.6 us (half of the units have a block); 131071 x 2048, 3 tokens 32.8 us
+// (140 MB, 4.3 TB/s; weights that change from pass to pass).
 #include "device_common.h"
 #include "internal.h"
 
@@ -577,9 +577,10 @@ hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K
     const auto *wb = static_cast<const uint8_t *>(w);
     const int tiles = (N + 15) / 16;
     // A wave per row tile takes time by K, the columns shared by a block's waves time by N.  Taken with a tile for every wave
-    // that fits the device (131071 x 2048, 3 tokens: 29 us, 39 shared; 30000 x 8192, 1 token 33 and 38), and down to a
-    // quarter of that where rows are many times the columns (1 token: 12000 x 512 5.9 and 7.4 us, 20000 x 2048 10.7 and
-    // 11.4; but 12000 x 2048 10.3 and 7.3, 20000 x 4096 18.9 and 15.5).
+    // that fits the device (131071 x 2048, 3 tokens: 33.7 us, 43.0 shared; 30000 x 8192, 1 token 40.5 and 40.4), and down
+    // to a quarter of that where rows are many times the columns (1 token: 12000 x 512 7.0 and 7.4 us; 20000 x 2048 10.6 and
+    // 9.5, the first blocks having all the tiles there; 12000 x 2048 10.3 and 7.4, 20000 x 4096 18.9 and 14.9, which are
+    // shared).
     const bool many = tiles >= kMvGrid * kMvWaves || (tiles >= kMvGrid * kMvWaves / 4 && N / 8 >= K);
     if (many && stream_lds(T, K) <= 128 * 1024) {
         // two blocks per unit where the tokens' terms and a wave's registers leave room, else more tiles per wave

@@ -20,6 +20,7 @@
 //   4. Output projection: the same GEMV with the residual as its bias, in place.
 #include "device_common.h"
 #include "internal.h"
+#include "rotary.h"
 
 namespace moe {
 namespace {

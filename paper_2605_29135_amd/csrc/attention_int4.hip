@@ -15,6 +15,7 @@
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
+#include "rotary.h"
 
 #include <math.h>
 

@@ -79,19 +79,6 @@ __device__ __forceinline__ uint64_t wave_reduce_u64(uint64_t v) {
     return join(__builtin_amdgcn_readlane(lo(v), 63), __builtin_amdgcn_readlane(hi(v), 63));
 }
 
-// Rotation of dimension pair (i, i + d/2) at position p: angle p * theta^(-2i/d).  The angle is formed and
-// reduced to [-pi, pi] in double, so thousands of positions keep full single precision in cos and sin.
-__device__ __forceinline__ void rope_cs(int p, int i, int d, float theta, float &c, float &s) {
-    const double inv_freq = exp2(-2.0 * double(i) / double(d) * log2(double(theta)));
-    const double ang = double(p) * inv_freq;
-    constexpr double kTwoPi = 6.283185307179586;
-    const double r = fma(-rint(ang * (1.0 / kTwoPi)), kTwoPi, ang);
-    double sd, cd;
-    sincos(r, &sd, &cd);
-    c = float(cd);
-    s = float(sd);
-}
-
 __device__ __forceinline__ float bf16_bits_to_float(uint32_t b16) { return __uint_as_float(b16 << 16); }
 
 __device__ __forceinline__ uint4 load16(const uint8_t *p) { return *reinterpret_cast<const uint4 *>(p); }

@@ -69,18 +69,20 @@ __device__ float row_dot(const uint8_t *w, const uint16_t *scale, const float *x
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 
+__device__ __forceinline__ float squares_of(float4 u) { return fmaf(u.x, u.x, fmaf(u.y, u.y, fmaf(u.z, u.z, u.w * u.w))); }
+
 // 1 / sqrt(mean x^2 + 1e-6) from the sum of squares, or, where that is past the largest number, from the squares of
-// x 2^-100 (element by element; an infinite x leaves 0, a NaN stays).
+// x 2^-100 (one lane, a group at a time; an infinite x leaves 0, a NaN stays).
 __device__ float norm_factor(float squares, const float *x, int K) {
     if (finite(squares)) return rsqrtf(squares / float(K) + 1e-6f);
     squares = 0.f;
 #pragma unroll 1
     for (int g = 0; g < K / 128; ++g) {
         float part = 0.f;
-#pragma unroll 1
-        for (int i = 0; i < 128; ++i) {
-            const float v = x[g * 128 + i] * 0x1p-100f;
-            part = fmaf(v, v, part);
+#pragma unroll 4
+        for (int i = 0; i < 32; ++i) {
+            const float4 u = dev::load_f4(reinterpret_cast<const float4 *>(x) + g * 32 + i);
+            part += squares_of(make_float4(u.x * 0x1p-100f, u.y * 0x1p-100f, u.z * 0x1p-100f, u.w * 0x1p-100f));
         }
         squares += part;
     }
@@ -127,7 +129,6 @@ __device__ __forceinline__ void store_terms(float4 u, int e2, bool odd, F operan
 __device__ __forceinline__ float top_of(float4 u) {
     return fmaxf(fmaxf(fabsf(u.x), fabsf(u.y)), fmaxf(fabsf(u.z), fabsf(u.w)));
 }
-__device__ __forceinline__ float squares_of(float4 u) { return fmaf(u.x, u.x, fmaf(u.y, u.y, fmaf(u.z, u.z, u.w * u.w))); }
 __device__ __forceinline__ int exponent_of(float top) { return top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0; }
 
 // Bytes of LDS: the waves' operands (2 T rows: the two terms of each token), then their partial sums.
@@ -363,17 +364,19 @@ __global__ __launch_bounds__(kMvBlock, 2) void matvec_int4_kernel(const float *_
                         part += red[((v * RB + o_row / 16) * 4 + (pr & 3)) * kWave + (pr >> 2) * 16 + (o_row & 15)];
                     total += part;
                 }
-                float inv = 1.f;
+                float inv = 1.f, squared = 0.f;
                 if constexpr (PRE) inv = pre.inv[o_token];
                 else if (norm) {
-                    float s = 0.f;
 #pragma unroll
-                    for (int v = 0; v < kMvWaves; ++v) s += sq[v][o_token];
-                    inv = norm_factor(s, x + size_t(o_token) * K, K);
+                    for (int v = 0; v < kMvWaves; ++v) squared += sq[v][o_token];
+                    inv = rsqrtf(squared / float(K) + 1e-6f);
                 }
                 total *= inv;
-                if (!finite(total))
-                    total = row_dot(w + size_t(row) * (K / 2), scales + size_t(row) * KG, x + size_t(o_token) * K, inv, K);
+                if (!finite(total) || inv == 0.f) {  // (0 where the squares' sum is infinite)
+                    const float *xr = x + size_t(o_token) * K;
+                    if (!PRE && norm) inv = norm_factor(squared, xr, K);
+                    total = row_dot(w + size_t(row) * (K / 2), scales + size_t(row) * KG, xr, inv, K);
+                }
                 y[at] = add ? addend + total : total;
             }
         }

@@ -26,6 +26,7 @@
 // positions in flight per wave instead of two: 37.8 us for the 37.1 of the first, 47.2 for the 45.8 of the second.  Rows
 // that fill only half of a tile (up to 8) share the lanes between a block's two tiles of positions, which halves the lane
 // arithmetic: 46.0 us for the 16 sequences, 48.3 without.
+#include "attend_common.h"
 #include "device_common.h"
 #include "internal.h"
 #include "kv4.h"
@@ -36,25 +37,14 @@
 namespace moe {
 namespace {
 
+using namespace attend;
 using namespace kv4;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
 // Blocks that fill the device, where rows and heads alone give fewer: one token of 64 heads over 131071 positions of
 // 8 heads takes 37.1 us (with the join) with 512, 39.9 with 256, 41.0 with 768 and 42.2 with 1024.
 constexpr int kTarget = 512;
 
-__device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ floatx4 mfma(f16x8 a, f16x8 b, floatx4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
 // The eight codes of a word as fp16: u 2^-24 (elements 0, 1, 4, 5) and 16 u 2^-24 (elements 2, 3, 6, 7).
 __device__ __forceinline__ f16x8 raw_codes(uint32_t w) {
     constexpr uint32_t L = 0x000F000Fu, H = 0x00F000F0u;
@@ -78,13 +68,6 @@ __device__ __forceinline__ f16x8 value_codes(uint32_t w) {
     return raw_codes(w) * f16x8{m, m, n, n, m, m, n, n} + f16x8{a, a, a, a, a, a, a, a};
 }
 
-__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // round to nearest even
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 v = {__bf16(lo), __bf16(hi)};
-    return __builtin_bit_cast(uint32_t, v);
-}
 __device__ __forceinline__ f16x2 pack_f16(float lo, float hi) {
     const f16x2 v = {_Float16(lo), _Float16(hi)};
     return v;
@@ -125,39 +108,11 @@ __device__ __forceinline__ float row_unit(float scale, int exp) {
 constexpr float kFar = 0x1p20f;
 __device__ __forceinline__ bool is_far(float off) { return !(fabsf(off) < kFar); }
 
-// What f makes of v over the four lanes (n, 0..3).
-template <typename F>
-__device__ __forceinline__ float over_c(float v, F f) {
-    auto pair = [](auto r) { return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1])); };
-    float2 u = pair(__builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    v = f(u.x, u.y);
-    u = pair(__builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    return f(u.x, u.y);
-}
-__device__ __forceinline__ float max_over_c(float v) {
-    return over_c(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float sum_over_c(float v) {
-    return over_c(v, [](float a, float b) { return a + b; });
-}
 // The value of lane n ^ 8.
 template <typename T>
 __device__ __forceinline__ T other_half(T v) {
     return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xF, 0xF, false));
 }
-// Sums over the lanes up to this one.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-#define SCAN(CTRL, ROWS) v += uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, ROWS, 0xF, true))
-    SCAN(0x111, 0xF);  // row_shr:1
-    SCAN(0x112, 0xF);
-    SCAN(0x114, 0xF);
-    SCAN(0x118, 0xF);
-    SCAN(0x142, 0xA);  // row_bcast:15 into rows 1 and 3
-    SCAN(0x143, 0xC);  // row_bcast:31 into rows 2 and 3
-#undef SCAN
-    return v;
-}
-
 struct AttendArgs {
     const void *q;
     void *out;
@@ -165,9 +120,7 @@ struct AttendArgs {
     float *part;  // [unit][head][tile][16 NT rows][d + 4]: unnormalised output, maximum, sum, the row's unit (row_unit)
     long long q_stride, out_stride;
     int n_heads, n_kv, group, window;
-    int target;  // splits of a whole batch (0: every sequence in one piece)
-    int least;   // blocks of positions that a piece has at least; the rest come in multiples of `unit`
-    int unit;
+    Split split;
     int tiles;   // row tiles of the largest sequence
     float scale;  // times log2(e)
     Batch batch;
@@ -184,79 +137,14 @@ __device__ __forceinline__ int seen_blocks(const Seq &s, int window) {
     return (s.len - 1) / kPos + 1 - first_seen(s, window) / kPos;
 }
 
-// The split of a batch: sequences are cut into pieces of `chunk` blocks of positions, at least `least`, so
-// that there are about `target` of them in all; a sequence has at least one piece.  Every wave works it out for
-// itself.  by_unit: which piece is number `want`; otherwise, the pieces of sequence `want`.
-struct Piece {
-    Seq s;
-    int seq, split, chunk;
-    int first, count;  // of the sequence's pieces (count 0: there is no such piece)
-};
-__device__ __forceinline__ Piece find_piece(const AttendArgs &a, int want, bool by_unit, int *err) {
-    const Batch &b = a.batch;
-    const int window = a.window, target = a.target;
-    const int lane = threadIdx.x & 63;
-    uint32_t total = 0;  // (a batch that is split has fewer than kTarget sequences of at most 2^21 blocks)
-    Seq s{0, 0, 0, false};
-    int nb = 0;
-    auto look = [&](int base) {
-        s = Seq{0, 0, 0, false};
-        if (base + lane < b.n_seq) s = sequence(b, base + lane);
-        nb = seen_blocks(s, window);
-    };
-#pragma unroll 1
-    for (int base = 0; base < b.n_seq; base += 64) {
-        look(base);
-        if (err && s.bad) atomicOr(err, kErrRange);
-        total += uint32_t(__builtin_amdgcn_readlane(int(wave_scan(uint32_t(nb))), 63));
-    }
-    Piece p{};
-    p.chunk = max(int((total + uint32_t(target) - 1) / uint32_t(target)), a.least);
-    p.chunk = (p.chunk + a.unit - 1) & -a.unit;
-    // (pieces rounded up may be more than run together, and the last few would take as long again: somewhat larger ones
-    // that do are better.  16 sequences of 4822 to 16384 positions: 54.0 us without, 45.8 with.  More sequences than lanes
-    // would have to be read again for every size tried.)
-    if (b.n_seq > 1 && b.n_seq <= 64) {
-        int chunk = p.chunk;
-#pragma unroll 1
-        for (int k = 1; k <= 8; ++k) {
-            const int count = s.n ? max(1, (nb + chunk - 1) / chunk) : 0;
-            if (__builtin_amdgcn_readlane(int(wave_scan(uint32_t(count))), 63) <= target) {
-                p.chunk = chunk;
-                break;
-            }
-            chunk = (p.chunk + p.chunk * k / 8 + a.unit - 1) & -a.unit;
-        }
-    }
-    int before = 0;
-#pragma unroll 1
-    for (int base = 0; base < b.n_seq; base += 64) {
-        if (b.n_seq > 64) look(base);
-        const int count = s.n ? max(1, (nb + p.chunk - 1) / p.chunk) : 0;
-        const int upto = int(wave_scan(uint32_t(count))), first = before + upto - count;
-        const bool mine = by_unit ? want >= first && want < first + count : base + lane == want;
-        const unsigned long long hit = __ballot(mine);
-        if (hit) {
-            const int l = __builtin_amdgcn_readfirstlane(__ffsll(hit) - 1);
-            p.seq = base + l;
-            p.first = __builtin_amdgcn_readlane(first, l);
-            p.count = __builtin_amdgcn_readlane(count, l);
-            p.s.t0 = __builtin_amdgcn_readlane(s.t0, l);
-            p.s.n = __builtin_amdgcn_readlane(s.n, l);
-            p.s.len = __builtin_amdgcn_readlane(s.len, l);
-            p.split = by_unit ? want - p.first : 0;
-            return p;
-        }
-        before += __builtin_amdgcn_readlane(upto, 63);
-    }
-    return p;
+__device__ __forceinline__ Piece split_piece(const AttendArgs &a, int want, bool by_unit, int *err) {
+    return find_piece(a.batch, a.split, [&](const Seq &s) { return seen_blocks(s, a.window); }, want, by_unit, err);
 }
-
 // This block's piece: grid (row tiles, key/value head, sequence), or (key/value head, row tiles, pieces), where the pieces
 // that there are not come last (among the others they would leave some of the eight dies with more blocks than run
 // together).
 __device__ __forceinline__ Piece this_piece(const AttendArgs &a, int tile, int *err) {
-    if (a.target) return find_piece(a, blockIdx.z, true, blockIdx.z == 0 ? err : nullptr);
+    if (a.split.target) return split_piece(a, blockIdx.z, true, blockIdx.z == 0 ? err : nullptr);
     Piece p{};
     p.seq = blockIdx.z;
     p.count = 1;
@@ -274,13 +162,6 @@ __device__ __forceinline__ int2 tile_blocks(const AttendArgs &a, const Piece &pi
                      piece.split == piece.count - 1 ? t_end : min(t_end, b_first + (piece.split + 1) * piece.chunk));
 }
 
-template <bool F32>
-__device__ __forceinline__ void store4(void *out, size_t at, float4 v) {
-    if constexpr (F32) *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = v;
-    else
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-}
-
 // grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces).
 // HALF: at most 8 rows.  They fill columns 0-7 and again 8-15, and lane (n, c) takes row n % 8's scores of the
 // positions of tile n / 8 alone: half the arithmetic per lane; the probabilities of tile 1 are handed to the lanes
@@ -294,7 +175,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
     __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS], unit_sh[ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int half = HALF ? n >> 3 : 0, n_row = HALF ? n & 7 : n;
-    const int tile = a.target ? blockIdx.y : blockIdx.x, h = a.target ? blockIdx.x : blockIdx.y;
+    const int tile = a.split.target ? blockIdx.y : blockIdx.x, h = a.split.target ? blockIdx.x : blockIdx.y;
     const Piece piece = this_piece(a, tile, tile == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
     if (piece.count == 0) return;
     const Seq &s = piece.s;
@@ -730,12 +611,6 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void kv4_attend_ke
 // 0.66.  Two groups of waves a phase apart: 401 us for the 366 that the first form took.
 constexpr int prompt_tiles(int d) { return d <= 128 ? 2 : 1; }  // row tiles of 16 per wave: what its registers hold
 
-// A barrier for what the block's waves pass one another through LDS; loads in flight stay so.
-__device__ __forceinline__ void lds_barrier() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 // The power of two that takes values of at most |m| + 15 s below 2^6: m, s pairs of bf16, L per lane (s >= 0).
 template <int L>
 __device__ __forceinline__ int held_exponent(const uint32_t (&m)[L], const uint32_t (&s)[L]) {
@@ -771,7 +646,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     __shared__ uint4 kf_sh[2][FRAGS][64], vf_sh[2][FRAGS][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     // (the last rows see the most positions: their blocks start first)
-    const int tile = a.tiles - 1 - int(a.target ? blockIdx.y : blockIdx.x), h = a.target ? blockIdx.x : blockIdx.y;
+    const int tile = a.tiles - 1 - int(a.split.target ? blockIdx.y : blockIdx.x), h = a.split.target ? blockIdx.x : blockIdx.y;
     const Piece piece = this_piece(a, tile, tile == a.tiles - 1 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
     if (piece.count == 0) return;
     const Seq &s = piece.s;
@@ -1089,97 +964,6 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : WAVES / 4) void kv4_promp
     }
 }
 
-// One more piece (its maximum, sum and the row's unit; four dims of its output).  As in the attention kernel: nothing
-// seen counts 0, NaN stays.
-__device__ __forceinline__ void join_piece(float &M, float &S, float4 &v, float4 ml, float4 u) {
-    const float now = fmaxf(M, ml.x);
-    const float f = M == -INFINITY && S == 0.f ? 0.f : __builtin_amdgcn_exp2f((M - now) * ml.z);
-    const float g = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - now) * ml.z);
-    M = now;
-    S = fmaf(S, f, ml.y * g);
-    v.x = fmaf(v.x, f, u.x * g);
-    v.y = fmaf(v.y, f, u.y * g);
-    v.z = fmaf(v.z, f, u.z * g);
-    v.w = fmaf(v.w, f, u.w * g);
-}
-
-// Joins the pieces of one row.  grid: (rows, key/value head, sequence); groups of d / 4 lanes take the pieces in
-// turn, a running maximum each.
-template <int NG, bool F32>
-__global__ __launch_bounds__(kAttBlock) void kv4_join_kernel(AttendArgs a, int tile_rows) {
-    constexpr int d = NG * kGroup, N4 = d / 4, SUB = kAttBlock / N4;
-    __shared__ float4 acc_sh[SUB][N4];
-    __shared__ float max_sh[SUB], sum_sh[SUB];
-    const Piece piece = find_piece(a, blockIdx.z, false, nullptr);
-    if (piece.count <= 1) return;
-    const Seq &s = piece.s;
-    const int G = a.group, row = blockIdx.x, h = blockIdx.y;
-    if (row >= s.n * G) return;
-    const int tid = threadIdx.x, i4 = tid % N4, sub = tid / N4;
-    const size_t step = size_t(a.n_kv) * a.tiles * tile_rows * (d + 4);
-    const float *p = a.part + ((size_t(piece.first) * a.n_kv + h) * a.tiles * tile_rows + row) * (d + 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float M = -INFINITY, S = 0.f, unit = 0.f;  // (the group that ends the work has the first piece)
-    if (sub < SUB) {
-#pragma unroll 4
-        for (int k = sub; k < piece.count; k += SUB) {
-            const float4 ml = *reinterpret_cast<const float4 *>(p + k * step + d);
-            const float4 u = *reinterpret_cast<const float4 *>(p + k * step + 4 * i4);
-            join_piece(M, S, v, ml, u);
-            unit = ml.z;
-        }
-        acc_sh[sub][i4] = v;
-        if (i4 == 0) {
-            max_sh[sub] = M;
-            sum_sh[sub] = S;
-        }
-    }
-    __syncthreads();
-    if (tid >= N4) return;
-    float top = max_sh[0];
-#pragma unroll
-    for (int k = 1; k < SUB; ++k) top = fmaxf(top, max_sh[k]);
-    S = 0.f;
-    v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < SUB; ++k) {
-        const float f = max_sh[k] == -INFINITY && sum_sh[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[k] - top) * unit);
-        const float4 u = acc_sh[k][tid];
-        S = fmaf(f, sum_sh[k], S);
-        v.x = fmaf(f, u.x, v.x);
-        v.y = fmaf(f, u.y, v.y);
-        v.z = fmaf(f, u.z, v.z);
-        v.w = fmaf(f, u.w, v.w);
-    }
-    const float inv = S == 0.f ? 0.f : 1.f / S;
-    v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-    store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * tid, v);
-}
-
-// The same for many rows: a group of d / 4 lanes takes one row and its pieces one after the other.  grid: (groups of
-// rows, key/value head, sequence)
-template <int NG, bool F32>
-__global__ __launch_bounds__(kAttBlock) void kv4_join_rows_kernel(AttendArgs a, int tile_rows) {
-    constexpr int d = NG * kGroup, N4 = d / 4, ROWS = kAttBlock / N4;
-    const Piece piece = find_piece(a, blockIdx.z, false, nullptr);
-    if (piece.count <= 1) return;
-    const Seq &s = piece.s;
-    const int G = a.group, i4 = threadIdx.x % N4, sub = threadIdx.x / N4, row = blockIdx.x * ROWS + sub, h = blockIdx.y;
-    if (sub >= ROWS || row >= s.n * G) return;
-    const size_t step = size_t(a.n_kv) * a.tiles * tile_rows * (d + 4);
-    const float *p = a.part + ((size_t(piece.first) * a.n_kv + h) * a.tiles * tile_rows + row) * (d + 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float M = -INFINITY, S = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < piece.count; ++k) {
-        const float4 ml = *reinterpret_cast<const float4 *>(p + k * step + d);
-        join_piece(M, S, v, ml, *reinterpret_cast<const float4 *>(p + k * step + 4 * i4));
-    }
-    const float inv = S == 0.f ? 0.f : 1.f / S;
-    v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-    store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
-}
-
 // What a call launches: from its sizes alone, since lengths are on the device (max_pos bounds them).
 struct AttendPlan {
     int prompt;     // waves of the kernel for many rows, or 0
@@ -1257,9 +1041,9 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     a.n_kv = n_kv;
     a.group = n_heads / n_kv;
     a.window = window;
-    a.target = p.target;
-    a.least = p.least;
-    a.unit = p.prompt ? 2 : 1;
+    a.split.target = p.target;
+    a.split.least = p.least;
+    a.split.unit = p.prompt ? 2 : 1;
     a.tiles = p.blocks;
     a.scale = scale * 1.44269504088896341f;
     a.batch = batch;
@@ -1289,16 +1073,8 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.target) return e;
-    const int rows = batch.max_q * a.group;
-    // One block per row has its pieces in flight together, a group of lanes per row needs fewer blocks: 64 tokens, 32 heads
-    // of 64, 4000 positions (2048 rows) 19.3 and 19.4 us with the attention, 128 (4096 rows) 26.1 and 22.7.
-    const bool many = (long long)rows * n_kv * batch.n_seq >= 2048;
-#define KV4_JOIN(NG, F)                                                                                             \
-    if (d == NG * kGroup && f32 == F) {                                                                             \
-        constexpr int per = kAttBlock / (NG * kGroup / 4);                                                          \
-        if (many) kv4_join_rows_kernel<NG, F><<<dim3((rows + per - 1) / per, n_kv, batch.n_seq), kAttBlock, 0, s>>>(a, p.tile_rows); \
-        else kv4_join_kernel<NG, F><<<dim3(rows, n_kv, batch.n_seq), kAttBlock, 0, s>>>(a, p.tile_rows);            \
-    }
+#define KV4_JOIN(NG, F) \
+    if (d == NG * kGroup && f32 == F) launch_join<NG, F>(a, batch.max_q * a.group, batch.n_seq, p.tile_rows, s);
     KV4_JOIN(1, false) KV4_JOIN(1, true) KV4_JOIN(2, false) KV4_JOIN(2, true)
     KV4_JOIN(3, false) KV4_JOIN(3, true) KV4_JOIN(4, false) KV4_JOIN(4, true)
 #undef KV4_JOIN

@@ -55,7 +55,7 @@ extern "C" {
 #define MOE_ERR_INVALID_ARG (-1)  /* bad size, null pointer, unsupported shape */
 #define MOE_ERR_RANGE (-2)        /* expert id outside [0, E); sequence outside its cache or token array */
 #define MOE_ERR_NONFINITE (-3)    /* NaN or +-inf router logit, or key or value to be quantised */
-#define MOE_ERR_BUDGET (-4)       /* budget below one expert, or a step needs more experts than fit */
+#define MOE_ERR_BUDGET (-4)       /* budget below one expert, or a step needs more experts or pages than there are */
 #define MOE_ERR_NOT_PINNED (-5)   /* host store is not page-locked (hipHostMalloc) memory */
 #define MOE_ERR_HIP (-6)          /* a HIP runtime call failed */
 #define MOE_ERR_COPY (-7)         /* a host-to-device fill failed; the slot stays unmapped */
@@ -108,8 +108,8 @@ MOE_API int moe_init(int device);
 MOE_API const char *moe_last_error(void);
 
 /* Synchronise `stream`, then read and clear the current device's sticky error
- * flags.  Returns MOE_ERR_RANGE, MOE_ERR_NONFINITE or MOE_ERR_NOT_RESIDENT
- * (first set, in that order) or MOE_OK. */
+ * flags.  Returns MOE_ERR_RANGE, MOE_ERR_NONFINITE, MOE_ERR_NOT_RESIDENT or
+ * MOE_ERR_BUDGET (first set, in that order) or MOE_OK. */
 MOE_API int moe_sync_check(void *stream);
 
 /* ======================================================================= */
@@ -312,6 +312,105 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
                               int n_seq, int n_heads, int n_kv, int head_dim, int max_pos, const int32_t *q_start,
                               int max_q, const int32_t *kv_len, int window, float scale, void *out,
                               long long out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ======================================================================= */
+/* Paged bf16 key/value cache: sequences that grow share one pool of pages,  */
+/* what a window has passed need not be held, drafted trees are verified in  */
+/* one call (memory-constrained execution, sec. 5)                           */
+/* ======================================================================= */
+
+/* The pool of one layer: keys and values, each device bf16 [n_pages][n_kv][page_size][head_dim], a page's values
+ * contiguous and k_page_stride / v_page_stride elements (at least n_kv * page_size * head_dim) from page to page.
+ * The page table is device int32 [n_seq][max_pages]: position p of sequence b lies in page table[b][p / page_size],
+ * at offset p % page_size; it is in slot page * page_size + offset of the pool.
+ * A batch of n_seq sequences with q_start, max_q and kv_len is as for the 4-bit cache above, with max_kv in place of
+ * max_pos: the most positions of a sequence (the launches go by it, too).
+ * Limits: head_dim 64, 128, 192 or 256; page_size a power of two from MOE_PAGE_MIN to MOE_PAGE_MAX; n_pages *
+ * page_size below 2^31; max_pages * page_size and max_kv at most MOE_PAGED_MAX_POS, max_kv at most max_pages *
+ * page_size; n_seq and n_kv at most 65535; T at most 2^30; max_q times the heads per key/value head at most 2^24.
+ * Pools, token arrays, their strides in bytes and the workspace must be multiples of 16 bytes, strides at most 2^40
+ * elements.  dtype (of tokens and outputs): MOE_F32 or MOE_BF16. */
+#define MOE_PAGE_MIN 16
+#define MOE_PAGE_MAX 32768
+#define MOE_PAGED_MAX_POS (1 << 26)
+#define MOE_MAX_TREE 256 /* drafted tokens of a sequence's tree */
+
+/* Pages for the tokens that a step adds to a batch, and where these lie.  Sequence b holds kv_len[b] positions (the
+ * pages of which its table row has) and gets n_new[b] more:
+ *   kv_len      device int32 [n_seq]
+ *   n_new       device int32 [n_seq], or NULL: one each
+ *   free_pages  device int32 [n_free]: pages to take, from entry *free_first on, in the order of the sequences and of
+ *               their positions
+ *   free_first  device int32 [1], or NULL: 0
+ *   table       device int32 [n_seq][max_pages]; entries ceil(kv_len / page_size) up to ceil((kv_len + n_new) /
+ *               page_size) of a row are written, the others left
+ *   kv_len_out  device int32 [n_seq] out: the lengths with the new tokens (may be kv_len)
+ *   q_start     device int32 [n_seq + 1] out: the rows of the new tokens, in the order of the sequences
+ *   positions   device int32 [T] out: each row's position, or NULL
+ *   slots       device int32 [T] out: its slot, or NULL
+ *   free_next   device int32 [1] out: the first entry of free_pages that was not taken, or NULL (may be free_first)
+ * Rows behind the last token get position and slot -1 (moe_paged_append passes over them).  A length or count that does not
+ * fit the table raises MOE_ERR_RANGE in the device flags: a sequence with such a length counts as one without positions
+ * or tokens, with such a count as one without tokens; tokens past row T are not added (MOE_ERR_RANGE).  Where the free
+ * pages end, entries and slots are -1, and MOE_ERR_BUDGET is raised.  A page outside [0, n_pages) counts as missing (entry
+ * and slot -1) and raises MOE_ERR_RANGE. */
+MOE_API int moe_page_tables(const int32_t *kv_len, const int32_t *n_new, int n_seq, int T, int page_size, int n_pages,
+                            const int32_t *free_pages, int n_free, const int32_t *free_first, int32_t *table, int max_pages,
+                            int32_t *kv_len_out, int32_t *q_start, int32_t *positions, int32_t *slots, int32_t *free_next,
+                            void *stream);
+
+/* Write the tokens' keys and values to their slots (rounded to bf16, ties to even).
+ *   k, v    device [T][n_kv][head_dim] of dtype, k_stride / v_stride elements from token to token
+ *   slots   device int32 [T]; -1: the token is not stored.  A slot outside the pool raises MOE_ERR_RANGE in the device
+ *           flags and is not stored.  Two tokens with one slot leave a mixture of both there.
+ * T == 0 is a no-op. */
+MOE_API int moe_paged_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T, int n_kv,
+                             int head_dim, const int32_t *slots, void *k_pool, void *v_pool, long long k_page_stride,
+                             long long v_page_stride, int n_pages, int page_size, void *stream);
+
+/* Which drafted tokens each token of a tree sees: itself and those above it.
+ *   parents    device int32 [T]: a token's parent, counted within its sequence's tokens and in front of it, or -1 for a
+ *              child of the last cached position.  Any other number raises MOE_ERR_RANGE and counts as -1.
+ *   q_start, max_q, kv_len: the batch (kv_len with the drafted tokens, NULL: none but them); max_q at most MOE_MAX_TREE
+ *   words      64-bit words of a row of masks: at least max_q / 64, at most MOE_MAX_TREE / 64
+ *   masks      device uint64 [T][words] out: bit j of a token's row: it sees token j of its sequence
+ *   positions  device int32 [T] out, or NULL: kv_len - (the sequence's tokens) + the token's depth (a child of the cache
+ *              has 0), the position by which it is rotated
+ * Rows from q_start[n_seq] on are not touched.  T or n_seq 0 is a no-op. */
+MOE_API int moe_tree_masks(const int32_t *parents, int T, int n_seq, const int32_t *q_start, int max_q, const int32_t *kv_len,
+                           uint64_t *masks, int words, int32_t *positions, void *stream);
+
+/* Device workspace bytes moe_paged_attention needs (either dtype; 0 for an unsupported shape). */
+MOE_API size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q,
+                                                   int max_kv);
+
+/* Attention of the tokens over the cache: out = sum_p softmax_p(scale q . K_p) V_p over the positions p that the token
+ * sees; query head j reads key/value head j / (n_heads / n_kv).  The tokens' own keys and values have been written before,
+ * at the last positions of their sequences.  A token at position t sees
+ *   tree NULL: the positions p <= t, with window > 0 (at most 2^30) those with p > t - window or p < sinks;
+ *   tree:      device uint64 [T][tree_words] as of moe_tree_masks (or any other bits), 64 tree_words >= max_q: of its
+ *              sequence's tokens those whose bit is set, and of the positions in front of them those that a token at
+ *              position (their number) + (its set bits) - 1 sees by the window; bits past the sequence's tokens count
+ *              for nothing.  A window must be 0 or at least max_q.
+ * A token before position 0 is padding.  A token that sees no position gets 0.  Positions that no token of the sequence
+ * sees (between the first `sinks` and the window of its first token) may hold anything, and their pages need not exist
+ * (any entry); a position that some token sees on a page outside [0, n_pages) counts as unseen and raises MOE_ERR_RANGE in
+ * the device flags.
+ * Exact products with fp32 sums, fp32 softmax; queries enter exactly (MOE_F32: as three bf16 terms, 2^-25), probabilities
+ * as bf16 terms of 2^-25 (MOE_F32) or 2^-17 (MOE_BF16).  For queries, keys and values up to
+ * 2^100 in magnitude whose scores stay within fp32.  A value that is not finite makes the outputs of the
+ * tokens that see it NaN, and no others.
+ *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
+ *   out        device, as q with out_stride, same dtype; rows from q_start[n_seq] on are not touched
+ *   scale      a factor of magnitude up to 2^32, as a rule 1 / sqrt(head_dim)
+ *   workspace  device, >= moe_paged_attention_workspace_bytes(...) (may be NULL when that is 0)
+ * T or n_seq 0 is a no-op. */
+MOE_API int moe_paged_attention(const void *q, int dtype, long long q_stride, const void *k_pool, const void *v_pool,
+                                long long k_page_stride, long long v_page_stride, int n_pages, int page_size,
+                                const int32_t *table, int max_pages, int T, int n_seq, int n_heads, int n_kv, int head_dim,
+                                const int32_t *q_start, int max_q, const int32_t *kv_len, int max_kv, int window, int sinks,
+                                const uint64_t *tree, int tree_words, float scale, void *out, long long out_stride,
+                                void *workspace, size_t workspace_bytes, void *stream);
 
 /* Device workspace bytes moe_matvec_int4 needs (0 for up to 3 tokens). */
 MOE_API size_t moe_matvec_int4_workspace_bytes(int T, int K);

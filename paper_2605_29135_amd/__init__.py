@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     moe_ffn_workspace_bytes, moe_init, moe_prefill_grouped, moe_prefill_workspace_bytes, moe_route_topk,
     moe_sync_check, moe_attention_decode, moe_attention_workspace_bytes, key_cache_layout, key_cache_plain,
     kv4_cache, moe_kv4_cache_bytes, moe_kv4_append, moe_kv4_read, moe_kv4_attention, moe_kv4_attention_workspace_bytes,
+    MOE_MAX_TREE, paged_cache, moe_page_tables, moe_paged_append, moe_tree_masks, moe_paged_attention,
+    moe_paged_attention_workspace_bytes,
     moe_matvec_int4, moe_matvec_int4_workspace_bytes, moe_attention_decode_int4, moe_attention_decode_int4_workspace_bytes)

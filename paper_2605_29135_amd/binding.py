@@ -29,6 +29,7 @@ EVENT_HIT, EVENT_MISS, EVENT_PREFETCH, EVENT_HOST = 0, 1, 2, 3
 MOE_SLOT_HOST = -2
 MAX_DECODE_TOKENS = 16
 MOE_KV4_GROUP, MOE_KV4_BLOCK = 64, 32
+MOE_MAX_TREE = 256
 
 
 class MoeError(RuntimeError):
@@ -95,6 +96,12 @@ def lib() -> C.CDLL:
             "moe_kv4_read": [P, SZ, I, I, I, I, I, P, I, P, P, P, I, LL, LL, P],
             "moe_kv4_attention_workspace_bytes": [I, I, I, I, I, I, I],
             "moe_kv4_attention": [P, I, LL, P, SZ, I, I, I, I, I, I, P, I, P, I, C.c_float, P, LL, P, SZ, P],
+            "moe_page_tables": [P, P, I, I, I, I, P, I, P, P, I, P, P, P, P, P, P],
+            "moe_paged_append": [P, P, I, LL, LL, I, I, I, P, P, P, LL, LL, I, I, P],
+            "moe_tree_masks": [P, I, I, P, I, P, P, I, P, P],
+            "moe_paged_attention_workspace_bytes": [I, I, I, I, I, I, I],
+            "moe_paged_attention": [P, I, LL, P, P, LL, LL, I, I, P, I, I, I, I, I, I, P, I, P, I, I, I, P, I, C.c_float, P, LL,
+                                    P, SZ, P],
             "moe_matvec_int4_workspace_bytes": [I, I],
             "moe_matvec_int4": [P, P, I, I, I, P, P, I, P, SZ, P],
             "moe_attention_decode_int4_workspace_bytes": [I, I, I, I, I, I],
@@ -131,7 +138,7 @@ def lib() -> C.CDLL:
         L.moe_ffn_workspace_bytes.restype = SZ
         L.moe_prefill_workspace_bytes.restype = SZ
         for name in ("moe_kv4_cache_bytes", "moe_kv4_attention_workspace_bytes", "moe_matvec_int4_workspace_bytes",
-                     "moe_attention_decode_int4_workspace_bytes"):
+                     "moe_attention_decode_int4_workspace_bytes", "moe_paged_attention_workspace_bytes"):
             getattr(L, name).restype = SZ
         _lib = L
     return _lib
@@ -544,6 +551,182 @@ def moe_kv4_attention(q, cache, kv_len, q_start=None, max_q: int | None = None, 
         _check(code, "moe_kv4_attention")
     if on is not None:
         on.used(q, cache, kv_len, q_start, out, workspace)
+    return out
+
+
+# ------------------------------------------------------------------- paged bf16 cache ---
+def paged_cache(n_pages: int, n_kv: int, page_size: int, head_dim: int, device=None):
+    """The pools of one layer's paged cache: (keys, values), each bf16 [n_pages, n_kv, page_size, head_dim]."""
+    import torch
+    shape = (n_pages, n_kv, page_size, head_dim)
+    return tuple(torch.empty(shape, dtype=torch.bfloat16, device="cuda" if device is None else device) for _ in range(2))
+
+
+def _pool(t, name, shape=None):
+    """(pointer, elements from page to page) of a pool [n_pages, n_kv, page_size, head_dim]; only the pages may be strided."""
+    import torch
+    if t.dtype is not torch.bfloat16 or t.dim() != 4 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} {t.dtype} {tuple(t.shape)}: expected bfloat16 "
+                         f"{'[n_pages, n_kv, page_size, head_dim]' if shape is None else list(shape)}")
+    _, n_kv, page, d = t.shape
+    s0, s1, s2, s3 = t.stride()
+    if s3 != 1 or s2 != d or (s1 != page * d and n_kv > 1):
+        raise ValueError(f"{name}: the heads, positions and dims of a page must be contiguous")
+    return t.data_ptr(), s0 if t.shape[0] > 1 else n_kv * page * d
+
+
+def _ints32(t, name, n=None):
+    """Pointer of a contiguous int32 tensor (of n elements), or None for None."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} {t.dtype} {tuple(t.shape)}: expected contiguous int32{'' if n is None else f', {n} of them'}")
+    return t.data_ptr()
+
+
+def _page_table(table, n_seq=None):
+    """(pointer, n_seq, max_pages) of a page table int32 [n_seq, max_pages]."""
+    if table.dim() != 2 or (n_seq is not None and table.shape[0] != n_seq):
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [{'n_seq' if n_seq is None else n_seq}, max_pages]")
+    return _ints32(table, "table"), table.shape[0], table.shape[1]
+
+
+def moe_page_tables(kv_len, n_new, free_pages, table, page_size: int, n_pages: int, T: int, free_first=None, kv_len_out=None,
+                    q_start=None, positions=None, slots=None, free_next=None, stream=None):
+    """Pages for the tokens that a step adds to a batch: sequence b holds kv_len[b] positions (int32 [n_seq]) and gets
+    n_new[b] more (None: one each); the pages it lacks come from free_pages (int32) from entry free_first (int32 [1], None:
+    0) on and are entered into table (int32 [n_seq, max_pages]).  Returns (kv_len_out, q_start, positions, slots, free_next):
+    the new lengths (kv_len_out may be kv_len), the rows of the tokens among T, their positions and slots (-1 for rows
+    behind the last), and the first entry of free_pages that is left (free_next may be free_first)."""
+    import torch
+    tp, n_seq, max_pages = _page_table(table)
+    device = _here(kv_len, n_new, free_pages, table, free_first, kv_len_out, q_start, positions, slots, free_next)
+    if not 0 <= T < 1 << 31:
+        raise ValueError(f"T={T}")
+    handle, on = _run_on(stream, device)
+    kv_len_out, q_start, positions, slots, free_next = (
+        _empty(on, n, torch.int32, device) if t is None else t
+        for t, n in ((kv_len_out, n_seq), (q_start, n_seq + 1), (positions, T), (slots, T), (free_next, 1)))
+    code = (_lib or lib()).moe_page_tables(
+        _ints32(kv_len, "kv_len", n_seq), _ints32(n_new, "n_new", n_seq), n_seq, T, page_size, n_pages,
+        _ints32(free_pages, "free_pages"), free_pages.numel(), _ints32(free_first, "free_first", 1), tp, max_pages,
+        _ints32(kv_len_out, "kv_len_out", n_seq), _ints32(q_start, "q_start", n_seq + 1), _ints32(positions, "positions", T),
+        _ints32(slots, "slots", T), _ints32(free_next, "free_next", 1), handle)
+    if code:
+        _check(code, "moe_page_tables")
+    if on is not None:
+        on.used(kv_len, n_new, free_pages, table, free_first, kv_len_out, q_start, positions, slots, free_next)
+    return kv_len_out, q_start, positions, slots, free_next
+
+
+def moe_paged_append(k, v, k_pool, v_pool, slots, stream=None):
+    """Write the tokens' keys and values (fp32 or bf16 [T, n_kv, d], tokens may be strided) to their slots (int32 [T], -1:
+    not stored) of the pools."""
+    kpp, kps = _pool(k_pool, "k_pool")
+    vpp, vps = _pool(v_pool, "v_pool", k_pool.shape)
+    n_pages, n_kv, page, d = k_pool.shape
+    T, dtype = k.shape[0], k.dtype
+    kp, ks = _rows(k, "k", n_kv, d)
+    vp, vs = _rows(v, "v", n_kv, d, T, dtype)
+    handle, on = _run_on(stream, _here(k, v, k_pool, v_pool, slots))
+    code = (_lib or lib()).moe_paged_append(kp, vp, _float_code(dtype, "k"), ks, vs, T, n_kv, d, _ints32(slots, "slots", T), kpp,
+                                            vpp, kps, vps, n_pages, page, handle)
+    if code:
+        _check(code, "moe_paged_append")
+    if on is not None:
+        on.used(k, v, k_pool, v_pool, slots)
+
+
+def _paged_batch(n_seq, T, kv_len, q_start, max_q):
+    lp = _ints32(kv_len, "kv_len", n_seq)
+    if q_start is None:
+        return lp, None, 1
+    max_q = max(T, 1) if max_q is None else max_q
+    if T and not 0 < max_q < 1 << 31:
+        raise ValueError(f"max_q={max_q}: a sequence has from 1 to 2^31 - 1 tokens")
+    return lp, _ints32(q_start, "q_start", n_seq + 1), max_q
+
+
+def moe_tree_masks(parents, q_start=None, max_q: int | None = None, kv_len=None, masks=None, positions=None, stream=None):
+    """Which drafted tokens each token of a tree sees, itself and those above it: parents int32 [T], each counted within its
+    sequence's tokens (rows q_start[b] .. q_start[b + 1); None: one token per sequence), -1 for a child of the cache; max_q:
+    most tokens of a sequence (T by default, at most 256).  Returns (masks, positions): masks int64 [T, max_q / 64], bit j of
+    a row for token j of its sequence, and positions int32 [T] (kv_len int32 [n_seq] with the drafted tokens, None: none
+    cached)."""
+    import torch
+    if parents.dim() != 1:
+        raise ValueError(f"parents has shape {tuple(parents.shape)}, expected [T]")
+    T = parents.numel()
+    n_seq = T if q_start is None else q_start.numel() - 1
+    lp, sp, mq = _paged_batch(n_seq, T, kv_len, q_start, max_q)
+    device = _here(parents, q_start, kv_len, masks, positions)
+    handle, on = _run_on(stream, device)
+    if masks is None:
+        masks = _empty(on, (T, (mq + 63) // 64), torch.int64, device)
+    if masks.dtype is not torch.int64 or masks.dim() != 2 or masks.shape[0] != T or not masks.is_contiguous():
+        raise ValueError(f"masks {masks.dtype} {tuple(masks.shape)}: expected contiguous int64 [{T}, words]")
+    if positions is None:
+        positions = _empty(on, T, torch.int32, device)
+    code = (_lib or lib()).moe_tree_masks(_ints32(parents, "parents"), T, n_seq, sp, mq, lp, masks.data_ptr(), masks.shape[1],
+                                          _ints32(positions, "positions", T), handle)
+    if code:
+        _check(code, "moe_tree_masks")
+    if on is not None:
+        on.used(parents, q_start, kv_len, masks, positions)
+    return masks, positions
+
+
+def moe_paged_attention_workspace_bytes(T: int, n_seq: int, n_heads: int, n_kv: int, head_dim: int, max_q: int,
+                                        max_kv: int) -> int:
+    return int((_lib or lib()).moe_paged_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, max_q, max_kv))
+
+
+def moe_paged_attention(q, k_pool, v_pool, table, kv_len, q_start=None, max_q: int | None = None, max_kv: int | None = None,
+                        window: int = 0, sinks: int = 0, tree=None, scale: float | None = None, out=None, workspace=None,
+                        stream=None):
+    """Causal attention of the tokens' queries (fp32 or bf16 [T, n_heads, d]) over a paged cache (pools as of paged_cache,
+    table int32 [n_seq, max_pages], kv_len int32 [n_seq] with the tokens), with window > 0 over the last `window` positions
+    and the first `sinks`; q_start int32 [n_seq + 1]: sequence b's rows, None for one token each; max_q, max_kv: most tokens
+    and positions of a sequence (T and what the table holds by default -- the launches go by them, so tight ones are
+    faster).  tree: masks of drafted tokens as of moe_tree_masks.  Scale 1 / sqrt(d) by default.  Returns out
+    [T, n_heads, d] of q's type; rows from q_start[-1] on are not written."""
+    import torch
+    kpp, kps = _pool(k_pool, "k_pool")
+    vpp, vps = _pool(v_pool, "v_pool", k_pool.shape)
+    n_pages, n_kv, page, d = k_pool.shape
+    tp, n_seq, max_pages = _page_table(table)
+    if q.dim() != 3:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [T, n_heads, {d}]")
+    T, n_heads, _ = q.shape
+    dtype = q.dtype
+    max_kv = max_pages * page if max_kv is None else max_kv
+    for name, n in (("window", window), ("sinks", sinks), ("max_kv", max_kv)):
+        if not 0 <= n <= 1 << 30:
+            raise ValueError(f"{name}={n} outside [0, 2^30]")
+    qp, qs = _rows(q, "q", n_heads, d)
+    lp, sp, mq = _paged_batch(n_seq, T, kv_len, q_start, max_q)
+    device = _here(q, k_pool, v_pool, table, kv_len, q_start, tree, out, workspace)
+    words = mp = 0
+    if tree is not None:
+        if tree.dtype is not torch.int64 or tree.dim() != 2 or tree.shape[0] != T or not tree.is_contiguous():
+            raise ValueError(f"tree {tree.dtype} {tuple(tree.shape)}: expected contiguous int64 [{T}, words]")
+        mp, words = tree.data_ptr(), tree.shape[1]
+    handle, on = _run_on(stream, device)
+    if out is None:
+        out = _empty(on, (T, n_heads, d), dtype, device)
+    op, os_ = _rows(out, "out", n_heads, d, T, dtype)
+    if workspace is None:
+        n = moe_paged_attention_workspace_bytes(T, n_seq, n_heads, n_kv, d, mq, max_kv)
+        workspace = _empty(on, max(n, 256), torch.uint8, device)
+    code = (_lib or lib()).moe_paged_attention(qp, _float_code(dtype, "q"), qs, kpp, vpp, kps, vps, n_pages, page, tp, max_pages,
+                                               T, n_seq, n_heads, n_kv, d, sp, mq, lp, max_kv, window, sinks, mp or None, words,
+                                               d ** -0.5 if scale is None else scale, op, os_, _dev(workspace, "workspace"),
+                                               workspace.nbytes, handle)
+    if code:
+        _check(code, "moe_paged_attention")
+    if on is not None:
+        on.used(q, k_pool, v_pool, table, kv_len, q_start, tree, out, workspace)
     return out
 
 

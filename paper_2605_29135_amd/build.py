@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmoe_budget.so")
 SOURCES = ["kernels.hip", "batch_ffn.hip", "prefill.hip", "attention.hip", "kv4_store.hip", "kv4_attention.hip",
-           "matvec_int4.hip", "attention_int4.hip", "residency.cpp", "residency_dev.hip", "capi.cpp", "stack.cpp",
+           "paged_store.hip", "paged_attention.hip", "matvec_int4.hip", "attention_int4.hip", "residency.cpp", "residency_dev.hip", "capi.cpp", "stack.cpp",
            "analysis.cpp"]
 # Host-only sources (the host tier's CPU GEMVs): built by the host compiler, then linked into the library.
 HOST_SOURCES = ["host_ffn.cpp"]

@@ -10,6 +10,7 @@
 
 #include "internal.h"
 #include "kv4.h"
+#include "paged.h"
 #include "../../include/moe_budget.h"
 
 namespace moe {
@@ -102,10 +103,10 @@ int moe_sync_check(void *stream) {
         return fail_hip(e, "reading device error flags");
     if (v) {
         if ((e = hipMemset(flags, 0, sizeof v)) != hipSuccess) return fail_hip(e, "clearing device error flags");
-        if (v & moe::kErrRange) return fail(MOE_ERR_RANGE, "an expert id was outside [0, E), or a sequence outside its cache or token array");
+        if (v & moe::kErrRange) return fail(MOE_ERR_RANGE, "an expert id was outside [0, E), or a sequence, page or slot outside its cache or token array");
         if (v & moe::kErrNonfinite) return fail(MOE_ERR_NONFINITE, "a router logit, or a key or value to be quantised, was not finite");
         if (v & moe::kErrNotResident) return fail(MOE_ERR_NOT_RESIDENT, "an expert had no slot");
-        if (v & moe::kErrBudget) return fail(MOE_ERR_BUDGET, "a device lookup needed more experts than slots");
+        if (v & moe::kErrBudget) return fail(MOE_ERR_BUDGET, "a device lookup needed more experts than slots, or a batch more pages than were free");
     }
     moe::clear_error();
     return MOE_OK;
@@ -407,6 +408,216 @@ int moe_kv4_attention(const void *q, int dtype, long long q_stride, const void *
     return finish_launch(moe::launch_kv4_attention(q, dtype, q_stride, cache, batch, n_heads, n_kv, head_dim, window, scale,
                                                    out, out_stride, workspace, eflags, static_cast<hipStream_t>(stream)),
                          "kv4 attention launch");
+}
+
+namespace {
+
+int page_shift(int page_size) {
+    int s = 0;
+    while ((1 << s) < page_size) ++s;
+    return s;
+}
+
+// What the calls on a paged cache ask of its pages.
+int check_pages(const char *what, int n_pages, int page_size) {
+    if (page_size < MOE_PAGE_MIN || page_size > MOE_PAGE_MAX || (page_size & (page_size - 1)))
+        return fail(MOE_ERR_INVALID_ARG, "%s: page_size must be a power of two from %d to %d (page_size=%d)", what, MOE_PAGE_MIN,
+                    MOE_PAGE_MAX, page_size);
+    if (n_pages < 1 || (long long)n_pages * page_size >= 1ll << 31)
+        return fail(MOE_ERR_INVALID_ARG, "%s: need 1 <= n_pages and fewer than 2^31 slots (n_pages=%d of %d)", what, n_pages,
+                    page_size);
+    return MOE_OK;
+}
+int check_max_pages(const char *what, int max_pages, int page_size) {
+    if (max_pages < 1 || (long long)max_pages * page_size > MOE_PAGED_MAX_POS)
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_pages=%d of %d positions outside [1, %d positions]", what, max_pages, page_size,
+                    MOE_PAGED_MAX_POS);
+    return MOE_OK;
+}
+int check_paged_heads(const char *what, int n_kv, int head_dim) {
+    if (n_kv < 1 || n_kv > 65535) return fail(MOE_ERR_INVALID_ARG, "%s: n_kv=%d outside [1, 65535]", what, n_kv);
+    if (head_dim != 64 && head_dim != 128 && head_dim != 192 && head_dim != 256)
+        return fail(MOE_ERR_INVALID_ARG, "%s: head_dim must be 64, 128, 192 or 256 (head_dim=%d)", what, head_dim);
+    return MOE_OK;
+}
+int check_pool(const char *what, const void *k, const void *v, long long k_stride, long long v_stride, int n_kv, int page_size,
+               int head_dim) {
+    if (!k || !v) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    const long long each = (long long)n_kv * page_size * head_dim;
+    auto bad = [&](const void *p, long long stride) { return !aligned16(p) || stride < each || stride > 1ll << 40 || stride % 8; };
+    if (bad(k, k_stride) || bad(v, v_stride))
+        return fail(MOE_ERR_INVALID_ARG, "%s: the pools need 16-byte aligned pages of at least n_kv * page_size * head_dim elements",
+                    what);
+    return MOE_OK;
+}
+// And of the batch; max_q becomes 1 without q_start.
+int check_paged_batch(const char *what, int T, int n_seq, int group, const int32_t *q_start, int *max_q) {
+    if (T < 0 || T > (1 << 30)) return fail(MOE_ERR_INVALID_ARG, "%s: T=%d outside [0, 2^30]", what, T);
+    if (n_seq < 0 || n_seq > 65535) return fail(MOE_ERR_INVALID_ARG, "%s: n_seq=%d outside [0, 65535]", what, n_seq);
+    if (!q_start) {
+        if (T != n_seq) return fail(MOE_ERR_INVALID_ARG, "%s: without q_start T must be n_seq (%d, %d)", what, T, n_seq);
+        *max_q = 1;
+    }
+    if (T > 0 && (*max_q < 1 || (long long)*max_q * group > (1 << 24)))
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_q=%d outside [1, 2^24 / (n_heads / n_kv)]", what, *max_q);
+    return MOE_OK;
+}
+int check_paged_attention(int T, int n_seq, int n_heads, int n_kv, int head_dim, const int32_t *q_start, int *max_q, int max_kv) {
+    const char *what = "paged attention";
+    const int st = check_paged_heads(what, n_kv, head_dim);
+    if (st != MOE_OK) return st;
+    if (n_heads < 1 || n_heads % n_kv)
+        return fail(MOE_ERR_INVALID_ARG, "%s: n_heads must be a multiple of n_kv (%d, %d)", what, n_heads, n_kv);
+    if (max_kv < 1 || max_kv > MOE_PAGED_MAX_POS)
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_kv=%d outside [1, %d]", what, max_kv, MOE_PAGED_MAX_POS);
+    return check_paged_batch(what, T, n_seq, n_heads / n_kv, q_start, max_q);
+}
+bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+
+int moe_page_tables(const int32_t *kv_len, const int32_t *n_new, int n_seq, int T, int page_size, int n_pages,
+                    const int32_t *free_pages, int n_free, const int32_t *free_first, int32_t *table, int max_pages,
+                    int32_t *kv_len_out, int32_t *q_start, int32_t *positions, int32_t *slots, int32_t *free_next, void *stream) {
+    const char *what = "page tables";
+    int st = check_pages(what, n_pages, page_size);
+    if (st == MOE_OK) st = check_max_pages(what, max_pages, page_size);
+    if (st != MOE_OK) return st;
+    if (n_seq < 0 || n_seq > 65535) return fail(MOE_ERR_INVALID_ARG, "%s: n_seq=%d outside [0, 65535]", what, n_seq);
+    if (T < 0 || T > (1 << 30)) return fail(MOE_ERR_INVALID_ARG, "%s: T=%d outside [0, 2^30]", what, T);
+    if (n_free < 0) return fail(MOE_ERR_INVALID_ARG, "%s: n_free=%d", what, n_free);
+    if ((n_seq && (!kv_len || !table || !kv_len_out)) || !q_start || (n_free && !free_pages))
+        return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    for (const void *p : {(const void *)kv_len, (const void *)n_new, (const void *)free_pages, (const void *)free_first,
+                          (const void *)table, (const void *)kv_len_out, (const void *)q_start, (const void *)positions,
+                          (const void *)slots, (const void *)free_next})
+        if (!aligned4(p)) return fail(MOE_ERR_INVALID_ARG, "%s: arrays must be 4-byte aligned", what);
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    moe::paged::TableArgs a;
+    a.kv_len = kv_len;
+    a.n_new = n_new;
+    a.free_pages = free_pages;
+    a.free_first = free_first;
+    a.table = table;
+    a.kv_len_out = kv_len_out;
+    a.q_start = q_start;
+    a.positions = positions;
+    a.slots = slots;
+    a.free_next = free_next;
+    a.n_seq = n_seq;
+    a.T = T;
+    a.max_pages = max_pages;
+    a.shift = page_shift(page_size);
+    a.n_pages = n_pages;
+    a.n_free = n_free;
+    return finish_launch(moe::launch_page_tables(a, eflags, static_cast<hipStream_t>(stream)), "page tables launch");
+}
+
+int moe_paged_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T, int n_kv,
+                     int head_dim, const int32_t *slots, void *k_pool, void *v_pool, long long k_page_stride,
+                     long long v_page_stride, int n_pages, int page_size, void *stream) {
+    const char *what = "paged append";
+    int st = check_paged_heads(what, n_kv, head_dim);
+    if (st == MOE_OK) st = check_pages(what, n_pages, page_size);
+    if (st != MOE_OK) return st;
+    if (dtype != MOE_F32 && dtype != MOE_BF16)
+        return fail(MOE_ERR_INVALID_ARG, "%s: dtype must be MOE_F32 or MOE_BF16 (dtype=%d)", what, dtype);
+    if (T < 0 || T > (1 << 30)) return fail(MOE_ERR_INVALID_ARG, "%s: T=%d outside [0, 2^30]", what, T);
+    if (T == 0) return MOE_OK;
+    if (!k || !v || !slots) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned4(slots)) return fail(MOE_ERR_INVALID_ARG, "%s: slots must be 4-byte aligned", what);
+    if (!rows_ok(k, k_stride, n_kv, head_dim, dtype) || !rows_ok(v, v_stride, n_kv, head_dim, dtype))
+        return fail(MOE_ERR_INVALID_ARG, "%s: k and v need 16-byte aligned rows of at least n_kv * head_dim elements", what);
+    if ((st = check_pool(what, k_pool, v_pool, k_page_stride, v_page_stride, n_kv, page_size, head_dim)) != MOE_OK) return st;
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::paged::Pages pages{static_cast<uint16_t *>(k_pool), static_cast<uint16_t *>(v_pool), k_page_stride,
+                                  v_page_stride, n_pages, page_shift(page_size)};
+    return finish_launch(moe::launch_paged_append(k, v, dtype, k_stride, v_stride, T, n_kv, head_dim, slots, pages, eflags,
+                                                  static_cast<hipStream_t>(stream)),
+                         "paged append launch");
+}
+
+int moe_tree_masks(const int32_t *parents, int T, int n_seq, const int32_t *q_start, int max_q, const int32_t *kv_len,
+                   uint64_t *masks, int words, int32_t *positions, void *stream) {
+    const char *what = "tree masks";
+    int st = check_paged_batch(what, T, n_seq, 1, q_start, &max_q);
+    if (st != MOE_OK) return st;
+    if (T == 0 || n_seq == 0) return MOE_OK;
+    if (max_q > MOE_MAX_TREE) return fail(MOE_ERR_INVALID_ARG, "%s: max_q=%d, a tree has at most %d tokens", what, max_q, MOE_MAX_TREE);
+    if (words < 1 || words > MOE_MAX_TREE / 64 || words * 64 < max_q)
+        return fail(MOE_ERR_INVALID_ARG, "%s: %d words a row, max_q=%d needs at least %d, at most %d", what, words, max_q,
+                    (max_q + 63) / 64, MOE_MAX_TREE / 64);
+    if (!parents || !masks) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned4(parents) || !aligned4(q_start) || !aligned4(kv_len) || !aligned4(positions) || reinterpret_cast<uintptr_t>(masks) % 8)
+        return fail(MOE_ERR_INVALID_ARG, "%s: arrays must be 4-byte aligned, masks 8-byte", what);
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::kv4::Batch batch{q_start, kv_len, T, n_seq, max_q, 0};
+    return finish_launch(moe::launch_tree_masks(parents, batch, words, masks, positions, eflags, static_cast<hipStream_t>(stream)),
+                         "tree masks launch");
+}
+
+size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q, int max_kv) {
+    // (a caller without q_start may pass any max_q: a plan for 1 is then what runs)
+    const int32_t some = 0;
+    max_q = std::max(max_q, 1);
+    if (check_paged_attention(T, n_seq, n_heads, n_kv, head_dim, &some, &max_q, max_kv) != MOE_OK || T == 0 || n_seq == 0)
+        return 0;
+    size_t n = moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, std::min(max_q, T), max_kv);
+    if (T == n_seq) n = std::max(n, moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, 1, max_kv));
+    return n;
+}
+
+int moe_paged_attention(const void *q, int dtype, long long q_stride, const void *k_pool, const void *v_pool,
+                        long long k_page_stride, long long v_page_stride, int n_pages, int page_size, const int32_t *table,
+                        int max_pages, int T, int n_seq, int n_heads, int n_kv, int head_dim, const int32_t *q_start, int max_q,
+                        const int32_t *kv_len, int max_kv, int window, int sinks, const uint64_t *tree, int tree_words,
+                        float scale, void *out, long long out_stride, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *what = "paged attention";
+    int st = check_paged_attention(T, n_seq, n_heads, n_kv, head_dim, q_start, &max_q, max_kv);
+    if (st == MOE_OK) st = check_pages(what, n_pages, page_size);
+    if (st == MOE_OK) st = check_max_pages(what, max_pages, page_size);
+    if (st != MOE_OK) return st;
+    if (dtype != MOE_F32 && dtype != MOE_BF16)
+        return fail(MOE_ERR_INVALID_ARG, "%s: dtype must be MOE_F32 or MOE_BF16 (dtype=%d)", what, dtype);
+    if (max_kv > max_pages * page_size)
+        return fail(MOE_ERR_INVALID_ARG, "%s: max_kv=%d, a row of the table has %d positions", what, max_kv, max_pages * page_size);
+    if (window < 0 || window > (1 << 30)) return fail(MOE_ERR_INVALID_ARG, "%s: window=%d outside [0, 2^30]", what, window);
+    if (sinks < 0 || sinks > (1 << 30)) return fail(MOE_ERR_INVALID_ARG, "%s: sinks=%d outside [0, 2^30]", what, sinks);
+    if (!(std::fabs(scale) <= 4294967296.f))
+        return fail(MOE_ERR_INVALID_ARG, "%s: the scale's magnitude must be at most 2^32", what);
+    if (T == 0 || n_seq == 0) return MOE_OK;
+    max_q = std::min(max_q, T);
+    if (tree) {
+        if (tree_words < 1 || tree_words > (1 << 20) || tree_words * 64ll < max_q)
+            return fail(MOE_ERR_INVALID_ARG, "%s: a tree of %d words a row, max_q=%d needs at least %d", what, tree_words, max_q,
+                        (max_q + 63) / 64);
+        if (window && window < max_q)
+            return fail(MOE_ERR_INVALID_ARG, "%s: with a tree the window must be 0 or at least max_q (%d, %d)", what, window, max_q);
+        if (reinterpret_cast<uintptr_t>(tree) % 8) return fail(MOE_ERR_INVALID_ARG, "%s: tree must be 8-byte aligned", what);
+    }
+    if (!q || !out || !table || !kv_len) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    if (!aligned4(table) || !aligned4(kv_len) || !aligned4(q_start))
+        return fail(MOE_ERR_INVALID_ARG, "%s: table, kv_len and q_start must be 4-byte aligned", what);
+    if (!rows_ok(q, q_stride, n_heads, head_dim, dtype) || !rows_ok(out, out_stride, n_heads, head_dim, dtype))
+        return fail(MOE_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows of at least n_heads * head_dim elements", what);
+    if ((st = check_pool(what, k_pool, v_pool, k_page_stride, v_page_stride, n_kv, page_size, head_dim)) != MOE_OK) return st;
+    const size_t need = moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, max_q, max_kv);
+    if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+        return fail(MOE_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes (%zu given)", what, need,
+                    workspace ? workspace_bytes : size_t(0));
+    int *eflags = moe::device_error_flags();
+    if (!eflags) return fail(MOE_ERR_HIP, "device error flags unavailable");
+    const moe::paged::Pages pages{static_cast<uint16_t *>(const_cast<void *>(k_pool)),
+                                  static_cast<uint16_t *>(const_cast<void *>(v_pool)), k_page_stride, v_page_stride, n_pages,
+                                  page_shift(page_size)};
+    const moe::kv4::Batch batch{q_start, kv_len, T, n_seq, max_q, max_kv};
+    return finish_launch(moe::launch_paged_attention(q, dtype, q_stride, pages, table, max_pages, batch, n_heads, n_kv, head_dim,
+                                                     window, sinks, tree, tree_words, scale, out, out_stride, workspace, eflags,
+                                                     static_cast<hipStream_t>(stream)),
+                         "paged attention launch");
 }
 
 size_t moe_matvec_int4_workspace_bytes(int T, int K) {

@@ -198,6 +198,22 @@ hipError_t launch_kv4_attention(const void *q, int dtype, long long q_stride, co
                                 int n_heads, int n_kv, int d, int window, float scale, void *out, long long out_stride,
                                 void *workspace, int *err, hipStream_t s);
 
+// Paged bf16 key/value cache (paged_store.hip, paged_attention.hip; Pages and TableArgs in paged.h).
+namespace paged {
+struct Pages;
+struct TableArgs;
+}
+hipError_t launch_page_tables(const paged::TableArgs &a, int *err, hipStream_t s);
+hipError_t launch_paged_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T,
+                               int n_kv, int d, const int32_t *slots, const paged::Pages &pages, int *err, hipStream_t s);
+hipError_t launch_tree_masks(const int32_t *parents, const kv4::Batch &batch, int words, uint64_t *masks, int32_t *positions,
+                             int *err, hipStream_t s);
+size_t paged_attention_workspace_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv);
+hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, const paged::Pages &pages,
+                                  const int32_t *table, int max_pages, const kv4::Batch &batch, int n_heads, int n_kv, int d,
+                                  int window, int sinks, const uint64_t *tree, int tree_words, float scale, void *out,
+                                  long long out_stride, void *workspace, int *err, hipStream_t s);
+
 // int4-g128 matrix-vector products (matvec_int4.hip): y = add + W h, h = x or its RMS norm; y may be add.
 size_t matvec_int4_workspace_bytes(int T, int K);
 hipError_t launch_matvec_int4(const float *x, const void *w, int T, int N, int K, const float *add, float *y, bool norm,

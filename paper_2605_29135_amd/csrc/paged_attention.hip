@@ -1,0 +1,543 @@
+// paged_attention.hip -- attention over a paged bf16 cache: one or many tokens per sequence, a window with first positions
+// that stay visible, trees of drafted tokens.
+//
+// Scores are formed transposed (positions x rows) by the 16x16x32 matrix product, so that a lane holds one row's
+// probabilities of the positions that are its operand of the value product (they stay in registers), and the outputs as
+// dims x rows, so that a row's running maximum and sum belong to its lane.  The value product wants eight positions of
+// one dim in a lane, the cache has eight dims of a position in a row: a lane loads the same dims of eight positions and
+// turns them in registers, one operation per pair.  Which dim is which row of the product is free: a lane's own eight
+// (or four) dims lie in as many products.
+//
+// Exact products of bf16, sums in fp32.  fp32 queries enter as three bf16 terms (2^-25 of the element), probabilities as
+// three (fp32) or two (bf16: 2^-17) of them: where few rows meet the cache the products cost nothing beside its bytes.
+//
+// A row is a (token, query head of the group) pair; a wave takes NT tiles of 16 rows over every fourth block of 32
+// positions, and the block's waves join their (max, sum, output) through LDS.  With few rows the positions are split over
+// more blocks (grid), whose partial results a second launch joins.  Blocks of positions that no token of the sequence sees
+// (between the first positions and the window) are stepped over: pages for them need not exist.
+#include "attend_common.h"
+#include "device_common.h"
+#include "internal.h"
+#include "paged.h"
+
+#include <algorithm>
+
+namespace moe {
+namespace {
+
+using namespace attend;
+using namespace paged;
+
+constexpr int kPos = 32;  // positions per block
+constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
+constexpr int kTarget = 512;  // blocks that fill the device, where rows and heads alone give fewer
+
+struct PagedArgs {
+    const void *q;
+    void *out;
+    Pages pages;
+    const int32_t *table;   // [n_seq][max_pages]
+    const uint32_t *tree;   // [T][tree_words] bits of the drafted tokens that a token sees, or NULL
+    float *part;            // [unit][head][tiles][rows of a tile][d + 4]: unnormalised output, maximum, sum, unit
+    long long q_stride, out_stride;
+    int max_pages, tree_words;
+    int n_kv, group, window, sinks;
+    int tiles;              // row tiles of the largest sequence
+    float unit;             // from scores to log2 units, positive
+    int negate;             // the scale's sign
+    Split split;
+    Batch batch;
+    int *err;
+};
+
+// The positions that tokens of a sequence see, as blocks: the first `sink` ones and those from `first` on.
+struct Seen {
+    int sink, first, count;  // blocks [0, sink) and [first, first + count - sink)
+    int from;                // the first position behind the sinks that some token sees
+    __device__ __forceinline__ int block(int v) const { return v < sink ? v : v - sink + first; }
+};
+__device__ __forceinline__ Seen seen(const Seq &s, int window, int sinks) {
+    Seen r{0, 0, 0, 0};
+    if (s.n == 0 || s.len == 0) return r;
+    // (a drafted token stands no earlier than behind the cached ones)
+    r.from = window ? max(0, s.len - s.n - window + 1) : 0;
+    r.first = r.from / kPos;
+    r.sink = min((min(sinks, r.from) + kPos - 1) / kPos, r.first);
+    r.count = r.sink + (s.len - 1) / kPos + 1 - r.first;
+    return r;
+}
+__device__ __forceinline__ Piece split_piece(const PagedArgs &a, int want, bool by_unit, int *err) {
+    return find_piece(a.batch, a.split, [&](const Seq &s) { return seen(s, a.window, a.sinks).count; }, want, by_unit, err);
+}
+// This block's piece: grid (row tiles, key/value head, sequence), or (key/value head, row tiles, pieces).
+__device__ __forceinline__ Piece this_piece(const PagedArgs &a, int *err) {
+    if (a.split.target) return split_piece(a, blockIdx.z, true, blockIdx.z == 0 ? err : nullptr);
+    Piece p{};
+    p.seq = blockIdx.z;
+    p.count = 1;
+    p.s = sequence(a.batch, p.seq);
+    if (p.s.bad && err && (threadIdx.x & 63) == 0) atomicOr(err, kErrRange);
+    return p;
+}
+
+// What a row sees: positions up to `hi` that are above `lo` or among the first; with a tree, of the drafted tokens those
+// whose bits are set (`drafted` of them: none for a row of padding).
+struct RowView {
+    int hi, lo, drafted;
+    const uint32_t *bits;
+};
+__device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, int i) {
+    const int cached = s.len - s.n, row = cached + i;
+    RowView v{row, row - a.window, 0, nullptr};
+    if (a.tree) {
+        v.bits = a.tree + size_t(s.t0 + i) * a.tree_words;
+        int set = 0;
+        for (int w = 0; 32 * w < s.n; ++w) set += __popc(v.bits[w] & (s.n - 32 * w < 32 ? (1u << (s.n - 32 * w)) - 1 : ~0u));
+        v.hi = row < 0 ? -1 : cached - 1;
+        v.lo = cached - 1 + set - a.window;
+        v.drafted = row < 0 ? 0 : s.n;
+    }
+    if (!a.window) v.lo = -1;
+    return v;
+}
+// Bit k: whether the row sees position p + 16 (k / 4) + k % 4.
+__device__ __forceinline__ uint32_t row_sees(const PagedArgs &a, const Seq &s, const RowView &v, int p) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int at = p + 16 * (k >> 2) + (k & 3);
+        m |= uint32_t((at <= v.hi) & ((at > v.lo) | (at < a.sinks))) << k;
+    }
+    if (a.tree)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int j = p + 16 * (k >> 2) + (k & 3) - (s.len - s.n);
+            if (j >= 0 && j < v.drafted) m |= (v.bits[j >> 5] >> (j & 31) & 1u) << k;
+        }
+    return m;
+}
+// Whether every one of rows i0..i1 sees all of positions p..p + count - 1.
+__device__ __forceinline__ bool all_visible(const PagedArgs &a, const Seq &s, int i0, int i1, int p, int count) {
+    const int cached = s.len - s.n, end = a.tree ? cached : cached + i0 + 1;
+    const int last = a.tree ? s.len - 1 : cached + i1;  // (a drafted token's position is at most the last one)
+    return cached + i0 >= 0 && p + count <= end && (!a.window || p > last - a.window || p + count <= a.sinks);
+}
+
+// The blocks that some of rows row..row_end - 1 sees, and of these (numbered as there) the piece's share: first, end.  Pieces
+// are cut by the sequence's blocks z.  Where rows see more first blocks than z has (their window has left them behind),
+// z has no gap and its numbers are the blocks'.
+__device__ __forceinline__ int2 tile_blocks(const PagedArgs &a, const Piece &piece, const Seen &z, int row, int row_end, Seen &t) {
+    const Seq &s = piece.s;
+    const int p_first = s.len - s.n + row / a.group;
+    const int p_last = a.tree ? s.len - 1 : s.len - s.n + (row_end - 1) / a.group;
+    t = z;
+    if (p_last < 0 || z.count == 0) return make_int2(0, 0);
+    if (a.window && !a.tree) {  // (rows of a tree stand in no order)
+        t.from = max(0, p_first - a.window + 1);
+        t.first = t.from / kPos;
+        t.sink = min((min(a.sinks, t.from) + kPos - 1) / kPos, t.first);
+    }
+    const int cut = piece.split * piece.chunk, first = t.first - z.first + z.sink, skip = first - t.sink;
+    const int end = z.sink + p_last / kPos + 1 - z.first;
+    const int cut_end = piece.split == piece.count - 1 ? end : min(end, cut + piece.chunk);
+    return make_int2(cut < t.sink ? cut : max(cut, first) - skip, max(min(cut_end, t.sink), cut_end - skip));
+}
+
+// x as TERMS bf16 operands, each rounding what the ones before leave.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TERMS]) {
+    float rest[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rest[e] = x[e];
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[e] = pack_bf16(rest[2 * e], rest[2 * e + 1]);
+            if (k + 1 < TERMS) {
+                rest[2 * e] -= low_half(w[e]);
+                rest[2 * e + 1] -= high_half(w[e]);
+            }
+        }
+        t[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+// Where a pair of bf16 is not finite: all ones in its half.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces).
+//
+// A value that is not finite would reach every row of the tile (0 times it is NaN): a wave that ends with outputs that are
+// not finite goes over its positions once more, with such values as zeros and the outputs of the rows that see one NaN.
+template <int NG, int NT, bool F32>
+__global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_kernel(PagedArgs a) {
+    constexpr int d = NG * 64, QT = F32 ? 3 : 1, PT = F32 ? 3 : 2, ROWS = 16;
+    constexpr int VE = NG % 2 ? 4 : 8, VG = d / (16 * VE);  // dims of a lane per group of products, groups
+    __shared__ float4 out_sh[kAttWaves][ROWS][d / 4 + 1];
+    __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
+    const int tile = a.split.target ? blockIdx.y : blockIdx.x, h = a.split.target ? blockIdx.x : blockIdx.y;
+    const Piece piece = this_piece(a, tile == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
+    if (piece.count == 0) return;
+    const Seq &s = piece.s;
+    const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
+    if (row0 >= rows) return;
+    const int i_first = row0 / G, i_last = min(s.n - 1, (row0 + ROWS * NT - 1) / G);
+    const Seen all = seen(s, a.window, a.sinks);
+    Seen z;
+    const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS * NT, rows), z);
+    const int32_t *table = a.table + size_t(piece.seq) * a.max_pages;
+    const int page_mask = (1 << a.pages.shift) - 1;
+
+    // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.
+    uint4 kc[2][2 * NG];
+    uint32_t vc[VG][8][VE / 2];
+    // Half a block lies in one page.  `there`: bits of the halves (four each) of which some token sees a position, and whose
+    // page is there; the others are read from the first page, and none of it is used.
+    uint32_t there = 0;
+    int page_at[2] = {0, 0};
+    auto find = [&](int b) __attribute__((always_inline)) {
+        there = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int p = b * kPos + 16 * u;
+            const bool needed = p < s.len && (p < a.sinks || p + 16 > all.from);
+            const int32_t page = needed ? table[p >> a.pages.shift] : 0;
+            const bool ok = uint32_t(page) < uint32_t(a.pages.n_pages);
+            if (!ok && lane == 0) atomicOr(a.err, kErrRange);
+            page_at[u] = ok ? page : 0;
+            there |= needed && ok ? 0xfu << (4 * u) : 0u;
+        }
+    };
+    auto row_at = [&](int p) { return ((size_t(h) << a.pages.shift) + (p & page_mask)) * d; };
+    auto load_k = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint16_t *src = a.pages.k + page_at[u] * a.pages.k_stride + row_at(b * kPos + 16 * u + n) + 8 * c;
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j) kc[u][j] = dev::load16(reinterpret_cast<const uint8_t *>(src + 32 * j));
+        }
+    };
+    auto load_v = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int u = i >> 2;
+            const uint16_t *src = a.pages.v + page_at[u] * a.pages.v_stride + row_at(b * kPos + 16 * u + 4 * c + (i & 3)) + VE * n;
+#pragma unroll
+            for (int g = 0; g < VG; ++g) {
+                if constexpr (VE == 8) {
+                    const uint4 w = dev::load16(reinterpret_cast<const uint8_t *>(src + 128 * g));
+                    vc[g][i][0] = w.x, vc[g][i][1] = w.y, vc[g][i][2] = w.z, vc[g][i][3] = w.w;
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(src + 64 * g);
+                    vc[g][i][0] = w.x, vc[g][i][1] = w.y;
+                }
+            }
+        }
+    };
+
+    // The tile's rows: their queries as operands (k = dims), what they see.  A row past the last repeats it and is not stored.
+    auto row_of = [&](int t) { return min(row0 + 16 * t + n, rows - 1); };
+    bf16x8 bq[NT][2 * NG][QT];
+    RowView view[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row_of(t), i = row / G;
+        const size_t at = size_t(s.t0 + i) * a.q_stride + size_t(h * G + row - i * G) * d + 8 * c;
+        view[t] = row_view(a, s, i);
+#pragma unroll
+        for (int j = 0; j < 2 * NG; ++j) {
+            if constexpr (F32) {
+                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 32 * j);
+                const float4 u = p[0], w = p[1];
+                const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+                split_terms<QT>(x, bq[t][j]);
+            } else {
+                bq[t][j][0] = __builtin_bit_cast(bf16x8, dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * j)));
+            }
+        }
+    }
+    const float sign = a.negate ? -1.f : 1.f;
+
+    floatx4 acc[NT][4 * NG];
+    float mx[NT], sum[NT];
+#pragma unroll 1
+    for (int careful = 0;; ++careful) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            mx[t] = -INFINITY;
+            sum[t] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (range.x + wave < range.y) {
+            const int b = z.block(range.x + wave);
+            find(b);
+            load_k(b);
+            load_v(b);
+        }
+#pragma unroll 1
+        for (int v = range.x + wave; v < range.y; v += kAttWaves) {
+            const int b = z.block(v), next = z.block(min(v + kAttWaves, range.y - 1));
+            const uint32_t there_mask = there;
+            const bool full = there_mask == 0xff && all_visible(a, s, i_first, i_last, b * kPos, kPos);
+            // ---- scores
+            float p[NT][8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    floatx4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = QT - 1; k >= 0; --k)
+#pragma unroll
+                        for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[u][j]), bq[t][j][k], y);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[t][4 * u + r] = y[r] * sign;
+                }
+            find(next);
+            load_k(next);
+            // ---- softmax
+            uint32_t sees[NT];
+            bf16x8 bp[NT][PT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                sees[t] = 0xff;
+                if (!full) {
+                    sees[t] = row_sees(a, s, view[t], b * kPos + 4 * c) & there_mask;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) p[t][k] = sees[t] >> k & 1 ? p[t][k] : -INFINITY;
+                }
+                float top = p[t][0];
+#pragma unroll
+                for (int k = 1; k < 8; ++k) top = fmaxf(top, p[t][k]);
+                const float was = mx[t], now = fmaxf(was, max_over_c(top)), to = now == -INFINITY ? 0.f : now;
+                if (__any(now > was)) {
+                    const float f = __builtin_amdgcn_exp2f((was - to) * a.unit);
+                    mx[t] = now;
+                    sum[t] *= f;
+#pragma unroll
+                    for (int i = 0; i < 4 * NG; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[t][i][r] *= f;
+                }
+                // (differences first: right at any size of the scores)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    p[t][k] = __builtin_amdgcn_exp2f((p[t][k] - to) * a.unit);
+                    sum[t] += p[t][k];
+                }
+                split_terms<PT>(p[t], bp[t]);
+            }
+            // ---- values
+            if (!full) {
+                // Positions that no token sees may hold anything: zeros.
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int at = b * kPos + 16 * (i >> 2) + 4 * c + (i & 3);
+                    const bool held = (there_mask >> i & 1) & (at < s.len) & ((at >= all.from) | (at < a.sinks));
+#pragma unroll
+                    for (int g = 0; g < VG; ++g)
+#pragma unroll
+                        for (int w = 0; w < VE / 2; ++w) vc[g][i][w] = held ? vc[g][i][w] : 0;
+                }
+            }
+            bf16x8 seen_by[NT];
+            if (careful) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = (sees[t] >> (2 * e) & 1) * 0x3f80u | (sees[t] >> (2 * e + 1) & 1) * 0x3f800000u;
+                    seen_by[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < VG; ++g)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        w[k] = __builtin_amdgcn_perm(vc[g][2 * k + 1][e / 2], vc[g][2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+                    const int i = g * VE + e;
+                    if (careful) {
+                        uint32_t f[4];
+                        bool any = false;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            f[k] = not_finite(w[k]);
+                            w[k] &= ~f[k];
+                            any |= f[k] != 0;
+                            f[k] &= 0x3f803f80u;
+                        }
+                        if (__any(any))
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                const floatx4 met = mfma(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])), seen_by[t],
+                                                         floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (met[r] > 0.f) acc[t][i][r] = NAN;
+                            }
+                    }
+                    const bf16x8 va = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int k = PT - 1; k >= 0; --k) acc[t][i] = mfma(va, bp[t][k], acc[t][i]);
+                }
+            load_v(next);
+        }
+        bool off = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4 * NG; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
+        if (careful || !__any(off)) break;
+    }
+
+    // Join the waves, one tile of rows at a time.
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float l = sum_over_c(sum[t]);
+        if (t) __syncthreads();
+        if (c == 0) {
+            max_sh[wave][n] = mx[t];
+            sum_sh[wave][n] = l;
+        }
+        // (row m = 4 c + r of product e of group g is dim 16 VE g + VE m + e)
+#pragma unroll
+        for (int g = 0; g < VG; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < VE; e += 4) {
+                    const int i = g * VE + e;
+                    out_sh[wave][n][(16 * VE * g + VE * (4 * c + r) + e) / 4] =
+                        make_float4(acc[t][i][r], acc[t][i + 1][r], acc[t][i + 2][r], acc[t][i + 3][r]);
+                }
+        __syncthreads();
+#pragma unroll 1
+        for (int idx = threadIdx.x; idx < ROWS * (d / 4); idx += kAttBlock) {
+            const int r = idx / (d / 4), i4 = idx % (d / 4), row = row0 + 16 * t + r;
+            if (row >= rows) continue;
+            float M = max_sh[0][r];
+#pragma unroll
+            for (int w = 1; w < kAttWaves; ++w) M = fmaxf(M, max_sh[w][r]);
+            float S = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAttWaves; ++w) {
+                // (a wave that saw nothing of the row has the maximum -inf and the sum 0; one whose scores are
+                // all NaN has the sum NaN, which stays)
+                const float f = max_sh[w][r] == -INFINITY && sum_sh[w][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[w][r] - M) * a.unit);
+                const float4 u = out_sh[w][r][i4];
+                S = fmaf(f, sum_sh[w][r], S);
+                v.x = fmaf(f, u.x, v.x);
+                v.y = fmaf(f, u.y, v.y);
+                v.z = fmaf(f, u.z, v.z);
+                v.w = fmaf(f, u.w, v.w);
+            }
+            if (piece.count > 1) {
+                float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
+                *reinterpret_cast<float4 *>(o + 4 * i4) = v;
+                if (i4 == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(M, S, a.unit, 0.f);
+                continue;
+            }
+            const float inv = S == 0.f ? 0.f : 1.f / S;  // (a row that sees nothing: 0)
+            v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
+            store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
+        }
+    }
+}
+
+// What a call launches: from its sizes alone, since lengths are on the device (max_kv bounds them).
+struct PagedPlan {
+    int tiles;              // tiles of 16 rows per wave
+    int tile_rows, blocks;  // rows per block, blocks of the largest sequence's rows
+    int target, least, units;
+    size_t workspace;
+};
+PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_kv, bool f32) {
+    const long long rows = (long long)max_q * group;
+    PagedPlan p{};
+    const int most = d <= 64 && !f32 ? 4 : d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
+    p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
+    p.tile_rows = 16 * p.tiles;
+    p.least = kAttWaves;
+    p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
+    const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
+    const long long pieces = ((max_kv - 1) / kPos + 1 + p.least - 1) / p.least;  // most that a sequence has
+    if (base * n_seq < kTarget && pieces > 1) {
+        p.target = int(std::min(std::max(1ll, kTarget / base), pieces * n_seq));
+        p.units = p.target + n_seq - 1;  // (rounding up leaves less than one piece more per sequence)
+        p.workspace = (size_t(p.units) * n_kv * p.blocks * p.tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
+    }
+    return p;
+}
+
+}  // namespace
+
+size_t paged_attention_workspace_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv) {
+    return std::max(paged_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_kv, false).workspace,
+                    paged_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_kv, true).workspace);
+}
+
+hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, const paged::Pages &pages,
+                                  const int32_t *table, int max_pages, const kv4::Batch &batch, int n_heads, int n_kv, int d,
+                                  int window, int sinks, const uint64_t *tree, int tree_words, float scale, void *out,
+                                  long long out_stride, void *workspace, int *err, hipStream_t s) {
+    const bool f32 = dtype == MOE_F32;
+    const PagedPlan p = paged_plan(batch.n_seq, n_kv, n_heads / n_kv, d, batch.max_q, batch.max_pos, f32);
+    PagedArgs a;
+    a.q = q;
+    a.out = out;
+    a.pages = pages;
+    a.table = table;
+    a.tree = reinterpret_cast<const uint32_t *>(tree);
+    a.part = static_cast<float *>(workspace);
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.max_pages = max_pages;
+    a.tree_words = 2 * tree_words;
+    a.n_kv = n_kv;
+    a.group = n_heads / n_kv;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.tiles = p.blocks;
+    // (never 0: -inf times it stays -inf)
+    a.unit = std::max(std::fabs(scale) * 1.44269504088896341f, 0x1p-126f);
+    a.negate = scale < 0.f;
+    a.split.target = p.target;
+    a.split.least = p.least;
+    a.split.unit = 1;
+    a.batch = batch;
+    a.err = err;
+    const dim3 grid = p.target ? dim3(n_kv, p.blocks, p.units) : dim3(p.blocks, n_kv, batch.n_seq);
+#define PAGED_CASE(NG, NT, F) \
+    case (NG * 2 + F) * 8 + NT: paged_attend_kernel<NG, NT, F><<<grid, kAttBlock, 0, s>>>(a); break;
+    switch ((d / 64 * 2 + f32) * 8 + p.tiles) {
+        PAGED_CASE(1, 1, false) PAGED_CASE(1, 2, false) PAGED_CASE(1, 4, false) PAGED_CASE(1, 1, true) PAGED_CASE(1, 2, true)
+        PAGED_CASE(2, 1, false) PAGED_CASE(2, 2, false) PAGED_CASE(2, 1, true)
+        PAGED_CASE(3, 1, false) PAGED_CASE(3, 1, true)
+        PAGED_CASE(4, 1, false) PAGED_CASE(4, 1, true)
+    default: return hipErrorInvalidValue;
+    }
+#undef PAGED_CASE
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.target) return e;
+#define PAGED_JOIN(NG, F) \
+    if (d == NG * 64 && f32 == F) launch_join<NG, F>(a, batch.max_q * a.group, batch.n_seq, p.tile_rows, s);
+    PAGED_JOIN(1, false) PAGED_JOIN(1, true) PAGED_JOIN(2, false) PAGED_JOIN(2, true)
+    PAGED_JOIN(3, false) PAGED_JOIN(3, true) PAGED_JOIN(4, false) PAGED_JOIN(4, true)
+#undef PAGED_JOIN
+    return hipGetLastError();
+}
+
+}  // namespace moe

@@ -21,6 +21,7 @@
 #include "paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace moe {
 namespace {
@@ -100,18 +101,19 @@ __device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, in
     if (!a.window) v.lo = -1;
     return v;
 }
-// Bit k: whether the row sees position p + 16 (k / 4) + k % 4.
+// Bit k < N: whether the row sees position p + STEP (k / 4) + k % 4.
+template <int N, int STEP>
 __device__ __forceinline__ uint32_t row_sees(const PagedArgs &a, const Seq &s, const RowView &v, int p) {
     uint32_t m = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int at = p + 16 * (k >> 2) + (k & 3);
+    for (int k = 0; k < N; ++k) {
+        const int at = p + STEP * (k >> 2) + (k & 3);
         m |= uint32_t((at <= v.hi) & ((at > v.lo) | (at < a.sinks))) << k;
     }
     if (a.tree)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int j = p + 16 * (k >> 2) + (k & 3) - (s.len - s.n);
+        for (int k = 0; k < N; ++k) {
+            const int j = p + STEP * (k >> 2) + (k & 3) - (s.len - s.n);
             if (j >= 0 && j < v.drafted) m |= (v.bits[j >> 5] >> (j & 31) & 1u) << k;
         }
     return m;
@@ -162,6 +164,13 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TER
         }
         t[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
     }
+}
+// Eight elements of a bf16 query, with the scale's sign.
+__device__ __forceinline__ bf16x8 load_query(const PagedArgs &a, size_t at) {
+    uint4 w = dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at));
+    const uint32_t flip = a.negate ? 0x80008000u : 0u;
+    w.x ^= flip, w.y ^= flip, w.z ^= flip, w.w ^= flip;
+    return __builtin_bit_cast(bf16x8, w);
 }
 // Where a pair of bf16 is not finite: all ones in its half.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
@@ -241,6 +250,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
 
     // The tile's rows: their queries as operands (k = dims), what they see.  A row past the last repeats it and is not stored.
     auto row_of = [&](int t) { return min(row0 + 16 * t + n, rows - 1); };
+    const float sign = a.negate ? -1.f : 1.f;
     bf16x8 bq[NT][2 * NG][QT];
     RowView view[NT];
 #pragma unroll
@@ -253,15 +263,13 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
             if constexpr (F32) {
                 const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 32 * j);
                 const float4 u = p[0], w = p[1];
-                const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+                const float x[8] = {u.x * sign, u.y * sign, u.z * sign, u.w * sign, w.x * sign, w.y * sign, w.z * sign, w.w * sign};
                 split_terms<QT>(x, bq[t][j]);
             } else {
-                bq[t][j][0] = __builtin_bit_cast(bf16x8, dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * j)));
+                bq[t][j][0] = load_query(a, at + 32 * j);
             }
         }
     }
-    const float sign = a.negate ? -1.f : 1.f;
-
     floatx4 acc[NT][4 * NG];
     float mx[NT], sum[NT];
 #pragma unroll 1
@@ -296,7 +304,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
 #pragma unroll
                         for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[u][j]), bq[t][j][k], y);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) p[t][4 * u + r] = y[r] * sign;
+                    for (int r = 0; r < 4; ++r) p[t][4 * u + r] = y[r];
                 }
             find(next);
             load_k(next);
@@ -307,7 +315,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
             for (int t = 0; t < NT; ++t) {
                 sees[t] = 0xff;
                 if (!full) {
-                    sees[t] = row_sees(a, s, view[t], b * kPos + 4 * c) & there_mask;
+                    sees[t] = row_sees<8, 16>(a, s, view[t], b * kPos + 4 * c) & there_mask;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) p[t][k] = sees[t] >> k & 1 ? p[t][k] : -INFINITY;
                 }
@@ -457,9 +465,309 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
     }
 }
 
+// ---- many rows (prompts, wide trees), bf16 tensors ---------------------------------------------------------------
+//
+// Where a block of positions meets hundreds of rows the arithmetic counts: a wave takes 32 rows, the 32x32x16 product does
+// twice the work per operand read, and the waves of a block share 64 positions' keys and values through LDS.  They lie there
+// as in the cache, a row of dims per position, with the pieces of 16 bytes of a row permuted by its number, so that what is
+// read together lies in different banks; the values are read by the transposing LDS load, which hands a lane four positions
+// of its dim.  The next positions are loaded into registers before the present ones are used and written behind them into
+// the other of two buffers, where positions that no token sees become zeros.
+//
+// Probabilities are one bf16 term here (2^-8), and their sum is that of the rounded ones, so that a row's weights add up to
+// one: a second term would cost half as many matrix products again.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;  // positions per step
+// A maximum is followed once a score is past it by so much (log2 units): probabilities of up to 2^8 lose nothing.
+constexpr float kSlack = 8.f;
+// Scores from here on (log2 units) are far: a row's offset, a rounded product, is off by 2^-12 at 2^12.  A step that has
+// one takes its exponentials of differences.
+constexpr float kFar = 0x1p12f;
+
+__device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Where piece `i` (16 bytes) of row `row` lies in the row.  Reads take 8 rows' same piece (keys), or four pieces of 8 rows
+// (values, 4 neighbouring rows per 16 lanes): over 256 bytes of banks each meets a bank as rarely as it can.
+template <int NG>
+__device__ __forceinline__ int swizzle(int row) {
+    return NG % 2 ? ((row >> 1 & 1) << 2) | (row >> 2 & 3) : ((row & 3) << 2) | (row >> 2 & 3);
+}
+__device__ __forceinline__ uint2 read_turned(const uint8_t *p) {
+    typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)p));
+}
+__device__ __forceinline__ float other_half32(float v) {  // what f(own, lane ^ 32) takes
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return (threadIdx.x & 32) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
+}
+// Whether some of rows i0..i1 sees some of the block of positions at p.
+__device__ __forceinline__ bool any_visible(const PagedArgs &a, const Seq &s, int i0, int i1, int p) {
+    const int cached = s.len - s.n;
+    if (a.tree) return p < s.len;
+    return p <= cached + i1 && (!a.window || p + kPos - 1 > cached + i0 - a.window || p < a.sinks);
+}
+
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces); 32 WAVES rows per block.
+template <int NG, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kernel(PagedArgs a) {
+    constexpr int d = NG * 64, THREADS = 64 * WAVES, ROWS = 32 * WAVES, PIECES = d / 8, ROW = 2 * d;
+    constexpr int LOADS = kTile * PIECES / THREADS, KS = d / 16, TD = d / 32;
+    constexpr int HALF = 16 * PIECES / 64;  // loads of a wave that make 16 positions
+    __shared__ uint4 k_sh[2][kTile * PIECES], v_sh[2][kTile * PIECES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, c = lane >> 5;
+    // (the last rows see the most positions: their blocks start first)
+    const int tile = a.tiles - 1 - int(a.split.target ? blockIdx.y : blockIdx.x), h = a.split.target ? blockIdx.x : blockIdx.y;
+    const Piece piece = this_piece(a, tile == a.tiles - 1 && h == 0 && tid < 64 ? a.err : nullptr);
+    if (piece.count == 0) return;
+    const Seq &s = piece.s;
+    const int G = a.group, rows = s.n * G, row0 = tile * ROWS;
+    if (row0 >= rows) return;
+    const Seen all = seen(s, a.window, a.sinks);
+    Seen z;
+    const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS, rows), z);
+    const int32_t *table = a.table + size_t(piece.seq) * a.max_pages;
+    const int page_mask = (1 << a.pages.shift) - 1;
+
+    // ---- staging: load l of a wave is 64 pieces of rows of one half of a block
+    uint4 kr[LOADS], vr[LOADS];
+    int entry[LOADS];         // the table's entries of the next positions, or -1
+    uint32_t hold = 0;        // bit l: this thread's row of the loaded positions is seen by some token, and there
+    auto position = [&](int v, int row) { return z.block(min(v + (row >> 5), range.y - 1)) * kPos + (row & 31); };
+    auto look = [&](int v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const int p = position(v, (l * WAVES + wave) / HALF * 16);
+            entry[l] = p < s.len && (p < a.sinks || p + 16 > all.from) ? table[p >> a.pages.shift] : -1;
+            if (p < s.len && (p < a.sinks || p + 16 > all.from) && uint32_t(entry[l]) >= uint32_t(a.pages.n_pages) && lane == 0)
+                atomicOr(a.err, kErrRange);
+        }
+    };
+    auto load = [&](int v) __attribute__((always_inline)) {
+        hold = 0;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const int q = l * THREADS + tid, row = q / PIECES, piece_of = q - row * PIECES, p = position(v, row);
+            const bool there = uint32_t(entry[l]) < uint32_t(a.pages.n_pages);
+            const size_t page = there ? entry[l] : 0, at = ((size_t(h) << a.pages.shift) + (p & page_mask)) * d + 8 * piece_of;
+            kr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.k + page * a.pages.k_stride + at));
+            vr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.v + page * a.pages.v_stride + at));
+            hold |= uint32_t(there & (p < s.len) & ((p >= all.from) | (p < a.sinks))) << l;
+        }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const int q = l * THREADS + tid, row = q / PIECES, piece_of = q - row * PIECES;
+            const int at = row * PIECES + (piece_of ^ swizzle<NG>(row));
+            k_sh[buf][at] = kr[l];
+            v_sh[buf][at] = hold >> l & 1 ? vr[l] : make_uint4(0, 0, 0, 0);
+        }
+    };
+    // Whether the halves of the step's blocks are there: every wave looks at all of them.
+    auto there_of = [&](int v) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int p = position(v, 16 * u);
+            const bool needed = p < s.len && (p < a.sinks || p + 16 > all.from);
+            m |= uint32_t(needed && uint32_t(table[p >> a.pages.shift]) < uint32_t(a.pages.n_pages)) << u;
+        }
+        return m;
+    };
+
+    // ---- the wave's rows; a row past the last repeats it and is not stored
+    const int w_row0 = row0 + 32 * wave, row = min(w_row0 + n, rows - 1), i_row = row / G;
+    const bool idle = w_row0 >= rows;
+    const int i_first = min(w_row0, rows - 1) / G, i_last = min(w_row0 + 31, rows - 1) / G;
+    bf16x8 bq[KS];
+    {
+        const size_t at = size_t(s.t0 + i_row) * a.q_stride + size_t(h * G + row - i_row * G) * d + 8 * c;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bq[j] = load_query(a, at + 16 * j);
+    }
+    const RowView view = row_view(a, s, i_row);
+
+    // ---- where the lane's operands lie in a buffer (bytes): keys of position n, values of dims of 16 lanes
+    const int k_at = n * ROW, k_swz = c ^ swizzle<NG>(n);
+    const int v_row = 4 * c + (lane & 15) / 4, v_piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+    const int v_at = v_row * ROW + 8 * (lane & 1);
+
+    floatx16 acc[TD];
+    float mx, sum;
+    auto pass = [&](auto careful) __attribute__((always_inline)) {
+        mx = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < TD; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+        if (range.x < range.y) {
+            look(range.x);
+            load(range.x);
+            store(0);
+            if (range.x + 2 < range.y) look(range.x + 2);
+        }
+        lds_barrier();
+        auto step = [&](int v, int buf) __attribute__((always_inline)) {
+            const bool more = v + 2 < range.y;
+            if (more) {
+                load(v + 2);
+                if (v + 4 < range.y) look(v + 4);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const int b[2] = {z.block(v), z.block(min(v + 1, range.y - 1))};
+            const bool two = v + 1 < range.y;
+            if (!idle && (any_visible(a, s, i_first, i_last, b[0] * kPos) || (two && any_visible(a, s, i_first, i_last, b[1] * kPos)))) {
+                const uint8_t *kb = reinterpret_cast<const uint8_t *>(k_sh[buf]), *vb = reinterpret_cast<const uint8_t *>(v_sh[buf]);
+                // ---- scores: positions x rows
+                floatx16 p[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[u][r] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < KS; ++j) {
+                        const uint4 w = *reinterpret_cast<const uint4 *>(kb + k_at + u * 32 * ROW + 16 * (2 * j ^ k_swz));
+                        p[u] = mfma32(__builtin_bit_cast(bf16x8, w), bq[j], p[u]);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // ---- softmax
+                const uint32_t there = there_of(v);
+                uint32_t sees[2] = {0xffff, 0xffff};
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bool full = (there >> (2 * u) & 3) == 3 && (u == 0 || two) && all_visible(a, s, i_first, i_last, b[u] * kPos, kPos);
+                    if (full) continue;
+                    sees[u] = row_sees<16, 8>(a, s, view, b[u] * kPos + 4 * c);
+                    sees[u] &= (there >> (2 * u) & 1 ? 0xffu : 0u) | (there >> (2 * u) & 2 ? 0xff00u : 0u);
+                    if (u && !two) sees[u] = 0;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[u][r] = sees[u] >> r & 1 ? p[u][r] : -INFINITY;
+                }
+                float top = p[0][0];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, p[u][r]);
+                top = fmaxf(top, other_half32(top));
+                if (__any((top - mx) * a.unit > kSlack)) {  // (the first score of a row is infinitely far past its maximum)
+                    const float now = fmaxf(mx, top), f = __builtin_amdgcn_exp2f(mx == now ? 0.f : (mx - now) * a.unit);
+                    mx = now;
+                    sum *= f;
+#pragma unroll
+                    for (int t = 0; t < TD; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[t][r] *= f;
+                }
+                const float to = mx == -INFINITY ? 0.f : mx;
+                float off = to * a.unit;
+                if (__any(!(fabsf(off) < kFar))) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) p[u][r] -= to;
+                    off = 0.f;
+                }
+                bf16x8 bp[4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[u][r] = __builtin_amdgcn_exp2f(fmaf(p[u][r], a.unit, -off));
+                    uint32_t w[8];
+                    const bf16x2 one = {__bf16(1.f), __bf16(1.f)};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        w[e] = pack_bf16(p[u][2 * e], p[u][2 * e + 1]);
+                        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), one, sum, false);
+                    }
+                    bp[2 * u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                    bp[2 * u + 1] = __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // ---- values: dims x rows
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int t = 0; t < TD; ++t) {
+                        uint2 w[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            w[e] = read_turned(vb + v_at + (16 * q + 8 * e) * ROW + 16 * ((4 * t + v_piece) ^ swizzle<NG>(v_row + 8 * e)));
+                        uint32_t x[4] = {w[0].x, w[0].y, w[1].x, w[1].y};
+                        if constexpr (decltype(careful)::value) {
+                            uint32_t f[4], g[4];
+                            bool any = false;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                f[k] = not_finite(x[k]);
+                                x[k] &= ~f[k];
+                                any |= f[k] != 0;
+                                f[k] &= 0x3f803f80u;
+                                const uint32_t m = sees[q >> 1] >> (8 * (q & 1) + 2 * k);
+                                g[k] = (m & 1) * 0x3f80u | (m >> 1 & 1) * 0x3f800000u;
+                            }
+                            if (__any(any)) {
+                                floatx16 met;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) met[r] = 0.f;
+                                met = mfma32(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])),
+                                             __builtin_bit_cast(bf16x8, make_uint4(g[0], g[1], g[2], g[3])), met);
+#pragma unroll
+                                for (int r = 0; r < 16; ++r)
+                                    if (met[r] > 0.f) acc[t][r] = NAN;
+                            }
+                        }
+                        acc[t] = mfma32(__builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3])), bp[q], acc[t]);
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) store(buf ^ 1);
+            lds_barrier();
+        };
+#pragma unroll 1
+        for (int v = range.x; v < range.y; v += 4) {
+            step(v, 0);
+            if (v + 2 < range.y) step(v + 2, 1);
+        }
+    };
+    pass(std::false_type());
+    bool off = false;
+#pragma unroll
+    for (int t = 0; t < TD; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) off |= !(fabsf(acc[t][r]) < INFINITY);
+    if (__builtin_expect(__syncthreads_or(off && !idle), 0)) pass(std::true_type());
+
+    const float l = sum + other_half32(sum);
+    if (w_row0 + n >= rows) return;
+    if (piece.count > 1) {
+        float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * ROWS + row) * (d + 4);
+#pragma unroll
+        for (int t = 0; t < TD; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<float4 *>(o + 32 * t + 2 * r + 4 * c) = make_float4(acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]);
+        if (c == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(mx, l, a.unit, 0.f);
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const size_t at = size_t(s.t0 + i_row) * a.out_stride + size_t(h * G + row - i_row * G) * d + 4 * c;
+#pragma unroll
+    for (int t = 0; t < TD; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            store4<false>(a.out, at + 32 * t + 2 * r, make_float4(acc[t][r] * inv, acc[t][r + 1] * inv, acc[t][r + 2] * inv, acc[t][r + 3] * inv));
+}
+
 // What a call launches: from its sizes alone, since lengths are on the device (max_kv bounds them).
 struct PagedPlan {
-    int tiles;              // tiles of 16 rows per wave
+    int prompt;             // waves of the kernel for many rows, or 0
+    int tiles;              // otherwise: tiles of 16 rows per wave
     int tile_rows, blocks;  // rows per block, blocks of the largest sequence's rows
     int target, least, units;
     size_t workspace;
@@ -467,15 +775,24 @@ struct PagedPlan {
 PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_kv, bool f32) {
     const long long rows = (long long)max_q * group;
     PagedPlan p{};
-    const int most = d <= 64 && !f32 ? 4 : d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
-    p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
-    p.tile_rows = 16 * p.tiles;
-    p.least = kAttWaves;
+    int fill = kTarget;
+    if (!f32 && rows >= 64) {
+        const long long eight = (rows + 255) / 256 * n_kv * n_seq;
+        p.prompt = d <= 128 && eight >= 256 ? 8 : 4;
+        p.tile_rows = 32 * p.prompt;
+        p.least = 8;
+        fill = p.prompt == 8 || d > 128 ? 256 : 512;
+    } else {
+        const int most = d <= 64 && !f32 ? 4 : d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
+        p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
+        p.tile_rows = 16 * p.tiles;
+        p.least = kAttWaves;
+    }
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
     const long long pieces = ((max_kv - 1) / kPos + 1 + p.least - 1) / p.least;  // most that a sequence has
-    if (base * n_seq < kTarget && pieces > 1) {
-        p.target = int(std::min(std::max(1ll, kTarget / base), pieces * n_seq));
+    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && pieces > 1) {
+        p.target = int(std::min(std::max(1ll, fill / base), pieces * n_seq));
         p.units = p.target + n_seq - 1;  // (rounding up leaves less than one piece more per sequence)
         p.workspace = (size_t(p.units) * n_kv * p.blocks * p.tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
     }
@@ -516,10 +833,16 @@ hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, 
     a.negate = scale < 0.f;
     a.split.target = p.target;
     a.split.least = p.least;
-    a.split.unit = 1;
+    a.split.unit = p.prompt ? 2 : 1;
     a.batch = batch;
     a.err = err;
     const dim3 grid = p.target ? dim3(n_kv, p.blocks, p.units) : dim3(p.blocks, n_kv, batch.n_seq);
+    if (p.prompt) {
+#define PAGED_PROMPT(NG, W) \
+    if (d == NG * 64 && p.prompt == W) paged_prompt_kernel<NG, W><<<grid, 64 * W, 0, s>>>(a);
+        PAGED_PROMPT(1, 4) PAGED_PROMPT(1, 8) PAGED_PROMPT(2, 4) PAGED_PROMPT(2, 8) PAGED_PROMPT(3, 4) PAGED_PROMPT(4, 4)
+#undef PAGED_PROMPT
+    } else {
 #define PAGED_CASE(NG, NT, F) \
     case (NG * 2 + F) * 8 + NT: paged_attend_kernel<NG, NT, F><<<grid, kAttBlock, 0, s>>>(a); break;
     switch ((d / 64 * 2 + f32) * 8 + p.tiles) {
@@ -530,6 +853,7 @@ hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, 
     default: return hipErrorInvalidValue;
     }
 #undef PAGED_CASE
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.target) return e;
 #define PAGED_JOIN(NG, F) \

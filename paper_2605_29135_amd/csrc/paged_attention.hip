@@ -145,6 +145,23 @@ __device__ __forceinline__ int2 tile_blocks(const PagedArgs &a, const Piece &pie
     return make_int2(cut < t.sink ? cut : max(cut, first) - skip, max(min(cut_end, t.sink), cut_end - skip));
 }
 
+// The sequence's row of the page table, read through the scalar cache: a vector load's result could only be waited for with
+// all of the keys and values in flight before it.
+typedef const __attribute__((address_space(4))) int32_t table_word;
+struct Table {
+    table_word *row;
+    int n_pages, shift, last;  // last: of the sequence's positions
+    // The entry of position p's page (any p: that of the last position behind it).
+    __device__ __forceinline__ int32_t entry(int p) const { return row[min(p, last) >> shift]; }
+};
+__device__ __forceinline__ Table sequence_table(const PagedArgs &a, const Piece &piece) {
+    return Table{(table_word *)(a.table + size_t(piece.seq) * a.max_pages), a.pages.n_pages, a.pages.shift, max(piece.s.len - 1, 0)};
+}
+// Whether some token sees one of the 16 positions from p on, which lie in one page.
+__device__ __forceinline__ bool half_seen(const PagedArgs &a, const Seq &s, const Seen &all, int p) {
+    return (p < s.len) & ((p < a.sinks) | (p + 16 > all.from));
+}
+
 // x as TERMS bf16 operands, each rounding what the ones before leave.
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TERMS]) {
@@ -198,26 +215,30 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
     const Seen all = seen(s, a.window, a.sinks);
     Seen z;
     const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS * NT, rows), z);
-    const int32_t *table = a.table + size_t(piece.seq) * a.max_pages;
+    const Table table = sequence_table(a, piece);
     const int page_mask = (1 << a.pages.shift) - 1;
 
     // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.
     uint4 kc[2][2 * NG];
     uint32_t vc[VG][8][VE / 2];
     // Half a block lies in one page.  `there`: bits of the halves (four each) of which some token sees a position, and whose
-    // page is there; the others are read from the first page, and none of it is used.
+    // page is there; the others are read from the first page, and none of it is used.  The table's entries are fetched a
+    // block ahead of the loads.
     uint32_t there = 0;
+    bool missing = false;
+    int32_t entry[2] = {0, 0};
     int page_at[2] = {0, 0};
+    auto fetch = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) entry[u] = table.entry(b * kPos + 16 * u);
+    };
     auto find = [&](int b) __attribute__((always_inline)) {
         there = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int p = b * kPos + 16 * u;
-            const bool needed = p < s.len && (p < a.sinks || p + 16 > all.from);
-            const int32_t page = needed ? table[p >> a.pages.shift] : 0;
-            const bool ok = uint32_t(page) < uint32_t(a.pages.n_pages);
-            if (!ok && lane == 0) atomicOr(a.err, kErrRange);
-            page_at[u] = ok ? page : 0;
+            const bool needed = half_seen(a, s, all, b * kPos + 16 * u), ok = uint32_t(entry[u]) < uint32_t(table.n_pages);
+            missing |= needed & !ok;
+            page_at[u] = ok ? entry[u] : 0;
             there |= needed && ok ? 0xfu << (4 * u) : 0u;
         }
     };
@@ -283,9 +304,11 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
         }
         if (range.x + wave < range.y) {
             const int b = z.block(range.x + wave);
+            fetch(b);
             find(b);
             load_k(b);
             load_v(b);
+            fetch(z.block(min(range.x + wave + kAttWaves, range.y - 1)));
         }
 #pragma unroll 1
         for (int v = range.x + wave; v < range.y; v += kAttWaves) {
@@ -308,6 +331,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 }
             find(next);
             load_k(next);
+            fetch(z.block(min(v + 2 * kAttWaves, range.y - 1)));
             // ---- softmax
             uint32_t sees[NT];
             bf16x8 bp[NT][PT];
@@ -409,6 +433,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
         if (careful || !__any(off)) break;
     }
+    if (missing && lane == 0) atomicOr(a.err, kErrRange);
 
     // Join the waves, one tile of rows at a time.
 #pragma unroll
@@ -518,6 +543,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     constexpr int LOADS = kTile * PIECES / THREADS, KS = d / 16, TD = d / 32;
     constexpr int HALF = 16 * PIECES / 64;  // loads of a wave that make 16 positions
     __shared__ uint4 k_sh[2][kTile * PIECES], v_sh[2][kTile * PIECES];
+    __shared__ alignas(16) uint32_t there_sh[2][4];  // bits of the halves of the two blocks that are there
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, c = lane >> 5;
     // (the last rows see the most positions: their blocks start first)
     const int tile = a.tiles - 1 - int(a.split.target ? blockIdx.y : blockIdx.x), h = a.split.target ? blockIdx.x : blockIdx.y;
@@ -529,33 +555,33 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     const Seen all = seen(s, a.window, a.sinks);
     Seen z;
     const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS, rows), z);
-    const int32_t *table = a.table + size_t(piece.seq) * a.max_pages;
+    const Table table = sequence_table(a, piece);
     const int page_mask = (1 << a.pages.shift) - 1;
 
     // ---- staging: load l of a wave is 64 pieces of rows of one half of a block
     uint4 kr[LOADS], vr[LOADS];
-    int entry[LOADS];         // the table's entries of the next positions, or -1
+    int32_t entry[LOADS];     // the table's entries of the next positions
+    bool there[LOADS];        // whether the loaded positions' half of a block is needed, and there
     uint32_t hold = 0;        // bit l: this thread's row of the loaded positions is seen by some token, and there
+    bool missing = false;
     auto position = [&](int v, int row) { return z.block(min(v + (row >> 5), range.y - 1)) * kPos + (row & 31); };
-    auto look = [&](int v) __attribute__((always_inline)) {
+    auto half_of = [&](int l) { return (l * WAVES + wave) / HALF; };
+    auto fetch = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) {
-            const int p = position(v, (l * WAVES + wave) / HALF * 16);
-            entry[l] = p < s.len && (p < a.sinks || p + 16 > all.from) ? table[p >> a.pages.shift] : -1;
-            if (p < s.len && (p < a.sinks || p + 16 > all.from) && uint32_t(entry[l]) >= uint32_t(a.pages.n_pages) && lane == 0)
-                atomicOr(a.err, kErrRange);
-        }
+        for (int l = 0; l < LOADS; ++l) entry[l] = table.entry(position(v, 16 * half_of(l)));
     };
     auto load = [&](int v) __attribute__((always_inline)) {
         hold = 0;
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-            const int q = l * THREADS + tid, row = q / PIECES, piece_of = q - row * PIECES, p = position(v, row);
-            const bool there = uint32_t(entry[l]) < uint32_t(a.pages.n_pages);
-            const size_t page = there ? entry[l] : 0, at = ((size_t(h) << a.pages.shift) + (p & page_mask)) * d + 8 * piece_of;
+            const int q = l * THREADS + tid, row = q / PIECES, p = position(v, row);
+            const bool needed = half_seen(a, s, all, position(v, 16 * half_of(l))), ok = uint32_t(entry[l]) < uint32_t(table.n_pages);
+            missing |= needed & !ok;
+            const size_t page = ok ? entry[l] : 0, at = ((size_t(h) << a.pages.shift) + (p & page_mask)) * d + 8 * (q - row * PIECES);
             kr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.k + page * a.pages.k_stride + at));
             vr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.v + page * a.pages.v_stride + at));
-            hold |= uint32_t(there & (p < s.len) & ((p >= all.from) | (p < a.sinks))) << l;
+            hold |= uint32_t(needed & ok & (p < s.len) & ((p >= all.from) | (p < a.sinks))) << l;
+            there[l] = needed & ok;
         }
     };
     auto store = [&](int buf) __attribute__((always_inline)) {
@@ -565,18 +591,8 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             const int at = row * PIECES + (piece_of ^ swizzle<NG>(row));
             k_sh[buf][at] = kr[l];
             v_sh[buf][at] = hold >> l & 1 ? vr[l] : make_uint4(0, 0, 0, 0);
+            if ((l * WAVES + wave) % HALF == 0 && lane == 0) there_sh[buf][half_of(l)] = there[l] ? 1u << half_of(l) : 0u;
         }
-    };
-    // Whether the halves of the step's blocks are there: every wave looks at all of them.
-    auto there_of = [&](int v) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int p = position(v, 16 * u);
-            const bool needed = p < s.len && (p < a.sinks || p + 16 > all.from);
-            m |= uint32_t(needed && uint32_t(table[p >> a.pages.shift]) < uint32_t(a.pages.n_pages)) << u;
-        }
-        return m;
     };
 
     // ---- the wave's rows; a row past the last repeats it and is not stored
@@ -606,17 +622,17 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
         if (range.x < range.y) {
-            look(range.x);
+            fetch(range.x);
             load(range.x);
+            fetch(min(range.x + 2, range.y - 1));
             store(0);
-            if (range.x + 2 < range.y) look(range.x + 2);
         }
         lds_barrier();
         auto step = [&](int v, int buf) __attribute__((always_inline)) {
             const bool more = v + 2 < range.y;
             if (more) {
                 load(v + 2);
-                if (v + 4 < range.y) look(v + 4);
+                fetch(min(v + 4, range.y - 1));
             }
             __builtin_amdgcn_sched_barrier(0);
             const int b[2] = {z.block(v), z.block(min(v + 1, range.y - 1))};
@@ -637,7 +653,8 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 // ---- softmax
-                const uint32_t there = there_of(v);
+                const uint4 halves = *reinterpret_cast<const uint4 *>(there_sh[buf]);
+                const uint32_t there = __builtin_amdgcn_readfirstlane(halves.x | halves.y | halves.z | halves.w);
                 uint32_t sees[2] = {0xffff, 0xffff};
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -743,6 +760,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
         for (int r = 0; r < 16; ++r) off |= !(fabsf(acc[t][r]) < INFINITY);
     if (__builtin_expect(__syncthreads_or(off && !idle), 0)) pass(std::true_type());
 
+    if (missing && lane == 0) atomicOr(a.err, kErrRange);
     const float l = sum + other_half32(sum);
     if (w_row0 + n >= rows) return;
     if (piece.count > 1) {

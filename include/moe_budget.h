@@ -320,7 +320,8 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
 /* ======================================================================= */
 
 /* The pool of one layer: keys and values, each device bf16 [n_pages][n_kv][page_size][head_dim], a page's values
- * contiguous and k_page_stride / v_page_stride elements (at least n_kv * page_size * head_dim) from page to page.
+ * contiguous and k_page_stride / v_page_stride elements (at least n_kv * page_size * head_dim, below 2^31) from page to
+ * page.
  * The page table is device int32 [n_seq][max_pages]: position p of sequence b lies in page table[b][p / page_size],
  * at offset p % page_size; it is in slot page * page_size + offset of the pool.
  * A batch of n_seq sequences with q_start, max_q and kv_len is as for the 4-bit cache above, with max_kv in place of

@@ -444,10 +444,9 @@ int check_pool(const char *what, const void *k, const void *v, long long k_strid
                int head_dim) {
     if (!k || !v) return fail(MOE_ERR_INVALID_ARG, "%s: NULL pointer", what);
     const long long each = (long long)n_kv * page_size * head_dim;
-    auto bad = [&](const void *p, long long stride) { return !aligned16(p) || stride < each || stride > 1ll << 40 || stride % 8; };
+    auto bad = [&](const void *p, long long stride) { return !aligned16(p) || stride < each || stride >= 1ll << 31 || stride % 8; };
     if (bad(k, k_stride) || bad(v, v_stride))
-        return fail(MOE_ERR_INVALID_ARG, "%s: the pools need 16-byte aligned pages of at least n_kv * page_size * head_dim elements",
-                    what);
+        return fail(MOE_ERR_INVALID_ARG, "%s: the pools need 16-byte aligned pages, from n_kv * page_size * head_dim to 2^31 elements apart", what);
     return MOE_OK;
 }
 // And of the batch; max_q becomes 1 without q_start.

@@ -81,41 +81,45 @@ __device__ __forceinline__ Piece this_piece(const PagedArgs &a, int *err) {
     return p;
 }
 
-// What a row sees: positions up to `hi` that are above `lo` or among the first; with a tree, of the drafted tokens those
-// whose bits are set (`drafted` of them: none for a row of padding).
+// What a row (of token i) sees: positions up to `hi` that are above `lo` or among the first; with a tree, of the drafted
+// tokens those whose bits are set (none for a row of padding).
 struct RowView {
-    int hi, lo, drafted;
-    const uint32_t *bits;
+    int i, hi, lo;
 };
+__device__ __forceinline__ const uint32_t *row_bits(const PagedArgs &a, const Seq &s, int i) {
+    return a.tree + size_t(s.t0 + i) * a.tree_words;
+}
 __device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, int i) {
     const int cached = s.len - s.n, row = cached + i;
-    RowView v{row, row - a.window, 0, nullptr};
+    RowView v{i, row, row - a.window};
     if (a.tree) {
-        v.bits = a.tree + size_t(s.t0 + i) * a.tree_words;
+        const uint32_t *bits = row_bits(a, s, i);
         int set = 0;
-        for (int w = 0; 32 * w < s.n; ++w) set += __popc(v.bits[w] & (s.n - 32 * w < 32 ? (1u << (s.n - 32 * w)) - 1 : ~0u));
+        for (int w = 0; 32 * w < s.n; ++w) set += __popc(bits[w] & (s.n - 32 * w < 32 ? (1u << (s.n - 32 * w)) - 1 : ~0u));
         v.hi = row < 0 ? -1 : cached - 1;
         v.lo = cached - 1 + set - a.window;
-        v.drafted = row < 0 ? 0 : s.n;
     }
     if (!a.window) v.lo = -1;
     return v;
 }
-// Bit k < N: whether the row sees position p + STEP (k / 4) + k % 4.
+// Whether the row sees position p of the sequence, drafted tokens of a tree aside.
+__device__ __forceinline__ bool row_sees(const PagedArgs &a, const RowView &v, int p) {
+    return (p <= v.hi) & ((p > v.lo) | (p < a.sinks));
+}
+// Bit k < N: whether the row sees position p + STEP (k / 4) + k % 4 as a drafted token of a tree.
 template <int N, int STEP>
-__device__ __forceinline__ uint32_t row_sees(const PagedArgs &a, const Seq &s, const RowView &v, int p) {
+__device__ __forceinline__ uint32_t row_drafts(const PagedArgs &a, const Seq &s, const RowView &v, int p) {
+    const int cached = s.len - s.n, first = p - cached;
     uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const int at = p + STEP * (k >> 2) + (k & 3);
-        m |= uint32_t((at <= v.hi) & ((at > v.lo) | (at < a.sinks))) << k;
-    }
-    if (a.tree)
+    if (a.tree && first + STEP * ((N - 1) >> 2) + 3 >= 0) {
+        const uint32_t *bits = row_bits(a, s, v.i);
+        const int drafted = cached + v.i < 0 ? 0 : s.n;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int j = p + STEP * (k >> 2) + (k & 3) - (s.len - s.n);
-            if (j >= 0 && j < v.drafted) m |= (v.bits[j >> 5] >> (j & 31) & 1u) << k;
+            const int j = first + STEP * (k >> 2) + (k & 3);
+            if (j >= 0 && j < drafted) m |= (bits[j >> 5] >> (j & 31) & 1u) << k;
         }
+    }
     return m;
 }
 // Whether every one of rows i0..i1 sees all of positions p..p + count - 1.
@@ -339,9 +343,13 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
             for (int t = 0; t < NT; ++t) {
                 sees[t] = 0xff;
                 if (!full) {
-                    sees[t] = row_sees<8, 16>(a, s, view[t], b * kPos + 4 * c) & there_mask;
+                    const uint32_t drafts = row_drafts<8, 16>(a, s, view[t], b * kPos + 4 * c);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) p[t][k] = sees[t] >> k & 1 ? p[t][k] : -INFINITY;
+                    for (int k = 0; k < 8; ++k) {
+                        const bool see = (row_sees(a, view[t], b * kPos + 16 * (k >> 2) + 4 * c + (k & 3)) | (drafts >> k & 1)) & (there_mask >> k & 1);
+                        p[t][k] = see ? p[t][k] : -INFINITY;
+                        if (careful) sees[t] &= ~(uint32_t(!see) << k);
+                    }
                 }
                 float top = p[t][0];
 #pragma unroll
@@ -521,7 +529,32 @@ template <int NG>
 __device__ __forceinline__ int swizzle(int row) {
     return NG % 2 ? ((row >> 1 & 1) << 2) | (row >> 2 & 3) : ((row & 3) << 2) | (row >> 2 & 3);
 }
-__device__ __forceinline__ uint2 read_turned(const uint8_t *p) {
+// N products with an operand from LDS each, which is read AHEAD products in front of its use.  (Left to itself the compiler
+// reads an operand, waits and multiplies: an LDS latency for each product.)
+template <int N, int AHEAD, typename READ, typename USE>
+__device__ __forceinline__ void products(READ read, USE use) {
+    uint4 w[AHEAD];
+#pragma unroll
+    for (int m = 0; m < AHEAD; ++m) w[m] = read(m);
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+        __builtin_amdgcn_sched_barrier(0);
+        use(m, w[m % AHEAD]);
+        if (m + AHEAD < N) w[m % AHEAD] = read(m + AHEAD);
+    }
+}
+// A number that the compiler takes as it is: it would otherwise keep dozens of sums with it in registers, not the few numbers.
+__device__ __forceinline__ int held_value(int v) {
+    asm("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ int held_scalar(int v) {
+    asm("" : "+s"(v));
+    return v;
+}
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef __attribute__((address_space(3))) dev::u32x4 lds_u32x4;
+__device__ __forceinline__ uint2 read_turned(const lds_byte *p) {
     typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)p));
 }
@@ -537,13 +570,20 @@ __device__ __forceinline__ bool any_visible(const PagedArgs &a, const Seq &s, in
 }
 
 // grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces); 32 WAVES rows per block.
+//
+// Eight waves are two to a SIMD and go in two groups half a step apart, a barrier between: while the one forms its products
+// (the values of its last positions, the scores of the next), the other takes its exponentials.  Four waves of a block are
+// one to a SIMD; another block, which runs in no step with it, fills the gaps.
 template <int NG, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kernel(PagedArgs a) {
     constexpr int d = NG * 64, THREADS = 64 * WAVES, ROWS = 32 * WAVES, PIECES = d / 8, ROW = 2 * d;
     constexpr int LOADS = kTile * PIECES / THREADS, KS = d / 16, TD = d / 32;
-    constexpr int HALF = 16 * PIECES / 64;  // loads of a wave that make 16 positions
-    __shared__ uint4 k_sh[2][kTile * PIECES], v_sh[2][kTile * PIECES];
-    __shared__ alignas(16) uint32_t there_sh[2][4];  // bits of the halves of the two blocks that are there
+    constexpr int HALF = 16 * PIECES / 64;   // loads of a wave that make 16 positions
+    constexpr bool TWO = WAVES == 8;
+    constexpr int AHEAD = 6;                 // products whose operands are in flight
+    constexpr int VBUF = TWO ? 3 : 2;        // (values are read a step after the keys)
+    __shared__ uint4 k_sh[2][kTile * PIECES], v_sh[VBUF][kTile * PIECES];
+    __shared__ alignas(16) uint32_t there_sh[VBUF][4];  // bits of the halves of the two blocks that are there
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, c = lane >> 5;
     // (the last rows see the most positions: their blocks start first)
     const int tile = a.tiles - 1 - int(a.split.target ? blockIdx.y : blockIdx.x), h = a.split.target ? blockIdx.x : blockIdx.y;
@@ -555,43 +595,100 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     const Seen all = seen(s, a.window, a.sinks);
     Seen z;
     const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS, rows), z);
+    const int steps = (range.y - range.x + 1) / 2;
     const Table table = sequence_table(a, piece);
     const int page_mask = (1 << a.pages.shift) - 1;
 
-    // ---- staging: load l of a wave is 64 pieces of rows of one half of a block
+    const uint8_t *head_k = reinterpret_cast<const uint8_t *>(a.pages.k + ((size_t(h) << a.pages.shift) * d));
+    const uint8_t *head_v = reinterpret_cast<const uint8_t *>(a.pages.v + ((size_t(h) << a.pages.shift) * d));
+    const uint32_t page_k = uint32_t(a.pages.k_stride) * 2, page_v = uint32_t(a.pages.v_stride) * 2;  // bytes (below 2^32)
+
+    // Steps whose 64 positions lie together and are all seen by some token, none of them past the last: most of them, and
+    // those that need no look at where their positions are (`plain`: first, end; positions there are p_plain + 64 i).
+    const int p_plain = (range.x - z.sink + z.first) * kPos;
+    const int2 plain = [&] {
+        const int gap = max(z.sink - range.x, 0);                                    // blocks in front of the window's
+        const int unseen = a.window ? max(all.from - p_plain, 0) : 0;                // positions in front of the first seen
+        return make_int2(max((gap + 1) / 2, (unseen + kTile - 1) / kTile), min((s.len - p_plain) / kTile, (range.y - range.x) / 2));
+    }();
+    auto half_at = [&](int i, int u) {  // where half u of step i's two blocks is
+        return z.block(min(range.x + 2 * i + (u >> 1), range.y - 1)) * kPos + 16 * (u & 1);
+    };
+
+    // ---- staging: load l of a wave is 64 pieces of one half of a block, which lies in one page, in one piece
     uint4 kr[LOADS], vr[LOADS];
-    int32_t entry[LOADS];     // the table's entries of the next positions
-    bool there[LOADS];        // whether the loaded positions' half of a block is needed, and there
+    int32_t entry[LOADS];     // the table's entries of the positions after those loaded
+    bool there[LOADS];        // (careful) whether the loaded positions' half of a block is needed, and there
     uint32_t hold = 0;        // bit l: this thread's row of the loaded positions is seen by some token, and there
     bool missing = false;
-    auto position = [&](int v, int row) { return z.block(min(v + (row >> 5), range.y - 1)) * kPos + (row & 31); };
     auto half_of = [&](int l) { return (l * WAVES + wave) / HALF; };
-    auto fetch = [&](int v) __attribute__((always_inline)) {
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l) entry[l] = table.entry(position(v, 16 * half_of(l)));
-    };
-    auto load = [&](int v) __attribute__((always_inline)) {
-        hold = 0;
+    auto piece_in = [&](int l) { return (l * THREADS + tid) % (16 * PIECES); };  // this thread's, of the half
+    // Where in a buffer (bytes) the thread's pieces go, and its operands lie: keys of position n, values of dims of 16 lanes
+    int k_off[KS], v_off[TD][2], store_at[LOADS];
+    {
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-            const int q = l * THREADS + tid, row = q / PIECES, p = position(v, row);
-            const bool needed = half_seen(a, s, all, position(v, 16 * half_of(l))), ok = uint32_t(entry[l]) < uint32_t(table.n_pages);
+            const int row = piece_in(l) / PIECES;
+            store_at[l] = held_value(16 * (16 * PIECES * half_of(l) + row * PIECES + ((piece_in(l) % PIECES) ^ swizzle<NG>(row))));
+        }
+        const int v_row = 4 * c + (lane & 15) / 4, v_piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) k_off[j] = held_value(n * ROW + 16 * ((2 * j + c) ^ swizzle<NG>(n)));
+#pragma unroll
+        for (int t = 0; t < TD; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                v_off[t][e] = held_value((v_row + 8 * e) * ROW + 16 * ((4 * t + v_piece) ^ swizzle<NG>(v_row + 8 * e)) + 8 * (lane & 1));
+    }
+
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        const bool easy = i >= plain.x && i < plain.y;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l)
+            entry[l] = table.row[(easy ? p_plain + kTile * i + 16 * half_of(l) : min(half_at(i, half_of(l)), table.last)) >> table.shift];
+    };
+    auto load = [&](int i, auto careful) __attribute__((always_inline)) {
+        const bool easy = i >= plain.x && i < plain.y;
+        hold = ~0u;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            int p0 = p_plain + kTile * i + 16 * half_of(l);
+            bool ok = uint32_t(entry[l]) < uint32_t(table.n_pages), needed = true;
+            if (!easy) {
+                p0 = half_at(i, half_of(l));
+                needed = half_seen(a, s, all, p0);
+                const int p = p0 + piece_in(l) / PIECES;
+                if (!((p < s.len) & ((p >= all.from) | (p < a.sinks)))) hold &= ~(1u << l);
+            }
             missing |= needed & !ok;
-            const size_t page = ok ? entry[l] : 0, at = ((size_t(h) << a.pages.shift) + (p & page_mask)) * d + 8 * (q - row * PIECES);
-            kr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.k + page * a.pages.k_stride + at));
-            vr[l] = dev::load16(reinterpret_cast<const uint8_t *>(a.pages.v + page * a.pages.v_stride + at));
-            hold |= uint32_t(needed & ok & (p < s.len) & ((p >= all.from) | (p < a.sinks))) << l;
-            there[l] = needed & ok;
+            if constexpr (decltype(careful)::value) {
+                there[l] = needed & ok;
+                if (!ok) hold &= ~(1u << l);
+            }
+            const uint64_t page = ok ? uint32_t(entry[l]) : 0u;
+            const uint32_t at = uint32_t(p0 & page_mask) * ROW + 16u * uint32_t(piece_in(l));
+            kr[l] = dev::load16(head_k + page * page_k + at);
+            vr[l] = dev::load16(head_v + page * page_v + at);
         }
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
+    auto store = [&](int i, auto careful) __attribute__((always_inline)) {
+        const int k_buf = held_scalar((i & 1) * int(sizeof k_sh[0])), v_buf = held_scalar(i % VBUF * int(sizeof v_sh[0]));
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-            const int q = l * THREADS + tid, row = q / PIECES, piece_of = q - row * PIECES;
-            const int at = row * PIECES + (piece_of ^ swizzle<NG>(row));
-            k_sh[buf][at] = kr[l];
-            v_sh[buf][at] = hold >> l & 1 ? vr[l] : make_uint4(0, 0, 0, 0);
-            if ((l * WAVES + wave) % HALF == 0 && lane == 0) there_sh[buf][half_of(l)] = there[l] ? 1u << half_of(l) : 0u;
+            const dev::u32x4 zero = {0, 0, 0, 0};
+            *(lds_u32x4 *)((lds_byte *)k_sh[0] + k_buf + store_at[l]) = __builtin_bit_cast(dev::u32x4, kr[l]);
+            *(lds_u32x4 *)((lds_byte *)v_sh[0] + v_buf + store_at[l]) = hold >> l & 1 ? __builtin_bit_cast(dev::u32x4, vr[l]) : zero;
+            if constexpr (decltype(careful)::value)
+                if ((l * WAVES + wave) % HALF == 0 && lane == 0) there_sh[i % VBUF][half_of(l)] = there[l] ? 1u << half_of(l) : 0u;
+        }
+    };
+    // The loaded positions (step i) go to LDS, those of the next are loaded.
+    auto stage = [&](int i, auto careful) __attribute__((always_inline)) {
+        if (i >= steps) return;
+        store(i, careful);
+        if (i + 1 < steps) {
+            load(i + 1, careful);
+            fetch(min(i + 2, steps - 1));
         }
     };
 
@@ -607,13 +704,135 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     }
     const RowView view = row_view(a, s, i_row);
 
-    // ---- where the lane's operands lie in a buffer (bytes): keys of position n, values of dims of 16 lanes
-    const int k_at = n * ROW, k_swz = c ^ swizzle<NG>(n);
-    const int v_row = 4 * c + (lane & 15) / 4, v_piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-    const int v_at = v_row * ROW + 8 * (lane & 1);
-
-    floatx16 acc[TD];
+    floatx16 acc[TD], p[2];
+    bf16x8 bp[4];
+    uint32_t sees[2] = {0, 0};
     float mx, sum;
+    // Steps that are plain and whose positions every row of the wave sees (first, end): they need no mask.
+    const int2 whole = [&] {
+        const int cached = s.len - s.n, end = a.tree ? cached : cached + i_first + 1, last = a.tree ? s.len - 1 : cached + i_last;
+        int x = plain.x;
+        if (a.window) x = max(x, max(0, last - a.window + 1 - p_plain + kTile - 1) / kTile);
+        return make_int2(x, cached + i_first < 0 ? 0 : min(plain.y, (end - p_plain) / kTile));
+    }();
+    // Whether the wave has work at step i.
+    auto live = [&](int i) {
+        if (i >= whole.x && i < whole.y) return !idle;
+        const int v = range.x + 2 * i;
+        return !idle && (any_visible(a, s, i_first, i_last, z.block(v) * kPos) ||
+                         (v + 1 < range.y && any_visible(a, s, i_first, i_last, z.block(v + 1) * kPos)));
+    };
+    auto scores = [&](int i) __attribute__((always_inline)) {  // positions x rows
+        const lds_byte *kb = (const lds_byte *)k_sh[0] + held_scalar((i & 1) * int(sizeof k_sh[0]));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[u][r] = 0.f;
+        products<2 * KS, AHEAD>(  // (the two halves in turn: their sums do not wait for one another)
+            [&](int m) { return __builtin_bit_cast(uint4, *(const lds_u32x4 *)(kb + k_off[m >> 1] + (m & 1) * 32 * ROW)); },
+            [&](int m, uint4 w) { p[m & 1] = mfma32(__builtin_bit_cast(bf16x8, w), bq[m >> 1], p[m & 1]); });
+    };
+    auto softmax = [&](int i, auto careful) __attribute__((always_inline)) {
+        sees[0] = sees[1] = 0xffff;
+        uint32_t held = 0xf;
+        if constexpr (decltype(careful)::value) {
+            const uint4 halves = *reinterpret_cast<const uint4 *>(there_sh[i % VBUF]);
+            held = __builtin_amdgcn_readfirstlane(halves.x | halves.y | halves.z | halves.w);
+        }
+        if (i < whole.x || i >= whole.y || held != 0xf) {
+            const int v = range.x + 2 * i;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int at = z.block(min(v + u, range.y - 1)) * kPos;
+                const uint32_t drafts = row_drafts<16, 8>(a, s, view, at + 4 * c);
+                uint32_t m = 0;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool see = (row_sees(a, view, at + 8 * (r >> 2) + 4 * c + (r & 3)) | (drafts >> r & 1)) &
+                                     (held >> (2 * u + (r >> 3)) & 1) & (v + u < range.y);
+                    p[u][r] = see ? p[u][r] : -INFINITY;
+                    if constexpr (decltype(careful)::value) m |= uint32_t(see) << r;
+                }
+                if constexpr (decltype(careful)::value) sees[u] = m;
+            }
+        }
+        float top = p[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, p[u][r]);
+        top = fmaxf(top, other_half32(top));
+        if (__any((top - mx) * a.unit > kSlack)) {  // (the first score of a row is infinitely far past its maximum)
+            const float now = fmaxf(mx, top), f = __builtin_amdgcn_exp2f(mx == now ? 0.f : (mx - now) * a.unit);
+            mx = now;
+            sum *= f;
+#pragma unroll
+            for (int t = 0; t < TD; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[t][r] *= f;
+        }
+        const float to = mx == -INFINITY ? 0.f : mx;
+        float off = to * a.unit;
+        if (__any(!(fabsf(off) < kFar))) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[u][r] -= to;
+            off = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[u][r] = __builtin_amdgcn_exp2f(fmaf(p[u][r], a.unit, -off));
+            uint32_t w[8];
+            const bf16x2 one = {__bf16(1.f), __bf16(1.f)};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = pack_bf16(p[u][2 * e], p[u][2 * e + 1]);
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), one, sum, false);
+            }
+            bp[2 * u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+            bp[2 * u + 1] = __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
+        }
+    };
+    auto values = [&](int i, auto careful) __attribute__((always_inline)) {  // dims x rows
+        const lds_byte *vb = (const lds_byte *)v_sh[0] + held_scalar(i % VBUF * int(sizeof v_sh[0]));
+        products<4 * TD, AHEAD>(
+            [&](int m) {
+                const int q = m / TD, t = m % TD;
+                const uint2 lo = read_turned(vb + v_off[t][0] + 16 * q * ROW), hi = read_turned(vb + v_off[t][1] + 16 * q * ROW);
+                return make_uint4(lo.x, lo.y, hi.x, hi.y);
+            },
+            [&](int m, uint4 w) {
+                const int q = m / TD, t = m % TD;
+                if constexpr (decltype(careful)::value) {
+                    uint32_t x[4] = {w.x, w.y, w.z, w.w}, f[4], g[4];
+                    bool any = false;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        f[k] = not_finite(x[k]);
+                        x[k] &= ~f[k];
+                        any |= f[k] != 0;
+                        f[k] &= 0x3f803f80u;
+                        const uint32_t b = sees[q >> 1] >> (8 * (q & 1) + 2 * k);
+                        g[k] = (b & 1) * 0x3f80u | (b >> 1 & 1) * 0x3f800000u;
+                    }
+                    w = make_uint4(x[0], x[1], x[2], x[3]);
+                    if (__any(any)) {
+                        floatx16 met;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) met[r] = 0.f;
+                        met = mfma32(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])),
+                                     __builtin_bit_cast(bf16x8, make_uint4(g[0], g[1], g[2], g[3])), met);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (met[r] > 0.f) acc[t][r] = NAN;
+                    }
+                }
+                acc[t] = mfma32(__builtin_bit_cast(bf16x8, w), bp[q], acc[t]);
+            });
+    };
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
     auto pass = [&](auto careful) __attribute__((always_inline)) {
         mx = -INFINITY;
         sum = 0.f;
@@ -621,135 +840,51 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
         for (int t = 0; t < TD; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
-        if (range.x < range.y) {
-            fetch(range.x);
-            load(range.x);
-            fetch(min(range.x + 2, range.y - 1));
-            store(0);
+        if (steps > 0) {
+            fetch(0);
+            load(0, careful);
+            fetch(min(1, steps - 1));
+            stage(0, careful);
         }
         lds_barrier();
-        auto step = [&](int v, int buf) __attribute__((always_inline)) {
-            const bool more = v + 2 < range.y;
-            if (more) {
-                load(v + 2);
-                fetch(min(v + 4, range.y - 1));
+        if constexpr (TWO) {
+            // Step i of the first group: products in phase 2 i, exponentials in 2 i + 1; of the second one phase later.
+            // Positions i + 1 are written in phases 2 i and 2 i + 1, when the last readers of the buffers are through.
+            const bool second = wave >= WAVES / 2;
+            if (second) {
+                stage(1, careful);
+                lds_barrier();
             }
-            __builtin_amdgcn_sched_barrier(0);
-            const int b[2] = {z.block(v), z.block(min(v + 1, range.y - 1))};
-            const bool two = v + 1 < range.y;
-            if (!idle && (any_visible(a, s, i_first, i_last, b[0] * kPos) || (two && any_visible(a, s, i_first, i_last, b[1] * kPos)))) {
-                const uint8_t *kb = reinterpret_cast<const uint8_t *>(k_sh[buf]), *vb = reinterpret_cast<const uint8_t *>(v_sh[buf]);
-                // ---- scores: positions x rows
-                floatx16 p[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[u][r] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < KS; ++j) {
-                        const uint4 w = *reinterpret_cast<const uint4 *>(kb + k_at + u * 32 * ROW + 16 * (2 * j ^ k_swz));
-                        p[u] = mfma32(__builtin_bit_cast(bf16x8, w), bq[j], p[u]);
-                    }
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                // ---- softmax
-                const uint4 halves = *reinterpret_cast<const uint4 *>(there_sh[buf]);
-                const uint32_t there = __builtin_amdgcn_readfirstlane(halves.x | halves.y | halves.z | halves.w);
-                uint32_t sees[2] = {0xffff, 0xffff};
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bool full = (there >> (2 * u) & 3) == 3 && (u == 0 || two) && all_visible(a, s, i_first, i_last, b[u] * kPos, kPos);
-                    if (full) continue;
-                    sees[u] = row_sees<16, 8>(a, s, view, b[u] * kPos + 4 * c);
-                    sees[u] &= (there >> (2 * u) & 1 ? 0xffu : 0u) | (there >> (2 * u) & 2 ? 0xff00u : 0u);
-                    if (u && !two) sees[u] = 0;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[u][r] = sees[u] >> r & 1 ? p[u][r] : -INFINITY;
-                }
-                float top = p[0][0];
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, p[u][r]);
-                top = fmaxf(top, other_half32(top));
-                if (__any((top - mx) * a.unit > kSlack)) {  // (the first score of a row is infinitely far past its maximum)
-                    const float now = fmaxf(mx, top), f = __builtin_amdgcn_exp2f(mx == now ? 0.f : (mx - now) * a.unit);
-                    mx = now;
-                    sum *= f;
-#pragma unroll
-                    for (int t = 0; t < TD; ++t)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[t][r] *= f;
-                }
-                const float to = mx == -INFINITY ? 0.f : mx;
-                float off = to * a.unit;
-                if (__any(!(fabsf(off) < kFar))) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) p[u][r] -= to;
-                    off = 0.f;
-                }
-                bf16x8 bp[4];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[u][r] = __builtin_amdgcn_exp2f(fmaf(p[u][r], a.unit, -off));
-                    uint32_t w[8];
-                    const bf16x2 one = {__bf16(1.f), __bf16(1.f)};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        w[e] = pack_bf16(p[u][2 * e], p[u][2 * e + 1]);
-                        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), one, sum, false);
-                    }
-                    bp[2 * u] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                    bp[2 * u + 1] = __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                // ---- values: dims x rows
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int t = 0; t < TD; ++t) {
-                        uint2 w[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            w[e] = read_turned(vb + v_at + (16 * q + 8 * e) * ROW + 16 * ((4 * t + v_piece) ^ swizzle<NG>(v_row + 8 * e)));
-                        uint32_t x[4] = {w[0].x, w[0].y, w[1].x, w[1].y};
-                        if constexpr (decltype(careful)::value) {
-                            uint32_t f[4], g[4];
-                            bool any = false;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                f[k] = not_finite(x[k]);
-                                x[k] &= ~f[k];
-                                any |= f[k] != 0;
-                                f[k] &= 0x3f803f80u;
-                                const uint32_t m = sees[q >> 1] >> (8 * (q & 1) + 2 * k);
-                                g[k] = (m & 1) * 0x3f80u | (m >> 1 & 1) * 0x3f800000u;
-                            }
-                            if (__any(any)) {
-                                floatx16 met;
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) met[r] = 0.f;
-                                met = mfma32(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])),
-                                             __builtin_bit_cast(bf16x8, make_uint4(g[0], g[1], g[2], g[3])), met);
-#pragma unroll
-                                for (int r = 0; r < 16; ++r)
-                                    if (met[r] > 0.f) acc[t][r] = NAN;
-                            }
-                        }
-                        acc[t] = mfma32(__builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3])), bp[q], acc[t]);
-                    }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (more) store(buf ^ 1);
-            lds_barrier();
-        };
+            bool was = false;
 #pragma unroll 1
-        for (int v = range.x; v < range.y; v += 4) {
-            step(v, 0);
-            if (v + 2 < range.y) step(v + 2, 1);
+            for (int i = 0; i <= steps; ++i) {
+                const bool now = i < steps && live(i);
+                fence();
+                if (was) values(i + VBUF - 1, careful);
+                if (now) scores(i);
+                fence();
+                lds_barrier();
+                if (now) softmax(i, careful);
+                fence();
+                if (i < steps) stage(second ? i + 2 : i + 1, careful);
+                lds_barrier();
+                was = now;
+            }
+            if (!second) lds_barrier();
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < steps; ++i) {
+                if (live(i)) {
+                    scores(i);
+                    fence();
+                    softmax(i, careful);
+                    fence();
+                    values(i, careful);
+                }
+                fence();
+                stage(i + 1, careful);
+                lds_barrier();
+            }
         }
     };
     pass(std::false_type());
@@ -758,8 +893,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     for (int t = 0; t < TD; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) off |= !(fabsf(acc[t][r]) < INFINITY);
-    if (__builtin_expect(__syncthreads_or(off && !idle), 0)) pass(std::true_type());
-
+    if (__builtin_expect(__syncthreads_or((off && !idle) || missing), 0)) pass(std::true_type());
     if (missing && lane == 0) atomicOr(a.err, kErrRange);
     const float l = sum + other_half32(sum);
     if (w_row0 + n >= rows) return;

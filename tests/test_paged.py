@@ -225,7 +225,7 @@ def test_append_refusals():
     good = dict(k=P, v=P, dtype=0, ks=256, vs=256, T=4, n_kv=4, d=64, slots=P, kp=P, vp=P, kps=4096, vps=4096, n_pages=9, page=16)
     bads = [dict(k=None), dict(v=None), dict(slots=None), dict(kp=None), dict(vp=None), dict(k=P + 8), dict(kp=P + 8),
             dict(dtype=2), dict(dtype=-1), dict(ks=252), dict(vs=258), dict(ks=-256), dict(T=-1), dict(n_kv=0), dict(n_kv=70000),
-            dict(d=32), dict(d=96), dict(kps=4088), dict(vps=4100), dict(kps=(1 << 40) + 8), dict(n_pages=0), dict(page=17),
+            dict(d=32), dict(d=96), dict(kps=4088), dict(vps=4100), dict(kps=1 << 31), dict(n_pages=0), dict(page=17),
             dict(slots=P + 2)]
     for b in bads:
         refused("moe_paged_append", *{**good, **b}.values(), None)

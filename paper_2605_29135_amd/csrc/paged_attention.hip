@@ -580,7 +580,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     constexpr int LOADS = kTile * PIECES / THREADS, KS = d / 16, TD = d / 32;
     constexpr int HALF = 16 * PIECES / 64;   // loads of a wave that make 16 positions
     constexpr bool TWO = WAVES == 8;
-    constexpr int AHEAD = 6;                 // products whose operands are in flight
+    constexpr int AHEAD = 4;                 // products whose operands are in flight
     constexpr int VBUF = TWO ? 3 : 2;        // (values are read a step after the keys)
     __shared__ uint4 k_sh[2][kTile * PIECES], v_sh[VBUF][kTile * PIECES];
     __shared__ alignas(16) uint32_t there_sh[VBUF][4];  // bits of the halves of the two blocks that are there
@@ -647,49 +647,51 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
         for (int l = 0; l < LOADS; ++l)
             entry[l] = table.row[(easy ? p_plain + kTile * i + 16 * half_of(l) : min(half_at(i, half_of(l)), table.last)) >> table.shift];
     };
-    auto load = [&](int i, auto careful) __attribute__((always_inline)) {
-        const bool easy = i >= plain.x && i < plain.y;
-        hold = ~0u;
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l) {
-            int p0 = p_plain + kTile * i + 16 * half_of(l);
-            bool ok = uint32_t(entry[l]) < uint32_t(table.n_pages), needed = true;
-            if (!easy) {
-                p0 = half_at(i, half_of(l));
-                needed = half_seen(a, s, all, p0);
-                const int p = p0 + piece_in(l) / PIECES;
-                if (!((p < s.len) & ((p >= all.from) | (p < a.sinks)))) hold &= ~(1u << l);
-            }
-            missing |= needed & !ok;
-            if constexpr (decltype(careful)::value) {
-                there[l] = needed & ok;
-                if (!ok) hold &= ~(1u << l);
-            }
-            const uint64_t page = ok ? uint32_t(entry[l]) : 0u;
-            const uint32_t at = uint32_t(p0 & page_mask) * ROW + 16u * uint32_t(piece_in(l));
-            kr[l] = dev::load16(head_k + page * page_k + at);
-            vr[l] = dev::load16(head_v + page * page_v + at);
+    // easy: positions i are plain
+    auto load = [&](int i, int l, bool easy, auto careful) __attribute__((always_inline)) {
+        int p0 = p_plain + kTile * i + 16 * half_of(l);
+        const bool ok = uint32_t(entry[l]) < uint32_t(table.n_pages);
+        bool needed = true, keep = true;
+        if (!easy) {
+            p0 = half_at(i, half_of(l));
+            needed = half_seen(a, s, all, p0);
+            const int p = p0 + piece_in(l) / PIECES;
+            keep = (p < s.len) & ((p >= all.from) | (p < a.sinks));
         }
+        missing |= needed & !ok;
+        if constexpr (decltype(careful)::value) {
+            there[l] = needed & ok;
+            keep &= ok;
+        }
+        hold = keep ? hold | 1u << l : hold & ~(1u << l);
+        const uint64_t page = ok ? uint32_t(entry[l]) : 0u;
+        const uint32_t at = uint32_t(p0 & page_mask) * ROW + 16u * uint32_t(piece_in(l));
+        kr[l] = dev::load16(head_k + page * page_k + at);
+        vr[l] = dev::load16(head_v + page * page_v + at);
     };
-    auto store = [&](int i, auto careful) __attribute__((always_inline)) {
+    auto store = [&](int i, int l, auto careful) __attribute__((always_inline)) {
         const int k_buf = held_scalar((i & 1) * int(sizeof k_sh[0])), v_buf = held_scalar(i % VBUF * int(sizeof v_sh[0]));
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l) {
-            const dev::u32x4 zero = {0, 0, 0, 0};
-            *(lds_u32x4 *)((lds_byte *)k_sh[0] + k_buf + store_at[l]) = __builtin_bit_cast(dev::u32x4, kr[l]);
-            *(lds_u32x4 *)((lds_byte *)v_sh[0] + v_buf + store_at[l]) = hold >> l & 1 ? __builtin_bit_cast(dev::u32x4, vr[l]) : zero;
-            if constexpr (decltype(careful)::value)
-                if ((l * WAVES + wave) % HALF == 0 && lane == 0) there_sh[i % VBUF][half_of(l)] = there[l] ? 1u << half_of(l) : 0u;
-        }
+        const dev::u32x4 zero = {0, 0, 0, 0};
+        *(lds_u32x4 *)((lds_byte *)k_sh[0] + k_buf + store_at[l]) = __builtin_bit_cast(dev::u32x4, kr[l]);
+        *(lds_u32x4 *)((lds_byte *)v_sh[0] + v_buf + store_at[l]) = hold >> l & 1 ? __builtin_bit_cast(dev::u32x4, vr[l]) : zero;
+        if constexpr (decltype(careful)::value)
+            if ((l * WAVES + wave) % HALF == 0 && lane == 0) there_sh[i % VBUF][half_of(l)] = there[l] ? 1u << half_of(l) : 0u;
     };
-    // The loaded positions (step i) go to LDS, those of the next are loaded.
+    // The loaded positions (step i) go to LDS, those of the next are loaded, the table's entries of the one after fetched.
     auto stage = [&](int i, auto careful) __attribute__((always_inline)) {
         if (i >= steps) return;
-        store(i, careful);
-        if (i + 1 < steps) {
-            load(i + 1, careful);
-            fetch(min(i + 2, steps - 1));
-        }
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) store(i, l, careful);
+        if (i + 1 >= steps) return;
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) load(i + 1, l, i + 1 >= plain.x && i + 1 < plain.y, careful);
+        fetch(min(i + 2, steps - 1));
+    };
+    // The same where these steps are plain, a piece of it behind each of the first few products.
+    auto stage_plain = [&](int i, int piece) __attribute__((always_inline)) {
+        if (piece < LOADS) store(i, piece, std::false_type());
+        else if (piece < 2 * LOADS) load(i + 1, piece - LOADS, true, std::false_type());
+        else if (piece == 2 * LOADS) fetch(i + 2);
     };
 
     // ---- the wave's rows; a row past the last repeats it and is not stored
@@ -730,7 +732,9 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             for (int r = 0; r < 16; ++r) p[u][r] = 0.f;
         products<2 * KS, AHEAD>(  // (the two halves in turn: their sums do not wait for one another)
             [&](int m) { return __builtin_bit_cast(uint4, *(const lds_u32x4 *)(kb + k_off[m >> 1] + (m & 1) * 32 * ROW)); },
-            [&](int m, uint4 w) { p[m & 1] = mfma32(__builtin_bit_cast(bf16x8, w), bq[m >> 1], p[m & 1]); });
+            [&](int m, uint4 w) {
+                p[m & 1] = mfma32(__builtin_bit_cast(bf16x8, w), bq[m >> 1], p[m & 1]);
+            });
     };
     auto softmax = [&](int i, auto careful) __attribute__((always_inline)) {
         sees[0] = sees[1] = 0xffff;
@@ -795,7 +799,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             bp[2 * u + 1] = __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
         }
     };
-    auto values = [&](int i, auto careful) __attribute__((always_inline)) {  // dims x rows
+    auto values = [&](int i, auto careful, auto beside) __attribute__((always_inline)) {  // dims x rows; beside(m): behind product m
         const lds_byte *vb = (const lds_byte *)v_sh[0] + held_scalar(i % VBUF * int(sizeof v_sh[0]));
         products<4 * TD, AHEAD>(
             [&](int m) {
@@ -830,6 +834,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
                     }
                 }
                 acc[t] = mfma32(__builtin_bit_cast(bf16x8, w), bp[q], acc[t]);
+                beside(m);
             });
     };
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
@@ -842,49 +847,82 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
         if (steps > 0) {
             fetch(0);
-            load(0, careful);
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) load(0, l, false, careful);
             fetch(min(1, steps - 1));
             stage(0, careful);
         }
         lds_barrier();
+        auto nothing = [](int) {};
+        // Steps easy.x up to easy.y: plain ones, with plain ones behind them as far as staging reaches, seen whole by the
+        // wave's rows.
+        const int2 easy = decltype(careful)::value || idle ? make_int2(0, 0) : make_int2(whole.x + 1, min(whole.y, plain.y - 2));
         if constexpr (TWO) {
             // Step i of the first group: products in phase 2 i, exponentials in 2 i + 1; of the second one phase later.
-            // Positions i + 1 are written in phases 2 i and 2 i + 1, when the last readers of the buffers are through.
+            // Positions i + 1 are written beside step i's products, in phases 2 i and 2 i + 1: the last readers of the
+            // buffers are through with phase 2 i - 1.
             const bool second = wave >= WAVES / 2;
-            if (second) {
-                stage(1, careful);
-                lds_barrier();
-            }
+            if (second) lds_barrier();
             bool was = false;
-#pragma unroll 1
-            for (int i = 0; i <= steps; ++i) {
+            auto step = [&](int i) __attribute__((always_inline)) {
                 const bool now = i < steps && live(i);
+                stage(i + 1, careful);
                 fence();
-                if (was) values(i + VBUF - 1, careful);
+                if (was) values(i + VBUF - 1, careful, nothing);
                 if (now) scores(i);
                 fence();
                 lds_barrier();
                 if (now) softmax(i, careful);
                 fence();
-                if (i < steps) stage(second ? i + 2 : i + 1, careful);
                 lds_barrier();
                 was = now;
-            }
+            };
+            int i = 0;
+#pragma unroll 1
+            for (; i <= steps && i < easy.x; ++i) step(i);
+            if constexpr (!decltype(careful)::value)
+#pragma unroll 1
+                for (; i < easy.y; ++i) {
+                    values(i + VBUF - 1, careful, [&](int m) __attribute__((always_inline)) { stage_plain(i + 1, m); });
+                    scores(i);
+                    fence();
+                    lds_barrier();
+                    softmax(i, careful);
+                    fence();
+                    lds_barrier();
+                }
+#pragma unroll 1
+            for (; i <= steps; ++i) step(i);
             if (!second) lds_barrier();
         } else {
-#pragma unroll 1
-            for (int i = 0; i < steps; ++i) {
+            auto step = [&](int i) __attribute__((always_inline)) {
                 if (live(i)) {
                     scores(i);
                     fence();
                     softmax(i, careful);
                     fence();
-                    values(i, careful);
+                    values(i, careful, nothing);
                 }
                 fence();
                 stage(i + 1, careful);
                 lds_barrier();
-            }
+            };
+            int i = 0;
+#pragma unroll 1
+            for (; i < steps && i < easy.x; ++i) step(i);
+            if constexpr (!decltype(careful)::value)
+#pragma unroll 1
+                for (; i < easy.y; ++i) {
+                    scores(i);
+                    fence();
+                    softmax(i, careful);
+                    fence();
+                    values(i, careful, [&](int m) __attribute__((always_inline)) { stage_plain(i + 1, m); });
+                    fence();
+                    lds_barrier();
+                }
+#pragma unroll 1
+            for (; i < steps; ++i) step(i);
         }
     };
     pass(std::false_type());

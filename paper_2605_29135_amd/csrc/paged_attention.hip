@@ -531,11 +531,13 @@ __device__ __forceinline__ int swizzle(int row) {
 }
 // N products with an operand from LDS each, which is read AHEAD products in front of its use.  (Left to itself the compiler
 // reads an operand, waits and multiplies: an LDS latency for each product.)
-template <int N, int AHEAD, typename READ, typename USE>
-__device__ __forceinline__ void products(READ read, USE use) {
-    uint4 w[AHEAD];
+template <int AHEAD, typename READ>
+__device__ __forceinline__ void read_first(uint4 (&w)[AHEAD], READ read) {
 #pragma unroll
     for (int m = 0; m < AHEAD; ++m) w[m] = read(m);
+}
+template <int N, int AHEAD, typename READ, typename USE>
+__device__ __forceinline__ void products(uint4 (&w)[AHEAD], READ read, USE use) {  // w: as of read_first
 #pragma unroll
     for (int m = 0; m < N; ++m) {
         __builtin_amdgcn_sched_barrier(0);
@@ -689,9 +691,16 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     };
     // The same where these steps are plain, a piece of it behind each of the first few products.
     auto stage_plain = [&](int i, int piece) __attribute__((always_inline)) {
-        if (piece < LOADS) store(i, piece, std::false_type());
-        else if (piece < 2 * LOADS) load(i + 1, piece - LOADS, true, std::false_type());
-        else if (piece == 2 * LOADS) fetch(i + 2);
+        if (piece < LOADS) {
+            hold = ~0u;
+            store(i, piece, std::false_type());
+        } else if (piece < 2 * LOADS) {
+            load(i + 1, piece - LOADS, true, std::false_type());
+        }
+    };
+    auto fetch_plain = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) entry[l] = table.row[uint32_t(p_plain + kTile * i + 16 * half_of(l)) >> table.shift];
     };
 
     // ---- the wave's rows; a row past the last repeats it and is not stored
@@ -724,26 +733,31 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
         return !idle && (any_visible(a, s, i_first, i_last, z.block(v) * kPos) ||
                          (v + 1 < range.y && any_visible(a, s, i_first, i_last, z.block(v + 1) * kPos)));
     };
-    auto scores = [&](int i) __attribute__((always_inline)) {  // positions x rows
-        const lds_byte *kb = (const lds_byte *)k_sh[0] + held_scalar((i & 1) * int(sizeof k_sh[0]));
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) p[u][r] = 0.f;
-        products<2 * KS, AHEAD>(  // (the two halves in turn: their sums do not wait for one another)
-            [&](int m) { return __builtin_bit_cast(uint4, *(const lds_u32x4 *)(kb + k_off[m >> 1] + (m & 1) * 32 * ROW)); },
-            [&](int m, uint4 w) {
-                p[m & 1] = mfma32(__builtin_bit_cast(bf16x8, w), bq[m >> 1], p[m & 1]);
-            });
+    // Scores: positions x rows, the two halves in turn, so that their sums do not wait for one another.
+    auto keys_at = [&](int i) { return (const lds_byte *)k_sh[0] + held_scalar((i & 1) * int(sizeof k_sh[0])); };
+    auto key = [&](const lds_byte *kb, int m) __attribute__((always_inline)) {
+        return __builtin_bit_cast(uint4, *(const lds_u32x4 *)(kb + k_off[m >> 1] + (m & 1) * 32 * ROW));
     };
-    auto softmax = [&](int i, auto careful) __attribute__((always_inline)) {
+    auto score = [&](int m, uint4 w) __attribute__((always_inline)) {
+        if (m < 2)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[m][r] = 0.f;
+        p[m & 1] = mfma32(__builtin_bit_cast(bf16x8, w), bq[m >> 1], p[m & 1]);
+    };
+    auto scores = [&](int i) __attribute__((always_inline)) {
+        const lds_byte *kb = keys_at(i);
+        uint4 w[AHEAD];
+        read_first(w, [&](int m) { return key(kb, m); });
+        products<2 * KS>(w, [&](int m) { return key(kb, m); }, score);
+    };
+    auto softmax = [&](int i, auto careful, auto masked) __attribute__((always_inline)) {
         sees[0] = sees[1] = 0xffff;
         uint32_t held = 0xf;
         if constexpr (decltype(careful)::value) {
             const uint4 halves = *reinterpret_cast<const uint4 *>(there_sh[i % VBUF]);
             held = __builtin_amdgcn_readfirstlane(halves.x | halves.y | halves.z | halves.w);
         }
-        if (i < whole.x || i >= whole.y || held != 0xf) {
+        if (decltype(masked)::value && (i < whole.x || i >= whole.y || held != 0xf)) {
             const int v = range.x + 2 * i;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -799,43 +813,50 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             bp[2 * u + 1] = __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7]));
         }
     };
-    auto values = [&](int i, auto careful, auto beside) __attribute__((always_inline)) {  // dims x rows; beside(m): behind product m
-        const lds_byte *vb = (const lds_byte *)v_sh[0] + held_scalar(i % VBUF * int(sizeof v_sh[0]));
-        products<4 * TD, AHEAD>(
-            [&](int m) {
-                const int q = m / TD, t = m % TD;
-                const uint2 lo = read_turned(vb + v_off[t][0] + 16 * q * ROW), hi = read_turned(vb + v_off[t][1] + 16 * q * ROW);
-                return make_uint4(lo.x, lo.y, hi.x, hi.y);
-            },
-            [&](int m, uint4 w) {
-                const int q = m / TD, t = m % TD;
-                if constexpr (decltype(careful)::value) {
-                    uint32_t x[4] = {w.x, w.y, w.z, w.w}, f[4], g[4];
-                    bool any = false;
+    // Outputs: dims x rows.
+    auto values_at = [&](int i) { return (const lds_byte *)v_sh[0] + held_scalar(i % VBUF * int(sizeof v_sh[0])); };
+    auto value = [&](const lds_byte *vb, int m) __attribute__((always_inline)) {
+        const int q = m / TD, t = m % TD;
+        const uint2 lo = read_turned(vb + v_off[t][0] + 16 * q * ROW), hi = read_turned(vb + v_off[t][1] + 16 * q * ROW);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    };
+    auto output = [&](int m, uint4 w, auto careful) __attribute__((always_inline)) {
+        const int q = m / TD, t = m % TD;
+        if constexpr (decltype(careful)::value) {
+            uint32_t x[4] = {w.x, w.y, w.z, w.w}, f[4], g[4];
+            bool any = false;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        f[k] = not_finite(x[k]);
-                        x[k] &= ~f[k];
-                        any |= f[k] != 0;
-                        f[k] &= 0x3f803f80u;
-                        const uint32_t b = sees[q >> 1] >> (8 * (q & 1) + 2 * k);
-                        g[k] = (b & 1) * 0x3f80u | (b >> 1 & 1) * 0x3f800000u;
-                    }
-                    w = make_uint4(x[0], x[1], x[2], x[3]);
-                    if (__any(any)) {
-                        floatx16 met;
+            for (int k = 0; k < 4; ++k) {
+                f[k] = not_finite(x[k]);
+                x[k] &= ~f[k];
+                any |= f[k] != 0;
+                f[k] &= 0x3f803f80u;
+                const uint32_t b = sees[q >> 1] >> (8 * (q & 1) + 2 * k);
+                g[k] = (b & 1) * 0x3f80u | (b >> 1 & 1) * 0x3f800000u;
+            }
+            w = make_uint4(x[0], x[1], x[2], x[3]);
+            if (__any(any)) {
+                floatx16 met;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) met[r] = 0.f;
-                        met = mfma32(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])),
-                                     __builtin_bit_cast(bf16x8, make_uint4(g[0], g[1], g[2], g[3])), met);
+                for (int r = 0; r < 16; ++r) met[r] = 0.f;
+                met = mfma32(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])),
+                             __builtin_bit_cast(bf16x8, make_uint4(g[0], g[1], g[2], g[3])), met);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (met[r] > 0.f) acc[t][r] = NAN;
-                    }
-                }
-                acc[t] = mfma32(__builtin_bit_cast(bf16x8, w), bp[q], acc[t]);
-                beside(m);
-            });
+                for (int r = 0; r < 16; ++r)
+                    if (met[r] > 0.f) acc[t][r] = NAN;
+            }
+        }
+        acc[t] = mfma32(__builtin_bit_cast(bf16x8, w), bp[q], acc[t]);
+    };
+    auto values = [&](int i, auto careful, auto beside) __attribute__((always_inline)) {  // beside(m): behind product m
+        const lds_byte *vb = values_at(i);
+        uint4 w[AHEAD];
+        read_first(w, [&](int m) { return value(vb, m); });
+        products<4 * TD>(w, [&](int m) { return value(vb, m); },
+                         [&](int m, uint4 x) __attribute__((always_inline)) {
+                             output(m, x, careful);
+                             beside(m);
+                         });
     };
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
     auto pass = [&](auto careful) __attribute__((always_inline)) {
@@ -856,7 +877,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
         auto nothing = [](int) {};
         // Steps easy.x up to easy.y: plain ones, with plain ones behind them as far as staging reaches, seen whole by the
         // wave's rows.
-        const int2 easy = decltype(careful)::value || idle ? make_int2(0, 0) : make_int2(whole.x + 1, min(whole.y, plain.y - 2));
+        const int2 easy = decltype(careful)::value || idle ? make_int2(0, 0) : make_int2(whole.x + 1, min(whole.y, plain.y - 3));
         if constexpr (TWO) {
             // Step i of the first group: products in phase 2 i, exponentials in 2 i + 1; of the second one phase later.
             // Positions i + 1 are written beside step i's products, in phases 2 i and 2 i + 1: the last readers of the
@@ -872,7 +893,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
                 if (now) scores(i);
                 fence();
                 lds_barrier();
-                if (now) softmax(i, careful);
+                if (now) softmax(i, careful, std::true_type());
                 fence();
                 lds_barrier();
                 was = now;
@@ -883,11 +904,21 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             if constexpr (!decltype(careful)::value)
 #pragma unroll 1
                 for (; i < easy.y; ++i) {
-                    values(i + VBUF - 1, careful, [&](int m) __attribute__((always_inline)) { stage_plain(i + 1, m); });
-                    scores(i);
+                    const lds_byte *vb = values_at(i + VBUF - 1), *kb = keys_at(i);
+                    auto operand = [&](int m) __attribute__((always_inline)) { return m < 4 * TD ? value(vb, m) : key(kb, m - 4 * TD); };
+                    uint4 w[AHEAD];
+                    read_first(w, operand);
+                    products<4 * TD + 2 * KS>(w, operand, [&](int m, uint4 x) __attribute__((always_inline)) {
+                        if (m < 4 * TD) output(m, x, careful);
+                        else score(m - 4 * TD, x);
+                        stage_plain(i + 1, m);
+                    });
                     fence();
                     lds_barrier();
-                    softmax(i, careful);
+                    fence();
+                    // (here, where no LDS read waits for the scalar cache)
+                    fetch_plain(i + 3);
+                    softmax(i, careful, std::false_type());
                     fence();
                     lds_barrier();
                 }
@@ -899,7 +930,7 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
                 if (live(i)) {
                     scores(i);
                     fence();
-                    softmax(i, careful);
+                    softmax(i, careful, std::true_type());
                     fence();
                     values(i, careful, nothing);
                 }
@@ -910,17 +941,20 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
             int i = 0;
 #pragma unroll 1
             for (; i < steps && i < easy.x; ++i) step(i);
-            if constexpr (!decltype(careful)::value)
+            if constexpr (!decltype(careful)::value) {
 #pragma unroll 1
                 for (; i < easy.y; ++i) {
                     scores(i);
                     fence();
-                    softmax(i, careful);
+                    fetch_plain(i + 2);
+                    softmax(i, careful, std::false_type());
                     fence();
                     values(i, careful, [&](int m) __attribute__((always_inline)) { stage_plain(i + 1, m); });
                     fence();
                     lds_barrier();
                 }
+                if (i < steps) fetch(min(i + 2, steps - 1));
+            }
 #pragma unroll 1
             for (; i < steps; ++i) step(i);
         }

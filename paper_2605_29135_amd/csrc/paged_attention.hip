@@ -205,6 +205,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 template <int NG, int NT, bool F32>
 __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_kernel(PagedArgs a) {
     constexpr int d = NG * 64, QT = F32 ? 3 : 1, PT = F32 ? 3 : 2, ROWS = 16;
+    constexpr int UB = NT == 1 && NG <= 2 && !(F32 && NG == 2) ? 2 : 1;  // blocks at a time
     constexpr int VE = NG % 2 ? 4 : 8, VG = d / (16 * VE);  // dims of a lane per group of products, groups
     __shared__ float4 out_sh[kAttWaves][ROWS][d / 4 + 1];
     __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
@@ -222,52 +223,70 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
     const Table table = sequence_table(a, piece);
     const int page_mask = (1 << a.pages.shift) - 1;
 
-    // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.
-    uint4 kc[2][2 * NG];
-    uint32_t vc[VG][8][VE / 2];
+    // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.  UB blocks
+    // at a time (kAttWaves apart), the next ones loaded as soon as the present ones have been used: the bytes in flight are
+    // what bounds a batch of single tokens.
+    uint4 kc[UB][2][2 * NG];
+    uint32_t vc[UB][VG][8][VE / 2];
     // Half a block lies in one page.  `there`: bits of the halves (four each) of which some token sees a position, and whose
     // page is there; the others are read from the first page, and none of it is used.  The table's entries are fetched a
     // block ahead of the loads.
-    uint32_t there = 0;
+    uint32_t there[UB] = {};
     bool missing = false;
-    int32_t entry[2] = {0, 0};
-    int page_at[2] = {0, 0};
-    auto fetch = [&](int b) __attribute__((always_inline)) {
+    int32_t entry[UB][2] = {};
+    int page_at[UB][2] = {};
+    auto block_at = [&](int v, int u) { return z.block(min(v + u * kAttWaves, range.y - 1)); };
+    auto fetch = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) entry[u] = table.entry(b * kPos + 16 * u);
+        for (int u = 0; u < UB; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) entry[u][e] = table.entry(block_at(v, u) * kPos + 16 * e);
     };
-    auto find = [&](int b) __attribute__((always_inline)) {
-        there = 0;
+    auto find = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const bool needed = half_seen(a, s, all, b * kPos + 16 * u), ok = uint32_t(entry[u]) < uint32_t(table.n_pages);
-            missing |= needed & !ok;
-            page_at[u] = ok ? entry[u] : 0;
-            there |= needed && ok ? 0xfu << (4 * u) : 0u;
+        for (int u = 0; u < UB; ++u) {
+            there[u] = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const bool needed = (v + u * kAttWaves < range.y) & half_seen(a, s, all, block_at(v, u) * kPos + 16 * e);
+                const bool ok = uint32_t(entry[u][e]) < uint32_t(table.n_pages);
+                missing |= needed & !ok;
+                page_at[u][e] = ok ? entry[u][e] : 0;
+                there[u] |= needed && ok ? 0xfu << (4 * e) : 0u;
+            }
         }
     };
     auto row_at = [&](int p) { return ((size_t(h) << a.pages.shift) + (p & page_mask)) * d; };
-    auto load_k = [&](int b) __attribute__((always_inline)) {
+    auto load_k = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint16_t *src = a.pages.k + page_at[u] * a.pages.k_stride + row_at(b * kPos + 16 * u + n) + 8 * c;
+        for (int u = 0; u < UB; ++u) {
+            if (v + u * kAttWaves >= range.y) break;
 #pragma unroll
-            for (int j = 0; j < 2 * NG; ++j) kc[u][j] = dev::load16(reinterpret_cast<const uint8_t *>(src + 32 * j));
+            for (int e = 0; e < 2; ++e) {
+                const uint16_t *src = a.pages.k + page_at[u][e] * a.pages.k_stride + row_at(block_at(v, u) * kPos + 16 * e + n) + 8 * c;
+#pragma unroll
+                for (int j = 0; j < 2 * NG; ++j) kc[u][e][j] = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 32 * j));
+            }
         }
     };
-    auto load_v = [&](int b) __attribute__((always_inline)) {
+    auto load_v = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int u = i >> 2;
-            const uint16_t *src = a.pages.v + page_at[u] * a.pages.v_stride + row_at(b * kPos + 16 * u + 4 * c + (i & 3)) + VE * n;
+        for (int u = 0; u < UB; ++u) {
+            if (v + u * kAttWaves >= range.y) break;
 #pragma unroll
-            for (int g = 0; g < VG; ++g) {
-                if constexpr (VE == 8) {
-                    const uint4 w = dev::load16(reinterpret_cast<const uint8_t *>(src + 128 * g));
-                    vc[g][i][0] = w.x, vc[g][i][1] = w.y, vc[g][i][2] = w.z, vc[g][i][3] = w.w;
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(src + 64 * g);
-                    vc[g][i][0] = w.x, vc[g][i][1] = w.y;
+            for (int i = 0; i < 8; ++i) {
+                const int e = i >> 2;
+                const uint16_t *src = a.pages.v + page_at[u][e] * a.pages.v_stride +
+                                      row_at(block_at(v, u) * kPos + 16 * e + 4 * c + (i & 3)) + VE * n;
+#pragma unroll
+                for (int g = 0; g < VG; ++g) {
+                    if constexpr (VE == 8) {
+                        const uint4 w = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 128 * g));
+                        vc[u][g][i][0] = w.x, vc[u][g][i][1] = w.y, vc[u][g][i][2] = w.z, vc[u][g][i][3] = w.w;
+                    } else {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(src + 64 * g);
+                        vc[u][g][i][0] = w.x, vc[u][g][i][1] = w.y;
+                    }
                 }
             }
         }
@@ -297,8 +316,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
     }
     floatx4 acc[NT][4 * NG];
     float mx[NT], sum[NT];
-#pragma unroll 1
-    for (int careful = 0;; ++careful) {
+    auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             mx[t] = -INFINITY;
@@ -307,53 +325,68 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
             for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
         if (range.x + wave < range.y) {
-            const int b = z.block(range.x + wave);
-            fetch(b);
-            find(b);
-            load_k(b);
-            load_v(b);
-            fetch(z.block(min(range.x + wave + kAttWaves, range.y - 1)));
+            fetch(range.x + wave);
+            find(range.x + wave);
+            load_k(range.x + wave);
+            load_v(range.x + wave);
+            fetch(range.x + wave + UB * kAttWaves);
         }
 #pragma unroll 1
-        for (int v = range.x + wave; v < range.y; v += kAttWaves) {
-            const int b = z.block(v), next = z.block(min(v + kAttWaves, range.y - 1));
-            const uint32_t there_mask = there;
-            const bool full = there_mask == 0xff && all_visible(a, s, i_first, i_last, b * kPos, kPos);
+        for (int v = range.x + wave; v < range.y; v += UB * kAttWaves) {
+            const int next = v + UB * kAttWaves;
+            uint32_t held[UB];
+            bool full[UB];
+#pragma unroll
+            for (int u = 0; u < UB; ++u) {
+                held[u] = there[u];
+                full[u] = held[u] == 0xff && all_visible(a, s, i_first, i_last, block_at(v, u) * kPos, kPos);
+            }
             // ---- scores
-            float p[NT][8];
+            float p[NT][UB][8];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < UB; ++u)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    floatx4 y = {0.f, 0.f, 0.f, 0.f};
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int k = QT - 1; k >= 0; --k)
+                    for (int t = 0; t < NT; ++t) {
+                        floatx4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[u][j]), bq[t][j][k], y);
+                        for (int k = QT - 1; k >= 0; --k)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) p[t][4 * u + r] = y[r];
-                }
-            find(next);
-            load_k(next);
-            fetch(z.block(min(v + 2 * kAttWaves, range.y - 1)));
+                            for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[u][e][j]), bq[t][j][k], y);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[t][u][4 * e + r] = y[r];
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+            if (next < range.y) {
+                find(next);
+                load_k(next);
+                fetch(next + UB * kAttWaves);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             // ---- softmax
-            uint32_t sees[NT];
-            bf16x8 bp[NT][PT];
+            uint32_t sees[NT][UB];
+            bf16x8 bp[NT][UB][PT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                sees[t] = 0xff;
-                if (!full) {
-                    const uint32_t drafts = row_drafts<8, 16>(a, s, view[t], b * kPos + 4 * c);
+#pragma unroll
+                for (int u = 0; u < UB; ++u) {
+                    sees[t][u] = 0xff;
+                    if (full[u]) continue;
+                    const int at = block_at(v, u) * kPos + 4 * c;
+                    const uint32_t drafts = row_drafts<8, 16>(a, s, view[t], at);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const bool see = (row_sees(a, view[t], b * kPos + 16 * (k >> 2) + 4 * c + (k & 3)) | (drafts >> k & 1)) & (there_mask >> k & 1);
-                        p[t][k] = see ? p[t][k] : -INFINITY;
-                        if (careful) sees[t] &= ~(uint32_t(!see) << k);
+                        const bool see = (row_sees(a, view[t], at + 16 * (k >> 2) + (k & 3)) | (drafts >> k & 1)) & (held[u] >> k & 1);
+                        p[t][u][k] = see ? p[t][u][k] : -INFINITY;
+                        if constexpr (decltype(careful)::value) sees[t][u] &= ~(uint32_t(!see) << k);
                     }
                 }
-                float top = p[t][0];
+                float top = p[t][0][0];
 #pragma unroll
-                for (int k = 1; k < 8; ++k) top = fmaxf(top, p[t][k]);
+                for (int u = 0; u < UB; ++u)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) top = fmaxf(top, p[t][u][k]);
                 const float was = mx[t], now = fmaxf(was, max_over_c(top)), to = now == -INFINITY ? 0.f : now;
                 if (__any(now > was)) {
                     const float f = __builtin_amdgcn_exp2f((was - to) * a.unit);
@@ -366,81 +399,90 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 }
                 // (differences first: right at any size of the scores)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    p[t][k] = __builtin_amdgcn_exp2f((p[t][k] - to) * a.unit);
-                    sum[t] += p[t][k];
+                for (int u = 0; u < UB; ++u) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        p[t][u][k] = __builtin_amdgcn_exp2f((p[t][u][k] - to) * a.unit);
+                        sum[t] += p[t][u][k];
+                    }
+                    split_terms<PT>(p[t][u], bp[t][u]);
                 }
-                split_terms<PT>(p[t], bp[t]);
             }
             // ---- values
-            if (!full) {
-                // Positions that no token sees may hold anything: zeros.
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int at = b * kPos + 16 * (i >> 2) + 4 * c + (i & 3);
-                    const bool held = (there_mask >> i & 1) & (at < s.len) & ((at >= all.from) | (at < a.sinks));
+            for (int u = 0; u < UB; ++u) {
+                if (!full[u]) {
+                    // Positions that no token sees may hold anything: zeros.
 #pragma unroll
-                    for (int g = 0; g < VG; ++g)
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = block_at(v, u) * kPos + 16 * (i >> 2) + 4 * c + (i & 3);
+                        const bool keep = (held[u] >> i & 1) & (at < s.len) & ((at >= all.from) | (at < a.sinks));
 #pragma unroll
-                        for (int w = 0; w < VE / 2; ++w) vc[g][i][w] = held ? vc[g][i][w] : 0;
-                }
-            }
-            bf16x8 seen_by[NT];
-            if (careful) {
+                        for (int g = 0; g < VG; ++g)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (sees[t] >> (2 * e) & 1) * 0x3f80u | (sees[t] >> (2 * e + 1) & 1) * 0x3f800000u;
-                    seen_by[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                }
-            }
-#pragma unroll
-            for (int g = 0; g < VG; ++g)
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        w[k] = __builtin_amdgcn_perm(vc[g][2 * k + 1][e / 2], vc[g][2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
-                    const int i = g * VE + e;
-                    if (careful) {
-                        uint32_t f[4];
-                        bool any = false;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            f[k] = not_finite(w[k]);
-                            w[k] &= ~f[k];
-                            any |= f[k] != 0;
-                            f[k] &= 0x3f803f80u;
-                        }
-                        if (__any(any))
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                const floatx4 met = mfma(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])), seen_by[t],
-                                                         floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (met[r] > 0.f) acc[t][i][r] = NAN;
-                            }
+                            for (int w = 0; w < VE / 2; ++w) vc[u][g][i][w] = keep ? vc[u][g][i][w] : 0;
                     }
-                    const bf16x8 va = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int k = PT - 1; k >= 0; --k) acc[t][i] = mfma(va, bp[t][k], acc[t][i]);
                 }
-            load_v(next);
+                bf16x8 seen_by[NT];
+                if constexpr (decltype(careful)::value) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = (sees[t][u] >> (2 * e) & 1) * 0x3f80u | (sees[t][u] >> (2 * e + 1) & 1) * 0x3f800000u;
+                        seen_by[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < VG; ++g)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            w[k] = __builtin_amdgcn_perm(vc[u][g][2 * k + 1][e / 2], vc[u][g][2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+                        const int i = g * VE + e;
+                        if constexpr (decltype(careful)::value) {
+                            uint32_t f[4];
+                            bool any = false;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                f[k] = not_finite(w[k]);
+                                w[k] &= ~f[k];
+                                any |= f[k] != 0;
+                                f[k] &= 0x3f803f80u;
+                            }
+                            if (__any(any))
+#pragma unroll
+                                for (int t = 0; t < NT; ++t) {
+                                    const floatx4 met = mfma(__builtin_bit_cast(bf16x8, make_uint4(f[0], f[1], f[2], f[3])), seen_by[t],
+                                                             floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r)
+                                        if (met[r] > 0.f) acc[t][i][r] = NAN;
+                                }
+                        }
+                        const bf16x8 va = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int k = PT - 1; k >= 0; --k) acc[t][i] = mfma(va, bp[t][u][k], acc[t][i]);
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (next < range.y) load_v(next);
         }
-        bool off = false;
+    };
+    pass(std::false_type());
+    bool off = false;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4 * NG; ++i)
+        for (int i = 0; i < 4 * NG; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
-        if (careful || !__any(off)) break;
-    }
+            for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
+    if (__builtin_expect(__any(off), 0)) pass(std::true_type());
     if (missing && lane == 0) atomicOr(a.err, kErrRange);
 
     // Join the waves, one tile of rows at a time.

@@ -47,6 +47,7 @@ struct PagedArgs {
     float unit;             // from scores to log2 units, positive
     int negate;             // the scale's sign
     Split split;
+    int shares;             // 1: the batch may be cut into shares
     Batch batch;
     int *err;
 };
@@ -67,17 +68,117 @@ __device__ __forceinline__ Seen seen(const Seq &s, int window, int sinks) {
     r.count = r.sink + (s.len - 1) / kPos + 1 - r.first;
     return r;
 }
-__device__ __forceinline__ Piece split_piece(const PagedArgs &a, int want, bool by_unit, int *err) {
-    return find_piece(a.batch, a.split, [&](const Seq &s) { return seen(s, a.window, a.sinks).count; }, want, by_unit, err);
+
+// The split of a batch.  Few blocks of positions: sequences are cut into pieces (find_piece).  Many, in the kernel for few
+// rows: the blocks of all sequences, one behind the other, are cut into shares for the grid's units, whatever sequences they
+// fall into, so that all units have the same to do (of pieces, as many as run together, the longest is a fifth longer than
+// the mean: 32 sequences of 4096 to 16384 positions 260 us, shares 220).  A second sequence in a share costs its start, some
+// 3 us, so shares have kShare blocks at least (8 sequences of 1024 to 4096: 26 us in pieces, 30 in shares of 10).  A sequence
+// with tokens has at least one block, so that its outputs are written.  Every wave works it out for itself.
+constexpr int kShare = 32;
+__device__ __forceinline__ int blocks_of(const PagedArgs &a, const Seq &s) {
+    return s.n ? max(1, seen(s, a.window, a.sinks).count) : 0;
 }
-// This block's piece: grid (row tiles, key/value head, sequence), or (key/value head, row tiles, pieces).
-__device__ __forceinline__ Piece this_piece(const PagedArgs &a, int *err) {
-    if (a.split.target) return split_piece(a, blockIdx.z, true, blockIdx.z == 0 ? err : nullptr);
+struct Spread {
+    uint32_t total;  // (a batch that is split has fewer than kTarget sequences of at most 2^21 blocks)
+    int chunk;
+};
+__device__ __forceinline__ Spread spread(const PagedArgs &a, int *err) {
+    const int lane = threadIdx.x & 63;
+    Spread r{0, 0};
+#pragma unroll 1
+    for (int base = 0; base < a.batch.n_seq; base += 64) {
+        Seq s{0, 0, 0, false};
+        if (base + lane < a.batch.n_seq) s = sequence(a.batch, base + lane);
+        if (err && s.bad) atomicOr(err, kErrRange);
+        r.total += uint32_t(__builtin_amdgcn_readlane(int(wave_scan(uint32_t(blocks_of(a, s)))), 63));
+    }
+    r.chunk = max(int((r.total + uint32_t(a.split.target) - 1) / uint32_t(a.split.target)), a.split.least);
+    return r;
+}
+// A part of one sequence: its blocks first..end - 1 (counted as in Seen).
+struct Share {
+    Seq s;
+    int seq, first, end;
+    int count;  // parts that the sequence has; 0: there is no such one, 1: its outputs are final
+    int part;   // number among all parts: those of a sequence follow one another
+};
+__device__ __forceinline__ Share piece_share(const PagedArgs &a, int want, bool by_unit, int *err) {
+    const Piece p = find_piece(a.batch, a.split, [&](const Seq &s) { return seen(s, a.window, a.sinks).count; }, want, by_unit, err);
+    return Share{p.s, p.seq, p.split * p.chunk, p.split == p.count - 1 ? 1 << 30 : (p.split + 1) * p.chunk, p.count, p.first + p.split};
+}
+// This block's piece: grid (row tiles, key/value head, sequence), one each, or with a target (key/value head, row tiles, units).
+__device__ __forceinline__ Share this_piece(const PagedArgs &a, int *err) {
+    if (a.split.target) return piece_share(a, blockIdx.z, true, blockIdx.z == 0 ? err : nullptr);
+    const Share r{sequence(a.batch, blockIdx.z), int(blockIdx.z), 0, 1 << 30, 1, 0};
+    if (r.s.bad && err && (threadIdx.x & 63) == 0) atomicOr(err, kErrRange);
+    return r;
+}
+// The share that begins with block g of the batch (below the total) and ends before g_end, or sequence `want`'s first.
+__device__ __forceinline__ Share share_at(const PagedArgs &a, int chunk, uint32_t g, uint32_t g_end, int want) {
+    const int lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    Share r{};
+#pragma unroll 1
+    for (int base = 0; base < a.batch.n_seq; base += 64) {
+        Seq s{0, 0, 0, false};
+        if (base + lane < a.batch.n_seq) s = sequence(a.batch, base + lane);
+        const int n = blocks_of(a, s);
+        const uint32_t upto = before + wave_scan(uint32_t(n));
+        const unsigned long long hit = __ballot(want < 0 ? upto > g : base + lane == want);
+        if (hit) {
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll(hit) - 1);
+            const int blocks = __builtin_amdgcn_readlane(n, l);
+            const uint32_t start = uint32_t(__builtin_amdgcn_readlane(int(upto), l)) - uint32_t(blocks);
+            if (want >= 0) g = start, g_end = start;
+            r.s.t0 = __builtin_amdgcn_readlane(s.t0, l);
+            r.s.n = __builtin_amdgcn_readlane(s.n, l);
+            r.s.len = __builtin_amdgcn_readlane(s.len, l);
+            r.seq = base + l;
+            r.first = int(g - start);
+            r.end = min(blocks, int(g_end - start));
+            const uint32_t unit = start / uint32_t(chunk);
+            r.count = blocks ? int((start + uint32_t(blocks) - 1) / uint32_t(chunk) - unit) + 1 : 0;
+            r.part = int(g / uint32_t(chunk)) + r.seq;
+            return r;
+        }
+        before = uint32_t(__builtin_amdgcn_readlane(int(upto), 63));
+    }
+    return r;
+}
+// The shares of a unit, one after the other, or its one piece.
+struct Shares {
+    uint32_t at, end;
+    int chunk;  // 0: a piece
+};
+__device__ __forceinline__ Shares first_share(const PagedArgs &a, int *err) {
+    const Spread sp = spread(a, blockIdx.z == 0 ? err : nullptr);
+    if (sp.chunk < kShare) return Shares{0, 1, 0};
+    const unsigned long long at = blockIdx.z * (unsigned long long)sp.chunk, total = sp.total;
+    return Shares{uint32_t(min(at, total)), uint32_t(min(at + sp.chunk, total)), sp.chunk};
+}
+__device__ __forceinline__ bool next_share(const PagedArgs &a, Shares &w, Share &r, int *err) {
+    if (w.at >= w.end) return false;
+    if (w.chunk) {
+        r = share_at(a, w.chunk, w.at, w.end, -1);
+        w.at += uint32_t(r.end - r.first);
+        return true;
+    }
+    w.at = w.end;
+    r = this_piece(a, nullptr);
+    return r.count > 0;
+}
+// For the joins: the parts of a sequence.
+__device__ __forceinline__ Piece split_piece(const PagedArgs &a, int want, bool, int *) {
+    Share r{};
+    const int chunk = a.shares ? spread(a, nullptr).chunk : 0;
+    if (chunk >= kShare) r = share_at(a, chunk, 0, 0, want);
+    else r = piece_share(a, want, false, nullptr);
     Piece p{};
-    p.seq = blockIdx.z;
-    p.count = 1;
-    p.s = sequence(a.batch, p.seq);
-    if (p.s.bad && err && (threadIdx.x & 63) == 0) atomicOr(err, kErrRange);
+    p.s = r.s;
+    p.seq = want;
+    p.first = r.part;
+    p.count = r.count;
     return p;
 }
 
@@ -129,11 +230,11 @@ __device__ __forceinline__ bool all_visible(const PagedArgs &a, const Seq &s, in
     return cached + i0 >= 0 && p + count <= end && (!a.window || p > last - a.window || p + count <= a.sinks);
 }
 
-// The blocks that some of rows row..row_end - 1 sees, and of these (numbered as there) the piece's share: first, end.  Pieces
-// are cut by the sequence's blocks z.  Where rows see more first blocks than z has (their window has left them behind),
+// The blocks that some of rows row..row_end - 1 sees, and of these (numbered as there) the share's: first, end.  Shares are
+// cut by the sequence's blocks z.  Where rows see more first blocks than z has (their window has left them behind),
 // z has no gap and its numbers are the blocks'.
-__device__ __forceinline__ int2 tile_blocks(const PagedArgs &a, const Piece &piece, const Seen &z, int row, int row_end, Seen &t) {
-    const Seq &s = piece.s;
+__device__ __forceinline__ int2 tile_blocks(const PagedArgs &a, const Share &sh, const Seen &z, int row, int row_end, Seen &t) {
+    const Seq &s = sh.s;
     const int p_first = s.len - s.n + row / a.group;
     const int p_last = a.tree ? s.len - 1 : s.len - s.n + (row_end - 1) / a.group;
     t = z;
@@ -143,9 +244,9 @@ __device__ __forceinline__ int2 tile_blocks(const PagedArgs &a, const Piece &pie
         t.first = t.from / kPos;
         t.sink = min((min(a.sinks, t.from) + kPos - 1) / kPos, t.first);
     }
-    const int cut = piece.split * piece.chunk, first = t.first - z.first + z.sink, skip = first - t.sink;
+    const int cut = sh.first, first = t.first - z.first + z.sink, skip = first - t.sink;
     const int end = z.sink + p_last / kPos + 1 - z.first;
-    const int cut_end = piece.split == piece.count - 1 ? end : min(end, cut + piece.chunk);
+    const int cut_end = min(end, sh.end);
     return make_int2(cut < t.sink ? cut : max(cut, first) - skip, max(min(cut_end, t.sink), cut_end - skip));
 }
 
@@ -158,8 +259,8 @@ struct Table {
     // The entry of position p's page (any p: that of the last position behind it).
     __device__ __forceinline__ int32_t entry(int p) const { return row[min(p, last) >> shift]; }
 };
-__device__ __forceinline__ Table sequence_table(const PagedArgs &a, const Piece &piece) {
-    return Table{(table_word *)(a.table + size_t(piece.seq) * a.max_pages), a.pages.n_pages, a.pages.shift, max(piece.s.len - 1, 0)};
+__device__ __forceinline__ Table sequence_table(const PagedArgs &a, const Share &sh) {
+    return Table{(table_word *)(a.table + size_t(sh.seq) * a.max_pages), a.pages.n_pages, a.pages.shift, max(sh.s.len - 1, 0)};
 }
 // Whether some token sees one of the 16 positions from p on, which lie in one page.
 __device__ __forceinline__ bool half_seen(const PagedArgs &a, const Seq &s, const Seen &all, int p) {
@@ -198,11 +299,11 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces).
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, units).
 //
 // A value that is not finite would reach every row of the tile (0 times it is NaN): a wave that ends with outputs that are
 // not finite goes over its positions once more, with such values as zeros and the outputs of the rows that see one NaN.
-template <int NG, int NT, bool F32>
+template <int NG, int NT, bool F32, bool SHARES>
 __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_kernel(PagedArgs a) {
     constexpr int d = NG * 64, QT = F32 ? 3 : 1, PT = F32 ? 3 : 2, ROWS = 16;
     constexpr int UB = NT == 1 && NG <= 2 && !(F32 && NG == 2) ? 2 : 1;  // blocks at a time
@@ -211,16 +312,25 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
     __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, c = lane >> 4;
     const int tile = a.split.target ? blockIdx.y : blockIdx.x, h = a.split.target ? blockIdx.x : blockIdx.y;
-    const Piece piece = this_piece(a, tile == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr);
-    if (piece.count == 0) return;
-    const Seq &s = piece.s;
+    int *bad_batch = tile == 0 && h == 0 && threadIdx.x < 64 ? a.err : nullptr;
+    Shares shares{};
+    Share sh;
+    if constexpr (SHARES) {
+        shares = first_share(a, bad_batch);
+        if (!next_share(a, shares, sh, bad_batch)) return;
+    } else {
+        sh = this_piece(a, bad_batch);
+        if (sh.count == 0) return;
+    }
+    do {
+    const Seq &s = sh.s;
     const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
-    if (row0 >= rows) return;
+    if (row0 >= rows) continue;
     const int i_first = row0 / G, i_last = min(s.n - 1, (row0 + ROWS * NT - 1) / G);
     const Seen all = seen(s, a.window, a.sinks);
     Seen z;
-    const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS * NT, rows), z);
-    const Table table = sequence_table(a, piece);
+    const int2 range = tile_blocks(a, sh, all, row0, min(row0 + ROWS * NT, rows), z);
+    const Table table = sequence_table(a, sh);
     const int page_mask = (1 << a.pages.shift) - 1;
 
     // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.  UB blocks
@@ -527,8 +637,8 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 v.z = fmaf(f, u.z, v.z);
                 v.w = fmaf(f, u.w, v.w);
             }
-            if (piece.count > 1) {
-                float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
+            if (sh.count > 1) {
+                float *o = a.part + ((size_t(sh.part) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
                 *reinterpret_cast<float4 *>(o + 4 * i4) = v;
                 if (i4 == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(M, S, a.unit, 0.f);
                 continue;
@@ -538,6 +648,8 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
             store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
         }
     }
+    if constexpr (SHARES) __syncthreads();  // (the next share's waves join through the same LDS)
+    } while (SHARES && next_share(a, shares, sh, bad_batch));
 }
 
 // ---- many rows (prompts, wide trees), bf16 tensors ---------------------------------------------------------------
@@ -613,7 +725,7 @@ __device__ __forceinline__ bool any_visible(const PagedArgs &a, const Seq &s, in
     return p <= cached + i1 && (!a.window || p + kPos - 1 > cached + i0 - a.window || p < a.sinks);
 }
 
-// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, pieces); 32 WAVES rows per block.
+// grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, units); 32 WAVES rows per block.
 //
 // Eight waves are two to a SIMD and go in two groups half a step apart, a barrier between: while the one forms its products
 // (the values of its last positions, the scores of the next), the other takes its exponentials.  Four waves of a block are
@@ -631,16 +743,16 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, c = lane >> 5;
     // (the last rows see the most positions: their blocks start first)
     const int tile = a.tiles - 1 - int(a.split.target ? blockIdx.y : blockIdx.x), h = a.split.target ? blockIdx.x : blockIdx.y;
-    const Piece piece = this_piece(a, tile == a.tiles - 1 && h == 0 && tid < 64 ? a.err : nullptr);
-    if (piece.count == 0) return;
-    const Seq &s = piece.s;
+    const Share sh = this_piece(a, tile == a.tiles - 1 && h == 0 && tid < 64 ? a.err : nullptr);
+    if (sh.count == 0) return;
+    const Seq &s = sh.s;
     const int G = a.group, rows = s.n * G, row0 = tile * ROWS;
     if (row0 >= rows) return;
     const Seen all = seen(s, a.window, a.sinks);
     Seen z;
-    const int2 range = tile_blocks(a, piece, all, row0, min(row0 + ROWS, rows), z);
+    const int2 range = tile_blocks(a, sh, all, row0, min(row0 + ROWS, rows), z);
     const int steps = (range.y - range.x + 1) / 2;
-    const Table table = sequence_table(a, piece);
+    const Table table = sequence_table(a, sh);
     const int page_mask = (1 << a.pages.shift) - 1;
 
     const uint8_t *head_k = reinterpret_cast<const uint8_t *>(a.pages.k + ((size_t(h) << a.pages.shift) * d));
@@ -1011,8 +1123,8 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
     if (missing && lane == 0) atomicOr(a.err, kErrRange);
     const float l = sum + other_half32(sum);
     if (w_row0 + n >= rows) return;
-    if (piece.count > 1) {
-        float *o = a.part + ((size_t(piece.first + piece.split) * a.n_kv + h) * a.tiles * ROWS + row) * (d + 4);
+    if (sh.count > 1) {
+        float *o = a.part + ((size_t(sh.part) * a.n_kv + h) * a.tiles * ROWS + row) * (d + 4);
 #pragma unroll
         for (int t = 0; t < TD; ++t)
 #pragma unroll
@@ -1036,6 +1148,7 @@ struct PagedPlan {
     int tiles;              // otherwise: tiles of 16 rows per wave
     int tile_rows, blocks;  // rows per block, blocks of the largest sequence's rows
     int target, least, units;
+    bool shares;            // enough positions, if sequences are long, for shares
     size_t workspace;
 };
 PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_kv, bool f32) {
@@ -1044,7 +1157,7 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
     int fill = kTarget;
     if (!f32 && rows >= 64) {
         const long long eight = (rows + 255) / 256 * n_kv * n_seq;
-        p.prompt = d <= 128 && eight >= 256 ? 8 : 4;
+        p.prompt = d <= 128 && eight > 192 && eight <= 256 ? 8 : 4;
         p.tile_rows = 32 * p.prompt;
         p.least = 8;
         fill = p.prompt == 8 || d > 128 ? 256 : 512;
@@ -1056,10 +1169,11 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
     }
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
-    const long long pieces = ((max_kv - 1) / kPos + 1 + p.least - 1) / p.least;  // most that a sequence has
-    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && pieces > 1) {
-        p.target = int(std::min(std::max(1ll, fill / base), pieces * n_seq));
+    const long long shares = ((max_kv - 1) / kPos + 1 + p.least - 1) / p.least;  // most that a sequence has
+    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && shares > 1) {
+        p.target = int(std::min(std::max(1ll, fill / base), shares * n_seq));
         p.units = p.target + n_seq - 1;  // (rounding up leaves less than one piece more per sequence)
+        p.shares = !p.prompt && n_seq > 1 && (long long)n_seq * max_kv >= (long long)kShare * kPos * p.target;
         p.workspace = (size_t(p.units) * n_kv * p.blocks * p.tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
     }
     return p;
@@ -1100,6 +1214,7 @@ hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, 
     a.split.target = p.target;
     a.split.least = p.least;
     a.split.unit = p.prompt ? 2 : 1;
+    a.shares = p.shares;
     a.batch = batch;
     a.err = err;
     const dim3 grid = p.target ? dim3(n_kv, p.blocks, p.units) : dim3(p.blocks, n_kv, batch.n_seq);
@@ -1110,7 +1225,10 @@ hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, 
 #undef PAGED_PROMPT
     } else {
 #define PAGED_CASE(NG, NT, F) \
-    case (NG * 2 + F) * 8 + NT: paged_attend_kernel<NG, NT, F><<<grid, kAttBlock, 0, s>>>(a); break;
+    case (NG * 2 + F) * 8 + NT:                                               \
+        if (p.shares) paged_attend_kernel<NG, NT, F, true><<<grid, kAttBlock, 0, s>>>(a); \
+        else paged_attend_kernel<NG, NT, F, false><<<grid, kAttBlock, 0, s>>>(a);         \
+        break;
     switch ((d / 64 * 2 + f32) * 8 + p.tiles) {
         PAGED_CASE(1, 1, false) PAGED_CASE(1, 2, false) PAGED_CASE(1, 4, false) PAGED_CASE(1, 1, true) PAGED_CASE(1, 2, true)
         PAGED_CASE(2, 1, false) PAGED_CASE(2, 2, false) PAGED_CASE(2, 1, true)

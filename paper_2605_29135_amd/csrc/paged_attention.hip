@@ -196,6 +196,7 @@ __device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, in
     if (a.tree) {
         const uint32_t *bits = row_bits(a, s, i);
         int set = 0;
+#pragma unroll 4
         for (int w = 0; 32 * w < s.n; ++w) set += __popc(bits[w] & (s.n - 32 * w < 32 ? (1u << (s.n - 32 * w)) - 1 : ~0u));
         v.hi = row < 0 ? -1 : cached - 1;
         v.lo = cached - 1 + set - a.window;
@@ -207,21 +208,18 @@ __device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, in
 __device__ __forceinline__ bool row_sees(const PagedArgs &a, const RowView &v, int p) {
     return (p <= v.hi) & ((p > v.lo) | (p < a.sinks));
 }
-// Bit k < N: whether the row sees position p + STEP (k / 4) + k % 4 as a drafted token of a tree.
-template <int N, int STEP>
+// Bit i: whether the row sees position p + i (i < 32) as a drafted token of a tree.
 __device__ __forceinline__ uint32_t row_drafts(const PagedArgs &a, const Seq &s, const RowView &v, int p) {
     const int cached = s.len - s.n, first = p - cached;
-    uint32_t m = 0;
-    if (a.tree && first + STEP * ((N - 1) >> 2) + 3 >= 0) {
-        const uint32_t *bits = row_bits(a, s, v.i);
-        const int drafted = cached + v.i < 0 ? 0 : s.n;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int j = first + STEP * (k >> 2) + (k & 3);
-            if (j >= 0 && j < drafted) m |= (bits[j >> 5] >> (j & 31) & 1u) << k;
-        }
-    }
-    return m;
+    if (!a.tree || first + 31 < 0) return 0;
+    const uint32_t *bits = row_bits(a, s, v.i);
+    const int words = (s.n + 31) >> 5, w = first >> 5;
+    const uint32_t tail = s.n & 31 ? (1u << (s.n & 31)) - 1 : ~0u;
+    uint32_t lo = 0, hi = 0;
+    if (w >= 0 && w < words) lo = bits[w] & (w == words - 1 ? tail : ~0u);
+    if (w + 1 < words) hi = bits[w + 1] & (w + 1 == words - 1 ? tail : ~0u);
+    const uint32_t m = uint32_t(((uint64_t(hi) << 32) | lo) >> (first & 31));
+    return cached + v.i < 0 ? 0 : m;
 }
 // Whether every one of rows i0..i1 sees all of positions p..p + count - 1.
 __device__ __forceinline__ bool all_visible(const PagedArgs &a, const Seq &s, int i0, int i1, int p, int count) {
@@ -483,11 +481,12 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 for (int u = 0; u < UB; ++u) {
                     sees[t][u] = 0xff;
                     if (full[u]) continue;
-                    const int at = block_at(v, u) * kPos + 4 * c;
-                    const uint32_t drafts = row_drafts<8, 16>(a, s, view[t], at);
+                    const int at = block_at(v, u) * kPos;
+                    const uint32_t drafts = row_drafts(a, s, view[t], at) >> (4 * c);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const bool see = (row_sees(a, view[t], at + 16 * (k >> 2) + (k & 3)) | (drafts >> k & 1)) & (held[u] >> k & 1);
+                        const int i = 16 * (k >> 2) + (k & 3);
+                        const bool see = (row_sees(a, view[t], at + 4 * c + i) | (drafts >> i & 1)) & (held[u] >> k & 1);
                         p[t][u][k] = see ? p[t][u][k] : -INFINITY;
                         if constexpr (decltype(careful)::value) sees[t][u] &= ~(uint32_t(!see) << k);
                     }
@@ -916,11 +915,12 @@ __global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kern
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int at = z.block(min(v + u, range.y - 1)) * kPos;
-                const uint32_t drafts = row_drafts<16, 8>(a, s, view, at + 4 * c);
+                const uint32_t drafts = row_drafts(a, s, view, at) >> (4 * c);
                 uint32_t m = 0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const bool see = (row_sees(a, view, at + 8 * (r >> 2) + 4 * c + (r & 3)) | (drafts >> r & 1)) &
+                    const int i = 8 * (r >> 2) + (r & 3);
+                    const bool see = (row_sees(a, view, at + 4 * c + i) | (drafts >> i & 1)) &
                                      (held >> (2 * u + (r >> 3)) & 1) & (v + u < range.y);
                     p[u][r] = see ? p[u][r] : -INFINITY;
                     if constexpr (decltype(careful)::value) m |= uint32_t(see) << r;

@@ -32,6 +32,9 @@ using namespace paged;
 constexpr int kPos = 32;  // positions per block
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
 constexpr int kTarget = 512;  // blocks that fill the device, where rows and heads alone give fewer
+// Caches that are never split: the second launch costs more (one token over 500 positions 11.2 us, 13.6 split; three prompts of
+// 100 tokens, 300 positions 18.6 and 21.5; 8 tokens over 1500 each 18.4, 17.2 split).
+constexpr int kWhole = 512;
 
 struct PagedArgs {
     const void *q;
@@ -1170,11 +1173,14 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
         p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
         p.tile_rows = 16 * p.tiles;
         p.least = kAttWaves;
+        // (where a wave's registers leave room for one block to a unit only: 4 tokens of 4 sequences over 4096 positions, 4 heads
+        // of 128, 8 queries each 20 us, 28 with 512; 16 single tokens, 8 heads of 256: 91 and 97)
+        if (d / 64 * p.tiles > 2) fill = 256;
     }
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
     const long long shares = ((max_kv - 1) / kPos + 1 + p.least - 1) / p.least;  // most that a sequence has
-    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && shares > 1) {
+    if ((p.prompt ? base * n_seq * 2 <= fill : base * n_seq < fill) && max_kv > kWhole) {
         p.target = int(std::min(std::max(1ll, fill / base), shares * n_seq));
         p.units = p.target + n_seq - 1;  // (rounding up leaves less than one piece more per sequence)
         p.shares = !p.prompt && n_seq > 1 && (long long)n_seq * max_kv >= (long long)kShare * kPos * p.target;

@@ -1158,7 +1158,10 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
     const long long rows = (long long)max_q * group;
     PagedPlan p{};
     int fill = kTarget;
-    if (!f32 && rows >= 64) {
+    // Many rows.  Heads of up to 128: from 33 rows on (5 tokens of 4 sequences, 8 queries a head, 4000 positions: 20 us, 24 in the
+    // other kernel; 16 of 8 sequences, 4 queries, 8000 positions: 62 and 80), or 160 over short caches (64 rows over 600 positions:
+    // 16.6 us, 13.9 in the other).  Larger heads: 40 tokens of 4 queries of 192 take 30 us, 27.5 in the other; 20 of 256 32 and 24.
+    if (!f32 && (d > 128 ? rows > 192 : rows > 32 && (rows >= 160 || max_kv > 1024))) {
         const long long eight = (rows + 255) / 256 * n_kv * n_seq;
         p.prompt = d <= 128 && eight > 192 && eight <= 256 ? 8 : 4;
         p.tile_rows = 32 * p.prompt;

@@ -503,12 +503,24 @@ CASES = [  # (d, n_kv, group, page, tokens, lengths, window, sinks, tree)
     (192, 2, 1, 16, [20], [700], 20, 33, "wide"),
     (128, 4, 8, 16, [200, 64], [900, 1100], 0, 0, "wide"),
     (128, 1, 4, 16, [9, 5], [4, 0], 0, 0, "deep"),             # drafted tokens before position 0
+    (128, 2, 8, 16, [20, 3, 14], [2000, 1100, 14], 0, 0, "wide"),  # (more than 32 rows over more than 1024 positions)
+    (64, 2, 8, 64, [9, 5], [1500, 1300], 700, 33, None),
+    (256, 1, 8, 16, [40, 3], [1500, 1300], 700, 33, None),     # (more than 192 rows of large heads)
+    (192, 1, 8, 16, [60, 25], [900, 1300], 0, 0, "deep"),
+    (128, 4, 8, 32, [840, 801], [1000, 1640], 0, 0, None),     # (193 to 256 blocks of 256 rows: eight waves a block)
+    (128, 4, 8, 32, [840, 840], [1640, 900], 300, 70, None),
+    (64, 4, 8, 16, [256, 250, 9, 1, 200, 256, 77], [700, 250, 500, 1, 333, 300, 400], 0, 0, "wide"),
+    (64, 8, 4, 16, [1500], [2100], 0, 0, None),
 ]
 
 
+def cases(both, bf16):
+    """Cases for both types, and ones whose kernels fp32 tensors do not reach."""
+    return pytest.mark.parametrize("case,dtype", [(c, t) for c in both for t in (F32, BF16)] + [(c, BF16) for c in bf16])
+
+
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("case", range(len(CASES)))
+@cases(range(32), range(32, len(CASES)))
 def test_attention_matches_the_plain_form(case, dtype):
     out, ref, amount, shift, (cache, _, _) = run_case(*CASES[case], dtype)
     flags()
@@ -521,9 +533,8 @@ def test_attention_matches_the_plain_form(case, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("scale,amplitude", [(0.0, 1.0), (-0.3, 1.0), (20.0, 30.0), (1e-30, 1.0), (2.0 ** 32, 1.0), (2.0 ** -20, 2.0 ** 20)])
-@pytest.mark.parametrize("case", [1, 12, 17, 27])
+@cases([1, 12, 17, 27], [37])
 def test_attention_scales(case, scale, amplitude, dtype):
     out, ref, amount, shift, (cache, _, _) = run_case(*CASES[case], dtype, scale=scale, amplitude=amplitude)
     err = (out.cpu().double() - ref).abs()
@@ -534,8 +545,7 @@ def test_attention_scales(case, scale, amplitude, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("case", [1, 2, 8, 12, 17, 18, 22, 26, 30])
+@cases([1, 2, 8, 12, 17, 18, 22, 26], [30, 34, 37, 38])
 def test_attention_strides_rows_behind_and_loose_bounds(case, dtype):
     """Tokens of a projection's rows, an output inside another, rows behind the last sequence, loose max_q and max_kv."""
     c = CASES[case]
@@ -563,9 +573,8 @@ def test_attention_strides_rows_behind_and_loose_bounds(case, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("case", [12, 16, 17, 20, 22, 24, 25, 27, 28])
+@cases([12, 16, 20, 24, 25, 28], [17, 18, 22, 27, 33, 34, 37, 38])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them(case, value, dtype):
     """One element of a value, seen by some of the tokens: their outputs of its dim are NaN, all else is what it was."""
     c = CASES[case]
@@ -606,8 +615,7 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them(case, value, dt
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("case", [2, 10, 17, 18, 25])
+@cases([2, 10, 17, 25], [18, 34, 37, 38])
 def test_a_page_that_is_missing_counts_as_unseen(case, dtype):
     c = CASES[case]
     d, n_kv, G, page, ns, ls, window, sinks, tree = c
@@ -689,6 +697,18 @@ def test_attention_long_and_split(n, dtype):
         assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, L)).all()
         assert relative_rms(out, ref) <= RMS[dtype]
     flags()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window,sinks,tree", [(0, 0, None), (0, 0, "deep"), (9000, 40, None), (100, 5, None)])
+def test_a_ragged_batch_in_equal_shares(window, sinks, tree, dtype):
+    """Sequences that share units and units that share sequences, ones without tokens and without positions among them; with
+    the short window the same call has few positions and cuts the sequences into pieces."""
+    ns, ls = [1, 3, 1, 0, 2, 1, 1, 1, 3], [9001, 3, 0, 500, 15000, 8000, 1, 63, 4999]
+    out, ref, amount, shift, _ = run_case(64, 16, 2, 16, ns, ls, window, sinks, tree, dtype)
+    flags()
+    assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, max(ls))).all()
 
 
 @pytest.mark.gpu

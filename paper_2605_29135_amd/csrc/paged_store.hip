@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a) {
 }
 
 // ---- store -----------------------------------------------------------------------------------------------------
-constexpr int kStoreBlock = 256;
+constexpr int kStoreBlock = 256, kStoreLaunch = 1 << 22;  // blocks of a launch, at most
 
 // A thread takes 8 dims of a token's head.  grid: (groups of tokens, keys or values)
 template <bool F32>
@@ -296,11 +296,16 @@ hipError_t launch_page_tables(const paged::TableArgs &a, int *err, hipStream_t s
 hipError_t launch_paged_append(const void *k, const void *v, int dtype, long long k_stride, long long v_stride, int T,
                                int n_kv, int d, const int32_t *slots, const paged::Pages &pages, int *err, hipStream_t s) {
     const int per_block = std::max(1, kStoreBlock / (n_kv * (d / 8)));
-    const dim3 grid((T + per_block - 1) / per_block, 2);
-    if (dtype == MOE_F32)
-        paged_append_kernel<true><<<grid, kStoreBlock, 0, s>>>(k, v, k_stride, v_stride, T, n_kv, d, slots, pages, per_block, err);
-    else
-        paged_append_kernel<false><<<grid, kStoreBlock, 0, s>>>(k, v, k_stride, v_stride, T, n_kv, d, slots, pages, per_block, err);
+    // A launch has fewer than 2^32 threads.
+    const int most = kStoreLaunch * per_block;
+    const size_t size = dtype == MOE_F32 ? 4 : 2;
+    for (int t0 = 0; t0 < T; t0 += most) {
+        const int count = std::min(T - t0, most);
+        const dim3 grid((count + per_block - 1) / per_block, 2);
+        const uint8_t *k0 = static_cast<const uint8_t *>(k) + t0 * k_stride * size, *v0 = static_cast<const uint8_t *>(v) + t0 * v_stride * size;
+        const auto kernel = dtype == MOE_F32 ? paged_append_kernel<true> : paged_append_kernel<false>;
+        kernel<<<grid, kStoreBlock, 0, s>>>(k0, v0, k_stride, v_stride, count, n_kv, d, slots + t0, pages, per_block, err);
+    }
     return hipGetLastError();
 }
 

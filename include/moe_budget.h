@@ -391,14 +391,15 @@ MOE_API size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads
  *   tree NULL: the positions p <= t, with window > 0 (at most 2^30) those with p > t - window or p < sinks;
  *   tree:      device uint64 [T][tree_words] as of moe_tree_masks (or any other bits), 64 tree_words >= max_q: of its
  *              sequence's tokens those whose bit is set, and of the positions in front of them those that a token at
- *              position (their number) + (its set bits) - 1 sees by the window; bits past the sequence's tokens count
- *              for nothing.  A window must be 0 or at least max_q.
+ *              position (their number) + (its set bits, at least one) - 1 sees by the window; bits past the sequence's
+ *              tokens count for nothing.  A window must be 0 or at least max_q.
  * A token before position 0 is padding.  A token that sees no position gets 0.  Positions that no token of the sequence
  * sees (between the first `sinks` and the window of its first token) may hold anything, and their pages need not exist
  * (any entry); a position that some token sees on a page outside [0, n_pages) counts as unseen and raises MOE_ERR_RANGE in
  * the device flags.
- * Exact products with fp32 sums, fp32 softmax; queries enter exactly (MOE_F32: as three bf16 terms, 2^-25), probabilities
- * as bf16 terms of 2^-25 (MOE_F32) or 2^-17 (MOE_BF16).  For queries, keys and values up to
+ * Exact products with fp32 sums, fp32 softmax.  Queries enter exactly (MOE_F32: as three bf16 terms, 2^-24 of the element),
+ * probabilities as three bf16 terms (MOE_F32, 2^-24), as two (MOE_BF16, 2^-16), or, in MOE_BF16 calls of many rows, as one
+ * (2^-8; their sum is then that of the rounded ones).  For queries, keys and values up to
  * 2^100 in magnitude whose scores stay within fp32.  A value that is not finite makes the outputs of the
  * tokens that see it NaN, and no others.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token

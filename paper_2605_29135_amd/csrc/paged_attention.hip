@@ -202,7 +202,7 @@ __device__ __forceinline__ RowView row_view(const PagedArgs &a, const Seq &s, in
 #pragma unroll 4
         for (int w = 0; 32 * w < s.n; ++w) set += __popc(bits[w] & (s.n - 32 * w < 32 ? (1u << (s.n - 32 * w)) - 1 : ~0u));
         v.hi = row < 0 ? -1 : cached - 1;
-        v.lo = cached - 1 + set - a.window;
+        v.lo = cached - 1 + max(set, 1) - a.window;
     }
     if (!a.window) v.lo = -1;
     return v;

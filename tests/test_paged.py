@@ -82,7 +82,7 @@ def sees(n, L, window, sinks, bits=None):
         row = L - n + i
         if row < 0:
             continue
-        at = row if bits is None else L - n - 1 + bin(bits[i] & ((1 << n) - 1)).count("1")
+        at = row if bits is None else L - n - 1 + max(1, bin(bits[i] & ((1 << n) - 1)).count("1"))
         near = (p > at - window) | (p < sinks) if window else torch.ones(L, dtype=torch.bool)
         out[i] = near & (p <= at)
         if bits is not None:
@@ -416,6 +416,22 @@ def test_append_writes_the_slots_and_nothing_else(dtype, d, n_kv, page, T, layou
 
 
 @pytest.mark.gpu
+def test_append_of_more_tokens_than_a_launch_takes():
+    T, n_kv, d, page = (1 << 24) + 100, 17, 64, 16  # one block a token; 36 GB, of which four tokens are stored
+    x = torch.empty((T, n_kv, d), dtype=BF16, device="cuda")
+    kp, vp = (x.zero_() for x in moe.paged_cache(2, n_kv, page, d))
+    slots = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    want = torch.zeros((2 * page, n_kv, d), dtype=BF16, device="cuda")
+    for slot, t in ((3, 0), (20, (1 << 22) + 1), (31, T - 100), (7, T - 1)):
+        x[t] = want[slot] = torch.randn((n_kv, d), device="cuda").to(BF16)
+        slots[t] = slot
+    moe.moe_paged_append(x, x, kp, vp, slots)
+    flags()
+    for pool in (kp, vp):
+        assert torch.equal(pool.transpose(1, 2).reshape(2 * page, n_kv, d), want)
+
+
+@pytest.mark.gpu
 def test_append_rounds_to_nearest_even():
     x = torch.tensor([1.0 + 2.0 ** -8, 1.0 + 3 * 2.0 ** -8, -1.0 - 2.0 ** -8 - 2.0 ** -20, 3.39e38, math.inf, math.nan, 2.0 ** -130, -0.0])
     k = x.repeat(8).view(1, 1, 64).cuda()
@@ -612,6 +628,29 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them(case, value, dt
     keep[n // 2, 0] = False
     assert not torch.isfinite(got2[~keep]).any() and torch.isfinite(got2[keep]).all()
     flags()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window,sinks", [(0, 0), (48, 3), (64, 0), (700, 33)])
+@pytest.mark.parametrize("d,n_kv,G,ns,ls", [(64, 2, 4, [5, 1, 7], [200, 97, 1300]), (128, 1, 8, [40, 33], [900, 41]),
+                                            (256, 1, 8, [48, 3], [1500, 700])])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_masks_of_any_bits(d, n_kv, G, ns, ls, window, sinks, dtype):
+    """Drafted tokens that see later ones, not themselves, or none; bits past the sequence's tokens; two words a row more."""
+    gen, rng = torch.Generator().manual_seed(d), random.Random(d)
+    bits = [[rng.choice((0, rng.getrandbits(n), 1 << rng.randrange(n))) for _ in range(n)] for n in ns]
+    visible = [sees(n, L, window, sinks, b) for n, L, b in zip(ns, ls, bits)]
+    # (the tokens' own keys and values are there, seen or not)
+    cache = Cache(ls, n_kv, d, 16, gen).put([v.any(0) | (torch.arange(L) >= L - n) for v, n, L in zip(visible, ns, ls)])
+    q = torch.randn((sum(ns), n_kv * G, d), generator=gen).to(dtype)
+    stray = [[x | rng.getrandbits(192 - n) << n for x in b] for n, b in zip(ns, bits)]
+    masks = torch.tensor([as_words(x, 3) for b in stray for x in b], dtype=torch.int64).cuda()
+    out = moe.moe_paged_attention(q.cuda(), cache.k, cache.v, cache.dev_table, ints(ls), q_start=ints(starts(ns)), max_q=max(ns),
+                                  max_kv=max(ls), window=window, sinks=sinks, tree=masks)
+    flags()
+    qs = [q[a:b].double() for a, b in zip(starts(ns), starts(ns)[1:])]
+    ref, amount, shift = attend(qs, [k.double() for k in cache.ks], [v.double() for v in cache.vs], visible, G, d ** -0.5, dtype is F32)
+    assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, max(ls))).all()
 
 
 @pytest.mark.gpu

@@ -307,7 +307,6 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 template <int NG, int NT, bool F32, bool SHARES>
 __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_kernel(PagedArgs a) {
     constexpr int d = NG * 64, QT = F32 ? 3 : 1, PT = F32 ? 3 : 2, ROWS = 16;
-    constexpr int UB = NT == 1 && NG <= 2 && !(F32 && NG == 2) ? 2 : 1;  // blocks at a time
     constexpr int VE = NG % 2 ? 4 : 8, VG = d / (16 * VE);  // dims of a lane per group of products, groups
     __shared__ float4 out_sh[kAttWaves][ROWS][d / 4 + 1];
     __shared__ float max_sh[kAttWaves][ROWS], sum_sh[kAttWaves][ROWS];
@@ -324,138 +323,118 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
         if (sh.count == 0) return;
     }
     do {
-    const Seq &s = sh.s;
-    const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
-    if (row0 >= rows) continue;
-    const int i_first = row0 / G, i_last = min(s.n - 1, (row0 + ROWS * NT - 1) / G);
-    const Seen all = seen(s, a.window, a.sinks);
-    Seen z;
-    const int2 range = tile_blocks(a, sh, all, row0, min(row0 + ROWS * NT, rows), z);
-    const Table table = sequence_table(a, sh);
-    const int page_mask = (1 << a.pages.shift) - 1;
+        const Seq &s = sh.s;
+        const int G = a.group, rows = s.n * G, row0 = tile * ROWS * NT;
+        if (row0 >= rows) continue;
+        const int i_first = row0 / G, i_last = min(s.n - 1, (row0 + ROWS * NT - 1) / G);
+        const Seen all = seen(s, a.window, a.sinks);
+        Seen z;
+        const int2 range = tile_blocks(a, sh, all, row0, min(row0 + ROWS * NT, rows), z);
+        const Table table = sequence_table(a, sh);
+        const int page_mask = (1 << a.pages.shift) - 1;
 
-    // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.  UB blocks
-    // at a time (kAttWaves apart), the next ones loaded as soon as the present ones have been used: the bytes in flight are
-    // what bounds a batch of single tokens.
-    uint4 kc[UB][2][2 * NG];
-    uint32_t vc[UB][VG][8][VE / 2];
-    // Half a block lies in one page.  `there`: bits of the halves (four each) of which some token sees a position, and whose
-    // page is there; the others are read from the first page, and none of it is used.  The table's entries are fetched a
-    // block ahead of the loads.
-    uint32_t there[UB] = {};
-    bool missing = false;
-    int32_t entry[UB][2] = {};
-    int page_at[UB][2] = {};
-    auto block_at = [&](int v, int u) { return z.block(min(v + u * kAttWaves, range.y - 1)); };
-    auto fetch = [&](int v) __attribute__((always_inline)) {
+        // A block's operands as they lie in the cache: keys as 16 positions of 8 dims, values as 8 positions of VE dims.  The next
+        // block's are loaded as soon as the present ones have been used: the bytes in flight are what bounds a batch of single
+        // tokens.  (Two blocks at a time: the same over long caches; 256 sequences of up to 500 positions, 8 heads of 64 36 us, 34
+        // with one; a window of 256 35 and 29, since more waves have nothing to do in a sequence's last blocks.)
+        uint4 kc[2][2 * NG];
+        uint32_t vc[VG][8][VE / 2];
+        // Half a block lies in one page.  `there`: bits of the halves (four each) of which some token sees a position, and whose
+        // page is there; the others are read from the first page, and none of it is used.  The table's entries are fetched a
+        // block ahead of the loads.
+        uint32_t there = 0;
+        bool missing = false;
+        int32_t entry[2] = {};
+        int page_at[2] = {};
+        auto block_at = [&](int v) { return z.block(min(v, range.y - 1)); };
+        auto fetch = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < UB; ++u)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) entry[u][e] = table.entry(block_at(v, u) * kPos + 16 * e);
-    };
-    auto find = [&](int v) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < UB; ++u) {
-            there[u] = 0;
+            for (int e = 0; e < 2; ++e) entry[e] = table.entry(block_at(v) * kPos + 16 * e);
+        };
+        auto find = [&](int v) __attribute__((always_inline)) {
+            there = 0;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const bool needed = (v + u * kAttWaves < range.y) & half_seen(a, s, all, block_at(v, u) * kPos + 16 * e);
-                const bool ok = uint32_t(entry[u][e]) < uint32_t(table.n_pages);
+                const bool needed = half_seen(a, s, all, block_at(v) * kPos + 16 * e);
+                const bool ok = uint32_t(entry[e]) < uint32_t(table.n_pages);
                 missing |= needed & !ok;
-                page_at[u][e] = ok ? entry[u][e] : 0;
-                there[u] |= needed && ok ? 0xfu << (4 * e) : 0u;
+                page_at[e] = ok ? entry[e] : 0;
+                there |= needed && ok ? 0xfu << (4 * e) : 0u;
             }
-        }
-    };
-    auto row_at = [&](int p) { return ((size_t(h) << a.pages.shift) + (p & page_mask)) * d; };
-    auto load_k = [&](int v) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < UB; ++u) {
-            if (v + u * kAttWaves >= range.y) break;
+        };
+        auto row_at = [&](int p) { return ((size_t(h) << a.pages.shift) + (p & page_mask)) * d; };
+        auto load_k = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint16_t *src = a.pages.k + page_at[u][e] * a.pages.k_stride + row_at(block_at(v, u) * kPos + 16 * e + n) + 8 * c;
+                const uint16_t *src = a.pages.k + page_at[e] * a.pages.k_stride + row_at(block_at(v) * kPos + 16 * e + n) + 8 * c;
 #pragma unroll
-                for (int j = 0; j < 2 * NG; ++j) kc[u][e][j] = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 32 * j));
+                for (int j = 0; j < 2 * NG; ++j) kc[e][j] = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 32 * j));
             }
-        }
-    };
-    auto load_v = [&](int v) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < UB; ++u) {
-            if (v + u * kAttWaves >= range.y) break;
+        };
+        auto load_v = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int e = i >> 2;
-                const uint16_t *src = a.pages.v + page_at[u][e] * a.pages.v_stride +
-                                      row_at(block_at(v, u) * kPos + 16 * e + 4 * c + (i & 3)) + VE * n;
+                const uint16_t *src = a.pages.v + page_at[e] * a.pages.v_stride + row_at(block_at(v) * kPos + 16 * e + 4 * c + (i & 3)) + VE * n;
 #pragma unroll
                 for (int g = 0; g < VG; ++g) {
                     if constexpr (VE == 8) {
                         const uint4 w = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 128 * g));
-                        vc[u][g][i][0] = w.x, vc[u][g][i][1] = w.y, vc[u][g][i][2] = w.z, vc[u][g][i][3] = w.w;
+                        vc[g][i][0] = w.x, vc[g][i][1] = w.y, vc[g][i][2] = w.z, vc[g][i][3] = w.w;
                     } else {
                         const uint2 w = *reinterpret_cast<const uint2 *>(src + 64 * g);
-                        vc[u][g][i][0] = w.x, vc[u][g][i][1] = w.y;
+                        vc[g][i][0] = w.x, vc[g][i][1] = w.y;
                     }
                 }
             }
-        }
-    };
+        };
 
-    // The tile's rows: their queries as operands (k = dims), what they see.  A row past the last repeats it and is not stored.
-    auto row_of = [&](int t) { return min(row0 + 16 * t + n, rows - 1); };
-    const float sign = a.negate ? -1.f : 1.f;
-    bf16x8 bq[NT][2 * NG][QT];
-    RowView view[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = row_of(t), i = row / G;
-        const size_t at = size_t(s.t0 + i) * a.q_stride + size_t(h * G + row - i * G) * d + 8 * c;
-        view[t] = row_view(a, s, i);
-#pragma unroll
-        for (int j = 0; j < 2 * NG; ++j) {
-            if constexpr (F32) {
-                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 32 * j);
-                const float4 u = p[0], w = p[1];
-                const float x[8] = {u.x * sign, u.y * sign, u.z * sign, u.w * sign, w.x * sign, w.y * sign, w.z * sign, w.w * sign};
-                split_terms<QT>(x, bq[t][j]);
-            } else {
-                bq[t][j][0] = load_query(a, at + 32 * j);
-            }
-        }
-    }
-    floatx4 acc[NT][4 * NG];
-    float mx[NT], sum[NT];
-    auto pass = [&](auto careful) __attribute__((always_inline)) {
+        // The tile's rows: their queries as operands (k = dims), what they see.  A row past the last repeats it and is not stored.
+        auto row_of = [&](int t) { return min(row0 + 16 * t + n, rows - 1); };
+        const float sign = a.negate ? -1.f : 1.f;
+        bf16x8 bq[NT][2 * NG][QT];
+        RowView view[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            mx[t] = -INFINITY;
-            sum[t] = 0.f;
+            const int row = row_of(t), i = row / G;
+            const size_t at = size_t(s.t0 + i) * a.q_stride + size_t(h * G + row - i * G) * d + 8 * c;
+            view[t] = row_view(a, s, i);
 #pragma unroll
-            for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
-        }
-        if (range.x + wave < range.y) {
-            fetch(range.x + wave);
-            find(range.x + wave);
-            load_k(range.x + wave);
-            load_v(range.x + wave);
-            fetch(range.x + wave + UB * kAttWaves);
-        }
-#pragma unroll 1
-        for (int v = range.x + wave; v < range.y; v += UB * kAttWaves) {
-            const int next = v + UB * kAttWaves;
-            uint32_t held[UB];
-            bool full[UB];
-#pragma unroll
-            for (int u = 0; u < UB; ++u) {
-                held[u] = there[u];
-                full[u] = held[u] == 0xff && all_visible(a, s, i_first, i_last, block_at(v, u) * kPos, kPos);
+            for (int j = 0; j < 2 * NG; ++j) {
+                if constexpr (F32) {
+                    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 32 * j);
+                    const float4 u = p[0], w = p[1];
+                    const float x[8] = {u.x * sign, u.y * sign, u.z * sign, u.w * sign, w.x * sign, w.y * sign, w.z * sign, w.w * sign};
+                    split_terms<QT>(x, bq[t][j]);
+                } else {
+                    bq[t][j][0] = load_query(a, at + 32 * j);
+                }
             }
-            // ---- scores
-            float p[NT][UB][8];
+        }
+        floatx4 acc[NT][4 * NG];
+        float mx[NT], sum[NT];
+        auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < UB; ++u)
+            for (int t = 0; t < NT; ++t) {
+                mx[t] = -INFINITY;
+                sum[t] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4 * NG; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+            if (range.x + wave < range.y) {
+                fetch(range.x + wave);
+                find(range.x + wave);
+                load_k(range.x + wave);
+                load_v(range.x + wave);
+                fetch(range.x + wave + kAttWaves);
+            }
+#pragma unroll 1
+            for (int v = range.x + wave; v < range.y; v += kAttWaves) {
+                const int next = v + kAttWaves, at = block_at(v) * kPos;
+                const uint32_t held = there;
+                const bool full = held == 0xff && all_visible(a, s, i_first, i_last, at, kPos);
+                // ---- scores
+                float p[NT][8];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -464,75 +443,65 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
 #pragma unroll
                         for (int k = QT - 1; k >= 0; --k)
 #pragma unroll
-                            for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[u][e][j]), bq[t][j][k], y);
+                            for (int j = 0; j < 2 * NG; ++j) y = mfma(__builtin_bit_cast(bf16x8, kc[e][j]), bq[t][j][k], y);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) p[t][u][4 * e + r] = y[r];
+                        for (int r = 0; r < 4; ++r) p[t][4 * e + r] = y[r];
                     }
-            __builtin_amdgcn_sched_barrier(0);
-            if (next < range.y) {
-                find(next);
-                load_k(next);
-                fetch(next + UB * kAttWaves);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            // ---- softmax
-            uint32_t sees[NT][UB];
-            bf16x8 bp[NT][UB][PT];
+                __builtin_amdgcn_sched_barrier(0);
+                if (next < range.y) {
+                    find(next);
+                    load_k(next);
+                    fetch(next + kAttWaves);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // ---- softmax
+                uint32_t sees[NT];
+                bf16x8 bp[NT][PT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+                for (int t = 0; t < NT; ++t) {
+                    sees[t] = 0xff;
+                    if (!full) {
+                        const uint32_t drafts = row_drafts(a, s, view[t], at) >> (4 * c);
 #pragma unroll
-                for (int u = 0; u < UB; ++u) {
-                    sees[t][u] = 0xff;
-                    if (full[u]) continue;
-                    const int at = block_at(v, u) * kPos;
-                    const uint32_t drafts = row_drafts(a, s, view[t], at) >> (4 * c);
+                        for (int k = 0; k < 8; ++k) {
+                            const int i = 16 * (k >> 2) + (k & 3);
+                            const bool see = (row_sees(a, view[t], at + 4 * c + i) | (drafts >> i & 1)) & (held >> k & 1);
+                            p[t][k] = see ? p[t][k] : -INFINITY;
+                            if constexpr (decltype(careful)::value) sees[t] &= ~(uint32_t(!see) << k);
+                        }
+                    }
+                    float top = p[t][0];
+#pragma unroll
+                    for (int k = 1; k < 8; ++k) top = fmaxf(top, p[t][k]);
+                    const float was = mx[t], now = fmaxf(was, max_over_c(top)), to = now == -INFINITY ? 0.f : now;
+                    if (__any(now > was)) {
+                        const float f = __builtin_amdgcn_exp2f((was - to) * a.unit);
+                        mx[t] = now;
+                        sum[t] *= f;
+#pragma unroll
+                        for (int i = 0; i < 4 * NG; ++i)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[t][i][r] *= f;
+                    }
+                    // (differences first: right at any size of the scores)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const int i = 16 * (k >> 2) + (k & 3);
-                        const bool see = (row_sees(a, view[t], at + 4 * c + i) | (drafts >> i & 1)) & (held[u] >> k & 1);
-                        p[t][u][k] = see ? p[t][u][k] : -INFINITY;
-                        if constexpr (decltype(careful)::value) sees[t][u] &= ~(uint32_t(!see) << k);
+                        p[t][k] = __builtin_amdgcn_exp2f((p[t][k] - to) * a.unit);
+                        sum[t] += p[t][k];
                     }
+                    split_terms<PT>(p[t], bp[t]);
                 }
-                float top = p[t][0][0];
-#pragma unroll
-                for (int u = 0; u < UB; ++u)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) top = fmaxf(top, p[t][u][k]);
-                const float was = mx[t], now = fmaxf(was, max_over_c(top)), to = now == -INFINITY ? 0.f : now;
-                if (__any(now > was)) {
-                    const float f = __builtin_amdgcn_exp2f((was - to) * a.unit);
-                    mx[t] = now;
-                    sum[t] *= f;
-#pragma unroll
-                    for (int i = 0; i < 4 * NG; ++i)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[t][i][r] *= f;
-                }
-                // (differences first: right at any size of the scores)
-#pragma unroll
-                for (int u = 0; u < UB; ++u) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        p[t][u][k] = __builtin_amdgcn_exp2f((p[t][u][k] - to) * a.unit);
-                        sum[t] += p[t][u][k];
-                    }
-                    split_terms<PT>(p[t][u], bp[t][u]);
-                }
-            }
-            // ---- values
-#pragma unroll
-            for (int u = 0; u < UB; ++u) {
-                if (!full[u]) {
+                // ---- values
+                if (!full) {
                     // Positions that no token sees may hold anything: zeros.
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int at = block_at(v, u) * kPos + 16 * (i >> 2) + 4 * c + (i & 3);
-                        const bool keep = (held[u] >> i & 1) & (at < s.len) & ((at >= all.from) | (at < a.sinks));
+                        const int pos = at + 16 * (i >> 2) + 4 * c + (i & 3);
+                        const bool keep = (held >> i & 1) & (pos < s.len) & ((pos >= all.from) | (pos < a.sinks));
 #pragma unroll
                         for (int g = 0; g < VG; ++g)
 #pragma unroll
-                            for (int w = 0; w < VE / 2; ++w) vc[u][g][i][w] = keep ? vc[u][g][i][w] : 0;
+                            for (int w = 0; w < VE / 2; ++w) vc[g][i][w] = keep ? vc[g][i][w] : 0;
                     }
                 }
                 bf16x8 seen_by[NT];
@@ -542,7 +511,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                         uint32_t w[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            w[e] = (sees[t][u] >> (2 * e) & 1) * 0x3f80u | (sees[t][u] >> (2 * e + 1) & 1) * 0x3f800000u;
+                            w[e] = (sees[t] >> (2 * e) & 1) * 0x3f80u | (sees[t] >> (2 * e + 1) & 1) * 0x3f800000u;
                         seen_by[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                     }
                 }
@@ -553,7 +522,7 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                         uint32_t w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            w[k] = __builtin_amdgcn_perm(vc[u][g][2 * k + 1][e / 2], vc[u][g][2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+                            w[k] = __builtin_amdgcn_perm(vc[g][2 * k + 1][e / 2], vc[g][2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
                         const int i = g * VE + e;
                         if constexpr (decltype(careful)::value) {
                             uint32_t f[4];
@@ -579,78 +548,77 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int k = PT - 1; k >= 0; --k) acc[t][i] = mfma(va, bp[t][u][k], acc[t][i]);
+                            for (int k = PT - 1; k >= 0; --k) acc[t][i] = mfma(va, bp[t][k], acc[t][i]);
                     }
+                __builtin_amdgcn_sched_barrier(0);
+                if (next < range.y) load_v(next);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if (next < range.y) load_v(next);
-        }
-    };
-    pass(std::false_type());
-    bool off = false;
+        };
+        pass(std::false_type());
+        bool off = false;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4 * NG; ++i)
+            for (int i = 0; i < 4 * NG; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
-    if (__builtin_expect(__any(off), 0)) pass(std::true_type());
-    if (missing && lane == 0) atomicOr(a.err, kErrRange);
+                for (int r = 0; r < 4; ++r) off |= !(fabsf(acc[t][i][r]) < INFINITY);
+        if (__builtin_expect(__any(off), 0)) pass(std::true_type());
+        if (missing && lane == 0) atomicOr(a.err, kErrRange);
 
-    // Join the waves, one tile of rows at a time.
+        // Join the waves, one tile of rows at a time.
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const float l = sum_over_c(sum[t]);
-        if (t) __syncthreads();
-        if (c == 0) {
-            max_sh[wave][n] = mx[t];
-            sum_sh[wave][n] = l;
-        }
-        // (row m = 4 c + r of product e of group g is dim 16 VE g + VE m + e)
+        for (int t = 0; t < NT; ++t) {
+            const float l = sum_over_c(sum[t]);
+            if (t) __syncthreads();
+            if (c == 0) {
+                max_sh[wave][n] = mx[t];
+                sum_sh[wave][n] = l;
+            }
+            // (row m = 4 c + r of product e of group g is dim 16 VE g + VE m + e)
 #pragma unroll
-        for (int g = 0; g < VG; ++g)
+            for (int g = 0; g < VG; ++g)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < VE; e += 4) {
-                    const int i = g * VE + e;
-                    out_sh[wave][n][(16 * VE * g + VE * (4 * c + r) + e) / 4] =
-                        make_float4(acc[t][i][r], acc[t][i + 1][r], acc[t][i + 2][r], acc[t][i + 3][r]);
-                }
-        __syncthreads();
+                    for (int e = 0; e < VE; e += 4) {
+                        const int i = g * VE + e;
+                        out_sh[wave][n][(16 * VE * g + VE * (4 * c + r) + e) / 4] =
+                            make_float4(acc[t][i][r], acc[t][i + 1][r], acc[t][i + 2][r], acc[t][i + 3][r]);
+                    }
+            __syncthreads();
 #pragma unroll 1
-        for (int idx = threadIdx.x; idx < ROWS * (d / 4); idx += kAttBlock) {
-            const int r = idx / (d / 4), i4 = idx % (d / 4), row = row0 + 16 * t + r;
-            if (row >= rows) continue;
-            float M = max_sh[0][r];
+            for (int idx = threadIdx.x; idx < ROWS * (d / 4); idx += kAttBlock) {
+                const int r = idx / (d / 4), i4 = idx % (d / 4), row = row0 + 16 * t + r;
+                if (row >= rows) continue;
+                float M = max_sh[0][r];
 #pragma unroll
-            for (int w = 1; w < kAttWaves; ++w) M = fmaxf(M, max_sh[w][r]);
-            float S = 0.f;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w = 1; w < kAttWaves; ++w) M = fmaxf(M, max_sh[w][r]);
+                float S = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < kAttWaves; ++w) {
-                // (a wave that saw nothing of the row has the maximum -inf and the sum 0; one whose scores are
-                // all NaN has the sum NaN, which stays)
-                const float f = max_sh[w][r] == -INFINITY && sum_sh[w][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[w][r] - M) * a.unit);
-                const float4 u = out_sh[w][r][i4];
-                S = fmaf(f, sum_sh[w][r], S);
-                v.x = fmaf(f, u.x, v.x);
-                v.y = fmaf(f, u.y, v.y);
-                v.z = fmaf(f, u.z, v.z);
-                v.w = fmaf(f, u.w, v.w);
+                for (int w = 0; w < kAttWaves; ++w) {
+                    // (a wave that saw nothing of the row has the maximum -inf and the sum 0; one whose scores are
+                    // all NaN has the sum NaN, which stays)
+                    const float f = max_sh[w][r] == -INFINITY && sum_sh[w][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f((max_sh[w][r] - M) * a.unit);
+                    const float4 u = out_sh[w][r][i4];
+                    S = fmaf(f, sum_sh[w][r], S);
+                    v.x = fmaf(f, u.x, v.x);
+                    v.y = fmaf(f, u.y, v.y);
+                    v.z = fmaf(f, u.z, v.z);
+                    v.w = fmaf(f, u.w, v.w);
+                }
+                if (sh.count > 1) {
+                    float *o = a.part + ((size_t(sh.part) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
+                    *reinterpret_cast<float4 *>(o + 4 * i4) = v;
+                    if (i4 == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(M, S, a.unit, 0.f);
+                    continue;
+                }
+                const float inv = S == 0.f ? 0.f : 1.f / S;  // (a row that sees nothing: 0)
+                v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
+                store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
             }
-            if (sh.count > 1) {
-                float *o = a.part + ((size_t(sh.part) * a.n_kv + h) * a.tiles * (ROWS * NT) + row) * (d + 4);
-                *reinterpret_cast<float4 *>(o + 4 * i4) = v;
-                if (i4 == 0) *reinterpret_cast<float4 *>(o + d) = make_float4(M, S, a.unit, 0.f);
-                continue;
-            }
-            const float inv = S == 0.f ? 0.f : 1.f / S;  // (a row that sees nothing: 0)
-            v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-            store4<F32>(a.out, size_t(s.t0 + row / G) * a.out_stride + size_t(h * G + row % G) * d + 4 * i4, v);
         }
-    }
-    if constexpr (SHARES) __syncthreads();  // (the next share's waves join through the same LDS)
+        if constexpr (SHARES) __syncthreads();  // (the next share's waves join through the same LDS)
     } while (SHARES && next_share(a, shares, sh, bad_batch));
 }
 

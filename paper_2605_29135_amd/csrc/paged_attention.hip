@@ -699,9 +699,11 @@ __device__ __forceinline__ bool any_visible(const PagedArgs &a, const Seq &s, in
 //
 // Eight waves are two to a SIMD and go in two groups half a step apart, a barrier between: while the one forms its products
 // (the values of its last positions, the scores of the next), the other takes its exponentials.  Four waves of a block are
-// one to a SIMD; another block, which runs in no step with it, fills the gaps.
+// one to a SIMD; another block, which runs in no step with it, fills the gaps; two others with heads of 64, whose registers
+// leave room (six prompts over a window of 1000, 16 heads: 70 us, 80 with one other; six of 700 tokens, 32 heads: 32 and 39;
+// 4096 tokens of one: 125 and 122).
 template <int NG, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, NG <= 2 ? 2 : 1) void paged_prompt_kernel(PagedArgs a) {
+__global__ __launch_bounds__(64 * WAVES, NG == 1 && WAVES == 4 ? 3 : NG <= 2 ? 2 : 1) void paged_prompt_kernel(PagedArgs a) {
     constexpr int d = NG * 64, THREADS = 64 * WAVES, ROWS = 32 * WAVES, PIECES = d / 8, ROW = 2 * d;
     constexpr int LOADS = kTile * PIECES / THREADS, KS = d / 16, TD = d / 32;
     constexpr int HALF = 16 * PIECES / 64;   // loads of a wave that make 16 positions

@@ -8,8 +8,8 @@
 // turns them in registers, one operation per pair.  Which dim is which row of the product is free: a lane's own eight
 // (or four) dims lie in as many products.
 //
-// Exact products of bf16, sums in fp32.  fp32 queries enter as three bf16 terms (2^-25 of the element), probabilities as
-// three (fp32) or two (bf16: 2^-17) of them: where few rows meet the cache the products cost nothing beside its bytes.
+// Exact products of bf16, sums in fp32.  fp32 queries enter as three bf16 terms (2^-24 of the element), probabilities as
+// three (fp32) or two (bf16: 2^-16) of them: where few rows meet the cache the products cost nothing beside its bytes.
 //
 // A row is a (token, query head of the group) pair; a wave takes NT tiles of 16 rows over every fourth block of 32
 // positions, and the block's waves join their (max, sum, output) through LDS.  With few rows the positions are split over
@@ -31,7 +31,10 @@ using namespace paged;
 
 constexpr int kPos = 32;  // positions per block
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
-constexpr int kTarget = 512;  // blocks that fill the device, where rows and heads alone give fewer
+// Blocks that fill the device, where rows and heads alone give fewer: two to a unit (32 sequences of up to 16384 positions, 8
+// heads of 128: 220 us, 276 with 256 and 259 with 384; 64 of up to 2000, 8 heads of 64, of whose blocks four fit: 37 us, 44
+// with 1024).
+constexpr int kTarget = 512;
 // Caches that are never split: the second launch costs more (one token over 500 positions 11.2 us, 13.6 split; three prompts of
 // 100 tokens, 300 positions 18.6 and 21.5; 8 tokens over 1500 each 18.4, 17.2 split).
 constexpr int kWhole = 512;
@@ -301,6 +304,13 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 }
 
 // grid: (row tiles, key/value head, sequence), or with a target (key/value head, row tiles, units).
+//
+// out_r = sum_p 2^(unit (s_rp - m_r)) V_p / sum_p 2^(unit (s_rp - m_r)), m_r the running maximum, in one pass.  What bounds it
+// are the cache's bytes, each of which is read once per tile of rows: 32 sequences of up to 16384 positions, 8 heads of 128, 4
+// queries each (1.40 GB) 216 us, 6.5 TB/s; 128 sequences that see 1028 positions, 8 heads of 64 (272 MB) 52 us, 5.2 TB/s; of one
+// token over 4096 positions (8.4 MB, 8.6 us and 3.9 for the join) the latencies of a launch, the table, the keys and the join.
+// Rows come in tiles of 16, since the queries of a token's head are 8 as a rule: tiles of 32 would multiply as much again for
+// nothing, and hold twice the outputs where registers hold the loads in flight.
 //
 // A value that is not finite would reach every row of the tile (0 times it is NaN): a wave that ends with outputs that are
 // not finite goes over its positions once more, with such values as zeros and the outputs of the rows that see one NaN.
@@ -702,6 +712,13 @@ __device__ __forceinline__ bool any_visible(const PagedArgs &a, const Seq &s, in
 // one to a SIMD; another block, which runs in no step with it, fills the gaps; two others with heads of 64, whose registers
 // leave room (six prompts over a window of 1000, 16 heads: 70 us, 80 with one other; six of 700 tokens, 32 heads: 32 and 39;
 // 4096 tokens of one: 125 and 122).
+//
+// What bounds it: per 64 positions a wave of heads of 128 has 32 products of 33 cycles and 1000 cycles of lane arithmetic (an
+// exponential per score takes 10, its difference, maximum, rounding and sum as many again), and two waves to a SIMD overlap
+// them in part only.  2048 tokens behind 6144, 32 heads over 4 of 128 (241 GFLOP): 256 us, 0.94 PFLOP/s; a matrix product of
+// 16384 rows and columns reaches 1.6 here.  Six prompts of up to 1789 tokens over a window of 1000, 16 heads over 4 of 64 (33.5
+// GFLOP): 69 us, the lane arithmetic of half as many products.  (Rows of 64 a wave, whose operands would serve twice, do not
+// fit the registers: 606 us; one wave to a SIMD that has its own exponentials beside its products: 370.)
 template <int NG, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, NG == 1 && WAVES == 4 ? 3 : NG <= 2 ? 2 : 1) void paged_prompt_kernel(PagedArgs a) {
     constexpr int d = NG * 64, THREADS = 64 * WAVES, ROWS = 32 * WAVES, PIECES = d / 8, ROW = 2 * d;
@@ -1132,6 +1149,10 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
     // other kernel; 16 of 8 sequences, 4 queries, 8000 positions: 62 and 80), or 160 over short caches (64 rows over 600 positions:
     // 16.6 us, 13.9 in the other).  Larger heads: 40 tokens of 4 queries of 192 take 30 us, 27.5 in the other; 20 of 256 32 and 24.
     if (!f32 && (d > 128 ? rows > 192 : rows > 32 && (rows >= 160 || max_kv > 1024))) {
+        // Eight waves a block where their blocks fill the device once (2048 tokens, 32 heads over 4 of 128: 8192 positions 260 us,
+        // 287 with four; 2048 positions 71 and 76; 1500 tokens of two sequences, 32 heads: 147 and 167; heads of 64, 8192
+        // positions 164 and 178).  Where some of them run behind the others, smaller blocks even out (4096 tokens 221 us, 188 with
+        // four; 3000 over 8192 427 and 393).
         const long long eight = (rows + 255) / 256 * n_kv * n_seq;
         p.prompt = d <= 128 && eight > 192 && eight <= 256 ? 8 : 4;
         p.tile_rows = 32 * p.prompt;
@@ -1142,6 +1163,7 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
         const long long tiles = (rows + p.tile_rows - 1) / p.tile_rows * n_kv * n_seq;
         fill = p.prompt == 8 || d > 128 || tiles <= 64 ? 256 : 512;
     } else {
+        // (a second tile halves the bytes of 17 rows and more, and needs as many registers again for its outputs)
         const int most = d <= 64 && !f32 ? 4 : d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
         p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
         p.tile_rows = 16 * p.tiles;

@@ -199,7 +199,9 @@ __global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a) {
 // ---- store -----------------------------------------------------------------------------------------------------
 constexpr int kStoreBlock = 256, kStoreLaunch = 1 << 22;  // blocks of a launch, at most
 
-// A thread takes 8 dims of a token's head.  grid: (groups of tokens, keys or values)
+// A thread takes 8 dims of a token's head, a block so many tokens that its threads have one such piece each.  Bytes bound it
+// (16384 tokens, 8 heads of 128 in bf16, 133 MB read and written: 26.3 us, 5.1 TB/s, a large copy 4.8); of few tokens, the
+// launch (2.5 us).  fp32 is rounded once, to nearest, ties to even.  grid: (groups of tokens, keys or values)
 template <bool F32>
 __global__ __launch_bounds__(kStoreBlock) void paged_append_kernel(const void *k, const void *v, long long k_stride,
                                                                    long long v_stride, int T, int n_kv, int d,
@@ -234,7 +236,8 @@ __global__ __launch_bounds__(kStoreBlock) void paged_append_kernel(const void *k
 // ---- trees -----------------------------------------------------------------------------------------------------
 //
 // A token's bits are its own and its parent's: with every round a token takes over those of the token that its chain has
-// reached and doubles the chain.  grid: sequences
+// reached and doubles the chain, so that a depth of 256 takes 8 rounds.  The rounds' latency is what it takes (16 trees of 25
+// tokens 5.3 us, one of 60 3.6).  grid: sequences
 __global__ __launch_bounds__(MOE_MAX_TREE) void tree_masks_kernel(const int32_t *parents, kv4::Batch batch, int words,
                                                                   unsigned long long *masks, int32_t *positions, int *err) {
     constexpr int W = MOE_MAX_TREE / 64;

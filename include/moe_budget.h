@@ -350,6 +350,8 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
  *   positions   device int32 [T] out: each row's position, or NULL
  *   slots       device int32 [T] out: its slot, or NULL
  *   free_next   device int32 [1] out: the first entry of free_pages that was not taken, or NULL (may be free_first)
+ * Entries behind a length are overwritten as it grows: who takes back positions (drafted tokens that were not accepted) puts
+ * the pages behind the shorter length back among the free ones.
  * Rows behind the last token get position and slot -1 (moe_paged_append passes over them).  A length or count that does not
  * fit the table raises MOE_ERR_RANGE in the device flags: a sequence with such a length counts as one without positions
  * or tokens, with such a count as one without tokens; tokens past row T are not added (MOE_ERR_RANGE).  Where the free

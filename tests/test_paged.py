@@ -829,6 +829,30 @@ def test_a_batch_served_from_pages_equals_plain_attention(window, sinks):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case,at", [(2, 2), (10, 2), (12, 1), (18, 1), (26, 1), (38, 3)])
+def test_parts_of_a_batch_called_by_themselves(case, at):
+    """A batch in two calls, each with its part of the lengths, of the starts and of the table, into one output."""
+    d, n_kv, G, page, ns, ls = CASES[case][:6]
+    _, ref, amount, shift, (cache, q, args) = run_case(*CASES[case], BF16)
+    masks, q = args["tree"], q.cuda()
+    out = torch.full_like(q, 5.0)
+    for lo, hi in ((at, len(ns)), (0, at)):
+        q_start, table, lens = args["q_start"][lo:hi + 1], cache.dev_table[lo:hi], ints(ls)[lo:hi]
+        if masks is not None:  # (a part's masks lie in the whole batch's rows, too)
+            part = torch.full_like(masks, 3 << 40)
+            moe.moe_tree_masks(ints([-1] * sum(ns)), q_start=q_start, max_q=max(ns[lo:hi]), kv_len=lens, masks=part)
+            first, last = starts(ns)[lo], starts(ns)[hi]
+            assert (part[:first] == 3 << 40).all() and (part[last:] == 3 << 40).all() and (part[first:last] != 3 << 40).all()
+        before = out.clone()
+        moe.moe_paged_attention(q, cache.k, cache.v, table, lens, out=out, **dict(args, q_start=q_start, max_q=max(ns[lo:hi]), max_kv=max(ls[lo:hi])))
+        keep = torch.ones(sum(ns), dtype=torch.bool)
+        keep[starts(ns)[lo]:starts(ns)[hi]] = False
+        assert torch.equal(out[keep.cuda()], before[keep.cuda()])
+    flags()
+    assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, BF16, max(ls))).all()
+
+
+@pytest.mark.gpu
 def test_captured_steps_replay_with_new_lengths():
     """Tables, store, masks and attention of a step captured twice, for one token each and for drafted trees, sharing pools
     and a workspace: replays in turn, with eager work between them, equal the eager calls."""

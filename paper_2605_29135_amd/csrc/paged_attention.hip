@@ -291,6 +291,13 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TER
         t[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
+// 8 or 16 bytes, read once or again.
+template <typename T, typename ONCE>
+__device__ __forceinline__ T read(const uint8_t *p, ONCE) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+    const words *w = reinterpret_cast<const words *>(p);
+    return __builtin_bit_cast(T, ONCE::value ? __builtin_nontemporal_load(w) : *w);
+}
 // Eight elements of a bf16 query, with the scale's sign.
 __device__ __forceinline__ bf16x8 load_query(const PagedArgs &a, size_t at) {
     uint4 w = dev::load16(reinterpret_cast<const uint8_t *>(static_cast<const uint16_t *>(a.q) + at));
@@ -372,31 +379,52 @@ __global__ __launch_bounds__(kAttBlock, NG * NT <= 2 ? 2 : 1) void paged_attend_
                 there |= needed && ok ? 0xfu << (4 * e) : 0u;
             }
         };
-        auto row_at = [&](int p) { return ((size_t(h) << a.pages.shift) + (p & page_mask)) * d; };
-        auto load_k = [&](int v) __attribute__((always_inline)) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint16_t *src = a.pages.k + page_at[e] * a.pages.k_stride + row_at(block_at(v) * kPos + 16 * e + n) + 8 * c;
-#pragma unroll
-                for (int j = 0; j < 2 * NG; ++j) kc[e][j] = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 32 * j));
+        // 16 positions of a block lie in a page: a base for all lanes, and offsets that stay.
+        const uint8_t *head_k = reinterpret_cast<const uint8_t *>(a.pages.k + ((size_t(h) << a.pages.shift) * d));
+        const uint8_t *head_v = reinterpret_cast<const uint8_t *>(a.pages.v + ((size_t(h) << a.pages.shift) * d));
+        const uint32_t page_k = uint32_t(a.pages.k_stride) * 2, page_v = uint32_t(a.pages.v_stride) * 2;  // bytes (below 2^32)
+        // Bytes that no other block reads pass through the caches as a stream, others stay there (32 sequences of up to 16384
+        // positions, one token each: 220 us, 246 through the caches; 1000 tokens over 2000 positions in fp32, 32 heads over 8 of
+        // 128: 141 us, 193 as a stream).
+        const bool alone = a.tiles == 1;
+        auto once_or_again = [&](auto load) __attribute__((always_inline)) {
+            if (alone) {  // (between fences, as the compiler would make one of the two)
+                asm volatile("" ::: "memory");
+                load(std::true_type());
+                asm volatile("" ::: "memory");
+            } else {
+                load(std::false_type());
             }
         };
+        const uint32_t k_lane = 2 * (n * d + 8 * c), v_lane = 2 * (4 * c * d + VE * n);
+        auto load_k = [&](int v) __attribute__((always_inline)) {
+            const int at = block_at(v) * kPos;
+            auto load = [&](auto once) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint8_t *src = head_k + (uint64_t(uint32_t(page_at[e])) * page_k + uint32_t((at + 16 * e) & page_mask) * (2 * d));
+#pragma unroll
+                    for (int j = 0; j < 2 * NG; ++j) kc[e][j] = read<uint4>(src + k_lane + 64 * j, once);
+                }
+            };
+            once_or_again(load);
+        };
         auto load_v = [&](int v) __attribute__((always_inline)) {
+            const int at = block_at(v) * kPos;
+            auto load = [&](auto once) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int e = i >> 2;
-                const uint16_t *src = a.pages.v + page_at[e] * a.pages.v_stride + row_at(block_at(v) * kPos + 16 * e + 4 * c + (i & 3)) + VE * n;
+                for (int i = 0; i < 8; ++i) {
+                    const int e = i >> 2;
+                    const uint8_t *src = head_v + (uint64_t(uint32_t(page_at[e])) * page_v + uint32_t((at + 16 * e) & page_mask) * (2 * d));
 #pragma unroll
-                for (int g = 0; g < VG; ++g) {
-                    if constexpr (VE == 8) {
-                        const uint4 w = dev::load16_stream(reinterpret_cast<const uint8_t *>(src + 128 * g));
-                        vc[g][i][0] = w.x, vc[g][i][1] = w.y, vc[g][i][2] = w.z, vc[g][i][3] = w.w;
-                    } else {
-                        const uint2 w = *reinterpret_cast<const uint2 *>(src + 64 * g);
+                    for (int g = 0; g < VG; ++g) {
+                        const auto w = read<std::conditional_t<VE == 8, uint4, uint2>>(src + v_lane + 2 * d * (i & 3) + 32 * VE * g, once);
                         vc[g][i][0] = w.x, vc[g][i][1] = w.y;
+                        if constexpr (VE == 8) vc[g][i][2] = w.z, vc[g][i][3] = w.w;
                     }
                 }
-            }
+            };
+            once_or_again(load);
         };
 
         // The tile's rows: their queries as operands (k = dims), what they see.  A row past the last repeats it and is not stored.

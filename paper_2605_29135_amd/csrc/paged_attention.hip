@@ -32,7 +32,7 @@ using namespace paged;
 constexpr int kPos = 32;  // positions per block
 constexpr int kAttWaves = 4, kAttBlock = 64 * kAttWaves;
 // Blocks that fill the device, where rows and heads alone give fewer: two to a unit (32 sequences of up to 16384 positions, 8
-// heads of 128: 220 us, 276 with 256 and 259 with 384; 64 of up to 2000, 8 heads of 64, of whose blocks four fit: 37 us, 44
+// heads of 128: 220 us, 276 with 256, 259 with 384; 64 of up to 2000, 8 heads of 64, of whose blocks four fit: 37 us, 44
 // with 1024).
 constexpr int kTarget = 512;
 // Caches that are never split: the second launch costs more (one token over 500 positions 11.2 us, 13.6 split; three prompts of
@@ -314,8 +314,8 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 //
 // out_r = sum_p 2^(unit (s_rp - m_r)) V_p / sum_p 2^(unit (s_rp - m_r)), m_r the running maximum, in one pass.  What bounds it
 // are the cache's bytes, each of which is read once per tile of rows: 32 sequences of up to 16384 positions, 8 heads of 128, 4
-// queries each (1.40 GB) 216 us, 6.5 TB/s; 128 sequences that see 1028 positions, 8 heads of 64 (272 MB) 52 us, 5.2 TB/s; of one
-// token over 4096 positions (8.4 MB, 8.6 us and 3.9 for the join) the latencies of a launch, the table, the keys and the join.
+// queries each (1.40 GB) 212 us, 6.6 TB/s; 128 sequences that see 1028 positions, 8 heads of 64 (272 MB) 48 us, 5.7 TB/s; of one
+// token over 4096 positions (8.4 MB, 8.3 us and 3.8 for the join) the latencies of a launch, the table, the keys and the join.
 // Rows come in tiles of 16, since the queries of a token's head are 8 as a rule: tiles of 32 would multiply as much again for
 // nothing, and hold twice the outputs where registers hold the loads in flight.
 //

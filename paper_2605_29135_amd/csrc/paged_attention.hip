@@ -1173,10 +1173,16 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
     const long long rows = (long long)max_q * group;
     PagedPlan p{};
     int fill = kTarget;
-    // Many rows.  Heads of up to 128: from 33 rows on (5 tokens of 4 sequences, 8 queries a head, 4000 positions: 20 us, 24 in the
-    // other kernel; 16 of 8 sequences, 4 queries, 8000 positions: 62 and 80), or 160 over short caches (64 rows over 600 positions:
-    // 16.6 us, 13.9 in the other).  Larger heads: 40 tokens of 4 queries of 192 take 30 us, 27.5 in the other; 20 of 256 32 and 24.
-    if (!f32 && (d > 128 ? rows > 192 : rows > 32 && (rows >= 160 || max_kv > 1024))) {
+    // More than 32 rows: the kernel for many, except where that for few has little to do, all of it at once (`few` blocks, a unit
+    // of the device each), since its blocks start faster.  Heads of 128 over up to 1024 positions: 64 tokens of 4 sequences, 8
+    // queries a head, 500 positions 16.5 us, 22.4 in the kernel for many; 16 of 4 over 900 17.1 and 19.5; 80 of 4 over 500
+    // (320 blocks) 29 and 22.5; 40 of 4 over 900 26 and 21; 25 of 32 sequences, 8 heads, 300 positions 51 and 20.  Longer ones:
+    // 5 of 4 over 4000 22 and 20; 16 of 8 over 8000, 8 heads 79 and 62.  Larger heads: 20 tokens of 2 sequences over 500, 4 queries
+    // of 256 18 and 36; 60 of 2 over 2000 33 and 37; 100 of 2 over 2000 48 and 42; 20 of 32 over 2000 190 and 84.  Heads of 64: 10 tokens
+    // of 8 sequences over 600 17.0 and 14.4.
+    const long long few = (rows + (d > 128 ? 15 : 31)) / (d > 128 ? 16 : 32) * n_kv * n_seq;
+    const bool little = d > 64 && few <= 256 && (d > 128 ? few * max_kv <= 1 << 18 : max_kv <= 1024 && few * max_kv <= 1 << 17);
+    if (!f32 && rows > 32 && !little) {
         // Eight waves a block where their blocks fill the device once (2048 tokens, 32 heads over 4 of 128: 8192 positions 260 us,
         // 287 with four; 2048 positions 71 and 76; 1500 tokens of two sequences, 32 heads: 147 and 167; heads of 64, 8192
         // positions 164 and 178).  Where some of them run behind the others, smaller blocks even out (4096 tokens 221 us, 188 with

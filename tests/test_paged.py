@@ -521,12 +521,19 @@ CASES = [  # (d, n_kv, group, page, tokens, lengths, window, sinks, tree)
     (128, 1, 4, 16, [9, 5], [4, 0], 0, 0, "deep"),             # drafted tokens before position 0
     (128, 2, 8, 16, [20, 3, 14], [2000, 1100, 14], 0, 0, "wide"),  # (more than 32 rows over more than 1024 positions)
     (64, 2, 8, 64, [9, 5], [1500, 1300], 700, 33, None),
-    (256, 1, 8, 16, [40, 3], [1500, 1300], 700, 33, None),     # (more than 192 rows of large heads)
+    (256, 1, 8, 16, [40, 3], [1500, 1300], 700, 33, None),
     (192, 1, 8, 16, [60, 25], [900, 1300], 0, 0, "deep"),
     (128, 4, 8, 32, [840, 801], [1000, 1640], 0, 0, None),     # (193 to 256 blocks of 256 rows: eight waves a block)
     (128, 4, 8, 32, [840, 840], [1640, 900], 300, 70, None),
     (64, 4, 8, 16, [256, 250, 9, 1, 200, 256, 77], [700, 250, 500, 1, 333, 300, 400], 0, 0, "wide"),
     (64, 8, 4, 16, [1500], [2100], 0, 0, None),
+    (256, 4, 4, 16, [130, 90, 70], [1500, 900, 70], 0, 0, None),   # (40: large heads of many rows, more than 256 blocks of 16)
+    (192, 4, 4, 32, [120, 20, 140], [700, 300, 1500], 200, 33, None),
+    (256, 4, 4, 16, [100, 65, 90], [100, 400, 90], 0, 0, "wide"),
+    (192, 4, 8, 16, [60, 25, 64], [900, 1300, 64], 70, 5, "deep"),
+    (128, 2, 8, 16, [150, 40], [1500, 1300], 300, 20, None),       # (more than 1024 positions)
+    (128, 2, 8, 16, [60, 17], [1500, 1100], 64, 4, "deep"),
+    (128, 4, 8, 16, [64, 40, 33, 50, 9], [500, 40, 100, 300, 9], 0, 0, None),  # (320 blocks of 32 rows)
 ]
 
 
@@ -550,7 +557,7 @@ def test_attention_matches_the_plain_form(case, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale,amplitude", [(0.0, 1.0), (-0.3, 1.0), (20.0, 30.0), (1e-30, 1.0), (2.0 ** 32, 1.0), (2.0 ** -20, 2.0 ** 20)])
-@cases([1, 12, 17, 27], [37])
+@cases([1, 12, 17, 27], [37, 40])
 def test_attention_scales(case, scale, amplitude, dtype):
     out, ref, amount, shift, (cache, _, _) = run_case(*CASES[case], dtype, scale=scale, amplitude=amplitude)
     err = (out.cpu().double() - ref).abs()
@@ -561,7 +568,7 @@ def test_attention_scales(case, scale, amplitude, dtype):
 
 
 @pytest.mark.gpu
-@cases([1, 2, 8, 12, 17, 18, 22, 26], [30, 34, 37, 38])
+@cases([1, 2, 8, 12, 17, 18, 22, 26], [30, 34, 37, 38, 41, 45])
 def test_attention_strides_rows_behind_and_loose_bounds(case, dtype):
     """Tokens of a projection's rows, an output inside another, rows behind the last sequence, loose max_q and max_kv."""
     c = CASES[case]
@@ -590,7 +597,7 @@ def test_attention_strides_rows_behind_and_loose_bounds(case, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
-@cases([12, 16, 20, 24, 25, 28], [17, 18, 22, 27, 33, 34, 37, 38])
+@cases([12, 16, 20, 24, 25, 28], [17, 18, 22, 27, 33, 34, 37, 38, 40, 43, 45])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them(case, value, dtype):
     """One element of a value, seen by some of the tokens: their outputs of its dim are NaN, all else is what it was."""
     c = CASES[case]
@@ -654,7 +661,7 @@ def test_masks_of_any_bits(d, n_kv, G, ns, ls, window, sinks, dtype):
 
 
 @pytest.mark.gpu
-@cases([2, 10, 17, 25], [18, 34, 37, 38])
+@cases([2, 10, 17, 25], [18, 34, 37, 38, 40, 45])
 def test_a_page_that_is_missing_counts_as_unseen(case, dtype):
     c = CASES[case]
     d, n_kv, G, page, ns, ls, window, sinks, tree = c

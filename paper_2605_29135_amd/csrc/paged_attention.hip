@@ -1198,8 +1198,8 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
         fill = p.prompt == 8 || d > 128 || tiles <= 64 ? 256 : 512;
     } else {
         // (a second tile halves the bytes of 17 rows and more, and needs as many registers again for its outputs)
-        const int most = d <= 64 && !f32 ? 4 : d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
-        p.tiles = rows <= 16 ? 1 : rows <= 32 ? std::min(2, most) : most;
+        const int most = d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
+        p.tiles = rows <= 16 ? 1 : most;
         p.tile_rows = 16 * p.tiles;
         p.least = kAttWaves;
         // (where a wave's registers leave room for one block to a unit only: 4 tokens of 4 sequences over 4096 positions, 4 heads
@@ -1269,7 +1269,7 @@ hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, 
         else paged_attend_kernel<NG, NT, F, false><<<grid, kAttBlock, 0, s>>>(a);         \
         break;
     switch ((d / 64 * 2 + f32) * 8 + p.tiles) {
-        PAGED_CASE(1, 1, false) PAGED_CASE(1, 2, false) PAGED_CASE(1, 4, false) PAGED_CASE(1, 1, true) PAGED_CASE(1, 2, true)
+        PAGED_CASE(1, 1, false) PAGED_CASE(1, 2, false) PAGED_CASE(1, 1, true) PAGED_CASE(1, 2, true)
         PAGED_CASE(2, 1, false) PAGED_CASE(2, 2, false) PAGED_CASE(2, 1, true)
         PAGED_CASE(3, 1, false) PAGED_CASE(3, 1, true)
         PAGED_CASE(4, 1, false) PAGED_CASE(4, 1, true)

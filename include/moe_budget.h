@@ -355,8 +355,9 @@ MOE_API int moe_kv4_attention(const void *q, int dtype, long long q_stride, cons
  * Rows behind the last token get position and slot -1 (moe_paged_append passes over them).  A length or count that does not
  * fit the table raises MOE_ERR_RANGE in the device flags: a sequence with such a length counts as one without positions
  * or tokens, with such a count as one without tokens; tokens past row T are not added (MOE_ERR_RANGE).  Where the free
- * pages end, entries and slots are -1, and MOE_ERR_BUDGET is raised.  A page outside [0, n_pages) counts as missing (entry
- * and slot -1) and raises MOE_ERR_RANGE. */
+ * pages end, entries and slots are -1, and MOE_ERR_BUDGET is raised.  A page outside [0, n_pages) counts as missing (slot -1)
+ * and raises MOE_ERR_RANGE: one of the free pages (its entry becomes -1), and one that the row has where a new token
+ * continues it (its entry stays; as after a step that ran out of pages). */
 MOE_API int moe_page_tables(const int32_t *kv_len, const int32_t *n_new, int n_seq, int T, int page_size, int n_pages,
                             const int32_t *free_pages, int n_free, const int32_t *free_first, int32_t *table, int max_pages,
                             int32_t *kv_len_out, int32_t *q_start, int32_t *positions, int32_t *slots, int32_t *free_next,

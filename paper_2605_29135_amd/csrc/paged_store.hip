@@ -46,6 +46,12 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *sums, uint3
     return lane ? capped(before, own) : before;
 }
 
+// Whether position `pos` lies on a page that its sequence had before the step (with `len` positions): the one that it
+// continues.  Such a page that is missing is an error of its own; what this step's list lacked or held wrong has been reported.
+__device__ __forceinline__ bool on_held_page(int pos, int len, int shift) {
+    return (pos >> shift) < ((len + (1 << shift) - 1) >> shift);
+}
+
 // The last of `n` ascending starts that is at most x (start[0] <= x).
 __device__ __forceinline__ int owner(const uint32_t *start, int n, uint32_t x) {
     int lo = 0, hi = n;
@@ -133,6 +139,7 @@ __global__ __launch_bounds__(kTabBlock) void page_tables_kernel(TableArgs a, int
                 const int b = owner(tok_sh, count, t), pos = len_sh[b] + int(t - tok_sh[b]);
                 const int32_t p = a.table[size_t(base + b) * a.max_pages + (pos >> a.shift)];
                 const bool there = uint32_t(p) < uint32_t(a.n_pages);
+                range |= !there && on_held_page(pos, len_sh[b], a.shift);
                 if (a.positions) a.positions[t] = pos;
                 if (a.slots) a.slots[t] = there ? (p << a.shift) + (pos & (page - 1)) : -1;
             }
@@ -156,12 +163,13 @@ __global__ __launch_bounds__(kTabBlock) void page_tables_kernel(TableArgs a, int
 
 // The rows of many tokens, behind page_tables_kernel<false>: 1024 of them per block.
 constexpr int kRowsBlock = 256, kRowsPer = 4;
-__global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a) {
+__global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a, int *err) {
     __shared__ uint32_t tok_sh[kTabSeqs];
     __shared__ int len_sh[kTabSeqs];
     const int tid = threadIdx.x;
     const uint32_t t0 = blockIdx.x * uint32_t(kRowsBlock * kRowsPer), t1 = min(t0 + kRowsBlock * kRowsPer, uint32_t(a.T));
     const uint32_t rows = uint32_t(a.q_start[a.n_seq]);
+    bool range = false;
 #pragma unroll 1
     for (int base = 0; base < a.n_seq; base += kTabSeqs) {
         const int count = min(kTabSeqs, a.n_seq - base);
@@ -183,6 +191,7 @@ __global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a) {
             const int b = owner(tok_sh, count, t), pos = len_sh[b] + int(t - tok_sh[b]);
             const int32_t p = a.table[size_t(base + b) * a.max_pages + (pos >> a.shift)];
             const bool there = uint32_t(p) < uint32_t(a.n_pages);
+            range |= !there && on_held_page(pos, len_sh[b], a.shift);
             if (a.positions) a.positions[t] = pos;
             if (a.slots) a.slots[t] = there ? (p << a.shift) + (pos & ((1 << a.shift) - 1)) : -1;
         }
@@ -194,6 +203,7 @@ __global__ __launch_bounds__(kRowsBlock) void page_rows_kernel(TableArgs a) {
         if (a.positions) a.positions[t] = -1;
         if (a.slots) a.slots[t] = -1;
     }
+    if (range) atomicOr(err, kErrRange);
 }
 
 // ---- store -----------------------------------------------------------------------------------------------------
@@ -291,7 +301,7 @@ hipError_t launch_page_tables(const paged::TableArgs &a, int *err, hipStream_t s
         page_tables_kernel<true><<<1, kTabBlock, 0, s>>>(a, err);
     } else {
         page_tables_kernel<false><<<1, kTabBlock, 0, s>>>(a, err);
-        page_rows_kernel<<<(a.T + kRowsBlock * kRowsPer - 1) / (kRowsBlock * kRowsPer), kRowsBlock, 0, s>>>(a);
+        page_rows_kernel<<<(a.T + kRowsBlock * kRowsPer - 1) / (kRowsBlock * kRowsPer), kRowsBlock, 0, s>>>(a, err);
     }
     return hipGetLastError();
 }

@@ -385,6 +385,37 @@ def test_tables_errors():
     flags()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("wrong", [-1, 1000, 2 ** 31 - 1])
+@pytest.mark.parametrize("T", [40, 9000])  # (the rows by one launch, and by one of their own)
+def test_tables_report_a_page_of_the_table_that_is_missing(T, wrong):
+    """A bad entry that a new token continues; one that no new token lies on is nobody's business."""
+    page, n_pages, lens, new = 16, 1000, [0, 35, 16, 20], [T - 10, 4, 2, 0]
+    blank = [-5] * 600
+    for entry in (901, wrong):
+        table = [blank, [900, 902, entry] + blank[3:], [903] + blank[1:], [904, wrong] + blank[2:]]
+        want = plain_tables(lens, new, list(range(700)), 0, table, page, T)
+        slots = [s if s < n_pages * page else -1 for s in want[4]]
+        assert slots.count(-1) == (4 if entry == 901 else 8)  # (rows of padding, and the second sequence's)
+        dev = ints(table)
+        got = moe.moe_page_tables(ints(lens), ints(new), ints(list(range(700))), dev, page, n_pages, T)
+        flags(None if entry == 901 else RANGE)
+        assert dev.cpu().tolist() == want[0]
+        assert [t.cpu().tolist() for t in got] == [*map(list, want[1:4]), slots, [want[5]]]
+
+
+@pytest.mark.gpu
+def test_tables_after_a_step_without_free_pages():
+    """Its own call raises MOE_ERR_BUDGET; tokens that the next one adds to the missing page are not dropped in silence."""
+    table = ints([[-5] * 4])
+    lens, _, _, slots, _ = moe.moe_page_tables(ints([0]), ints([20]), ints([7]), table, 16, 100, 20)
+    assert slots.cpu().tolist() == [*range(112, 128)] + [-1] * 4
+    flags(BUDGET)
+    lens, _, _, slots, _ = moe.moe_page_tables(lens, ints([14]), ints([8]), table, 16, 100, 14)
+    assert slots.cpu().tolist() == [-1] * 12 + [128, 129] and table.cpu().tolist() == [[7, -1, 8, -5]]
+    flags(RANGE)
+
+
 # ------------------------------------------------------------------------------------------------- append ---
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])

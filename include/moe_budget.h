@@ -384,7 +384,8 @@ MOE_API int moe_paged_append(const void *k, const void *v, int dtype, long long 
 MOE_API int moe_tree_masks(const int32_t *parents, int T, int n_seq, const int32_t *q_start, int max_q, const int32_t *kv_len,
                            uint64_t *masks, int words, int32_t *positions, void *stream);
 
-/* Device workspace bytes moe_paged_attention needs (either dtype; 0 for an unsupported shape). */
+/* Device workspace bytes moe_paged_attention needs (either dtype; 0 for an unsupported shape), in this call and in every other
+ * of these heads with no more of T, n_seq, max_q and max_kv: one workspace of the largest serves prompts and steps. */
 MOE_API size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q,
                                                    int max_kv);
 

@@ -679,6 +679,7 @@ def moe_tree_masks(parents, q_start=None, max_q: int | None = None, kv_len=None,
 
 def moe_paged_attention_workspace_bytes(T: int, n_seq: int, n_heads: int, n_kv: int, head_dim: int, max_q: int,
                                         max_kv: int) -> int:
+    """Bytes that serve every call of these heads with no more tokens, sequences, max_q and max_kv."""
     return int((_lib or lib()).moe_paged_attention_workspace_bytes(T, n_seq, n_heads, n_kv, head_dim, max_q, max_kv))
 
 

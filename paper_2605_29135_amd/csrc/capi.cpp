@@ -559,14 +559,12 @@ int moe_tree_masks(const int32_t *parents, int T, int n_seq, const int32_t *q_st
 }
 
 size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads, int n_kv, int head_dim, int max_q, int max_kv) {
-    // (a caller without q_start may pass any max_q: a plan for 1 is then what runs)
+    // (a caller without q_start may pass any max_q: a plan for 1, which asks for no more, is then what runs)
     const int32_t some = 0;
     max_q = std::max(max_q, 1);
     if (check_paged_attention(T, n_seq, n_heads, n_kv, head_dim, &some, &max_q, max_kv) != MOE_OK || T == 0 || n_seq == 0)
         return 0;
-    size_t n = moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, std::min(max_q, T), max_kv);
-    if (T == n_seq) n = std::max(n, moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, 1, max_kv));
-    return n;
+    return moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, std::min(max_q, T), max_kv);
 }
 
 int moe_paged_attention(const void *q, int dtype, long long q_stride, const void *k_pool, const void *v_pool,
@@ -603,7 +601,7 @@ int moe_paged_attention(const void *q, int dtype, long long q_stride, const void
     if (!rows_ok(q, q_stride, n_heads, head_dim, dtype) || !rows_ok(out, out_stride, n_heads, head_dim, dtype))
         return fail(MOE_ERR_INVALID_ARG, "%s: q and out need 16-byte aligned rows of at least n_heads * head_dim elements", what);
     if ((st = check_pool(what, k_pool, v_pool, k_page_stride, v_page_stride, n_kv, page_size, head_dim)) != MOE_OK) return st;
-    const size_t need = moe::paged_attention_workspace_bytes(n_seq, n_heads, n_kv, head_dim, max_q, max_kv);
+    const size_t need = moe::paged_attention_call_bytes(n_seq, n_heads, n_kv, head_dim, max_q, max_kv, dtype == MOE_F32);
     if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(MOE_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes (%zu given)", what, need,
                     workspace ? workspace_bytes : size_t(0));

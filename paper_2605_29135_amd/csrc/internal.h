@@ -208,6 +208,8 @@ hipError_t launch_paged_append(const void *k, const void *v, int dtype, long lon
                                int n_kv, int d, const int32_t *slots, const paged::Pages &pages, int *err, hipStream_t s);
 hipError_t launch_tree_masks(const int32_t *parents, const kv4::Batch &batch, int words, uint64_t *masks, int32_t *positions,
                              int *err, hipStream_t s);
+// What a call needs, and a bound of it over all calls of at most these sizes.
+size_t paged_attention_call_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv, bool f32);
 size_t paged_attention_workspace_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv);
 hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, const paged::Pages &pages,
                                   const int32_t *table, int max_pages, const kv4::Batch &batch, int n_heads, int n_kv, int d,

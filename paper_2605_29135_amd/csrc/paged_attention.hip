@@ -1160,6 +1160,12 @@ __global__ __launch_bounds__(64 * WAVES, NG == 1 && WAVES == 4 ? 3 : NG <= 2 ? 2
             store4<false>(a.out, at + 32 * t + 2 * r, make_float4(acc[t][r] * inv, acc[t][r + 1] * inv, acc[t][r + 2] * inv, acc[t][r + 3] * inv));
 }
 
+constexpr int kLeastMany = 8;  // blocks of positions of a piece, at least, in the kernel for many rows
+constexpr int most_tiles(int d, bool f32) { return d <= 128 && !(f32 && d > 64) ? 2 : 1; }  // what a wave's registers hold
+// Blocks that are taken to fill the device (the reasons stand in paged_plan).
+constexpr int few_fill(int d, int tiles) { return d / 64 * tiles > 2 ? 256 : kTarget; }
+constexpr int many_fill(int d, bool one_each) { return one_each || d > 128 ? 256 : 512; }
+
 // What a call launches: from its sizes alone, since lengths are on the device (max_kv bounds them).
 struct PagedPlan {
     int prompt;             // waves of the kernel for many rows, or 0
@@ -1172,7 +1178,7 @@ struct PagedPlan {
 PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_kv, bool f32) {
     const long long rows = (long long)max_q * group;
     PagedPlan p{};
-    int fill = kTarget;
+    int fill;
     // More than 32 rows: the kernel for many, except where that for few has little to do, all of it at once (`few` blocks, a unit
     // of the device each), since its blocks start faster.  Heads of 128 over up to 1024 positions: 64 tokens of 4 sequences, 8
     // queries a head, 500 positions 16.5 us, 22.4 in the kernel for many; 16 of 4 over 900 17.1 and 19.5; 80 of 4 over 500
@@ -1190,21 +1196,20 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
         const long long eight = (rows + 255) / 256 * n_kv * n_seq;
         p.prompt = d <= 128 && eight > 192 && eight <= 256 ? 8 : 4;
         p.tile_rows = 32 * p.prompt;
-        p.least = 8;
+        p.least = kLeastMany;
         // Two blocks to a unit of the device; one where few rows are split into many pieces, whose outputs cost more than the
         // second gives (60 drafted tokens, 8 heads of 128, 8252 positions: 34 us, 40 with two; 16 tokens, 60000 positions: 58
         // and 63; sixteen sequences of 25, 4 heads: 70 us, 67 with two).
         const long long tiles = (rows + p.tile_rows - 1) / p.tile_rows * n_kv * n_seq;
-        fill = p.prompt == 8 || d > 128 || tiles <= 64 ? 256 : 512;
+        fill = many_fill(d, p.prompt == 8 || tiles <= 64);
     } else {
         // (a second tile halves the bytes of 17 rows and more, and needs as many registers again for its outputs)
-        const int most = d <= 128 && !(f32 && d > 64) ? 2 : 1;  // what a wave's registers hold
-        p.tiles = rows <= 16 ? 1 : most;
+        p.tiles = rows <= 16 ? 1 : most_tiles(d, f32);
         p.tile_rows = 16 * p.tiles;
         p.least = kAttWaves;
         // (where a wave's registers leave room for one block to a unit only: 4 tokens of 4 sequences over 4096 positions, 4 heads
         // of 128, 8 queries each 20 us, 28 with 512; 16 single tokens, 8 heads of 256: 91 and 97)
-        if (d / 64 * p.tiles > 2) fill = 256;
+        fill = few_fill(d, p.tiles);
     }
     p.blocks = int((rows + p.tile_rows - 1) / p.tile_rows);
     const long long base = (long long)p.blocks * n_kv;  // blocks per sequence or piece
@@ -1220,9 +1225,33 @@ PagedPlan paged_plan(int n_seq, int n_kv, int group, int d, int max_q, int max_k
 
 }  // namespace
 
+size_t paged_attention_call_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv, bool f32) {
+    return paged_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_kv, f32).workspace;
+}
+
+// What a call asks for does not grow with its sizes: splits end where rows, heads and sequences fill the device, and the
+// kernel for many rows begins at 33.  A caller sizes one workspace by the largest call, so this bounds what every call of at
+// most these sizes asks for, kernel by kernel: units x base blocks (paged_plan) are target base + (n_seq - 1) base, of which the
+// first is at most `fill` and what a piece's least positions leave, the second below what keeps a batch split.
 size_t paged_attention_workspace_bytes(int n_seq, int n_heads, int n_kv, int d, int max_q, int max_kv) {
-    return std::max(paged_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_kv, false).workspace,
-                    paged_plan(n_seq, n_kv, n_heads / n_kv, d, max_q, max_kv, true).workspace);
+    if (max_kv <= kWhole) return 0;
+    const long long rows = (long long)max_q * (n_heads / n_kv), blocks_kv = (max_kv - 1) / kPos + 1;
+    auto bound = [&](int tile_rows, long long most_rows, int least, int fill, int rest) {
+        const long long base = (std::min(rows, most_rows) + tile_rows - 1) / tile_rows * n_kv;
+        const long long pieces = (blocks_kv + least - 1) / least * n_seq, most = fill;
+        const long long units = std::min(most, std::min(most, pieces) * std::min(most, base)) + std::min<long long>(rest, (n_seq - 1) * base);
+        return (size_t(units) * tile_rows * (d + 4) * sizeof(float) + 255) & ~size_t(255);
+    };
+    size_t n = 0;
+    for (const bool f32 : {false, true}) {
+        const int most = most_tiles(d, f32);
+        const long long few = most == 1 ? rows : 16;
+        n = std::max(n, bound(16, few, kAttWaves, few_fill(d, 1), few_fill(d, 1) - 1));
+        if (rows > 16 && most > 1) n = std::max(n, bound(16 * most, rows, kAttWaves, few_fill(d, most), few_fill(d, most) - 1));
+    }
+    // (eight waves a block are never split)
+    if (rows > 32) n = std::max(n, bound(32 * 4, rows, kLeastMany, many_fill(d, false), many_fill(d, false) / 2));
+    return n;
 }
 
 hipError_t launch_paged_attention(const void *q, int dtype, long long q_stride, const paged::Pages &pages,

@@ -798,6 +798,66 @@ def test_more_sequences_than_a_wave_has_lanes():
     flags()
 
 
+SIZES = ("T", "n_seq", "n_heads", "n_kv", "head_dim", "max_q", "max_kv")
+
+
+def random_sizes(rng):
+    """Sizes of an attention call and of one with the same heads that is no larger in any of them."""
+    log = lambda hi: int(hi ** rng.random())
+    n_kv, group, d = rng.choice([1, 2, 3, 4, 8, 16, 24]), rng.choice([1, 2, 3, 4, 5, 8, 16]), rng.choice([64, 128, 192, 256])
+    n_seq, max_q, max_kv = log(1000), log(4096), log(1 << 20)
+    T = n_seq * log(max_q)
+    large = (T, n_seq, n_kv * group, n_kv, d, max_q, max_kv)
+    small = [rng.randint(1, n) if rng.random() < 0.7 else n for n in (T, n_seq, max_q, max_kv)]
+    return large, (small[0], min(small[1], small[0]), n_kv * group, n_kv, d, *small[2:])
+
+
+def test_a_workspace_serves_smaller_calls_too():
+    size, rng = moe.moe_paged_attention_workspace_bytes, random.Random(2)
+    for _ in range(20000):
+        large, small = random_sizes(rng)
+        assert size(*small) <= size(*large), (dict(zip(SIZES, small)), dict(zip(SIZES, large)))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls that pass all checks would run, on addresses that are none")
+def test_what_a_call_asks_for_is_within_the_size():
+    L, rng, P = moe.lib(), random.Random(3), OK_PTR
+    asked = 0
+    for _ in range(20000):
+        T, n_seq, heads, n_kv, d, max_q, max_kv = random_sizes(rng)[1]
+        each = n_kv * 16 * d
+        for dtype in (0, 1):
+            code = L.moe_paged_attention(P, dtype, heads * d, P, P, each, each, 9, 16, P, 1 << 16, T, n_seq, heads, n_kv, d, P, max_q,
+                                         P, max_kv, 0, 0, None, 0, 0.125, P, heads * d, None, 0, None)
+            message = L.moe_last_error().decode()
+            need = int(message.split("workspace of ")[1].split()[0]) if code == -1 else 0
+            assert code == -6 or need > 0, message  # (no device, or no workspace)
+            assert need <= moe.moe_paged_attention_workspace_bytes(T, n_seq, heads, n_kv, d, max_q, max_kv)
+            asked += need > 0
+    assert asked > 2000
+
+
+@pytest.mark.gpu
+def test_one_workspace_for_prompts_and_steps():
+    """Sized once by the largest bounds, taken by every smaller call; what lies behind it is left alone."""
+    gen = torch.Generator().manual_seed(9)
+    n_kv, G, d, page = 8, 4, 128, 16
+    lens = [3000, 17, 900, 2100]
+    cache = Cache(lens, n_kv, d, page, gen, spare=4).put()
+    size = moe.moe_paged_attention_workspace_bytes(32 * 256, 32, n_kv * G, n_kv, d, 256, 16384)
+    ws = torch.full((size + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+    for dtype in (F32, BF16):
+        for n in (1, 4, 9, 16, 64):
+            for max_kv in (3000, 3072):
+                q = torch.randn((4 * n, n_kv * G, d), generator=gen).to(dtype).cuda()
+                args = dict(q_start=ints([0, n, 2 * n, 3 * n, 4 * n]), max_q=n, max_kv=max_kv)
+                ref = moe.moe_paged_attention(q, cache.k, cache.v, cache.dev_table, ints(lens), **args)
+                out = moe.moe_paged_attention(q, cache.k, cache.v, cache.dev_table, ints(lens), workspace=ws[:size], **args)
+                assert torch.equal(out, ref)
+    assert (ws[size:] == 0x5a).all()
+    flags()
+
+
 # -------------------------------------------------------------------------- graphs, streams, together (GPU) ---
 def rotate(x, positions):
     """A stand-in for what a model does between projection and cache: something that depends on the position."""

@@ -401,11 +401,13 @@ MOE_API size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads
  * sees (between the first `sinks` and the window of its first token) may hold anything, and their pages need not exist
  * (any entry); a position that some token sees on a page outside [0, n_pages) counts as unseen and raises MOE_ERR_RANGE in
  * the device flags.
- * Exact products with fp32 sums, fp32 softmax.  Queries enter exactly (MOE_F32: as three bf16 terms, 2^-24 of the element),
- * probabilities as three bf16 terms (MOE_F32, 2^-24), as two (MOE_BF16, 2^-16), or, in MOE_BF16 calls of many rows, as one
- * (2^-8; their sum is then that of the rounded ones).  For queries, keys and values up to
- * 2^100 in magnitude whose scores stay within fp32.  A value that is not finite makes the outputs of the
- * tokens that see it NaN, and no others.
+ * Exact products with fp32 sums, fp32 softmax.  Queries enter exactly (MOE_F32: as three bf16 terms, 2^-24 of the element).
+ * Probabilities enter as three bf16 terms (MOE_F32, 2^-24), as two (MOE_BF16, 2^-16), or, in MOE_BF16 calls of many rows, as
+ * one (2^-8; their sum is then that of the rounded ones).  A MOE_BF16 call of up to 32 rows, max_q n_heads / n_kv, always has
+ * two.  What a larger one has follows from n_seq, n_kv, head_dim, max_q and max_kv, never from the lengths; a caller who needs
+ * more there passes MOE_F32 queries.  For queries, keys and values up to 2^100 in magnitude whose products q . K stay
+ * within fp32 (a scale below 2^-126 in magnitude counts as one of 2^-126, which products below 2^100 do not tell from 0).
+ * A value that is not finite makes the outputs of the tokens that see it NaN, and no others.
  *   q          device [T][n_heads][head_dim] of dtype, q_stride elements from token to token
  *   out        device, as q with out_stride, same dtype; rows from q_start[n_seq] on are not touched
  *   scale      a factor of magnitude up to 2^32, as a rule 1 / sqrt(head_dim)

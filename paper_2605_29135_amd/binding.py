@@ -690,8 +690,9 @@ def moe_paged_attention(q, k_pool, v_pool, table, kv_len, q_start=None, max_q: i
     table int32 [n_seq, max_pages], kv_len int32 [n_seq] with the tokens), with window > 0 over the last `window` positions
     and the first `sinks`; q_start int32 [n_seq + 1]: sequence b's rows, None for one token each; max_q, max_kv: most tokens
     and positions of a sequence (T and what the table holds by default -- the launches go by them, so tight ones are
-    faster).  tree: masks of drafted tokens as of moe_tree_masks.  Scale 1 / sqrt(d) by default.  Returns out
-    [T, n_heads, d] of q's type; rows from q_start[-1] on are not written."""
+    faster).  tree: masks of drafted tokens as of moe_tree_masks.  Scale 1 / sqrt(d) by default.  Probabilities are exact to
+    2^-24 with fp32 queries and to 2^-16 with bf16 ones, to 2^-8 in bf16 calls of many rows (never with max_q * n_heads / n_kv
+    up to 32).  Returns out [T, n_heads, d] of q's type; rows from q_start[-1] on are not written."""
     import torch
     kpp, kps = _pool(k_pool, "k_pool")
     vpp, vps = _pool(v_pool, "v_pool", k_pool.shape)

@@ -586,6 +586,62 @@ def test_attention_matches_the_plain_form(case, dtype):
         assert relative_rms(out, ref) <= RMS[dtype]
 
 
+# Calls of at most 32 rows (a sequence's tokens times the query heads of a key/value head) take probabilities as two bf16
+# terms: rounding to one leaves up to 2^-8 of it, rounding that to another 2^-16.  Over values of one size the error is then
+# the output's own rounding: of normal values of any scale 1.66e-3 to 1.67e-3 rms, of 16384 and more sampled to 1 % or so.  One
+# term would add as much again from the probabilities, 2.35e-3 together.
+FEW_RMS = 1.72e-3
+FEW = [  # (d, n_kv, group, page, tokens, lengths, window, sinks, tree)
+    (128, 8, 4, 16, [1] * 6, [40, 100, 700, 1500, 3000, 2049], 0, 0, None),
+    (128, 8, 8, 32, [4, 3, 4], [500, 700, 4000], 0, 0, None),
+    (64, 16, 8, 16, [1] * 3, [200, 900, 5000], 300, 5, None),
+    (64, 16, 4, 16, [8, 5, 7], [400, 2500, 1300], 0, 0, "wide"),
+    (192, 8, 2, 16, [1, 5, 3], [300, 900, 2000], 0, 0, None),
+    (256, 4, 4, 16, [8, 2, 6], [100, 700, 2500], 0, 0, "deep"),
+]
+
+
+def few_tolerance(ref, amount, shift, L):
+    return tolerance(ref, amount, shift, F32, L) - ref.abs() * 2.0 ** -24 + amount * 2.0 ** -16 + ref.abs() * torch.finfo(BF16).eps / 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_calls_of_few_rows_keep_two_terms_of_a_probability(case):
+    out, ref, amount, shift, (cache, _, _) = run_case(*FEW[case], BF16, seed=case)
+    flags()
+    err = (out.cpu().double() - ref).abs()
+    tol = few_tolerance(ref, amount, shift, max(cache.ls))
+    assert (err <= tol).all(), (float((err / tol).max()), int((err > tol).sum()))
+    assert ref.numel() >= 16384 and relative_rms(out, ref) <= FEW_RMS
+
+
+def test_the_bounds_tell_one_term_from_two():
+    """The plain form with its probabilities as one bf16 term, or two, and the output rounded: only two pass."""
+    gen = torch.Generator().manual_seed(4)
+    n, L, kv, G, d = 4, 700, 4, 8, 128
+    q = torch.randn((n, kv * G, d), generator=gen).to(BF16).double()
+    K, V = (torch.randn((L, kv, d), generator=gen).to(BF16).double() for _ in range(2))
+    see = sees(n, L, 0, 0)
+    ref, amount, shift = attend([q], [K], [V], [see], G, d ** -0.5, False)
+    passed = []
+    for terms in (1, 2):
+        out = torch.zeros_like(ref)
+        for h in range(kv):
+            z = (q[:, h * G:(h + 1) * G] @ K[:, h].T * d ** -0.5).masked_fill(~see.unsqueeze(1), -math.inf)
+            p = torch.exp(z - z.amax(-1, keepdim=True))
+            kept, rest = torch.zeros_like(p), p.clone()
+            for _ in range(terms):
+                t = rest.to(BF16).double()
+                kept, rest = kept + t, rest - t
+            out[:, h * G:(h + 1) * G] = kept @ V[:, h] / (kept if terms == 1 else p).sum(-1, keepdim=True)
+        out = out.to(BF16)
+        err = (out.double() - ref).abs()
+        passed.append((bool((err <= few_tolerance(ref, amount, shift, L)).all()), relative_rms(out, ref) <= FEW_RMS))
+        assert (err <= tolerance(ref, amount, shift, BF16, L)).all()
+    assert passed == [(False, False), (True, True)]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale,amplitude", [(0.0, 1.0), (-0.3, 1.0), (20.0, 30.0), (1e-30, 1.0), (2.0 ** 32, 1.0), (2.0 ** -20, 2.0 ** 20)])
 @cases([1, 12, 17, 27], [37, 40])

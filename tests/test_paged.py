@@ -844,6 +844,59 @@ def test_a_ragged_batch_in_equal_shares(window, sinks, tree, dtype):
     assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, max(ls))).all()
 
 
+LONG, HALF, EVEN = ([9001, 3, 0, 500, 15000, 8000, 1, 63, 4999], [5001, 3, 0, 300, 7000, 3500, 1, 63, 2499],
+                    [1200, 1100, 1213, 1150, 1190, 1212, 1213, 1170, 1100])
+
+
+def share_blocks(case, dtype):
+    """(tiles of 16 rows of a wave, row blocks, blocks of positions in a share) by the sizes alone, which have to give shares."""
+    d, n_kv, G, _, ns, ls, window, sinks, tree = case
+    f32, rows = dtype is F32, max(ns) * G
+    tiles = 1 if rows <= 16 or d > 128 or (f32 and d > 64) else 2
+    blocks = -(-rows // (16 * tiles))
+    if not f32 and rows > 32:  # (the kernel for few rows all the same)
+        few = blocks * n_kv * len(ns)
+        assert d > 128 and few <= 256 and few * max(ls) <= 1 << 18
+    fill = 256 if d // 64 * tiles > 2 else 512
+    target = fill // (blocks * n_kv)
+    assert blocks * n_kv * len(ns) < fill and len(ns) * max(ls) >= 1024 * target
+    total = 0
+    for n, L in zip(ns, ls):
+        first = max(0, L - n - window + 1) // 32 if window else 0
+        assert first == 0 or sinks <= 32 * first
+        total += max(1, (-(-sinks // 32) if first else 0) + -(-L // 32) - first) if n else 0
+    return tiles, blocks, -(-total // target)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case,tiles,blocks,dtype", [
+    ((64, 16, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], LONG, 0, 0, None), 2, 1, BF16),
+    ((64, 16, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], LONG, 0, 0, "deep"), 2, 1, F32),
+    ((64, 16, 8, 16, [1, 5, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 2, 2, F32),
+    ((128, 16, 4, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], LONG, 0, 0, None), 1, 1, BF16),
+    ((128, 16, 4, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], LONG, 10000, 40, None), 1, 1, F32),
+    ((128, 16, 8, 32, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 2, 1, BF16),
+    ((128, 16, 8, 16, [1, 3, 1, 0, 2, 1, 4, 1, 3], HALF, 6000, 40, "deep"), 2, 1, BF16),
+    ((128, 16, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 1, 2, F32),
+    ((192, 16, 4, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 1, 1, BF16),
+    ((192, 8, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, "wide"), 1, 2, F32),
+    ((256, 16, 4, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, "deep"), 1, 1, BF16),
+    ((256, 8, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 1, 2, BF16),
+    ((256, 8, 8, 16, [1, 3, 1, 0, 2, 1, 1, 1, 3], HALF, 0, 0, None), 1, 2, F32),
+    ((256, 8, 16, 16, [1, 3, 1, 2, 2, 1, 1, 3, 3], EVEN, 0, 0, None), 1, 3, BF16),
+])
+def test_equal_shares_of_every_head_size_and_number_of_rows(case, tiles, blocks, dtype):
+    """One tile of rows or two, one block of rows or more, of which a sequence of few tokens has fewer."""
+    found = share_blocks(case, dtype)
+    assert found[:2] == (tiles, blocks) and found[2] >= 32
+    out, ref, amount, shift, _ = run_case(*case, dtype)
+    flags()
+    L = max(case[5])
+    few = dtype is BF16 and max(case[4]) * case[2] <= 32
+    err, tol = (out.cpu().double() - ref).abs(), few_tolerance(ref, amount, shift, L) if few else tolerance(ref, amount, shift, dtype, L)
+    assert (err <= tol).all(), float((err / tol).max())
+
+
 @pytest.mark.gpu
 def test_more_sequences_than_a_wave_has_lanes():
     ns, ls = [1 + b % 3 for b in range(150)], [1 + 37 * b % 411 for b in range(150)]

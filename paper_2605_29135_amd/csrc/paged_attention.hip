@@ -676,8 +676,10 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;  // positions per step
-// A maximum is followed once a score is past it by so much (log2 units): probabilities of up to 2^8 lose nothing.
-constexpr float kSlack = 8.f;
+// A maximum is followed once a score is past it by so much (log2 units): probabilities of up to 2^8 lose nothing.  Sums of 2^26
+// of them with values of up to 2^100 would pass fp32, though: from kLarge on a block goes over its positions once more and
+// follows every maximum (sums below 2^126), and what stays below it in the parts of a sequence (512 at most) adds up to less.
+constexpr float kSlack = 8.f, kLarge = 0x1p112f;
 // Scores from here on (log2 units) are far: a row's offset, a rounded product, is off by 2^-12 at 2^12.  A step that has
 // one takes its exponentials of differences.
 constexpr float kFar = 0x1p12f;
@@ -952,7 +954,7 @@ __global__ __launch_bounds__(64 * WAVES, NG == 1 && WAVES == 4 ? 3 : NG <= 2 ? 2
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, p[u][r]);
         top = fmaxf(top, other_half32(top));
-        if (__any((top - mx) * a.unit > kSlack)) {  // (the first score of a row is infinitely far past its maximum)
+        if (__any((top - mx) * a.unit > (decltype(careful)::value ? 0.f : kSlack))) {  // (the first score of a row is infinitely far past its maximum)
             const float now = fmaxf(mx, top), f = __builtin_amdgcn_exp2f(mx == now ? 0.f : (mx - now) * a.unit);
             mx = now;
             sum *= f;
@@ -1136,7 +1138,7 @@ __global__ __launch_bounds__(64 * WAVES, NG == 1 && WAVES == 4 ? 3 : NG <= 2 ? 2
 #pragma unroll
     for (int t = 0; t < TD; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) off |= !(fabsf(acc[t][r]) < INFINITY);
+        for (int r = 0; r < 16; ++r) off |= !(fabsf(acc[t][r]) < kLarge);
     if (__builtin_expect(__syncthreads_or((off && !idle) || missing), 0)) pass(std::true_type());
     if (missing && lane == 0) atomicOr(a.err, kErrRange);
     const float l = sum + other_half32(sum);

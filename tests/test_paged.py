@@ -833,6 +833,27 @@ def test_attention_long_and_split(n, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,n_seq,L", [(1, 1, 1 << 22), (40, 1, 1 << 22), (40, 512, 1 << 21)])  # (many rows: split, and whole)
+def test_long_sums_of_large_values(n, n_seq, L):
+    """Scores that rise behind the first positions of every piece by 7.9 in log2 units, which many rows do not follow at once:
+    probabilities of 2^7.9 with values of 2^100 would add up to 2^128.9 and more.  All values of a dim are one power of two, so
+    that is what comes out, rounded: probabilities that follow the maximum are 1, whose sums are whole numbers below 2^24, and
+    of the first ones, a 64th of the positions at 2^-7.9 each, all may be lost beside them (2^-13)."""
+    d, page = 64, 64
+    k, v = moe.paged_cache(L // page, 1, page, d)
+    k.fill_(1.0), v.fill_(2.0 ** 100)
+    k[::64] = 0.0
+    v[..., 1::2] = -2.0 ** 99
+    table = torch.arange(L // page, dtype=torch.int32, device="cuda").repeat(n_seq, 1)
+    q = torch.ones((n_seq * n, 1, d), dtype=BF16, device="cuda")
+    out = moe.moe_paged_attention(q, k, v, table, ints([L] * n_seq), q_start=ints([n * b for b in range(n_seq + 1)]), max_q=n,
+                                  scale=5.5 / d)
+    flags()
+    want = v[0, 0, 0].double().cpu().expand(n_seq * n, 1, d)
+    assert ((out.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -11)).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("window,sinks,tree", [(0, 0, None), (0, 0, "deep"), (9000, 40, None), (100, 5, None)])
 def test_a_ragged_batch_in_equal_shares(window, sinks, tree, dtype):

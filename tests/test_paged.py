@@ -405,6 +405,21 @@ def test_tables_report_a_page_of_the_table_that_is_missing(T, wrong):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n_seq,most,page,width", [(5000, 30, 16, 6), (65535, 3, 32, 2), (2049, 200, 16, 16)])
+def test_tables_of_many_sequences_and_rows(n_seq, most, page, width):
+    """Rows by a launch of their own, of more sequences than it looks at in one go."""
+    lens, new, table, pool = requests(n_seq, most, page, n_seq, width=width)
+    T = sum(new) + 3000
+    assert T > 3 * 8192
+    want = plain_tables(lens, new, pool, 0, table, page, T)
+    dev = ints(table)
+    got = moe.moe_page_tables(ints(lens), ints(new), ints(pool), dev, page, 1 << 20, T)
+    flags()
+    assert dev.cpu().tolist() == want[0]
+    assert [t.cpu().tolist() for t in got] == [*map(list, want[1:5]), [want[5]]]
+
+
+@pytest.mark.gpu
 def test_tables_after_a_step_without_free_pages():
     """Its own call raises MOE_ERR_BUDGET; tokens that the next one adds to the missing page are not dropped in silence."""
     table = ints([[-5] * 4])
@@ -986,6 +1001,33 @@ def test_one_workspace_for_prompts_and_steps():
                 assert torch.equal(out, ref)
     assert (ws[size:] == 0x5a).all()
     flags()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,G,n,n_seq,lo,hi,dtype", [
+    (64, 2, 3, 150, 1, 1500, BF16), (128, 4, 1, 300, 1, 2000, F32), (256, 3, 2, 100, 1, 900, BF16),  # pieces of few rows
+    (64, 4, 2, 150, 2500, 6000, BF16), (128, 8, 1, 200, 1500, 4000, F32),                            # shares
+    (128, 8, 7, 100, 1, 1500, BF16), (64, 16, 5, 130, 1, 1200, BF16),                                # pieces of many rows
+])
+def test_more_sequences_than_lanes_split(d, G, n, n_seq, lo, hi, dtype):
+    rng = random.Random(n_seq)
+    ns, ls = [rng.randint(0, n) for _ in range(n_seq)], [rng.randint(lo, hi) for _ in range(n_seq)]
+    ns[5], ls[5], ls[70] = n, hi, 0
+    for window, sinks in ((0, 0), (400, 33)):
+        out, ref, amount, shift, _ = run_case(d, 1, G, 16, ns, ls, window, sinks, None, dtype)
+        assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, hi)).all()
+    flags()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [(128, 1, 64, 16, [1, 1, 2], [3000, 20, 700], 0, 0, None), (64, 1, 128, 16, [1, 2], [700, 1800], 64, 5, None),
+                                  (256, 1, 71, 16, [1, 1], [900, 31], 0, 0, None), (128, 2, 13, 32, [3, 1], [500, 2000], 0, 0, "deep"),
+                                  (192, 1, 33, 16, [1], [40], 0, 0, None)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_query_heads_per_key_value_head(case, dtype):
+    out, ref, amount, shift, (cache, _, _) = run_case(*case, dtype)
+    flags()
+    assert ((out.cpu().double() - ref).abs() <= tolerance(ref, amount, shift, dtype, max(cache.ls))).all()
 
 
 # -------------------------------------------------------------------------- graphs, streams, together (GPU) ---

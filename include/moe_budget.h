@@ -376,7 +376,7 @@ MOE_API int moe_paged_append(const void *k, const void *v, int dtype, long long 
  *   parents    device int32 [T]: a token's parent, counted within its sequence's tokens and in front of it, or -1 for a
  *              child of the last cached position.  Any other number raises MOE_ERR_RANGE and counts as -1.
  *   q_start, max_q, kv_len: the batch (kv_len with the drafted tokens, NULL: none but them); max_q at most MOE_MAX_TREE
- *   words      64-bit words of a row of masks: at least max_q / 64, at most MOE_MAX_TREE / 64
+ *   words      64-bit words of a row of masks: at least max_q / 64, rounded up, at most MOE_MAX_TREE / 64
  *   masks      device uint64 [T][words] out: bit j of a token's row: it sees token j of its sequence
  *   positions  device int32 [T] out, or NULL: kv_len - (the sequence's tokens) + the token's depth (a child of the cache
  *              has 0), the position by which it is rotated
@@ -412,6 +412,8 @@ MOE_API size_t moe_paged_attention_workspace_bytes(int T, int n_seq, int n_heads
  *   out        device, as q with out_stride, same dtype; rows from q_start[n_seq] on are not touched
  *   scale      a factor of magnitude up to 2^32, as a rule 1 / sqrt(head_dim)
  *   workspace  device, >= moe_paged_attention_workspace_bytes(...) (may be NULL when that is 0)
+ * The launches go by max_q and max_kv.  A batch of a long prompt and many single tokens over long caches is one call or, much
+ * faster, two: each with its rows of the table, its kv_len and its part of q_start, over the same token arrays.
  * T or n_seq 0 is a no-op. */
 MOE_API int moe_paged_attention(const void *q, int dtype, long long q_stride, const void *k_pool, const void *v_pool,
                                 long long k_page_stride, long long v_page_stride, int n_pages, int page_size,

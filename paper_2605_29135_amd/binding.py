@@ -650,9 +650,9 @@ def _paged_batch(n_seq, T, kv_len, q_start, max_q):
 
 def moe_tree_masks(parents, q_start=None, max_q: int | None = None, kv_len=None, masks=None, positions=None, stream=None):
     """Which drafted tokens each token of a tree sees, itself and those above it: parents int32 [T], each counted within its
-    sequence's tokens (rows q_start[b] .. q_start[b + 1); None: one token per sequence), -1 for a child of the cache; max_q:
-    most tokens of a sequence (T by default, at most 256).  Returns (masks, positions): masks int64 [T, max_q / 64], bit j of
-    a row for token j of its sequence, and positions int32 [T] (kv_len int32 [n_seq] with the drafted tokens, None: none
+    sequence's tokens (rows q_start[b] up to q_start[b + 1]; None: one token per sequence), -1 for a child of the cache; max_q:
+    most tokens of a sequence (T by default, at most 256).  Returns (masks, positions): masks int64 [T, ceil(max_q / 64)],
+    bit j of a row for token j of its sequence, and positions int32 [T] (kv_len int32 [n_seq] with the drafted tokens, None: none
     cached)."""
     import torch
     if parents.dim() != 1:
@@ -690,7 +690,7 @@ def moe_paged_attention(q, k_pool, v_pool, table, kv_len, q_start=None, max_q: i
     table int32 [n_seq, max_pages], kv_len int32 [n_seq] with the tokens), with window > 0 over the last `window` positions
     and the first `sinks`; q_start int32 [n_seq + 1]: sequence b's rows, None for one token each; max_q, max_kv: most tokens
     and positions of a sequence (T and what the table holds by default -- the launches go by them, so tight ones are
-    faster).  tree: masks of drafted tokens as of moe_tree_masks.  Scale 1 / sqrt(d) by default.  Probabilities are exact to
+    faster, and so are a long prompt and many single tokens in two calls).  tree: masks of drafted tokens as of moe_tree_masks.  Scale 1 / sqrt(d) by default.  Probabilities are exact to
     2^-24 with fp32 queries and to 2^-16 with bf16 ones, to 2^-8 in bf16 calls of many rows (never with max_q * n_heads / n_kv
     up to 32).  Returns out [T, n_heads, d] of q's type; rows from q_start[-1] on are not written."""
     import torch

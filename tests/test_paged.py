@@ -988,12 +988,12 @@ def test_one_workspace_for_prompts_and_steps():
     gen = torch.Generator().manual_seed(9)
     n_kv, G, d, page = 8, 4, 128, 16
     lens = [3000, 17, 900, 2100]
-    cache = Cache(lens, n_kv, d, page, gen, spare=4).put()
+    cache = Cache(lens, n_kv, d, page, gen, spare=3).put()
     size = moe.moe_paged_attention_workspace_bytes(32 * 256, 32, n_kv * G, n_kv, d, 256, 16384)
     ws = torch.full((size + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
     for dtype in (F32, BF16):
         for n in (1, 4, 9, 16, 64):
-            for max_kv in (3000, 3072):
+            for max_kv in (3000, 3050):
                 q = torch.randn((4 * n, n_kv * G, d), generator=gen).to(dtype).cuda()
                 args = dict(q_start=ints([0, n, 2 * n, 3 * n, 4 * n]), max_q=n, max_kv=max_kv)
                 ref = moe.moe_paged_attention(q, cache.k, cache.v, cache.dev_table, ints(lens), **args)
